@@ -110,6 +110,70 @@ RP_API rp_status rp_op_attn_bwd(void* stream, const void* q, const void* k, cons
                          long ldv, long ldo, long lddo, long lddq, long lddk, long lddv, int batch, int seq, int a, int kh,
                          int d);
 
+/* ---- what a decoder layer other than the stage's is built from: rotary positions, cross attention, the router's balance loss ----
+ * These calls find the device of `stream` themselves (the current one for the NULL stream), also when another one is current. */
+
+/* Rotary positions scaled for contexts longer than the trained one.  Pair i of rot / 2 turns by p * theta_i at position p:
+ *   RP_ROPE_PLAIN     theta_i = base^(-2i/rot)
+ *   RP_ROPE_LINEAR    theta_i / factor (positions interpolated)
+ *   RP_ROPE_BASE      the base times factor^(rot / (rot - 2)): the slowest pair as RP_ROPE_LINEAR, the fastest unchanged (rot > 2)
+ *   RP_ROPE_BY_PARTS  pairs that turn more than `fast` times over trained_len positions unchanged, those below `slow` turns as
+ *                     RP_ROPE_LINEAR, in between by the share keep = (turns - slow) / (fast - slow):  theta_i (keep + (1 - keep) / factor)
+ * amplitude multiplies cosine and sine (1 for plain rotations).  factor > 0; fields that a kind does not name are not read. */
+enum { RP_ROPE_PLAIN = 0, RP_ROPE_LINEAR = 1, RP_ROPE_BASE = 2, RP_ROPE_BY_PARTS = 3 };
+typedef struct {
+  uint32_t struct_size;   /* sizeof(rp_rope_scaling) */
+  int32_t kind;
+  float base, factor;
+  float slow, fast;       /* slow < fast */
+  int32_t trained_len;
+  float amplitude;
+} rp_rope_scaling;
+/* cs: float2 [n_pos][rot / 2] = amplitude * (cos, sin)(p theta_i), angles in 64 bits; rot even, 2 .. 512.  With rot = d it is also what
+ * rp_op_qknorm_rope takes. */
+RP_API rp_status rp_op_rope_table_scaled(void* stream, void* cs, const rp_rope_scaling* scaling, int n_pos, int rot);
+/* Rotation of a query heads and k key heads of d elements (a multiple of 8, up to 512), the first rot of them (even), the rest carried over.
+ * layout 0: half-split pairs (i, i + rot/2);  1: neighbouring pairs (2i, 2i + 1).  bwd 1: in_* are gradients of the rotated heads, out_* the
+ * gradients of the heads (the transpose).  pos [dev] int32 [T]: a token's row of cs; NULL: t % seq.  A position outside 0 .. n_pos - 1 has no
+ * row: the rotated part of such a token becomes NaN.  Row strides ld_* in elements; T any number; out_* is in_* with the same stride (in place) or
+ * does not overlap it; a or k 0: its pointers are not used. */
+RP_API rp_status rp_op_rope(void* stream, int bwd, int layout, int d, int rot, const void* in_q, const void* in_k, long ld_in_q, long ld_in_k,
+                     void* out_q, void* out_k, long ld_out_q, long ld_out_k, const void* cs, int n_pos, const int* pos, int T, int seq, int a,
+                     int k);
+
+/* Grouped-query attention of every query to all keys of another sequence (a decoder's cross attention; with few queries, the step of a
+ * generation), flash style.  q, o [batch * seq_q, a, d]; k, v [batch * seq_kv, kh, d], d 64 or 128; row strides ld* in elements; any lengths from 0
+ * on.  q_len, kv_len [dev] int32 [batch], or NULL for full sequences: how many rows of a padded sequence are in use.  Keys behind kv_len
+ * are not read; rows of o behind q_len, and all rows where kv_len is 0, become 0.  scale > 0 multiplies q.k.  lse fp32 [batch, a, seq_q]
+ * (natural log; -inf for the rows that become 0), or NULL.
+ * scratch [dev, scratch_bytes] or NULL: where there are few rows, the keys are cut into slices that are joined in order, as many as its size
+ * allows (rp_op_cross_attn_scratch: what the calls make use of).  It holds nothing between calls; two calls that may run at the same time need
+ * one each.  No output may overlap an input, the scratch or another output (columns of one array beside each other do not). */
+RP_API rp_status rp_op_cross_attn_scratch(int batch, int seq_q, int seq_kv, int a, int kh, int d, size_t* fwd_bytes, size_t* bwd_bytes);
+RP_API rp_status rp_op_cross_attn_fwd(void* stream, const void* q, const void* k, const void* v, void* o, float* lse, long ldq, long ldk, long ldv,
+                               long ldo, const int* q_len, const int* kv_len, int batch, int seq_q, int seq_kv, int a, int kh, int d, float scale,
+                               void* scratch, size_t scratch_bytes);
+/* o, lse: the forward's.  delta fp32 [batch, a, seq_q] is scratch.  dq [batch * seq_q, a, d], dk, dv [batch * seq_kv, kh, d] overwritten; rows behind
+ * q_len and kv_len become 0. */
+RP_API rp_status rp_op_cross_attn_bwd(void* stream, const void* q, const void* k, const void* v, const void* o, const void* dout, const float* lse,
+                               float* delta, void* dq, void* dk, void* dv, long ldq, long ldk, long ldv, long ldo, long lddo, long lddq,
+                               long lddk, long lddv, const int* q_len, const int* kv_len, int batch, int seq_q, int seq_kv, int a, int kh, int d,
+                               float scale, void* scratch, size_t scratch_bytes);
+
+/* Balance loss of a router, forward and backward in one call.  The T tokens are groups of `seq` (T for one group; a sequence each to balance
+ * every sequence); mask [dev] uint8 [T], 0 for padding, or NULL.  logits [dev] fp32 [T, E], E <= 1024; idx [dev] int32 [T, top_k]: the experts of every token
+ * (rp_op_moe_route_plan's; numbers outside 0 .. E - 1 are not counted).  Over the N valid tokens, with p = softmax(logits) over all experts
+ * and f_ge = counts_ge / (n_g top_k):
+ *   loss_balance = E / N sum_t sum_e f_ge p_te;   loss_z = 1 / N sum_t (log sum_e exp logits_te)^2;   loss = coef loss_balance + z_coef loss_z
+ * counts [dev] int32 [T / seq, E], tokens [dev] int32 [T / seq + 1] (n_g, then N); loss_out [dev] fp32 [3]: loss, loss_balance, loss_z (all 0 for N = 0).
+ * dlogits [dev] fp32 [T, E] or NULL = grad_scale * the gradient of the loss (the counts are constants) + dlogits_in, the gradient the layer has
+ * left (rp_stage_backward's d_router_logits), or NULL; dlogits may be dlogits_in.  Padding, and a token whose logits are all -inf, adds nothing to
+ * the losses and gets no gradient.  scratch [dev, scratch_bytes], rp_op_moe_balance_scratch bytes; a call of its own each. */
+RP_API rp_status rp_op_moe_balance_scratch(int T, int seq, int E, size_t* scratch_bytes);
+RP_API rp_status rp_op_moe_balance(void* stream, const float* logits, const int* idx, const unsigned char* mask, int T, int seq, int E, int top_k,
+                            float coef, float z_coef, float grad_scale, int* counts, int* tokens, float* loss_out, const float* dlogits_in,
+                            float* dlogits, void* scratch, size_t scratch_bytes);
+
 /* Per-kernel timeline of the stage calls on a ctx (measurement aid; the only calls that synchronise).
  * rp_trace_start: from now on every kernel a stage/head call enqueues is preceded by a timing event (at most
  * max_records ops are recorded).  rp_trace_stop: waits for the compute stream, writes up to cap records

@@ -14,6 +14,7 @@ RP_MAX_SLOTS = 4
 IGNORE_INDEX = -100
 LORA_BITS = {"q": 1, "k": 2, "v": 4, "o": 8, "gate": 16, "up": 32, "down": 64}
 GEMM_NT, GEMM_NN, GEMM_TN = 0, 1, 2
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = range(4)
 PHASE_RECOMPUTE, PHASE_BACKWARD, PHASE_BOTH = 1, 2, 3
 
 TENSOR_IDS = ["G1", "WQKV", "GQ", "GK", "WO", "G2", "WGU", "WD", "WR", "LA_Q", "LA_K", "LA_V", "LB_Q", "LB_K", "LB_V",
@@ -49,6 +50,11 @@ class GemmDesc(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("A", "B", "A2", "B2", "R", "C")] + \
                [(n, C.c_long) for n in ("lda", "ldb", "lda2", "ldb2", "ldr", "ldc")] + \
                [(n, C.c_int) for n in ("layout", "out_f32", "M", "N", "K", "K2", "beta")] + [("alpha", C.c_float)]
+
+
+class RopeScaling(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("kind", C.c_int32), ("base", C.c_float), ("factor", C.c_float), ("slow", C.c_float),
+                ("fast", C.c_float), ("trained_len", C.c_int32), ("amplitude", C.c_float)]
 
 
 class RpError(RuntimeError):
@@ -115,6 +121,14 @@ _SIGS = {
     "rp_op_attn_fwd": [_vp, _vp, _vp, _vp, _vp, _vp, _l, _l, _l, _l, _i, _i, _i, _i, _i],
     "rp_op_attn_bwd": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _l, _l, _l, _l, _l, _l, _l, _l, _i, _i, _i,
                        _i, _i],
+    "rp_op_rope_table_scaled": [_vp, _vp, C.POINTER(RopeScaling), _i, _i],
+    "rp_op_rope": [_vp, _i, _i, _i, _i, _vp, _vp, _l, _l, _vp, _vp, _l, _l, _vp, _i, _vp, _i, _i, _i, _i],
+    "rp_op_cross_attn_scratch": [_i, _i, _i, _i, _i, _i, _psz, _psz],
+    "rp_op_cross_attn_fwd": [_vp, _vp, _vp, _vp, _vp, _vp, _l, _l, _l, _l, _vp, _vp, _i, _i, _i, _i, _i, _i, _f, _vp, _sz],
+    "rp_op_cross_attn_bwd": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _l, _l, _l, _l, _l, _l, _l, _l, _vp, _vp, _i, _i, _i, _i,
+                             _i, _i, _f, _vp, _sz],
+    "rp_op_moe_balance_scratch": [_i, _i, _i, _psz],
+    "rp_op_moe_balance": [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _f, _f, _f, _vp, _vp, _vp, _vp, _vp, _vp, _sz],
 }
 EXPORTS = sorted(list(_SIGS) + ["rp_last_error"])
 for _name, _args in _SIGS.items():
@@ -378,3 +392,51 @@ def rp_op_attn_bwd(stream, q, k, v, o, dout, lse, delta, dq, dk, dv, scratch, ld
     _check(lib.rp_op_attn_bwd(stream, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(lse), _ptr(delta), _ptr(dq),
                               _ptr(dk), _ptr(dv), _ptr(scratch), ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv, batch, seq, a,
                               kh, d))
+
+
+def make_rope_scaling(kind=ROPE_PLAIN, base=1.0e6, factor=1.0, slow=1.0, fast=32.0, trained_len=4096, amplitude=1.0):
+    return RopeScaling(C.sizeof(RopeScaling), kind, base, factor, slow, fast, trained_len, amplitude)
+
+
+def rp_op_rope_table_scaled(stream, cs, scaling, n_pos, rot):
+    _check(lib.rp_op_rope_table_scaled(stream, _ptr(cs), C.byref(scaling), n_pos, rot))
+
+
+def rp_op_rope(stream, bwd, layout, d, rot, in_q, in_k, ld_in_q, ld_in_k, out_q, out_k, ld_out_q, ld_out_k, cs, n_pos, pos, T_, seq, a, k):
+    _check(lib.rp_op_rope(stream, bwd, layout, d, rot, _ptr(in_q), _ptr(in_k), ld_in_q, ld_in_k, _ptr(out_q), _ptr(out_k), ld_out_q,
+                          ld_out_k, _ptr(cs), n_pos, _ptr(pos), T_, seq, a, k))
+
+
+def _bytes(t):
+    return t.numel() * t.element_size() if t is not None else 0
+
+
+def rp_op_cross_attn_scratch(batch, seq_q, seq_kv, a, kh, d):
+    """Returns the bytes of scratch that the forward and the backward call make use of."""
+    f, b = C.c_size_t(), C.c_size_t()
+    _check(lib.rp_op_cross_attn_scratch(batch, seq_q, seq_kv, a, kh, d, C.byref(f), C.byref(b)))
+    return f.value, b.value
+
+
+def rp_op_cross_attn_fwd(stream, q, k, v, o, lse, ldq, ldk, ldv, ldo, q_len, kv_len, batch, seq_q, seq_kv, a, kh, d, scale, scratch=None):
+    _check(lib.rp_op_cross_attn_fwd(stream, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), ldq, ldk, ldv, ldo, _ptr(q_len), _ptr(kv_len),
+                                    batch, seq_q, seq_kv, a, kh, d, scale, _ptr(scratch), _bytes(scratch)))
+
+
+def rp_op_cross_attn_bwd(stream, q, k, v, o, dout, lse, delta, dq, dk, dv, ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv, q_len, kv_len,
+                         batch, seq_q, seq_kv, a, kh, d, scale, scratch=None):
+    _check(lib.rp_op_cross_attn_bwd(stream, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(lse), _ptr(delta), _ptr(dq), _ptr(dk),
+                                    _ptr(dv), ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv, _ptr(q_len), _ptr(kv_len), batch, seq_q, seq_kv,
+                                    a, kh, d, scale, _ptr(scratch), _bytes(scratch)))
+
+
+def rp_op_moe_balance_scratch(T_, seq, E):
+    n = C.c_size_t()
+    _check(lib.rp_op_moe_balance_scratch(T_, seq, E, C.byref(n)))
+    return n.value
+
+
+def rp_op_moe_balance(stream, logits, idx, mask, T_, seq, E, top_k, coef, z_coef, grad_scale, counts, tokens, loss, dlogits_in, dlogits,
+                      scratch):
+    _check(lib.rp_op_moe_balance(stream, _ptr(logits), _ptr(idx), _ptr(mask), T_, seq, E, top_k, coef, z_coef, grad_scale, _ptr(counts),
+                                 _ptr(tokens), _ptr(loss), _ptr(dlogits_in), _ptr(dlogits), _ptr(scratch), _bytes(scratch)))

@@ -1,0 +1,1098 @@
+// Attention of one sequence's queries to another sequence's keys (a decoder attending to an encoder's states), forward and backward:
+// no causal mask, lengths of their own for queries and keys, padded batches.
+//
+//   S = scale q k^T over the keys before kv_len;  lse = log sum exp S;  P = exp(S - lse);  o = P v
+//   dV = P^T dO;  dP = dO V^T;  delta = rowsum(P dP) (= rowsum(dO o));  dS = P (dP - delta);  dQ = scale dS K;  dK = scale dS^T Q
+//
+// Without a causal mask nothing tells the query heads of a key head's group apart: the grp query heads times q_len queries of one key head
+// are simply grp q_len ROWS against the same keys (row r is query r % q_len of head r / q_len; the padded queries come behind them all).
+// Tiles are cut from the rows, so short sequences of many heads fill them, one workgroup's keys serve all heads of the group, and dK, dV of a
+// group need no partials per head.  The tiles, fragments and instructions are those of attention.hip.
+//
+//   forward: workgroup = NW waves x 32 rows, loop over 64-key tiles
+//   dQ     : the same; delta on the way
+//   dK, dV : workgroup = 128 keys, loop over 64-row tiles (d = 128: eight waves, pairs of which share 32 keys; d = 64: four waves)
+// Where there are too few workgroups for the chip, the loop is cut into `splits` slices, whose results another kernel joins in slice
+// order (fp32 partials in the caller's scratch; no atomics, so the result does not depend on timing).
+// Keys behind kv_len are never read (they may hold anything); rows behind q_len get zeros, and lse -inf.
+#include "attention_device.hpp"
+#include "layer_ops.hpp"
+
+namespace {
+
+// Lengths and places of one sequence and key head.  Lengths that the caller got wrong count as the nearest possible one.
+struct Rows {
+  int b, g, grp, qlen, kvlen, valid, total, seq_q;   // valid = grp * qlen rows hold queries, total = grp * seq_q
+  RP_DEV Rows(const CrossArgs& p, int hb) {
+    b = hb / p.kh;
+    g = hb - b * p.kh;
+    grp = p.a / p.kh;
+    seq_q = p.seq_q;
+    qlen = p.q_len ? min(max(p.q_len[b], 0), p.seq_q) : p.seq_q;
+    kvlen = p.kv_len ? min(max(p.kv_len[b], 0), p.seq_kv) : p.seq_kv;
+    valid = grp * qlen;
+    total = grp * seq_q;
+  }
+  // head within the group and query of row r < total
+  RP_DEV void at(int r, int& h, int& q) const {
+    if (r < valid) {
+      h = r / qlen;
+      q = r - h * qlen;
+    } else {
+      const int j = r - valid, pad = seq_q - qlen;
+      h = j / pad;
+      q = qlen + j - h * pad;
+    }
+  }
+  // offset of row r in a [T, heads, d] tensor of row stride ld, from its first element
+  RP_DEV long offset(int r, long ld, int d) const {
+    int h, q;
+    at(r, h, q);
+    return ((long)b * seq_q + q) * ld + (long)(g * grp + h) * d;
+  }
+  RP_DEV long stat(int r, int a) const {   // in a [batch, a, seq_q] array
+    int h, q;
+    at(r, h, q);
+    return ((long)b * a + g * grp + h) * seq_q + q;
+  }
+};
+
+// Slice `s` of `n` steps cut into `splits`: [first, last).  The number of slices that have any is used again where they are joined.
+RP_DEV void slice_of(int n, int splits, int s, int& first, int& last) {
+  const int per = (n + splits - 1) / splits;
+  first = min(s * per, n);
+  last = min(first + per, n);
+}
+RP_DEV int slices_used(int n, int splits) {
+  if (n == 0) return 0;
+  const int per = (n + splits - 1) / splits;
+  return (n + per - 1) / per;
+}
+
+// A 64-key tile, through a descriptor of its own that ends with the sequence: rows past the end read as zero, and no offset outgrows 32
+// bits however long the sequence is.
+template <int D, int NT>
+struct KeyTile {
+  using T64 = Tile64<D, NT>;
+  const bf16* base;
+  long ld;
+  int len;
+  RP_DEV KeyTile(const bf16* b, long l, int n) : base(b), ld(l), len(n) {}
+  RP_DEV void load(uint4 (&r)[T64::NREG], int key0, int tid) const {
+    const int left = min(64, len - key0);      // >= 1
+    const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base + (long)key0 * ld), 0, (int)(((long)(left - 1) * ld + D) * 2), 0x00020000);
+    T64::load(r, rs, ld, 0, tid);
+  }
+};
+
+// Zeros for the rows of [r0, r0 + n) that are behind the queries, all threads of the block.
+template <int D, int NT>
+RP_DEV void zero_rows(const CrossArgs& p, const Rows& s, bf16* out, long ld, float* lse, int r0, int n, int tid) {
+  constexpr int CH = D / 8;
+  for (int i = tid; i < n * CH; i += NT) {
+    const int r = r0 + i / CH;
+    if (r < s.valid || r >= s.total) continue;
+    *reinterpret_cast<uint4*>(out + s.offset(r, ld, D) + (i % CH) * 8) = make_uint4(0u, 0u, 0u, 0u);
+    if (lse && i % CH == 0) lse[s.stat(r, p.a)] = -INFINITY;
+  }
+}
+
+// ================================================================================================ forward
+template <int D, int NW, bool SPLIT>
+__global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_fwd_kernel(const CrossArgs p) {
+  constexpr int LDK = D + 8, LDV = D + 32, KS = D / 16, DT = D / 32, NT = NW * 64, BQ = NW * 32;
+  using T64 = Tile64<D, NT>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // fwd_smem_bytes(D, NW)
+  bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);
+  constexpr bool DB = NW >= 8;      // two sets of K/V tiles, one barrier per key tile
+  constexpr int SET = 64 * LDK + 64 * LDV;
+  bf16* const Ks = smem;
+  bf16* const Vs = smem + 64 * LDK;
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, lk = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nhb = p.kh * p.batch;
+  const int rest = (int)blockIdx.x / nhb;
+  const int hb = xcd_head((int)blockIdx.x % nhb, nhb);      // an XCD keeps to few key heads
+  const int split = SPLIT ? rest % p.splits : 0;
+  const int r0 = (SPLIT ? rest / p.splits : rest) * BQ;
+  const Rows s(p, hb);
+  if (r0 >= s.valid) {      // uniform over the workgroup, before any barrier
+    if (!SPLIT) zero_rows<D, NT>(p, s, p.o, p.ldo, p.lse, r0, BQ, tid);
+    return;
+  }
+  int j0 = 0, j1 = (s.kvlen + 63) / 64;
+  if (SPLIT) {
+    slice_of(j1, p.splits, split, j0, j1);
+    if (j0 >= j1) return;
+  }
+  const KeyTile<D, NT> kt_(p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D, p.ldk, s.kvlen), vt_(p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D, p.ldv, s.kvlen);
+
+  const int row = r0 + 32 * w + lr;     // the lane's row
+  const bool live = row < s.valid;
+  uint4 qf[KS];
+  {
+    const bf16* const qr = live ? p.q + s.offset(row, p.ldq, D) : p.q;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (live) qf[ks] = *reinterpret_cast<const uint4*>(qr + 16 * ks + 8 * lk);
+    }
+  }
+
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16 oacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) oacc[dt][v] = 0.f;
+
+  const bf16* const kfrag0 = Ks + lr * LDK + 8 * lk;
+  const bf16* const vfrag0 = Vs + tr_base32<LDV>(lane);
+  uint4 kreg[T64::NREG], vreg[T64::NREG];
+  auto load_tiles = [&](int j) {
+    kt_.load(kreg, j * 64, tid);
+    vt_.load(vreg, j * 64, tid);
+  };
+  auto store_tiles = [&](int set) {
+    T64::template store<LDK>(kreg, Ks + set * SET, tid);
+    T64::template store<LDV>(vreg, Vs + set * SET, tid);
+  };
+  if (j0 < j1) load_tiles(j0);
+  if constexpr (DB) {     // the first tile into its set, the second on its way
+    if (j0 < j1) store_tiles(j0 & 1);
+    if (j0 + 1 < j1) load_tiles(j0 + 1);
+  }
+  for (int j = j0; j < j1; ++j) {
+    __syncthreads();
+    if constexpr (DB) {
+      if (j + 1 < j1) store_tiles((j + 1) & 1);
+      if (j + 2 < j1) load_tiles(j + 2);
+    } else {
+      store_tiles(0);
+      __syncthreads();
+      if (j + 1 < j1) load_tiles(j + 1);
+    }
+    const bf16* const kfrag = kfrag0 + (DB ? (j & 1) * SET : 0);
+    const bf16* const vfrag = vfrag0 + (DB ? (j & 1) * SET : 0);
+    const int kv0 = j * 64;
+    f32x16 sT[2];
+    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    constexpr int AHEAD = 3;      // LDS fragments are requested that many products early
+    {
+      constexpr int NS = 2 * KS;
+      auto sfrag_at = [&](int n) { return *reinterpret_cast<const uint4*>(kfrag + 32 * (n & 1) * LDK + 16 * (n >> 1)); };
+      uint4 ring[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) ring[n] = sfrag_at(n);
+      MFMA_PHASE_BEGIN();
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        const uint4 a = ring[n % AHEAD];
+        if (n + AHEAD < NS) ring[n % AHEAD] = sfrag_at(n + AHEAD);
+        sT[n & 1] = mfma32(a, qf[n >> 1], n < 2 ? zero16 : sT[n & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      MFMA_PHASE_END();
+    }
+    constexpr int NU = 4 * DT;
+    auto ufrag_at = [&](int n) { return read_frag_tr32<LDV>(vfrag, n / DT, 32 * (n % DT)); };
+    uint4 uring[AHEAD];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
+    __builtin_amdgcn_sched_barrier(0);
+    if (kv0 + 64 > s.kvlen) {      // uniform: the last tile
+      const int klim = s.kvlen - 1 - (kv0 + 4 * lk);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sT[kt][v] = (32 * kt + 8 * (v >> 2) + (v & 3) > klim) ? -INFINITY : sT[kt][v];
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sT[kt][v]);
+    mx = (NW < 8 ? half_max(mx) : fmaxf(mx, __shfl_xor(mx, 32, 64))) * p.scale_log2e;
+    // m_run is a reference exponent that moves only when a row's maximum outgrows it by 2^8 (see attention.hip); every tile has a key,
+    // so it is finite from the first one on
+    const bool grow = mx > m_run + 8.f;
+    if (__builtin_amdgcn_ballot_w64(grow) != 0ull) {
+      const float m_new = grow ? mx : m_run;
+      float alpha = fast_exp2(m_run - m_new);
+      asm volatile("" : "+v"(alpha));
+      l_run *= alpha;
+      m_run = m_new;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
+    }
+    float psum = 0.f;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float e = fast_exp2(__builtin_fmaf(sT[kt][v], p.scale_log2e, -m_run));
+        sT[kt][v] = e;
+        psum += e;
+      }
+    l_run += psum;
+    {
+      uint4 pf[4];      // P in bf16, as the matrix instruction takes it: relative 2^-9 a term, on sums held in fp32
+#pragma unroll
+      for (int gk = 0; gk < 4; ++gk) pf[gk] = pack_frag32(sT[gk >> 1], 8 * (gk & 1));
+      MFMA_PHASE_BEGIN();
+#pragma unroll
+      for (int n = 0; n < NU; ++n) {
+        const uint4 a = uring[n % AHEAD];
+        if (n + AHEAD < NU) uring[n % AHEAD] = ufrag_at(n + AHEAD);
+        oacc[n % DT] = mfma32(a, pf[n / DT], oacc[n % DT]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      MFMA_PHASE_END();
+    }
+  }
+
+  const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+  if constexpr (SPLIT) {
+    const long at = ((long)split * nhb + hb) * s.total + row;
+    if (live) {
+      if (lk == 0) p.part_ml[at] = make_float2(m_run, l_tot);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int vg = 0; vg < 4; ++vg)
+          *reinterpret_cast<float4*>(p.part + at * D + 32 * dt + 8 * vg + 4 * lk) =
+              make_float4(oacc[dt][4 * vg], oacc[dt][4 * vg + 1], oacc[dt][4 * vg + 2], oacc[dt][4 * vg + 3]);
+    }
+  } else {
+    const bool some = live && j0 < j1;      // a row without keys: o = 0, lse = -inf
+    const float mul = some ? 1.f / l_tot : 0.f;
+    if (p.lse && lk == 0 && row < s.total) p.lse[s.stat(row, p.a)] = some ? m_run * 0.6931471805599453f + logf(l_tot) : -INFINITY;
+    __syncthreads();
+    bf16* const stage = smem + w * 32 * LDK;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int vg = 0; vg < 4; ++vg) {
+        const uint2 u = make_uint2(pack_bf16x2(oacc[dt][4 * vg] * mul, oacc[dt][4 * vg + 1] * mul), pack_bf16x2(oacc[dt][4 * vg + 2] * mul, oacc[dt][4 * vg + 3] * mul));
+        *reinterpret_cast<uint2*>(stage + lr * LDK + 32 * dt + 8 * vg + 4 * lk) = some ? u : make_uint2(0u, 0u);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < (32 * (D / 8)) / 64; ++it) {
+      const int idx = it * 64 + lane, rr = idx / (D / 8), ch = idx % (D / 8), r = r0 + 32 * w + rr;
+      if (r < s.total) *reinterpret_cast<uint4*>(p.o + s.offset(r, p.ldo, D) + ch * 8) = *reinterpret_cast<const uint4*>(stage + rr * LDK + ch * 8);
+    }
+  }
+}
+
+// Joins the slices of a row: weights exp2(m_i - max m), in slice order.  D / 8 threads per row.
+template <int D>
+__global__ void __launch_bounds__(256) cross_fwd_join_kernel(const CrossArgs p) {
+  constexpr int CH = D / 8;
+  const int total = (p.a / p.kh) * p.seq_q, nhb = p.kh * p.batch;
+  const long idx = (long)blockIdx.x * 256 + threadIdx.x;
+  const long item = idx / CH;
+  const int ch = (int)(idx % CH);
+  if (item >= (long)nhb * total) return;
+  const int hb = (int)(item / total), r = (int)(item - (long)hb * total);
+  const Rows s(p, hb);
+  const int n = r < s.valid ? slices_used((s.kvlen + 63) / 64, p.splits) : 0;
+  float m = -INFINITY;
+  for (int i = 0; i < n; ++i) m = fmaxf(m, p.part_ml[((long)i * nhb + hb) * total + r].x);
+  float l = 0.f, acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  for (int i = 0; i < n; ++i) {
+    const long at = ((long)i * nhb + hb) * total + r;
+    const float2 ml = p.part_ml[at];
+    const float wgt = fast_exp2(ml.x - m);
+    const float4 x0 = *reinterpret_cast<const float4*>(p.part + at * D + ch * 8), x1 = *reinterpret_cast<const float4*>(p.part + at * D + ch * 8 + 4);
+    l += wgt * ml.y;
+    acc[0] += wgt * x0.x; acc[1] += wgt * x0.y; acc[2] += wgt * x0.z; acc[3] += wgt * x0.w;
+    acc[4] += wgt * x1.x; acc[5] += wgt * x1.y; acc[6] += wgt * x1.z; acc[7] += wgt * x1.w;
+  }
+  const float mul = n ? 1.f / l : 0.f;
+  if (p.lse && ch == 0) p.lse[s.stat(r, p.a)] = n ? m * 0.6931471805599453f + logf(l) : -INFINITY;
+  *reinterpret_cast<uint4*>(p.o + s.offset(r, p.ldo, D) + ch * 8) =
+      make_uint4(pack_bf16x2(acc[0] * mul, acc[1] * mul), pack_bf16x2(acc[2] * mul, acc[3] * mul), pack_bf16x2(acc[4] * mul, acc[5] * mul),
+                 pack_bf16x2(acc[6] * mul, acc[7] * mul));
+}
+
+// ================================================================================================ dQ
+// delta comes from the stored output, as in attention.hip, where many keys share a row's weight.  With few keys a row may put nearly all of it on
+// one, dP - delta cancels there, and the rounding of the stored output (2^-9 of delta) would show in what is left: up to EXACT_DELTA keys
+// the scores are made twice, and delta = sum P dP is as exact as they are.
+constexpr int EXACT_DELTA = 512;
+
+template <int D, int NW, bool SPLIT>
+__global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(const CrossArgs p) {
+  constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, NT = NW * 64, BQ = NW * 32;
+  using T64 = Tile64<D, NT>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // dq_smem_bytes(D, NW)
+  bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);
+  constexpr bool DB = NW >= 8;
+  constexpr int SET = 2 * 64 * LD;
+  bf16* const Ks = smem;
+  bf16* const Vs = smem + 64 * LD;
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nhb = p.kh * p.batch;
+  const int rest = (int)blockIdx.x / nhb;
+  const int hb = xcd_head((int)blockIdx.x % nhb, nhb);
+  const int split = SPLIT ? rest % p.splits : 0;
+  const int r0 = (SPLIT ? rest / p.splits : rest) * BQ;
+  const Rows s(p, hb);
+  if (r0 >= s.valid) {
+    if (!SPLIT) zero_rows<D, NT>(p, s, p.dq, p.lddq, nullptr, r0, BQ, tid);
+    return;
+  }
+  const int tiles = (s.kvlen + 63) / 64;
+  int j0 = 0, j1 = tiles;
+  if (SPLIT) {
+    slice_of(tiles, p.splits, split, j0, j1);
+    if (j0 >= j1 && split > 0) return;
+  }
+  const bool exact_delta = s.kvlen <= EXACT_DELTA;
+  const KeyTile<D, NT> kt_(p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D, p.ldk, s.kvlen), vt_(p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D, p.ldv, s.kvlen);
+
+  uint4 qf[2][KS], dof[2][KS];     // a lane's rows: column tiles c = 0, 1
+  float lse2[2], dl[2];
+  long stat[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int row = r0 + 32 * w + 16 * c + lr;
+    const bool ok = row < s.valid;
+    const int rc = ok ? row : 0;
+    const bf16* const qr = p.q + s.offset(rc, p.ldq, D) + 8 * lg;
+    const bf16* const dor = p.dout + s.offset(rc, p.lddo, D) + 8 * lg;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      dof[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (ok) {
+        qf[c][ks] = *reinterpret_cast<const uint4*>(qr + 32 * ks);
+        dof[c][ks] = *reinterpret_cast<const uint4*>(dor + 32 * ks);
+      }
+    }
+    stat[c] = s.stat(rc, p.a);
+    lse2[c] = ok ? p.lse_in[stat[c]] * 1.4426950408889634f : INFINITY;   // rows past the end get P = 0
+    dl[c] = 0.f;
+    if (!exact_delta) {
+      float sum = 0.f;
+      if (ok) {
+        const bf16* const orow = p.o_in + s.offset(rc, p.ldo, D) + 8 * lg;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const uint4 u = *reinterpret_cast<const uint4*>(orow + 32 * ks), d = dof[c][ks];
+          sum += bf16_lo(u.x) * bf16_lo(d.x) + bf16_hi(u.x) * bf16_hi(d.x) + bf16_lo(u.y) * bf16_lo(d.y) + bf16_hi(u.y) * bf16_hi(d.y) +
+                 bf16_lo(u.z) * bf16_lo(d.z) + bf16_hi(u.z) * bf16_hi(d.z) + bf16_lo(u.w) * bf16_lo(d.w) + bf16_hi(u.w) * bf16_hi(d.w);
+        }
+      }
+      dl[c] = column_sum(sum);
+    }
+  }
+
+  const bf16* const kfrag0 = Ks + lr * LD + 8 * lg;
+  const bf16* const ktfrag0 = Ks + tr_base<LD>(lane);
+  uint4 kreg[T64::NREG], vreg[T64::NREG];
+  auto load_tiles = [&](int j) {
+    kt_.load(kreg, j * 64, tid);
+    vt_.load(vreg, j * 64, tid);
+  };
+  auto store_tiles = [&](int set) {
+    T64::template store<LD>(kreg, Ks + set * SET, tid);
+    T64::template store<LD>(vreg, Vs + set * SET, tid);
+  };
+  // scores and dP of 32 keys, transposed: [16 keys][16 rows]; kfrag: the set's K, its V lies 64 rows further on
+  auto scores = [&](const bf16* kfrag, int k2, f32x4 (&sT)[2][2], f32x4 (&dpT)[2][2]) {
+    const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
+    constexpr int NS = 4 * KS, AHEAD = 4;     // n = (ks * 2 + kt) * 2 + which
+    auto sfrag_at = [&](int n) { return *reinterpret_cast<const uint4*>(kfrag + (32 * k2 + 16 * ((n >> 1) & 1) + 64 * (n & 1)) * LD + 32 * (n >> 2)); };
+    uint4 ring[AHEAD];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) ring[n] = sfrag_at(n);
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      const uint4 a = ring[n % AHEAD];
+      if (n + AHEAD < NS) ring[n % AHEAD] = sfrag_at(n + AHEAD);
+      const int ks = n >> 2, kt = (n >> 1) & 1;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        if (n & 1) dpT[kt][c] = mfma16(a, dof[c][ks], ks == 0 ? zero4 : dpT[kt][c]);
+        else sT[kt][c] = mfma16(a, qf[c][ks], ks == 0 ? zero4 : sT[kt][c]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  if (exact_delta) {      // uniform over the workgroup
+    for (int j = 0; j < tiles; ++j) {
+      load_tiles(j);
+      __syncthreads();
+      store_tiles(0);
+      __syncthreads();
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        f32x4 sT[2][2], dpT[2][2];
+        scores(kfrag0, k2, sT, dpT);
+        const int klim = s.kvlen - 1 - (j * 64 + 32 * k2 + 4 * lg);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float pr = fast_exp2(__builtin_fmaf(sT[kt][c][e], p.scale_log2e, -lse2[c]));
+              dl[c] += 16 * kt + e > klim ? 0.f : pr * dpT[kt][c][e];
+            }
+      }
+    }
+    dl[0] = column_sum(dl[0]);
+    dl[1] = column_sum(dl[1]);
+    __syncthreads();      // the tiles are stored anew below
+  }
+  if (split == 0 && lg == 0) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      if (r0 + 32 * w + 16 * c + lr < s.valid) p.delta[stat[c]] = dl[c];
+  }
+
+  f32x4 dqacc[DT][2];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) dqacc[dt][0] = dqacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (j0 < j1) load_tiles(j0);
+  if constexpr (DB) {
+    if (j0 < j1) store_tiles(j0 & 1);
+    if (j0 + 1 < j1) load_tiles(j0 + 1);
+  }
+  for (int j = j0; j < j1; ++j) {
+    __syncthreads();
+    if constexpr (DB) {
+      if (j + 1 < j1) store_tiles((j + 1) & 1);
+      if (j + 2 < j1) load_tiles(j + 2);
+    } else {
+      store_tiles(0);
+      __syncthreads();
+      if (j + 1 < j1) load_tiles(j + 1);
+    }
+    const int set = DB ? (j & 1) * SET : 0;
+    const bool need_mask = j * 64 + 64 > s.kvlen;
+    // the two 32-key halves of the tile one after the other: half as many score registers live at a time
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) {
+      f32x4 sT[2][2], dpT[2][2];
+      scores(kfrag0 + set, k2, sT, dpT);
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sT[kt][c][e] = fast_exp2(__builtin_fmaf(sT[kt][c][e], p.scale_log2e, -lse2[c])) * (dpT[kt][c][e] - dl[c]);   // dS^T
+      if (need_mask) {
+        const int klim = s.kvlen - 1 - (j * 64 + 32 * k2 + 4 * lg);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sT[kt][c][e] = 16 * kt + e > klim ? 0.f : sT[kt][c][e];
+      }
+      constexpr int AHEAD = 2;      // K^T fragments requested that many pairs of products early
+      const uint4 df[2] = {pack_frag(sT[0][0], sT[1][0]), pack_frag(sT[0][1], sT[1][1])};
+      auto ufrag_at = [&](int n) { return read_frag_tr<LD>(ktfrag0 + set + 32 * k2 * LD + 16 * n); };
+      uint4 uring[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
+#pragma unroll
+      for (int n = 0; n < DT; ++n) {
+        const uint4 a = uring[n % AHEAD];
+        if (n + AHEAD < DT) uring[n % AHEAD] = ufrag_at(n + AHEAD);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) dqacc[n][c] = mfma16(a, df[c], dqacc[n][c]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  if constexpr (SPLIT) {
+    if (j0 >= j1) return;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int row = r0 + 32 * w + 16 * c + lr;
+      if (row < s.valid) {
+        float* const out = p.part + (((long)split * nhb + hb) * s.total + row) * D + 4 * lg;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          *reinterpret_cast<float4*>(out + 16 * dt) = make_float4(dqacc[dt][c][0], dqacc[dt][c][1], dqacc[dt][c][2], dqacc[dt][c][3]);
+      }
+    }
+  } else {
+    __syncthreads();
+    bf16* const stage = smem + w * 32 * (D + 8);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        *reinterpret_cast<uint2*>(stage + (16 * c + lr) * (D + 8) + 16 * dt + 4 * lg) =
+            make_uint2(pack_bf16x2(dqacc[dt][c][0] * p.scale, dqacc[dt][c][1] * p.scale), pack_bf16x2(dqacc[dt][c][2] * p.scale, dqacc[dt][c][3] * p.scale));
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < (32 * (D / 8)) / 64; ++it) {
+      const int idx = it * 64 + lane, rr = idx / (D / 8), ch = idx % (D / 8), r = r0 + 32 * w + rr;
+      if (r < s.total)
+        *reinterpret_cast<uint4*>(p.dq + s.offset(r, p.lddq, D) + ch * 8) =
+            r < s.valid ? *reinterpret_cast<const uint4*>(stage + rr * (D + 8) + ch * 8) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+}
+
+// dq = scale * the sum of a row's slices, in slice order.
+template <int D>
+__global__ void __launch_bounds__(256) cross_dq_join_kernel(const CrossArgs p) {
+  constexpr int CH = D / 8;
+  const int total = (p.a / p.kh) * p.seq_q, nhb = p.kh * p.batch;
+  const long idx = (long)blockIdx.x * 256 + threadIdx.x;
+  const long item = idx / CH;
+  const int ch = (int)(idx % CH);
+  if (item >= (long)nhb * total) return;
+  const int hb = (int)(item / total), r = (int)(item - (long)hb * total);
+  const Rows s(p, hb);
+  const int n = r < s.valid ? slices_used((s.kvlen + 63) / 64, p.splits) : 0;
+  float acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  for (int i = 0; i < n; ++i) {
+    const float* const src = p.part + (((long)i * nhb + hb) * total + r) * D + ch * 8;
+    const float4 x0 = *reinterpret_cast<const float4*>(src), x1 = *reinterpret_cast<const float4*>(src + 4);
+    acc[0] += x0.x; acc[1] += x0.y; acc[2] += x0.z; acc[3] += x0.w;
+    acc[4] += x1.x; acc[5] += x1.y; acc[6] += x1.z; acc[7] += x1.w;
+  }
+  const float mul = p.scale;
+  *reinterpret_cast<uint4*>(p.dq + s.offset(r, p.lddq, D) + ch * 8) =
+      make_uint4(pack_bf16x2(acc[0] * mul, acc[1] * mul), pack_bf16x2(acc[2] * mul, acc[3] * mul), pack_bf16x2(acc[4] * mul, acc[5] * mul),
+                 pack_bf16x2(acc[6] * mul, acc[7] * mul));
+}
+
+// ================================================================================================ dK, dV
+// A thread's share of the 64-row tiles of q and dO: which head and query each of its 16-byte pieces belongs to.  Rows past the last query
+// read row 0 again (their P is made zero, see row_start).
+template <int D, int NT>
+struct RowTile {
+  static constexpr int CH = D / 8, NREG = 64 * CH / NT;
+  int h[NREG], q[NREG];
+  int qlen, grp, step_h, step_q;
+  RP_DEV void start(const Rows& s, int row0, int tid) {
+    qlen = max(s.qlen, 1);
+    grp = s.grp;
+    step_h = 64 / qlen;
+    step_q = 64 - step_h * qlen;
+#pragma unroll
+    for (int it = 0; it < NREG; ++it) {
+      const int r = row0 + (it * NT + tid) / CH;
+      h[it] = r / qlen;
+      q[it] = r - h[it] * qlen;
+    }
+  }
+  // base: the group's first head of the sequence's first query
+  RP_DEV void load(uint4 (&r)[NREG], const bf16* base, long ld, int tid) const {
+#pragma unroll
+    for (int it = 0; it < NREG; ++it) {
+      const bool in = h[it] < grp;
+      r[it] = *reinterpret_cast<const uint4*>(base + (long)(in ? q[it] : 0) * ld + (in ? h[it] : 0) * D + ((it * NT + tid) % CH) * 8);
+    }
+  }
+  RP_DEV void next() {
+#pragma unroll
+    for (int it = 0; it < NREG; ++it) {
+      h[it] += step_h;
+      q[it] += step_q;
+      if (q[it] >= qlen) { q[it] -= qlen; ++h[it]; }
+    }
+  }
+};
+
+// What the products start from for a row (wave 0: -lse / scale, wave 1: -delta), so that they come out as q.k - lse / scale and
+// dO.v - delta; rows past the end get P = exp(-inf) = 0.
+RP_DEV float row_start(float raw, int wave, bool in, float scale) { return wave == 0 ? (in ? -raw / scale : -INFINITY) : (in ? -raw : 0.f); }
+
+// lse and delta of a 64-row tile, a row per lane of waves 0 and 1.  The load is only issued here; row_start comes a tile later.
+struct RowStat {
+  int h, q, qlen, grp, step_h, step_q, seq_q;
+  const float* base;
+  RP_DEV void start(const CrossArgs& p, const Rows& s, int row0, int lane, int wave) {
+    qlen = max(s.qlen, 1);
+    grp = s.grp;
+    seq_q = s.seq_q;
+    step_h = 64 / qlen;
+    step_q = 64 - step_h * qlen;
+    const int r = row0 + lane;
+    h = r / qlen;
+    q = r - h * qlen;
+    base = (wave == 0 ? p.lse_in : p.delta) + ((long)s.b * p.a + s.g * grp) * seq_q;
+  }
+  RP_DEV float load() {      // and on to the next tile
+    const bool in = h < grp;
+    const float v = base[in ? (long)h * seq_q + q : 0];
+    h += step_h;
+    q += step_q;
+    if (q >= qlen) { q -= qlen; ++h; }
+    return v;
+  }
+};
+
+// P = exp(s) and dS = P dP in place.
+RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], float scale_log2e) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float pr = fast_exp2(s[qt][c][e] * scale_log2e);
+        s[qt][c][e] = pr;
+        dp[qt][c][e] = pr * dp[qt][c][e];
+      }
+}
+
+// Zeros for the keys of a 128-key tile that are behind the sequence.
+template <int D, int NT>
+RP_DEV void zero_keys(const CrossArgs& p, const Rows& s, int kv0, int tid) {
+  constexpr int CH = D / 8;
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  for (int i = tid; i < 128 * CH; i += NT) {
+    const int key = kv0 + i / CH;
+    if (key < s.kvlen || key >= p.seq_kv) continue;
+    const long t = (long)s.b * p.seq_kv + key;
+    *reinterpret_cast<uint4*>(p.dk + t * p.lddk + s.g * D + (i % CH) * 8) = zero;
+    *reinterpret_cast<uint4*>(p.dv + t * p.lddv + s.g * D + (i % CH) * 8) = zero;
+  }
+}
+
+// The keys of a workgroup do not mix: a column of the score tiles is a key's own, so keys behind the sequence need no mask here; what comes out for
+// them is not stored.
+template <int D>
+__global__ void __launch_bounds__(256) cross_dkv_kernel(const CrossArgs p) {
+  constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16;
+  using T64 = Tile64<D, 256>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];
+  bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);             // Q | dO | what the rows start from
+  bf16* const Qs = smem;
+  bf16* const dOs = smem + 64 * LD;
+  float* const stat = reinterpret_cast<float*>(smem + 2 * 64 * LD);     // [2][64]
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nhb = p.kh * p.batch;
+  const int rest = (int)blockIdx.x / nhb;
+  const int hb = xcd_head((int)blockIdx.x % nhb, nhb);
+  const int split = rest % p.splits, kv0 = (rest / p.splits) * 128, kw0 = kv0 + 32 * w;
+  const Rows s(p, hb);
+  if (p.splits == 1) zero_keys<D, 256>(p, s, kv0, tid);
+  if (kv0 >= s.kvlen) return;      // uniform, before any barrier
+  int u0, u1;
+  slice_of((s.valid + 63) / 64, p.splits, split, u0, u1);
+  if (p.splits > 1 && u0 >= u1) return;
+  const int kpos[2] = {kw0 + lr, kw0 + 16 + lr};
+  const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
+  const bf16* const vb = p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D;
+
+  uint4 kf[2][KS], vf[2][KS];
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      vf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (kpos[c] < s.kvlen) {
+        kf[c][ks] = *reinterpret_cast<const uint4*>(kb + (long)kpos[c] * p.ldk + 32 * ks + 8 * lg);
+        vf[c][ks] = *reinterpret_cast<const uint4*>(vb + (long)kpos[c] * p.ldv + 32 * ks + 8 * lg);
+      }
+    }
+  f32x4 dkacc[DT][2], dvacc[DT][2];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) dkacc[dt][0] = dkacc[dt][1] = dvacc[dt][0] = dvacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const bf16* qfrag = Qs + lr * LD + 8 * lg;
+  const bf16* dofrag = dOs + lr * LD + 8 * lg;
+  const bf16* qtfrag = Qs + tr_base<LD>(lane);
+  const bf16* dotfrag = dOs + tr_base<LD>(lane);
+
+  const bf16* const qb = p.q + (long)s.b * p.seq_q * p.ldq + (long)s.g * s.grp * D;
+  const bf16* const dob = p.dout + (long)s.b * p.seq_q * p.lddo + (long)s.g * s.grp * D;
+  uint4 qreg[T64::NREG], doreg[T64::NREG];
+  float st_reg = 0.f;
+  RowTile<D, 256> rows;
+  RowStat rstat;
+  rows.start(s, u0 * 64, tid);
+  rstat.start(p, s, u0 * 64, lane, w);
+  auto prefetch = [&]() {
+    rows.load(qreg, qb, p.ldq, tid);
+    rows.load(doreg, dob, p.lddo, tid);
+    rows.next();
+    if (w < 2) st_reg = rstat.load();
+  };
+  if (u0 < u1) prefetch();
+  for (int u = u0; u < u1; ++u) {
+    __syncthreads();
+    T64::template store<LD>(qreg, Qs, tid);
+    T64::template store<LD>(doreg, dOs, tid);
+    if (w < 2) stat[64 * w + lane] = row_start(st_reg, w, u * 64 + lane < s.valid, p.scale);
+    __syncthreads();
+    if (u + 1 < u1) prefetch();
+    // the two 32-row halves of the tile one after the other: half as many score registers live at a time
+#pragma unroll
+    for (int t2 = 0; t2 < 2; ++t2) {
+      f32x4 sc[2][2], dp[2][2], s0[2], dp0[2];     // [16 rows][16 keys]; what they start from
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) {
+        s0[qt] = *reinterpret_cast<const f32x4*>(stat + 32 * t2 + 16 * qt + 4 * lg);
+        dp0[qt] = *reinterpret_cast<const f32x4*>(stat + 64 + 32 * t2 + 16 * qt + 4 * lg);
+      }
+      constexpr int AHEAD = 4;
+      {
+        constexpr int NS = 4 * KS;     // n = (ks * 2 + qt) * 2 + which
+        auto sfrag_at = [&](int n) { return *reinterpret_cast<const uint4*>(((n & 1) ? dofrag : qfrag) + (32 * t2 + 16 * ((n >> 1) & 1)) * LD + 32 * (n >> 2)); };
+        uint4 ring[AHEAD];
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) ring[n] = sfrag_at(n);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          const uint4 a = ring[n % AHEAD];
+          if (n + AHEAD < NS) ring[n % AHEAD] = sfrag_at(n + AHEAD);
+          const int ks = n >> 2, qt = (n >> 1) & 1;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (n & 1) dp[qt][c] = mfma16(a, vf[c][ks], ks == 0 ? dp0[qt] : dp[qt][c]);
+            else sc[qt][c] = mfma16(a, kf[c][ks], ks == 0 ? s0[qt] : sc[qt][c]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      constexpr int NU = 2 * DT;
+      auto ufrag_at = [&](int n) { return read_frag_tr<LD>(((n & 1) ? qtfrag : dotfrag) + 32 * t2 * LD + 16 * (n >> 1)); };
+      uint4 uring[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
+      __builtin_amdgcn_sched_barrier(0);
+      probabilities(sc, dp, p.scale_log2e);
+      {
+        const uint4 pfg[2] = {pack_frag(sc[0][0], sc[1][0]), pack_frag(sc[0][1], sc[1][1])};
+        const uint4 dfg[2] = {pack_frag(dp[0][0], dp[1][0]), pack_frag(dp[0][1], dp[1][1])};
+#pragma unroll
+        for (int n = 0; n < NU; ++n) {
+          const uint4 a = uring[n % AHEAD];
+          if (n + AHEAD < NU) uring[n % AHEAD] = ufrag_at(n + AHEAD);
+          const int dt = n >> 1;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (n & 1) dkacc[dt][c] = mfma16(a, dfg[c], dkacc[dt][c]);
+            else dvacc[dt][c] = mfma16(a, pfg[c], dvacc[dt][c]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const long tok0 = (long)s.b * p.seq_kv;
+  if (p.splits == 1) {
+    store_acc_T<D>(dkacc, p.scale, smem + w * 32 * (D + 8), p.dk + tok0 * p.lddk + s.g * D, p.lddk, kw0, s.kvlen, lane);
+    store_acc_T<D>(dvacc, 1.f, smem + w * 32 * (D + 8), p.dv + tok0 * p.lddv + s.g * D, p.lddv, kw0, s.kvlen, lane);
+  } else {
+    float* const stage = reinterpret_cast<float*>(smem) + w * 32 * (D + 4);
+    const long ldp = (long)p.kh * D, each = (long)p.batch * p.seq_kv * ldp;
+    float* const out = p.part + split * each + tok0 * ldp + s.g * D;
+    store_acc_T_f32<D>(dkacc, p.scale, stage, out, ldp, kw0, s.kvlen, lane);
+    store_acc_T_f32<D>(dvacc, 1.f, stage, out + p.splits * each, ldp, kw0, s.kvlen, lane);
+  }
+}
+
+// Two waves per SIMD at d = 128 (see attn_bwd_dkv_pair_kernel in attention.hip): the 32 keys of a pair of waves are shared, wave h of it keeps
+// the accumulators of half h of the head dimension, makes the scores of rows 32 h .. of each tile and hands P and dS to its partner through LDS.
+template <int D>
+__global__ void __launch_bounds__(512) cross_dkv_pair_kernel(const CrossArgs p) {
+  constexpr int LD = tile_ld(D), KS = D / 32, DH = D / 32;
+  using T64 = Tile64<D, 512>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];
+  bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);             // two sets (tile parity) of Q | dO, then the exchange
+  constexpr int TSET = 2 * 64 * LD;
+  uint4* const exch = reinterpret_cast<uint4*>(smem + 2 * TSET);    // [8 waves][4 fragments][64 lanes]
+  float* const stat = reinterpret_cast<float*>(exch + 8 * 4 * 64);  // [2 sets][2][64]
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w = w8 >> 1, h = w8 & 1;
+  const int nhb = p.kh * p.batch;
+  const int rest = (int)blockIdx.x / nhb;
+  const int hb = xcd_head((int)blockIdx.x % nhb, nhb);
+  const int split = rest % p.splits, kv0 = (rest / p.splits) * 128, kw0 = kv0 + 32 * w;
+  const Rows s(p, hb);
+  if (p.splits == 1) zero_keys<D, 512>(p, s, kv0, tid);
+  if (kv0 >= s.kvlen) return;      // uniform, before any barrier
+  int u0, u1;
+  slice_of((s.valid + 63) / 64, p.splits, split, u0, u1);
+  if (p.splits > 1 && u0 >= u1) return;
+  const int kpos[2] = {kw0 + lr, kw0 + 16 + lr};
+  const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
+  const bf16* const vb = p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D;
+
+  uint4 kf[2][KS], vf[2][KS];
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      vf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (kpos[c] < s.kvlen) {
+        kf[c][ks] = *reinterpret_cast<const uint4*>(kb + (long)kpos[c] * p.ldk + 32 * ks + 8 * lg);
+        vf[c][ks] = *reinterpret_cast<const uint4*>(vb + (long)kpos[c] * p.ldv + 32 * ks + 8 * lg);
+      }
+    }
+  f32x4 dkacc[DH][2], dvacc[DH][2];
+#pragma unroll
+  for (int dt = 0; dt < DH; ++dt) dkacc[dt][0] = dkacc[dt][1] = dvacc[dt][0] = dvacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const bf16* qfrag = smem + (32 * h + lr) * LD + 8 * lg;           // this wave's 32 rows of a tile
+  const bf16* dofrag = qfrag + 64 * LD;
+  const bf16* qtfrag = smem + tr_base<LD>(lane) + 16 * DH * h;      // its half of the head dimension
+  const bf16* dotfrag = qtfrag + 64 * LD;
+  uint4* const ex_mine = exch + (w8 * 4) * 64 + lane;
+  const uint4* const ex_theirs = exch + ((w8 ^ 1) * 4) * 64 + lane;
+
+  const bf16* const qb = p.q + (long)s.b * p.seq_q * p.ldq + (long)s.g * s.grp * D;
+  const bf16* const dob = p.dout + (long)s.b * p.seq_q * p.lddo + (long)s.g * s.grp * D;
+  uint4 qreg[T64::NREG], doreg[T64::NREG];
+  float st_reg = 0.f;
+  RowTile<D, 512> rows;
+  RowStat rstat;
+  rows.start(s, u0 * 64, tid);
+  rstat.start(p, s, u0 * 64, lane, w8);
+  auto prefetch = [&]() {
+    rows.load(qreg, qb, p.ldq, tid);
+    rows.load(doreg, dob, p.lddo, tid);
+    rows.next();
+    if (w8 < 2) st_reg = rstat.load();
+  };
+  if (u0 < u1) prefetch();
+
+  constexpr int AHEAD = 2;     // two waves per SIMD cover each other's LDS latency: a short ring is enough
+  auto update_half = [&](int set, int t2, const uint4 (&pf)[2], const uint4 (&df)[2]) {
+    constexpr int NU = 2 * DH;     // n = dt * 2 + which
+    auto ufrag_at = [&](int n) { return read_frag_tr<LD>(((n & 1) ? qtfrag : dotfrag) + set * TSET + 32 * t2 * LD + 16 * (n >> 1)); };
+    uint4 uring[AHEAD];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
+    MFMA_PHASE_BEGIN();
+#pragma unroll
+    for (int n = 0; n < NU; ++n) {
+      const uint4 a = uring[n % AHEAD];
+      if (n + AHEAD < NU) uring[n % AHEAD] = ufrag_at(n + AHEAD);
+      const int dt = n >> 1;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        if (n & 1) dkacc[dt][c] = mfma16(a, df[c], dkacc[dt][c]);
+        else dvacc[dt][c] = mfma16(a, pf[c], dvacc[dt][c]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    MFMA_PHASE_END();
+  };
+  // Two barriers per tile.  After the first one every wave is done with the previous tile's scores and has published its fragments: the
+  // new tile is stored (into the other set) while the accumulators take the partner's half of the PREVIOUS tile.
+  auto partner_update = [&](int prev) {
+    const uint4 ppf[2] = {ex_theirs[0], ex_theirs[64]};
+    const uint4 pdf[2] = {ex_theirs[128], ex_theirs[192]};
+    update_half(prev & 1, h ^ 1, ppf, pdf);
+  };
+  const int n_tiles = u1 - u0;
+  for (int i = 0; i < n_tiles; ++i) {
+    __syncthreads();
+    bf16* const q_set = smem + (i & 1) * TSET;
+    T64::template store<LD>(qreg, q_set, tid);
+    T64::template store<LD>(doreg, q_set + 64 * LD, tid);
+    if (w8 < 2) stat[128 * (i & 1) + 64 * w8 + lane] = row_start(st_reg, w8, (u0 + i) * 64 + lane < s.valid, p.scale);
+    if (i > 0) partner_update(i - 1);
+    __syncthreads();
+    if (i + 1 < n_tiles) prefetch();
+    f32x4 sc[2][2], dp[2][2], s0[2], dp0[2];      // [16 rows][16 keys]; what they start from
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      s0[qt] = *reinterpret_cast<const f32x4*>(stat + 128 * (i & 1) + 32 * h + 16 * qt + 4 * lg);
+      dp0[qt] = *reinterpret_cast<const f32x4*>(stat + 128 * (i & 1) + 64 + 32 * h + 16 * qt + 4 * lg);
+    }
+    {
+      constexpr int NS = 4 * KS;     // n = (ks * 2 + qt) * 2 + which
+      auto sfrag_at = [&](int n) { return *reinterpret_cast<const uint4*>(((n & 1) ? dofrag : qfrag) + (i & 1) * TSET + 16 * ((n >> 1) & 1) * LD + 32 * (n >> 2)); };
+      uint4 ring[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) ring[n] = sfrag_at(n);
+      MFMA_PHASE_BEGIN();
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        const uint4 a = ring[n % AHEAD];
+        if (n + AHEAD < NS) ring[n % AHEAD] = sfrag_at(n + AHEAD);
+        const int ks = n >> 2, qt = (n >> 1) & 1;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if (n & 1) dp[qt][c] = mfma16(a, vf[c][ks], ks == 0 ? dp0[qt] : dp[qt][c]);
+          else sc[qt][c] = mfma16(a, kf[c][ks], ks == 0 ? s0[qt] : sc[qt][c]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      MFMA_PHASE_END();
+    }
+    probabilities(sc, dp, p.scale_log2e);
+    const uint4 pfg[2] = {pack_frag(sc[0][0], sc[1][0]), pack_frag(sc[0][1], sc[1][1])};
+    const uint4 dfg[2] = {pack_frag(dp[0][0], dp[1][0]), pack_frag(dp[0][1], dp[1][1])};
+    // the partner read last tile's fragments before the barrier above: the slots are free
+    ex_mine[0] = pfg[0]; ex_mine[64] = pfg[1]; ex_mine[128] = dfg[0]; ex_mine[192] = dfg[1];
+    update_half(i & 1, h, pfg, dfg);
+  }
+  __syncthreads();
+  if (n_tiles > 0) partner_update(n_tiles - 1);
+  __syncthreads();
+  const long tok0 = (long)s.b * p.seq_kv;
+  const int d0 = s.g * D + h * (D / 2);
+  if (p.splits == 1) {
+    bf16* const stage = smem + w8 * 32 * (D / 2 + 8);
+    store_acc_T<D / 2>(dkacc, p.scale, stage, p.dk + tok0 * p.lddk + d0, p.lddk, kw0, s.kvlen, lane);
+    store_acc_T<D / 2>(dvacc, 1.f, stage, p.dv + tok0 * p.lddv + d0, p.lddv, kw0, s.kvlen, lane);
+  } else {
+    float* const stage = reinterpret_cast<float*>(smem) + w8 * 32 * (D / 2 + 4);
+    const long ldp = (long)p.kh * D, each = (long)p.batch * p.seq_kv * ldp;
+    float* const out = p.part + split * each + tok0 * ldp + d0;
+    store_acc_T_f32<D / 2>(dkacc, p.scale, stage, out, ldp, kw0, s.kvlen, lane);
+    store_acc_T_f32<D / 2>(dvacc, 1.f, stage, out + p.splits * each, ldp, kw0, s.kvlen, lane);
+  }
+}
+
+// dk, dv = the sum of a key's slices, in slice order; zero behind the sequence.  Eight elements of dk or of dv per thread.
+template <int D>
+__global__ void __launch_bounds__(256) cross_dkv_join_kernel(const CrossArgs p) {
+  const int ch_row = p.kh * (D / 8);
+  const long T = (long)p.batch * p.seq_kv, per = T * ch_row;
+  long idx = (long)blockIdx.x * 256 + threadIdx.x;
+  if (idx >= 2 * per) return;
+  const bool is_v = idx >= per;
+  if (is_v) idx -= per;
+  const long t = idx / ch_row;
+  const int c = (int)(idx - t * ch_row);
+  const int b = (int)(t / p.seq_kv), key = (int)(t - (long)b * p.seq_kv);
+  const Rows s(p, b * p.kh);
+  const int n = key < s.kvlen ? slices_used((s.valid + 63) / 64, p.splits) : 0;
+  const long each = T * p.kh * D;
+  const float* src = p.part + (is_v ? p.splits * each : 0) + t * p.kh * D + c * 8;
+  float acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  for (int i = 0; i < n; ++i, src += each) {
+    const float4 x0 = *reinterpret_cast<const float4*>(src), x1 = *reinterpret_cast<const float4*>(src + 4);
+    acc[0] += x0.x; acc[1] += x0.y; acc[2] += x0.z; acc[3] += x0.w;
+    acc[4] += x1.x; acc[5] += x1.y; acc[6] += x1.z; acc[7] += x1.w;
+  }
+  bf16* const dst = is_v ? p.dv + t * p.lddv + c * 8 : p.dk + t * p.lddk + c * 8;
+  *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]), pack_bf16x2(acc[4], acc[5]), pack_bf16x2(acc[6], acc[7]));
+}
+
+// operand tiles, or the epilogue's staging of every wave's 32 x d block, whichever is larger
+constexpr int max_i(int a, int b) { return a > b ? a : b; }
+constexpr int fwd_smem_bytes(int d, int nw) { return max_i((nw >= 8 ? 2 : 1) * (64 * (d + 8) + 64 * (d + 32)), nw * 32 * (d + 8)) * 2; }
+constexpr int dq_smem_bytes(int d, int nw) { return max_i((nw >= 8 ? 2 : 1) * (2 * 64 * tile_ld(d)), nw * 32 * (d + 8)) * 2; }
+constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 512, 4 * 32 * (d + 4) * 4); }
+constexpr int dkv_pair_smem_bytes(int d) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * 4 * 64 * 16 + 1024; }
+
+template <typename K>
+hipError_t launch(K kern, int grid, int threads, int smem, hipStream_t st, const CrossArgs& p) {
+  // (a host-side table entry, not a stream operation: allowed while a graph is captured)
+  if (smem > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != hipSuccess) return e;
+  }
+  RP_LAUNCH(kern, dim3(grid), dim3(threads), smem, st, p);
+  return hipGetLastError();
+}
+
+// Slices of a loop over `steps` tiles that would run in `groups` workgroups: enough for two workgroups per CU, each with
+// two tiles at least, as many as the scratch holds.
+int splits_for(long groups, int steps, size_t bytes_each, size_t scratch_bytes) {
+  if (groups < 1 || groups >= 256 || steps < 4) return 1;
+  long n = 512 / groups;
+  if (n > steps / 2) n = steps / 2;
+  if (bytes_each && n > (long)(scratch_bytes / bytes_each)) n = (long)(scratch_bytes / bytes_each);
+  return n < 2 ? 1 : (int)n;
+}
+int ceil_div(long a, int b) { return (int)((a + b - 1) / b); }
+long row_count(const CrossArgs& p) { return (long)(p.a / p.kh) * p.seq_q; }
+size_t row_part_bytes(const CrossArgs& p, int d) { return (size_t)p.kh * p.batch * row_count(p) * (d + 2) * 4; }      // o or dq, and (m, l)
+size_t key_part_bytes(const CrossArgs& p, int d) { return (size_t)2 * p.batch * p.seq_kv * p.kh * d * 4; }
+int row_splits(const CrossArgs& p, int d, size_t bytes) { return splits_for((long)ceil_div(row_count(p), 128) * p.kh * p.batch, ceil_div(p.seq_kv, 64), row_part_bytes(p, d), bytes); }
+int key_splits(const CrossArgs& p, int d, size_t bytes) { return splits_for((long)ceil_div(p.seq_kv, 128) * p.kh * p.batch, ceil_div(row_count(p), 64), key_part_bytes(p, d), bytes); }
+
+template <int D>
+hipError_t fwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
+  const int nhb = p.kh * p.batch;
+  const long rows = row_count(p);
+  p.splits = row_splits(p, D, bytes);
+  if (p.splits > 1) {
+    p.part = static_cast<float*>(scratch);
+    p.part_ml = reinterpret_cast<float2*>(p.part + (size_t)p.splits * nhb * rows * D);
+    const hipError_t e = launch(cross_fwd_kernel<D, 4, true>, ceil_div(rows, 128) * nhb * p.splits, 256, fwd_smem_bytes(D, 4), st, p);
+    if (e != hipSuccess) return e;
+    return launch(cross_fwd_join_kernel<D>, ceil_div(nhb * rows * (D / 8), 256), 256, 0, st, p);
+  }
+  if (D == 128 && (long)ceil_div(rows, 256) * nhb >= 1024)
+    return launch(cross_fwd_kernel<D, 8, false>, ceil_div(rows, 256) * nhb, 512, fwd_smem_bytes(D, 8), st, p);
+  return launch(cross_fwd_kernel<D, 4, false>, ceil_div(rows, 128) * nhb, 256, fwd_smem_bytes(D, 4), st, p);
+}
+
+template <int D>
+hipError_t bwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
+  const int nhb = p.kh * p.batch;
+  const long rows = row_count(p);
+  p.part = static_cast<float*>(scratch);
+  // dQ first: it works out delta, which dK/dV reads
+  p.splits = row_splits(p, D, bytes);
+  hipError_t e = hipSuccess;
+  if (rows == 0) {
+    // no queries: dk and dv are zero
+  } else if (p.splits > 1) {
+    e = launch(cross_dq_kernel<D, 4, true>, ceil_div(rows, 128) * nhb * p.splits, 256, dq_smem_bytes(D, 4), st, p);
+    if (e == hipSuccess) e = launch(cross_dq_join_kernel<D>, ceil_div(nhb * rows * (D / 8), 256), 256, 0, st, p);
+  } else if (D == 128 && (long)ceil_div(rows, 256) * nhb >= 1024) {
+    e = launch(cross_dq_kernel<D, 8, false>, ceil_div(rows, 256) * nhb, 512, dq_smem_bytes(D, 8), st, p);
+  } else {
+    e = launch(cross_dq_kernel<D, 4, false>, ceil_div(rows, 128) * nhb, 256, dq_smem_bytes(D, 4), st, p);
+  }
+  if (e != hipSuccess || p.seq_kv == 0) return e;
+  p.splits = key_splits(p, D, bytes);
+  const int grid = ceil_div(p.seq_kv, 128) * nhb * p.splits;
+  if constexpr (D == 128) e = launch(cross_dkv_pair_kernel<D>, grid, 512, dkv_pair_smem_bytes(D), st, p);
+  else e = launch(cross_dkv_kernel<D>, grid, 256, dkv_smem_bytes(D), st, p);
+  if (e != hipSuccess || p.splits == 1) return e;
+  return launch(cross_dkv_join_kernel<D>, ceil_div((long)2 * p.batch * p.seq_kv * p.kh * (D / 8), 256), 256, 0, st, p);
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------------------ launchers
+void k_cross_attn_scratch(const CrossArgs& p, int d, size_t* fwd_bytes, size_t* bwd_bytes) {
+  const size_t all = ~(size_t)0;
+  const int rs = row_splits(p, d, all), ks = key_splits(p, d, all);
+  const size_t r = rs > 1 ? rs * row_part_bytes(p, d) : 0, k = ks > 1 ? ks * key_part_bytes(p, d) : 0;
+  *fwd_bytes = r;
+  *bwd_bytes = r > k ? r : k;
+}
+
+hipError_t k_cross_attn_fwd(hipStream_t st, const CrossArgs& p, int d, void* scratch, size_t bytes) {
+  if (p.batch == 0 || p.seq_q == 0) return hipSuccess;
+  return d == 128 ? fwd<128>(st, p, scratch, bytes) : fwd<64>(st, p, scratch, bytes);
+}
+
+hipError_t k_cross_attn_bwd(hipStream_t st, const CrossArgs& p, int d, void* scratch, size_t bytes) {
+  if (p.batch == 0 || (p.seq_q == 0 && p.seq_kv == 0)) return hipSuccess;
+  return d == 128 ? bwd<128>(st, p, scratch, bytes) : bwd<64>(st, p, scratch, bytes);
+}

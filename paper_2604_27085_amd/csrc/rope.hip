@@ -1,0 +1,205 @@
+// Rotary positions beyond the stage's own (elementwise.hip: half-split pairs over the whole head, one base): both pair layouts, a
+// rotated part of the head, positions given per token, and the tables of contexts longer than the trained one.
+//
+// A pair (x, y) of a head at position p turns by the angle p theta_i:  (x c - y s, x s + y c) with (c, s) = A (cos, sin)(p theta_i).
+// The rotation is linear, so its backward is the transpose: the same with -s, on the gradients.
+#include "layer_ops.hpp"
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------ table
+// cs[p][i] = A (cos, sin)(p theta_i).  Angles are kept as turns, p theta_i / 2 pi, in 64 bits: only then does a position of 2^20 leave the
+// 30 bits of a turn that an fp32 cosine needs.  The whole turns and the quarter turns come off exactly, which leaves |x| <= pi / 4, where
+// the Taylor polynomials of sine (to x^11) and cosine (to x^12) are off by less than 1e-11.  A thread keeps one frequency, whose
+// exponential costs more than a position does, over its positions.
+RP_DEV double frequency(const RopeScale& r, int i) {      // turns a position
+  const double theta = exp2(-(double)i * r.log2_base_step);
+  double f = 1.0;
+  if (r.by_parts) {
+    const double turns = r.trained_len * theta * 0.15915494309189535;
+    const double keep = fmin(fmax((turns - r.slow) * r.inv_span, 0.0), 1.0);
+    f = keep + (1.0 - keep) * r.inv_factor;
+  } else {
+    f = r.inv_factor;
+  }
+  return theta * f * 0.15915494309189535;
+}
+
+RP_DEV float2 cos_sin_turns(double turns, double amplitude) {
+  double t = turns - rint(turns);          // [-1/2, 1/2]: exact
+  const double quarter = rint(4.0 * t);
+  const double x = fma(quarter, -0.25, t) * 6.283185307179586;
+  const double z = x * x;
+  double s = -1.0 / 39916800.0, c = 1.0 / 479001600.0;
+  s = fma(s, z, 1.0 / 362880.0);
+  c = fma(c, z, -1.0 / 3628800.0);
+  s = fma(s, z, -1.0 / 5040.0);
+  c = fma(c, z, 1.0 / 40320.0);
+  s = fma(s, z, 1.0 / 120.0);
+  c = fma(c, z, -1.0 / 720.0);
+  s = fma(s, z, -1.0 / 6.0);
+  c = fma(c, z, 1.0 / 24.0);
+  s = fma(s * z, x, x);
+  c = fma(c, z, -0.5);
+  c = fma(c, z, 1.0);
+  const int q = (int)quarter & 3;          // -2 and 2 are the same half turn
+  const double co = (q & 1) ? s : c, si = (q & 1) ? c : s;
+  return make_float2((float)((q == 1 || q == 2) ? -amplitude * co : amplitude * co), (float)((q & 2) ? -amplitude * si : amplitude * si));
+}
+
+// Thread = one pair index and every (rows a block)-th of the block's positions.
+__global__ void __launch_bounds__(256) rope_table_scaled_kernel(float2* __restrict__ cs, int n_pos, int half, int rows, int per_block, const RopeScale r) {
+  const int i0 = (int)threadIdx.x % half, lane_row = (int)threadIdx.x / half;      // (half <= 256)
+  if (lane_row >= rows) return;
+  const double f = frequency(r, i0);
+  const long p0 = (long)blockIdx.x * per_block;
+  for (int k = lane_row; k < per_block; k += rows) {
+    const long p = p0 + k;
+    if (p >= n_pos) break;
+    cs[p * half + i0] = cos_sin_turns((double)p * f, r.amplitude);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ rotation
+template <int V> struct Words;
+template <> struct Words<8> { typedef uint4 type; };
+template <> struct Words<4> { typedef uint2 type; };
+template <> struct Words<2> { typedef uint32_t type; };
+template <> struct Words<1> { typedef unsigned short type; };
+
+template <int V>
+RP_DEV void unpack(const typename Words<V>::type& w, float (&f)[V]) {
+  if constexpr (V == 1) {
+    f[0] = bf16_bits_to_f32(w);
+  } else {
+    const uint32_t* u = reinterpret_cast<const uint32_t*>(&w);
+#pragma unroll
+    for (int e = 0; e < V / 2; ++e) { f[2 * e] = bf16_lo(u[e]); f[2 * e + 1] = bf16_hi(u[e]); }
+  }
+}
+template <int V>
+RP_DEV typename Words<V>::type pack(const float (&f)[V]) {
+  typename Words<V>::type w;
+  if constexpr (V == 1) {
+    w = (unsigned short)f32_to_bf16_bits(f[0]);
+  } else {
+    uint32_t* u = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+    for (int e = 0; e < V / 2; ++e) u[e] = pack_bf16x2(f[2 * e], f[2 * e + 1]);
+  }
+  return w;
+}
+
+// A thread owns the same V elements of NH heads of one token, so that what it reads of the table serves all of them, and has their loads
+// in flight together.  Half-split pairs (PAIRS false): V pairs, elements u V .. of both halves of the rotated part; neighbouring pairs:
+// V / 2 pairs.  Units past the rotated part carry the rest of the head over (none when the call is in place: nunits leaves them out).
+// Bound by memory: every element is read and written once.  Each thread reads all it changes before it writes, so in == out is fine.
+template <int V, bool PAIRS, int NH>
+__global__ void __launch_bounds__(256) rope_kernel(const RotateArgs p) {
+  constexpr int NCS = PAIRS ? (V + 1) / 2 : V;
+  typedef typename Words<V>::type word;
+  const int heads = p.a + p.k, nhg = (heads + NH - 1) / NH;
+  const int per = nhg * p.nunits;
+  const int nrot = PAIRS ? p.rot / V : p.rot / (2 * V);     // units of the rotated part
+  const int tl = (int)threadIdx.x / per;
+  const int t = (int)blockIdx.x * p.tokens_per_block + (p.tokens_per_block > 1 ? tl : 0);
+  if (t >= p.T || (p.tokens_per_block > 1 && tl >= p.tokens_per_block)) return;
+  const int pos = p.pos ? p.pos[t] : t % p.seq;
+  const bool in_table = pos >= 0 && pos < p.n_pos;
+  for (int it = p.tokens_per_block > 1 ? (int)threadIdx.x - tl * per : (int)threadIdx.x; it < per; it += 256) {
+    const int u = it % p.nunits, h0 = it / p.nunits;
+    const bool turn = u < nrot;
+    const int x0 = turn ? u * V : p.rot + (u - nrot) * V;
+    float co[NCS], si[NCS];
+    if (turn) {
+      const float2* row = p.cs + (long)pos * (p.rot / 2) + u * NCS;
+#pragma unroll
+      for (int e = 0; e < NCS; ++e) {
+        const float2 v = in_table ? row[e] : make_float2(NAN, NAN);
+        co[e] = v.x;
+        si[e] = p.bwd ? -v.y : v.y;
+      }
+    }
+    word w0[NH], w1[NH];
+#pragma unroll
+    for (int i = 0; i < NH; ++i) {
+      const int head = h0 + i * nhg;
+      if (head >= heads) break;
+      const bf16* src = head < p.a ? p.in_q + (long)t * p.ld_in_q + (long)head * p.d : p.in_k + (long)t * p.ld_in_k + (long)(head - p.a) * p.d;
+      w0[i] = *reinterpret_cast<const word*>(src + x0);
+      if (!PAIRS && turn) w1[i] = *reinterpret_cast<const word*>(src + x0 + p.rot / 2);
+    }
+#pragma unroll
+    for (int i = 0; i < NH; ++i) {
+      const int head = h0 + i * nhg;
+      if (head >= heads) break;
+      bf16* dst = head < p.a ? p.out_q + (long)t * p.ld_out_q + (long)head * p.d : p.out_k + (long)t * p.ld_out_k + (long)(head - p.a) * p.d;
+      if (turn) {
+        float x[V];
+        unpack<V>(w0[i], x);
+        if constexpr (PAIRS) {
+#pragma unroll
+          for (int e = 0; e < V / 2; ++e) {
+            const float a = x[2 * e], b = x[2 * e + 1];
+            x[2 * e] = a * co[e] - b * si[e];
+            x[2 * e + 1] = b * co[e] + a * si[e];
+          }
+        } else {
+          float y[V], z[V];
+          unpack<V>(w1[i], y);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            z[e] = y[e] * co[e] + x[e] * si[e];
+            x[e] = x[e] * co[e] - y[e] * si[e];
+          }
+          *reinterpret_cast<word*>(dst + x0 + p.rot / 2) = pack<V>(z);
+        }
+        w0[i] = pack<V>(x);
+      }
+      *reinterpret_cast<word*>(dst + x0) = w0[i];
+    }
+  }
+}
+
+template <int V, bool PAIRS>
+hipError_t launch_rope(hipStream_t st, RotateArgs p, bool in_place) {
+  constexpr int NH = 4;
+  const int heads = p.a + p.k;
+  p.nunits = (PAIRS ? p.rot / V : p.rot / (2 * V)) + (in_place ? 0 : (p.d - p.rot) / V);
+  const int per = ((heads + NH - 1) / NH) * p.nunits;
+  p.tokens_per_block = per < 256 ? 256 / per : 1;
+  const int blocks = (int)(((long)p.T + p.tokens_per_block - 1) / p.tokens_per_block);
+  RP_LAUNCH((rope_kernel<V, PAIRS, NH>), dim3(blocks), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------------------ launchers
+hipError_t k_rope_table_scaled(hipStream_t st, float2* cs, int n_pos, int rot, const RopeScale& r) {
+  if (n_pos == 0) return hipSuccess;
+  const int half = rot / 2;
+  const int rows = 256 / half;
+  // enough blocks to fill the chip; then positions share a frequency's exponential, 16 a thread at most
+  int each = (int)((long)n_pos / ((long)rows * 2048));
+  each = each < 1 ? 1 : each > 16 ? 16 : each;
+  const int per_block = rows * each;
+  RP_LAUNCH(rope_table_scaled_kernel, dim3((unsigned)(((long)n_pos + per_block - 1) / per_block)), dim3(256), 0, st, cs, n_pos, half, rows, per_block, r);
+  return hipGetLastError();
+}
+
+// Elements per access: the widest power of two that divides the rotated part (its half, for half-split pairs) is right for every row,
+// whose starts are multiples of 16 bytes.
+hipError_t k_rope(hipStream_t st, int layout, const RotateArgs& p) {
+  if (p.T == 0 || p.a + p.k == 0) return hipSuccess;
+  const bool in_place = p.in_q == p.out_q && (p.k == 0 || p.in_k == p.out_k);
+  if (layout) {
+    if (p.rot % 8 == 0) return launch_rope<8, true>(st, p, in_place);
+    return launch_rope<2, true>(st, p, in_place);
+  }
+  const int half = p.rot / 2;
+  if (half % 8 == 0) return launch_rope<8, false>(st, p, in_place);
+  if (half % 4 == 0) return launch_rope<4, false>(st, p, in_place);
+  if (half % 2 == 0) return launch_rope<2, false>(st, p, in_place);
+  return launch_rope<1, false>(st, p, in_place);
+}

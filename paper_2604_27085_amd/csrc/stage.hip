@@ -12,6 +12,7 @@
 #include "../../include/rp_ops.h"
 #include "gemm.hpp"
 #include "kernels.hpp"
+#include "layer_ops.hpp"
 #include "layout.hpp"
 #include "transfers.hpp"
 
@@ -1277,6 +1278,162 @@ rp_status rp_op_attn_bwd(void* stream, const void* q, const void* k, const void*
   for (int i = 0; i < 3 && e == hipSuccess; ++i)
     e = k_attn_bwd(st, order[in_place][i], q, k, v, dout, lse, delta, dq, dk, dv, scratch, ldq, ldk, ldv, lddo, lddq, lddk, lddv, batch, seq,
                    a, kh, d, nullptr, in_place ? nullptr : o, ldo);
+  OP_RET(e);
+}
+
+
+// ---- rotary positions, cross attention, balance loss ------------------------------------------------------------------
+// Makes the stream's device current for a call, and puts back what was.
+namespace {
+struct StreamDevice {
+  int before = -1;
+  hipError_t err = hipSuccess;
+  explicit StreamDevice(hipStream_t st) {
+    if (!st) return;
+    int now = -1;
+    hipDevice_t dev = -1;
+    err = hipGetDevice(&now);
+    if (err == hipSuccess) err = hipStreamGetDevice(st, &dev);
+    if (err != hipSuccess || dev == now) return;
+    err = hipSetDevice(dev);
+    if (err == hipSuccess) before = now;
+  }
+  ~StreamDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+bool off16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 != 0; }
+
+// A [rows, heads, d] tensor with a row stride: present unless it is empty, on 16-byte boundaries, rows apart.
+bool bad_heads(const void* p, long rows, int heads, int d, long ld) {
+  return (rows > 0 && heads > 0 && !p) || off16(p) || ld % 8 || ld < (long)heads * d || ld > (1l << 23);
+}
+}  // namespace
+
+rp_status rp_op_rope_table_scaled(void* stream, void* cs, const rp_rope_scaling* s, int n_pos, int rot) {
+  if (!s || s->struct_size != sizeof(rp_rope_scaling)) return fail(nullptr, RP_EINVAL, "rp_op_rope_table_scaled: scaling is NULL or of another size");
+  if (n_pos < 0 || (n_pos && !cs) || reinterpret_cast<uintptr_t>(cs) % 8 || rot < 2 || rot > 512 || rot % 2)
+    return fail(nullptr, RP_EINVAL, "rp_op_rope_table_scaled: bad arguments");
+  if (s->kind < RP_ROPE_PLAIN || s->kind > RP_ROPE_BY_PARTS || !(s->base > 0.f) || !isfinite(s->base) || !isfinite(s->amplitude) ||
+      (s->kind != RP_ROPE_PLAIN && (!(s->factor > 0.f) || !isfinite(s->factor))) || (s->kind == RP_ROPE_BASE && rot == 2) ||
+      (s->kind == RP_ROPE_BY_PARTS && (!(s->slow < s->fast) || !isfinite(s->fast - s->slow) || s->trained_len <= 0)))
+    return fail(nullptr, RP_EINVAL, "rp_op_rope_table_scaled: bad scaling");
+  RopeScale r{};
+  const double base = s->kind == RP_ROPE_BASE ? log2((double)s->base) + log2((double)s->factor) * rot / (rot - 2.0) : log2((double)s->base);
+  r.log2_base_step = 2.0 * base / rot;
+  r.by_parts = s->kind == RP_ROPE_BY_PARTS;
+  r.inv_factor = r.by_parts || s->kind == RP_ROPE_LINEAR ? 1.0 / (double)s->factor : 1.0;
+  if (r.by_parts) { r.trained_len = s->trained_len; r.slow = s->slow; r.inv_span = 1.0 / ((double)s->fast - (double)s->slow); }
+  r.amplitude = s->amplitude;
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_rope_table_scaled(reinterpret_cast<hipStream_t>(stream), static_cast<float2*>(cs), n_pos, rot, r);
+  OP_RET(e);
+}
+
+rp_status rp_op_rope(void* stream, int bwd, int layout, int d, int rot, const void* in_q, const void* in_k, long ld_in_q, long ld_in_k, void* out_q,
+                     void* out_k, long ld_out_q, long ld_out_k, const void* cs, int n_pos, const int* pos, int T, int seq, int a, int k) {
+  if (T < 0 || a < 0 || k < 0 || layout < 0 || layout > 1 || d < 8 || d > 512 || d % 8 || rot < 2 || rot > d || rot % 2 || n_pos < 0 || (n_pos && !cs) ||
+      reinterpret_cast<uintptr_t>(cs) % 8 || (!pos && (seq <= 0 || n_pos < (T < seq ? T : seq))))
+    return fail(nullptr, RP_EINVAL, "rp_op_rope: bad arguments");
+  if ((a && (bad_heads(in_q, T, a, d, ld_in_q) || bad_heads(out_q, T, a, d, ld_out_q))) ||
+      (k && (bad_heads(in_k, T, k, d, ld_in_k) || bad_heads(out_k, T, k, d, ld_out_k))))
+    return fail(nullptr, RP_EINVAL, "rp_op_rope: heads missing, not on 16-byte boundaries, or bad strides");
+  if ((a && in_q == out_q && ld_in_q != ld_out_q) || (k && in_k == out_k && ld_in_k != ld_out_k))
+    return fail(nullptr, RP_EINVAL, "rp_op_rope: in place, the strides have to agree");
+  RotateArgs p{};
+  p.in_q = static_cast<const bf16*>(in_q); p.in_k = static_cast<const bf16*>(in_k); p.out_q = static_cast<bf16*>(out_q); p.out_k = static_cast<bf16*>(out_k);
+  p.ld_in_q = ld_in_q; p.ld_in_k = ld_in_k; p.ld_out_q = ld_out_q; p.ld_out_k = ld_out_k;
+  p.cs = static_cast<const float2*>(cs); p.pos = pos; p.n_pos = n_pos; p.T = T; p.seq = seq; p.a = a; p.k = k; p.d = d; p.rot = rot; p.bwd = bwd != 0;
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_rope(reinterpret_cast<hipStream_t>(stream), layout, p);
+  OP_RET(e);
+}
+
+namespace {
+// Sizes that the cross attention's kernels cover; fills what they share.
+bool cross_args(CrossArgs& p, int batch, int seq_q, int seq_kv, int a, int kh, int d, float scale) {
+  if (batch < 0 || seq_q < 0 || seq_kv < 0 || a <= 0 || kh <= 0 || a % kh || (d != 64 && d != 128) || !(scale > 0.f) || !isfinite(scale)) return false;
+  // rows of a key head, and workgroups and threads of every launch (up to 256 slices of 128 rows or keys, 16 threads a row), are counted in 31 bits
+  const double rows = (double)(a / kh) * seq_q, nhb = (double)kh * batch;
+  if (rows > 1.0e9 || seq_kv > 1000000000 || rows * nhb * (d / 8) > 2.0e9 || 2.0 * nhb * seq_kv * (d / 8) > 256.0 * 2.0e9) return false;
+  p.batch = batch; p.seq_q = seq_q; p.seq_kv = seq_kv; p.a = a; p.kh = kh;
+  p.scale = scale;
+  p.scale_log2e = scale * 1.4426950408889634f;
+  return true;
+}
+}  // namespace
+
+rp_status rp_op_cross_attn_scratch(int batch, int seq_q, int seq_kv, int a, int kh, int d, size_t* fwd_bytes, size_t* bwd_bytes) {
+  CrossArgs p{};
+  if (!cross_args(p, batch, seq_q, seq_kv, a, kh, d, 1.f)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_scratch: bad arguments");
+  size_t f = 0, b = 0;
+  k_cross_attn_scratch(p, d, &f, &b);
+  if (fwd_bytes) *fwd_bytes = f;
+  if (bwd_bytes) *bwd_bytes = b;
+  return RP_OK;
+}
+
+rp_status rp_op_cross_attn_fwd(void* stream, const void* q, const void* k, const void* v, void* o, float* lse, long ldq, long ldk, long ldv, long ldo,
+                               const int* q_len, const int* kv_len, int batch, int seq_q, int seq_kv, int a, int kh, int d, float scale, void* scratch,
+                               size_t scratch_bytes) {
+  CrossArgs p{};
+  if (!cross_args(p, batch, seq_q, seq_kv, a, kh, d, scale)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_fwd: bad sizes or scale");
+  const long tq = (long)batch * seq_q, tk = (long)batch * seq_kv;
+  if (bad_heads(q, tq, a, d, ldq) || bad_heads(o, tq, a, d, ldo) || bad_heads(k, tk, kh, d, ldk) || bad_heads(v, tk, kh, d, ldv))
+    return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_fwd: tensors missing, not on 16-byte boundaries, or bad strides");
+  if (off16(scratch) || (scratch_bytes && !scratch)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_fwd: bad scratch");
+  p.q = static_cast<const bf16*>(q); p.k = static_cast<const bf16*>(k); p.v = static_cast<const bf16*>(v); p.o = static_cast<bf16*>(o); p.lse = lse;
+  p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo; p.q_len = q_len; p.kv_len = kv_len;
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_cross_attn_fwd(reinterpret_cast<hipStream_t>(stream), p, d, scratch, scratch_bytes);
+  OP_RET(e);
+}
+
+rp_status rp_op_cross_attn_bwd(void* stream, const void* q, const void* k, const void* v, const void* o, const void* dout, const float* lse, float* delta,
+                               void* dq, void* dk, void* dv, long ldq, long ldk, long ldv, long ldo, long lddo, long lddq, long lddk, long lddv,
+                               const int* q_len, const int* kv_len, int batch, int seq_q, int seq_kv, int a, int kh, int d, float scale, void* scratch,
+                               size_t scratch_bytes) {
+  CrossArgs p{};
+  if (!cross_args(p, batch, seq_q, seq_kv, a, kh, d, scale)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_bwd: bad sizes or scale");
+  const long tq = (long)batch * seq_q, tk = (long)batch * seq_kv;
+  if (bad_heads(q, tq, a, d, ldq) || bad_heads(o, tq, a, d, ldo) || bad_heads(dout, tq, a, d, lddo) || bad_heads(dq, tq, a, d, lddq) ||
+      bad_heads(k, tk, kh, d, ldk) || bad_heads(v, tk, kh, d, ldv) || bad_heads(dk, tk, kh, d, lddk) || bad_heads(dv, tk, kh, d, lddv) ||
+      (tq && (!lse || !delta)))
+    return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_bwd: tensors missing, not on 16-byte boundaries, or bad strides");
+  if (off16(scratch) || (scratch_bytes && !scratch)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_bwd: bad scratch");
+  p.q = static_cast<const bf16*>(q); p.k = static_cast<const bf16*>(k); p.v = static_cast<const bf16*>(v); p.o_in = static_cast<const bf16*>(o);
+  p.dout = static_cast<const bf16*>(dout); p.lse_in = lse; p.delta = delta;
+  p.dq = static_cast<bf16*>(dq); p.dk = static_cast<bf16*>(dk); p.dv = static_cast<bf16*>(dv);
+  p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo; p.lddo = lddo; p.lddq = lddq; p.lddk = lddk; p.lddv = lddv; p.q_len = q_len; p.kv_len = kv_len;
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_cross_attn_bwd(reinterpret_cast<hipStream_t>(stream), p, d, scratch, scratch_bytes);
+  OP_RET(e);
+}
+
+rp_status rp_op_moe_balance_scratch(int T, int seq, int E, size_t* scratch_bytes) {
+  if (!scratch_bytes || T < 0 || seq <= 0 || T % seq || E <= 0 || E > 1024) return fail(nullptr, RP_EINVAL, "rp_op_moe_balance_scratch: bad arguments");
+  *scratch_bytes = k_moe_balance_scratch(T, seq, E);
+  return RP_OK;
+}
+
+rp_status rp_op_moe_balance(void* stream, const float* logits, const int* idx, const unsigned char* mask, int T, int seq, int E, int top_k, float coef,
+                            float z_coef, float grad_scale, int* counts, int* tokens, float* loss_out, const float* dlogits_in, float* dlogits,
+                            void* scratch, size_t scratch_bytes) {
+  if (T < 0 || seq <= 0 || T % seq || E <= 0 || E > 1024 || top_k <= 0 || top_k > E || !tokens || !loss_out || (T && (!logits || !idx || !counts)) ||
+      (dlogits_in && !dlogits))
+    return fail(nullptr, RP_EINVAL, "rp_op_moe_balance: bad arguments");
+  if (T && (!scratch || off16(scratch) || scratch_bytes < k_moe_balance_scratch(T, seq, E)))
+    return fail(nullptr, RP_EINVAL, "rp_op_moe_balance: scratch holds %zu bytes, %zu needed", scratch ? scratch_bytes : 0, k_moe_balance_scratch(T, seq, E));
+  BalanceArgs p{};
+  p.logits = logits; p.idx = idx; p.mask = mask; p.dlogits_in = dlogits_in; p.dlogits = dlogits; p.counts = counts; p.tokens = tokens; p.loss = loss_out;
+  p.seq = seq; p.E = E; p.top_k = top_k; p.coef = coef; p.z_coef = z_coef; p.grad_scale = grad_scale;
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_moe_balance(reinterpret_cast<hipStream_t>(stream), p, T, scratch);
   OP_RET(e);
 }
 
