@@ -144,7 +144,7 @@ RP_API rp_status rp_op_rope(void* stream, int bwd, int layout, int d, int rot, c
 /* Grouped-query attention of every query to all keys of another sequence (a decoder's cross attention; with few queries, the step of a
  * generation), flash style.  q, o [batch * seq_q, a, d]; k, v [batch * seq_kv, kh, d], d 64 or 128; row strides ld* in elements; any lengths from 0
  * on.  q_len, kv_len [dev] int32 [batch], or NULL for full sequences: how many rows of a padded sequence are in use.  Keys behind kv_len
- * are not read; rows of o behind q_len, and all rows where kv_len is 0, become 0.  scale > 0 multiplies q.k.  lse fp32 [batch, a, seq_q]
+ * are not read; rows of o behind q_len, and all rows where kv_len is 0, become 0.  scale (1e-30 to 1e30) multiplies q.k.  lse fp32 [batch, a, seq_q]
  * (natural log; -inf for the rows that become 0), or NULL.
  * scratch [dev, scratch_bytes] or NULL: where there are few rows, the keys are cut into slices that are joined in order, as many as its size
  * allows (rp_op_cross_attn_scratch: what the calls make use of).  It holds nothing between calls; two calls that may run at the same time need

@@ -9,15 +9,16 @@
 // pass gives both, and no mean probability is ever formed.
 //
 //   count : choices and valid tokens of a slice of a group, in LDS (integers: any order gives the same), a row of counts per slice
-//   rows  : a few lanes hold a token's logits; every block first adds the slices' counts of its group up; loss terms leave one pair of fp32 sums
-//           per block
+//   rows  : a few lanes hold a token's logits, the next token's on their way; every block first adds the slices' counts of its group up; loss
+//           terms leave one pair of fp32 sums per block
 //   total : one block adds the pairs in a fixed order
+//   small : all of it in one block, for batches that one block is through with before the other launches would have started
 #include "kernels.hpp"
 #include "layer_ops.hpp"
 
 namespace {
 
-// Sum over the lanes of a block, in 64 bits where it counts: thread 0 has it.  red: one entry per wave.
+// Sum over the threads of a block, in all of them.  red: one entry per wave.
 template <typename T>
 RP_DEV T block_sum(T v, T* red) {
 #pragma unroll
@@ -30,33 +31,41 @@ RP_DEV T block_sum(T v, T* red) {
   return s;
 }
 
-// hist[g][slice][e], tok[g][slice].  Choices outside 0 .. E-1 are not counted.
-__global__ void __launch_bounds__(256) balance_count_kernel(const BalanceArgs p) {
-  __shared__ int s_hist[1024];
-  __shared__ int red[4];
-  const int tid = threadIdx.x, slice = (int)blockIdx.x % p.slices;
-  const long g = (int)blockIdx.x / p.slices;
-  for (int e = tid; e < p.E; e += 256) s_hist[e] = 0;
+// Counts the choices of tokens t0 .. t1 - 1 of a group into s_hist [E] (zeroed here); returns the number of valid ones, in all threads.
+// Choices outside 0 .. E-1 are not counted.
+template <int NT>
+RP_DEV int count_choices(const BalanceArgs& p, long base, int t0, int t1, int* s_hist, int* red) {
+  const int tid = threadIdx.x;
+  for (int e = tid; e < p.E; e += NT) s_hist[e] = 0;
   __syncthreads();
-  const int per = (p.seq + p.slices - 1) / p.slices;
-  const int t0 = slice * per, t1 = t0 + per < p.seq ? t0 + per : p.seq;
-  const long base = g * p.seq;
   int valid = 0;
   if (p.mask) {
-    for (int t = t0 + tid; t < t1; t += 256) valid += p.mask[base + t] != 0;
+    for (int t = t0 + tid; t < t1; t += NT) valid += p.mask[base + t] != 0;
   } else if (tid == 0) {
-    valid = t1 > t0 ? t1 - t0 : 0;
+    valid = t1 - t0;
   }
-  const long n = t1 > t0 ? (long)(t1 - t0) * p.top_k : 0;
   const int* const idx = p.idx + (base + t0) * p.top_k;
-  for (long i = tid; i < n; i += 256) {
+  const unsigned n = (unsigned)(t1 - t0) * (unsigned)p.top_k;
+#pragma unroll 8
+  for (unsigned i = tid; i < n; i += NT) {
     const int e = idx[i];
-    if (e >= 0 && e < p.E && (!p.mask || p.mask[base + t0 + i / p.top_k])) atomicAdd(&s_hist[e], 1);
+    if (e >= 0 && e < p.E && (!p.mask || p.mask[base + t0 + (int)(i / (unsigned)p.top_k)])) atomicAdd(&s_hist[e], 1);
   }
-  const int all = block_sum(valid, red);      // (its barriers order the counts as well)
-  int* const out = p.hist + (g * p.slices + slice) * p.E;
-  for (int e = tid; e < p.E; e += 256) out[e] = s_hist[e];
-  if (tid == 0) p.tok[g * p.slices + slice] = all;
+  return block_sum(valid, red);      // (its barriers order the counts as well)
+}
+
+// hist[g][slice][e], tok[g][slice]
+__global__ void __launch_bounds__(1024) balance_count_kernel(const BalanceArgs p) {
+  __shared__ int s_hist[1024];
+  __shared__ int red[16];
+  const int tid = threadIdx.x, slice = (int)blockIdx.x % p.slices;
+  const long g = (int)blockIdx.x / p.slices;
+  const int per = (p.seq + p.slices - 1) / p.slices;
+  const int t0 = min(slice * per, p.seq), t1 = min(t0 + per, p.seq);
+  const int valid = count_choices<1024>(p, g * p.seq, t0, t1, s_hist, red);
+  int* const out = p.hist + (long)blockIdx.x * p.E;
+  for (int e = tid; e < p.E; e += 1024) out[e] = s_hist[e];
+  if (tid == 0) p.tok[blockIdx.x] = valid;
 }
 
 // Tokens of all groups, for masked batches of many groups (else the rows' blocks add them up themselves).
@@ -68,18 +77,106 @@ __global__ void __launch_bounds__(1024) balance_tokens_kernel(const BalanceArgs 
   if (threadIdx.x == 0) p.tokens[p.groups] = n;
 }
 
-// L lanes per token, C accesses of VEC logits a lane: element (lane + L i) VEC + v.
+// A block's share of the rows: L lanes per token, C accesses of VEC logits a lane, element (lane + L i) VEC + v.
+template <int L, int C, int VEC, int NT>
+struct RowPass {
+  typedef float fvec __attribute__((ext_vector_type(VEC)));
+  static constexpr int ROWS = NT / L;
+  fvec x[C], given[C];
+  bool on;
+
+  // the logits of token t of the group, and what is there of the gradient; -inf where there is no token, or a padded one
+  RP_DEV void load(const BalanceArgs& p, long base, int t, int t1, int sub) {
+    const bool in = t < t1;
+    const long row = base + t;
+    on = in && (!p.mask || p.mask[row]);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int e0 = (sub + L * c) * VEC;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) { x[c][v] = -INFINITY; given[c][v] = 0.f; }
+      if (in && e0 < p.E) {
+        x[c] = *reinterpret_cast<const fvec*>(p.logits + row * p.E + e0);
+        if (p.dlogits_in) given[c] = *reinterpret_cast<const fvec*>(p.dlogits_in + row * p.E + e0);
+      }
+    }
+  }
+
+  // rows t0 .. t1 - 1, the first of them loaded already; kb, kz: what the gradient's two terms are multiplied with
+  RP_DEV void run(const BalanceArgs& p, long base, int t0, int t1, const float* s_f, float kb, float kz, float& sum_b, float& sum_z) {
+    const int sub = (int)threadIdx.x % L, row_in = (int)threadIdx.x / L;
+    fvec f[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const int e = (sub + L * c) * VEC + v;
+        f[c][v] = e < p.E ? s_f[e] : 0.f;
+      }
+    for (int t = t0 + row_in; t - row_in < t1; t += ROWS) {
+      fvec y[C], was[C];
+      const bool live = on;
+      float m = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        was[c] = given[c];
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          y[c][v] = live ? x[c][v] : -INFINITY;
+          m = fmaxf(m, y[c][v]);
+        }
+      }
+      if (t - row_in + ROWS < t1) load(p, base, t + ROWS, t1, sub);
+#pragma unroll
+      for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+      const bool some = m != -INFINITY;      // a row of -inf has no probabilities
+      const float ref = some ? m : 0.f;
+      float l = 0.f, dot = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          y[c][v] = __expf(y[c][v] - ref);
+          l += y[c][v];
+          dot += f[c][v] * y[c][v];
+        }
+#pragma unroll
+      for (int o = L / 2; o > 0; o >>= 1) { l += __shfl_xor(l, o, 64); dot += __shfl_xor(dot, o, 64); }
+      const float inv_l = some ? 1.f / l : 0.f, lse = some ? m + logf(l) : 0.f;
+      dot *= inv_l;
+      if (sub == 0) { sum_b += dot; sum_z += lse * lse; }
+      if (t < t1 && p.dlogits) {
+        const float shift = kz * lse - kb * dot;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int e0 = (sub + L * c) * VEC;
+          if (e0 < p.E) {
+            fvec d;
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) d[v] = was[c][v] + (live ? y[c][v] * inv_l * (kb * f[c][v] + shift) : 0.f);
+            *reinterpret_cast<fvec*>(p.dlogits + (base + t) * p.E + e0) = d;
+          }
+        }
+      }
+    }
+  }
+};
+
 template <int L, int C, int VEC>
 __global__ void __launch_bounds__(256) balance_rows_kernel(const BalanceArgs p) {
+  __shared__ int s_cnt[1024];
   __shared__ float s_f[1024];
   __shared__ int red[4];
   __shared__ float redf[4];
-  typedef float fvec __attribute__((ext_vector_type(VEC)));
   const int tid = threadIdx.x, chunk = (int)blockIdx.x % p.chunks;
-  const long g = (int)blockIdx.x / p.chunks;
+  const long g = (int)blockIdx.x / p.chunks, base = g * p.seq;
+  const int t0 = chunk * p.rows_per_block, t1 = min(p.seq, t0 + p.rows_per_block);
+  RowPass<L, C, VEC, 256> rows;
+  rows.load(p, base, t0 + tid / L, t1, tid % L);
+  for (int e = tid; e < p.E; e += 256) s_cnt[e] = 0;
   int part = 0;
   for (int i = tid; i < p.slices; i += 256) part += p.tok[g * p.slices + i];
-  const int n_g = block_sum(part, red);
+  const int n_g = block_sum(part, red);      // (and s_cnt is zero everywhere)
   int total = n_g;
   if (p.groups > 1) {
     if (!p.mask) {
@@ -92,83 +189,70 @@ __global__ void __launch_bounds__(256) balance_rows_kernel(const BalanceArgs p) 
       total = block_sum(part, red);
     }
   }
+  // the slices' counts of an expert: several threads share it where there are more threads than experts
+  const int lanes = p.E < 256 ? 256 / p.E : 1;
+  const int mine = tid / p.E;
+  if (p.E >= 256 || mine < lanes) {
+    for (int e = p.E >= 256 ? tid : tid - mine * p.E; e < p.E; e += 256) {
+      int n = 0;
+#pragma unroll 16
+      for (int s = p.E >= 256 ? 0 : mine; s < p.slices; s += lanes) n += p.hist[(g * p.slices + s) * p.E + e];
+      atomicAdd(&s_cnt[e], n);
+    }
+  }
+  __syncthreads();
   const float inv_choices = n_g ? 1.f / ((float)n_g * (float)p.top_k) : 0.f;
   for (int e = tid; e < p.E; e += 256) {
-    int n = 0;
-    for (int s = 0; s < p.slices; ++s) n += p.hist[(g * p.slices + s) * p.E + e];
-    s_f[e] = (float)n * inv_choices;
-    if (chunk == 0) p.counts[g * p.E + e] = n;
+    s_f[e] = (float)s_cnt[e] * inv_choices;
+    if (chunk == 0) p.counts[g * p.E + e] = s_cnt[e];
   }
   if (chunk == 0 && tid == 0) {
     p.tokens[g] = n_g;
     if (g == 0 && !(p.groups > 1 && p.mask && p.total_given)) p.tokens[p.groups] = total;
   }
   __syncthreads();
-  const int sub = tid % L, row_in = tid / L;
-  constexpr int ROWS = 256 / L;
-  fvec f[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      const int e = (sub + L * c) * VEC + v;
-      f[c][v] = e < p.E ? s_f[e] : 0.f;
-    }
   const float inv_n = total ? 1.f / (float)total : 0.f;
-  const float kb = p.grad_scale * p.coef * (float)p.E * inv_n, kz = p.grad_scale * 2.f * p.z_coef * inv_n;
   float sum_b = 0.f, sum_z = 0.f;
-  const int t1 = min(p.seq, (chunk + 1) * p.rows_per_block);
-  for (int t0 = chunk * p.rows_per_block; t0 < t1; t0 += ROWS) {
-    const int t = t0 + row_in;
-    const bool in = t < t1;
-    const long row = g * p.seq + t;
-    const bool on = in && (!p.mask || p.mask[row]);
-    fvec x[C], given[C];
-    float m = -INFINITY;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int e0 = (sub + L * c) * VEC;
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) { x[c][v] = -INFINITY; given[c][v] = 0.f; }
-      if (on && e0 < p.E) x[c] = *reinterpret_cast<const fvec*>(p.logits + row * p.E + e0);
-      if (in && p.dlogits_in && e0 < p.E) given[c] = *reinterpret_cast<const fvec*>(p.dlogits_in + row * p.E + e0);
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) m = fmaxf(m, x[c][v]);
-    }
-#pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    float l = 0.f, dot = 0.f;
-    const float ref = m == -INFINITY ? 0.f : m;      // a row of -inf has no probabilities
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        x[c][v] = __expf(x[c][v] - ref);
-        l += x[c][v];
-        dot += f[c][v] * x[c][v];
-      }
-#pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) { l += __shfl_xor(l, o, 64); dot += __shfl_xor(dot, o, 64); }
-    const bool some = m != -INFINITY;
-    const float inv_l = some ? 1.f / l : 0.f, lse = some ? m + logf(l) : 0.f;
-    dot *= inv_l;
-    if (sub == 0) { sum_b += dot; sum_z += lse * lse; }
-    if (in && p.dlogits) {
-      const float shift = kz * lse - kb * dot;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int e0 = (sub + L * c) * VEC;
-        if (e0 < p.E) {
-          fvec d;
-#pragma unroll
-          for (int v = 0; v < VEC; ++v) d[v] = given[c][v] + (on ? x[c][v] * inv_l * (kb * f[c][v] + shift) : 0.f);
-          *reinterpret_cast<fvec*>(p.dlogits + row * p.E + e0) = d;
-        }
-      }
-    }
-  }
+  rows.run(p, base, t0, t1, s_f, p.grad_scale * p.coef * (float)p.E * inv_n, p.grad_scale * 2.f * p.z_coef * inv_n, sum_b, sum_z);
   const float tb = block_sum(sum_b, redf), tz = block_sum(sum_z, redf);
   if (tid == 0) p.part[blockIdx.x] = make_float2(tb, tz);
+}
+
+RP_DEV void write_loss(const BalanceArgs& p, double b, double z, int N) {
+  const double inv = N ? 1.0 / N : 0.0;
+  b *= inv * p.E;
+  z *= inv;
+  p.loss[0] = (float)(p.coef * b + p.z_coef * z);
+  p.loss[1] = (float)b;
+  p.loss[2] = (float)z;
+}
+
+// One group in one block.
+template <int L, int C, int VEC>
+__global__ void __launch_bounds__(1024) balance_small_kernel(const BalanceArgs p) {
+  __shared__ int s_hist[1024];
+  __shared__ float s_f[1024];
+  __shared__ int red[16];
+  __shared__ float redf[16];
+  const int tid = threadIdx.x;
+  RowPass<L, C, VEC, 1024> rows;
+  rows.load(p, 0, tid / L, p.seq, tid % L);
+  const int n = count_choices<1024>(p, 0, 0, p.seq, s_hist, red);
+  const float inv_choices = n ? 1.f / ((float)n * (float)p.top_k) : 0.f;
+  for (int e = tid; e < p.E; e += 1024) {
+    s_f[e] = (float)s_hist[e] * inv_choices;
+    p.counts[e] = s_hist[e];
+  }
+  __syncthreads();
+  const float inv_n = n ? 1.f / (float)n : 0.f;
+  float sum_b = 0.f, sum_z = 0.f;
+  rows.run(p, 0, 0, p.seq, s_f, p.grad_scale * p.coef * (float)p.E * inv_n, p.grad_scale * 2.f * p.z_coef * inv_n, sum_b, sum_z);
+  sum_b = block_sum(sum_b, redf);
+  sum_z = block_sum(sum_z, redf);
+  if (tid == 0) {
+    p.tokens[0] = p.tokens[1] = n;
+    write_loss(p, sum_b, sum_z, n);
+  }
 }
 
 // loss = {coef L_b + z_coef L_z, L_b, L_z}
@@ -182,31 +266,25 @@ __global__ void __launch_bounds__(1024) balance_total_kernel(const BalanceArgs p
   }
   b = block_sum(b, red);
   z = block_sum(z, red);
-  if (threadIdx.x == 0) {
-    const int N = p.tokens[p.groups];
-    const double inv = N ? 1.0 / N : 0.0;
-    b *= inv * p.E;
-    z *= inv;
-    p.loss[0] = (float)(p.coef * b + p.z_coef * z);
-    p.loss[1] = (float)b;
-    p.loss[2] = (float)z;
-  }
+  if (threadIdx.x == 0) write_loss(p, b, z, p.tokens[p.groups]);
 }
 
 struct Shape { int slices, rows_per_block, chunks; };
 
-// Slices of a group for counting and blocks of its rows.  A slice is worth about 4096 tokens' choices at one a token; rows go out in at
-// most 2048 blocks altogether, of 32 rows at least.
-Shape shape_of(long T, int seq) {
-  const int groups = (int)(T / seq);
+// Lanes per token: 16-byte accesses where the rows lie on such boundaries.
+int lanes_of(int E) { return E <= 16 ? 4 : E <= 32 ? 8 : E <= 64 ? 16 : E <= 128 ? 32 : 64; }
+
+// Slices of a group for counting, of about 8192 choices; blocks of its rows, each going over its 256 threads' worth of rows once or, where
+// that would make more than 1024 blocks, several times.
+Shape shape_of(int T, int seq, int E, int top_k) {
+  const int groups = T / seq;
   Shape s;
-  s.slices = (seq + 1023) / 1024;
-  s.slices = s.slices < 1 ? 1 : s.slices > 32 ? 32 : s.slices;
-  const int most = groups < 2048 ? 2048 / groups : 1;
-  int rows = (seq + most - 1) / most;
-  rows = rows < 32 ? 32 : (rows + 31) / 32 * 32;
-  s.rows_per_block = rows;
-  s.chunks = (seq + rows - 1) / rows;
+  const long slices = ((long)seq * top_k + 8191) / 8192;
+  s.slices = slices > 32 ? 32 : (int)slices;
+  const int rows = 256 / lanes_of(E);
+  const int passes = (seq + rows - 1) / rows, most = groups < 1024 ? 1024 / groups : 1;
+  s.rows_per_block = rows * ((passes + most - 1) / most);
+  s.chunks = (seq + s.rows_per_block - 1) / s.rows_per_block;
   return s;
 }
 
@@ -215,11 +293,18 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 }  // namespace
 
 // ------------------------------------------------------------------------------------------------ launchers
+// The counts of up to 32 slices a group (as many choices a token as there can be: the size does not depend on top_k), and the loss terms.
 size_t k_moe_balance_scratch(int T, int seq, int E) {
   if (T == 0) return 0;
-  const Shape s = shape_of(T, seq);
+  const Shape s = shape_of(T, seq, E, 64);
   const size_t groups = (size_t)(T / seq);
   return up256(groups * s.slices * E * 4) + up256(groups * s.slices * 4) + up256(groups * s.chunks * 8);
+}
+
+template <int L, int C, int VEC>
+static void launch_rows(hipStream_t st, const BalanceArgs& p, bool small) {
+  if (small) RP_LAUNCH((balance_small_kernel<L, C, VEC>), dim3(1), dim3(1024), 0, st, p);
+  else RP_LAUNCH((balance_rows_kernel<L, C, VEC>), dim3(p.groups * p.chunks), dim3(256), 0, st, p);
 }
 
 hipError_t k_moe_balance(hipStream_t st, BalanceArgs p, int T, void* scratch) {
@@ -227,7 +312,7 @@ hipError_t k_moe_balance(hipStream_t st, BalanceArgs p, int T, void* scratch) {
     const hipError_t e = k_fill_u32(st, p.loss, 3, 0u);
     return e == hipSuccess ? k_fill_u32(st, p.tokens, 1, 0u) : e;
   }
-  const Shape s = shape_of(T, p.seq);
+  const Shape s = shape_of(T, p.seq, p.E, p.top_k < 64 ? p.top_k : 64);
   p.groups = T / p.seq;
   p.slices = s.slices;
   p.rows_per_block = s.rows_per_block;
@@ -239,25 +324,30 @@ hipError_t k_moe_balance(hipStream_t st, BalanceArgs p, int T, void* scratch) {
   at += up256((size_t)p.groups * s.slices * 4);
   p.part = reinterpret_cast<float2*>(at);
   p.total_given = p.groups > 1 && p.mask && (long)p.groups * s.slices > 1024;
-  RP_LAUNCH(balance_count_kernel, dim3(p.groups * s.slices), dim3(256), 0, st, p);
-  if (p.total_given) RP_LAUNCH(balance_tokens_kernel, dim3(1), dim3(1024), 0, st, p);
-#define RP_LAUNCH_BR(L, C, VEC) RP_LAUNCH((balance_rows_kernel<L, C, VEC>), dim3(p.groups * s.chunks), dim3(256), 0, st, p)
+  // one block is through with 16384 logits (and their choices) in the time of the two launches it saves
+  const bool small = p.groups == 1 && (long)T * p.E <= 16384 && (long)T * p.top_k <= 8192;
+  if (!small) {
+    RP_LAUNCH(balance_count_kernel, dim3(p.groups * s.slices), dim3(1024), 0, st, p);
+    if (p.total_given) RP_LAUNCH(balance_tokens_kernel, dim3(1), dim3(1024), 0, st, p);
+  }
   const uintptr_t at16 = reinterpret_cast<uintptr_t>(p.logits) | reinterpret_cast<uintptr_t>(p.dlogits) | reinterpret_cast<uintptr_t>(p.dlogits_in);
   if (p.E % 4 == 0 && at16 % 16 == 0) {      // rows on 16-byte boundaries: 16-byte accesses
-    if (p.E <= 16) RP_LAUNCH_BR(4, 1, 4);
-    else if (p.E <= 32) RP_LAUNCH_BR(8, 1, 4);
-    else if (p.E <= 64) RP_LAUNCH_BR(16, 1, 4);
-    else if (p.E <= 128) RP_LAUNCH_BR(32, 1, 4);
-    else if (p.E <= 256) RP_LAUNCH_BR(64, 1, 4);
-    else if (p.E <= 512) RP_LAUNCH_BR(64, 2, 4);
-    else RP_LAUNCH_BR(64, 4, 4);
+    switch (lanes_of(p.E)) {
+      case 4: launch_rows<4, 1, 4>(st, p, small); break;
+      case 8: launch_rows<8, 1, 4>(st, p, small); break;
+      case 16: launch_rows<16, 1, 4>(st, p, small); break;
+      case 32: launch_rows<32, 1, 4>(st, p, small); break;
+      default:
+        if (p.E <= 256) launch_rows<64, 1, 4>(st, p, small);
+        else if (p.E <= 512) launch_rows<64, 2, 4>(st, p, small);
+        else launch_rows<64, 4, 4>(st, p, small);
+    }
   } else {
-    if (p.E <= 16) RP_LAUNCH_BR(16, 1, 1);
-    else if (p.E <= 64) RP_LAUNCH_BR(64, 1, 1);
-    else if (p.E <= 256) RP_LAUNCH_BR(64, 4, 1);
-    else RP_LAUNCH_BR(64, 16, 1);
+    if (p.E <= 16) launch_rows<16, 1, 1>(st, p, small);
+    else if (p.E <= 64) launch_rows<64, 1, 1>(st, p, small);
+    else if (p.E <= 256) launch_rows<64, 4, 1>(st, p, small);
+    else launch_rows<64, 16, 1>(st, p, small);
   }
-#undef RP_LAUNCH_BR
-  RP_LAUNCH(balance_total_kernel, dim3(1), dim3(1024), 0, st, p, (long)p.groups * s.chunks);
+  if (!small) RP_LAUNCH(balance_total_kernel, dim3(1), dim3(1024), 0, st, p, (long)p.groups * s.chunks);
   return hipGetLastError();
 }

@@ -14,6 +14,9 @@
 //   dK, dV : workgroup = 128 keys, loop over 64-row tiles (d = 128: eight waves, pairs of which share 32 keys; d = 64: four waves)
 // Where there are too few workgroups for the chip, the loop is cut into `splits` slices, whose results another kernel joins in slice
 // order (fp32 partials in the caller's scratch; no atomics, so the result does not depend on timing).
+// Launch order: the key head changes fastest, so that (workgroups go round the eight XCDs) one XCD's L2 keeps to the key heads of its residue, and
+// the sequences of a padded batch spread over all of them (neighbouring key heads per XCD, as attention.hip has it, leaves the longest sequence
+// to two XCDs of a batch of four).
 // Keys behind kv_len are never read (they may hold anything); rows behind q_len get zeros, and lse -inf.
 #include "attention_device.hpp"
 #include "layer_ops.hpp"
@@ -113,7 +116,7 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_fwd_kernel(con
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nhb = p.kh * p.batch;
   const int rest = (int)blockIdx.x / nhb;
-  const int hb = xcd_head((int)blockIdx.x % nhb, nhb);      // an XCD keeps to few key heads
+  const int hb = (int)blockIdx.x % nhb;
   const int split = SPLIT ? rest % p.splits : 0;
   const int r0 = (SPLIT ? rest / p.splits : rest) * BQ;
   const Rows s(p, hb);
@@ -288,32 +291,220 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_fwd_kernel(con
   }
 }
 
-// Joins the slices of a row: weights exp2(m_i - max m), in slice order.  D / 8 threads per row.
+// ---- few rows: the step of a generation -----------------------------------------------------------------------
+// At most 16 NC rows per key head (the queries of a step times the heads of the group).  Bound by reading K and V once, so a wave works alone, without
+// barriers: the four waves of a workgroup take its 32-key steps in turn, K goes from memory straight into the fragments of the matrix
+// instruction (16 rows x 64 bytes a load: a whole row is used by one wave), V through a piece of LDS of the wave's own, since its
+// reduction runs over the keys.  The next step's K and V are on their way during a step.  At the end the waves join in LDS.
+template <int D, int NC, bool SPLIT>
+__global__ void __launch_bounds__(256) cross_step_kernel(const CrossArgs p) {
+  constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, CH = D / 8, NV = 32 * CH / 64;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // step_smem_bytes(D, NC)
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  bf16* const Vs = reinterpret_cast<bf16*>(dyn_smem) + w * 32 * LD;
+  const int nhb = p.kh * p.batch;
+  const int hb = (int)blockIdx.x % nhb, split = (int)blockIdx.x / nhb;
+  const Rows s(p, hb);
+  int j0 = 0, j1 = (s.kvlen + 31) / 32;
+  if (SPLIT) {
+    slice_of(j1, p.splits, split, j0, j1);
+    if (j0 >= j1) return;      // uniform, before any barrier
+  }
+  const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
+  const bf16* const vb = p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D;
+
+  uint4 qf[NC][KS];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int row = 16 * c + lr;
+    const bool live = row < s.valid;
+    const bf16* const qr = live ? p.q + s.offset(row, p.ldq, D) + 8 * lg : p.q;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (live) qf[c][ks] = *reinterpret_cast<const uint4*>(qr + 32 * ks);
+    }
+  }
+  float m_run[NC], l_run[NC];
+  f32x4 oacc[DT][NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    m_run[c] = -INFINITY;
+    l_run[c] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) oacc[dt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  u32x4 kreg[2][KS], vreg[NV];
+  auto load_step = [&](int j) {      // rows past the end read as zero
+    const int left = min(32, s.kvlen - 32 * j);
+    const rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(kb + (long)(32 * j) * p.ldk), 0, (int)(((long)(left - 1) * p.ldk + D) * 2), 0x00020000);
+    const rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(vb + (long)(32 * j) * p.ldv), 0, (int)(((long)(left - 1) * p.ldv + D) * 2), 0x00020000);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        kreg[kt][ks] = __builtin_amdgcn_raw_buffer_load_b128(rk, (int)(((16 * kt + lr) * (int)p.ldk + 32 * ks + 8 * lg) * 2), 0, 0);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = 64 * i + lane;
+      vreg[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, (int)(((c / CH) * (int)p.ldv + (c % CH) * 8) * 2), 0, 0);
+    }
+  };
+  if (j0 + w < j1) load_step(j0 + w);
+  const bf16* const vfrag = Vs + tr_base<LD>(lane);
+  for (int j = j0 + w; j < j1; j += 4) {
+    f32x4 sT[2][NC];      // [16 keys][16 rows]
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          sT[kt][c] = mfma16(__builtin_bit_cast(uint4, kreg[kt][ks]), qf[c][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sT[kt][c]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = 64 * i + lane;
+      *reinterpret_cast<u32x4*>(Vs + (c / CH) * LD + (c % CH) * 8) = vreg[i];
+    }
+    if (j + 4 < j1) load_step(j + 4);
+    if (32 * j + 32 > s.kvlen) {      // uniform: the last step
+      const int klim = s.kvlen - 1 - (32 * j + 4 * lg);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sT[kt][c][e] = 16 * kt + e > klim ? -INFINITY : sT[kt][c][e];
+    }
+    uint4 pf[NC];
+    bool grow = false;
+    float mx[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      mx[c] = fmaxf(fmaxf(fmaxf(sT[0][c][0], sT[0][c][1]), fmaxf(sT[0][c][2], sT[0][c][3])), fmaxf(fmaxf(sT[1][c][0], sT[1][c][1]), fmaxf(sT[1][c][2], sT[1][c][3])));
+      grow = grow || mx[c] * p.scale_log2e > m_run[c] + 8.f;
+    }
+    // the reference exponent is the same in the four lanes of a column, and moves only when one of them outgrows it by 2^8
+    if (__builtin_amdgcn_ballot_w64(grow) != 0ull) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float m = fmaxf(mx[c], __shfl_xor(mx[c], 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64)) * p.scale_log2e;
+        const float m_new = m > m_run[c] + 8.f ? m : m_run[c];
+        const float alpha = fast_exp2(m_run[c] - m_new);
+        l_run[c] *= alpha;
+        m_run[c] = m_new;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) oacc[dt][c] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sT[kt][c][e] = fast_exp2(__builtin_fmaf(sT[kt][c][e], p.scale_log2e, -m_run[c]));
+          l_run[c] += sT[kt][c][e];
+        }
+      pf[c] = pack_frag(sT[0][c], sT[1][c]);
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const uint4 a = read_frag_tr<LD>(vfrag + 16 * dt);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) oacc[dt][c] = mfma16(a, pf[c], oacc[dt][c]);
+    }
+  }
+
+  // the waves join: wave w's reference exponent and sum of every row, then its rows of O^T
+  float* const ml = reinterpret_cast<float*>(dyn_smem);      // [4][2][16 NC]
+  float* const os = ml + 8 * 16 * NC;                        // [4][16 NC][D + 4]
+  __syncthreads();
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const float l = column_sum(l_run[c]);
+    if (lg == 0) {
+      ml[(2 * w) * 16 * NC + 16 * c + lr] = m_run[c];
+      ml[(2 * w + 1) * 16 * NC + 16 * c + lr] = l;
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      *reinterpret_cast<f32x4*>(os + (w * 16 * NC + 16 * c + lr) * (D + 4) + 16 * dt + 4 * lg) = oacc[dt][c];
+  }
+  __syncthreads();
+  for (int i = tid; i < 16 * NC * CH; i += 256) {
+    const int row = i / CH, ch = i % CH;
+    if (row >= s.total) break;
+    const bool live = row < s.valid && j0 < j1;
+    if (SPLIT && !live) continue;
+    float m = -INFINITY, l = 0.f, acc[8];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) m = fmaxf(m, ml[2 * u * 16 * NC + row]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float mu = ml[2 * u * 16 * NC + row];
+      const float wgt = mu == -INFINITY ? 0.f : fast_exp2(mu - m);      // (a wave without a step)
+      l += wgt * ml[(2 * u + 1) * 16 * NC + row];
+      const float* const src = os + (u * 16 * NC + row) * (D + 4) + 8 * ch;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += wgt * src[e];
+    }
+    if constexpr (SPLIT) {
+      const long at = ((long)split * nhb + hb) * s.total + row;
+      if (ch == 0) p.part_ml[at] = make_float2(m, l);
+      *reinterpret_cast<float4*>(p.part + at * D + 8 * ch) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      *reinterpret_cast<float4*>(p.part + at * D + 8 * ch + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    } else {
+      const float mul = live ? 1.f / l : 0.f;
+      if (p.lse && ch == 0) p.lse[s.stat(row, p.a)] = live ? m * 0.6931471805599453f + logf(l) : -INFINITY;
+      const uint4 u = make_uint4(pack_bf16x2(acc[0] * mul, acc[1] * mul), pack_bf16x2(acc[2] * mul, acc[3] * mul), pack_bf16x2(acc[4] * mul, acc[5] * mul),
+                                 pack_bf16x2(acc[6] * mul, acc[7] * mul));
+      *reinterpret_cast<uint4*>(p.o + s.offset(row, p.ldo, D) + 8 * ch) = live ? u : make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+}
+
+// Joins the slices of a row, weights exp2(m_i - max m): one wave per row, whose 512 / D lane groups take every (512 / D)-th slice and are added up in a
+// fixed order.  unit: keys a step of the kernel that cut the slices.
 template <int D>
-__global__ void __launch_bounds__(256) cross_fwd_join_kernel(const CrossArgs p) {
-  constexpr int CH = D / 8;
+__global__ void __launch_bounds__(256) cross_fwd_join_kernel(const CrossArgs p, int unit) {
+  constexpr int CH = D / 8, GROUPS = 64 / CH;
   const int total = (p.a / p.kh) * p.seq_q, nhb = p.kh * p.batch;
-  const long idx = (long)blockIdx.x * 256 + threadIdx.x;
-  const long item = idx / CH;
-  const int ch = (int)(idx % CH);
+  const int lane = threadIdx.x & 63, ch = lane % CH, grp = lane / CH;
+  const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (item >= (long)nhb * total) return;
   const int hb = (int)(item / total), r = (int)(item - (long)hb * total);
   const Rows s(p, hb);
-  const int n = r < s.valid ? slices_used((s.kvlen + 63) / 64, p.splits) : 0;
+  const int n = r < s.valid ? slices_used((s.kvlen + unit - 1) / unit, p.splits) : 0;
   float m = -INFINITY;
-  for (int i = 0; i < n; ++i) m = fmaxf(m, p.part_ml[((long)i * nhb + hb) * total + r].x);
+  for (int i = lane; i < n; i += 64) m = fmaxf(m, p.part_ml[((long)i * nhb + hb) * total + r].x);
+  m = wave_max(m);
   float l = 0.f, acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-  for (int i = 0; i < n; ++i) {
+#pragma unroll 4
+  for (int i = grp; i < n; i += GROUPS) {
     const long at = ((long)i * nhb + hb) * total + r;
     const float2 ml = p.part_ml[at];
-    const float wgt = fast_exp2(ml.x - m);
     const float4 x0 = *reinterpret_cast<const float4*>(p.part + at * D + ch * 8), x1 = *reinterpret_cast<const float4*>(p.part + at * D + ch * 8 + 4);
+    const float wgt = fast_exp2(ml.x - m);
     l += wgt * ml.y;
     acc[0] += wgt * x0.x; acc[1] += wgt * x0.y; acc[2] += wgt * x0.z; acc[3] += wgt * x0.w;
     acc[4] += wgt * x1.x; acc[5] += wgt * x1.y; acc[6] += wgt * x1.z; acc[7] += wgt * x1.w;
   }
+#pragma unroll
+  for (int o = CH; o < 64; o <<= 1) {
+    l += __shfl_xor(l, o, 64);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+  }
+  if (grp) return;
   const float mul = n ? 1.f / l : 0.f;
   if (p.lse && ch == 0) p.lse[s.stat(r, p.a)] = n ? m * 0.6931471805599453f + logf(l) : -INFINITY;
   *reinterpret_cast<uint4*>(p.o + s.offset(r, p.ldo, D) + ch * 8) =
@@ -342,7 +533,7 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(cons
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nhb = p.kh * p.batch;
   const int rest = (int)blockIdx.x / nhb;
-  const int hb = xcd_head((int)blockIdx.x % nhb, nhb);
+  const int hb = (int)blockIdx.x % nhb;
   const int split = SPLIT ? rest % p.splits : 0;
   const int r0 = (SPLIT ? rest / p.splits : rest) * BQ;
   const Rows s(p, hb);
@@ -602,7 +793,9 @@ struct RowTile {
 #pragma unroll
     for (int it = 0; it < NREG; ++it) {
       const bool in = h[it] < grp;
-      r[it] = *reinterpret_cast<const uint4*>(base + (long)(in ? q[it] : 0) * ld + (in ? h[it] : 0) * D + ((it * NT + tid) % CH) * 8);
+      typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));      // (copied as a struct, the pieces would live in scratch memory)
+      const u32x4 v = *reinterpret_cast<const u32x4*>(base + (long)(in ? q[it] : 0) * ld + (in ? h[it] : 0) * D + ((it * NT + tid) % CH) * 8);
+      r[it] = make_uint4(v.x, v.y, v.z, v.w);
     }
   }
   RP_DEV void next() {
@@ -617,7 +810,7 @@ struct RowTile {
 
 // What the products start from for a row (wave 0: -lse / scale, wave 1: -delta), so that they come out as q.k - lse / scale and
 // dO.v - delta; rows past the end get P = exp(-inf) = 0.
-RP_DEV float row_start(float raw, int wave, bool in, float scale) { return wave == 0 ? (in ? -raw / scale : -INFINITY) : (in ? -raw : 0.f); }
+RP_DEV float row_start(float raw, int wave, bool in, float inv_scale) { return wave == 0 ? (in ? -raw * inv_scale : -INFINITY) : (in ? -raw : 0.f); }
 
 // lse and delta of a 64-row tile, a row per lane of waves 0 and 1.  The load is only issued here; row_start comes a tile later.
 struct RowStat {
@@ -688,7 +881,7 @@ __global__ void __launch_bounds__(256) cross_dkv_kernel(const CrossArgs p) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nhb = p.kh * p.batch;
   const int rest = (int)blockIdx.x / nhb;
-  const int hb = xcd_head((int)blockIdx.x % nhb, nhb);
+  const int hb = (int)blockIdx.x % nhb;
   const int split = rest % p.splits, kv0 = (rest / p.splits) * 128, kw0 = kv0 + 32 * w;
   const Rows s(p, hb);
   if (p.splits == 1) zero_keys<D, 256>(p, s, kv0, tid);
@@ -740,7 +933,7 @@ __global__ void __launch_bounds__(256) cross_dkv_kernel(const CrossArgs p) {
     __syncthreads();
     T64::template store<LD>(qreg, Qs, tid);
     T64::template store<LD>(doreg, dOs, tid);
-    if (w < 2) stat[64 * w + lane] = row_start(st_reg, w, u * 64 + lane < s.valid, p.scale);
+    if (w < 2) stat[64 * w + lane] = row_start(st_reg, w, u * 64 + lane < s.valid, p.inv_scale);
     __syncthreads();
     if (u + 1 < u1) prefetch();
     // the two 32-row halves of the tile one after the other: half as many score registers live at a time
@@ -828,7 +1021,7 @@ __global__ void __launch_bounds__(512) cross_dkv_pair_kernel(const CrossArgs p) 
   const int w = w8 >> 1, h = w8 & 1;
   const int nhb = p.kh * p.batch;
   const int rest = (int)blockIdx.x / nhb;
-  const int hb = xcd_head((int)blockIdx.x % nhb, nhb);
+  const int hb = (int)blockIdx.x % nhb;
   const int split = rest % p.splits, kv0 = (rest / p.splits) * 128, kw0 = kv0 + 32 * w;
   const Rows s(p, hb);
   if (p.splits == 1) zero_keys<D, 512>(p, s, kv0, tid);
@@ -914,7 +1107,7 @@ __global__ void __launch_bounds__(512) cross_dkv_pair_kernel(const CrossArgs p) 
     bf16* const q_set = smem + (i & 1) * TSET;
     T64::template store<LD>(qreg, q_set, tid);
     T64::template store<LD>(doreg, q_set + 64 * LD, tid);
-    if (w8 < 2) stat[128 * (i & 1) + 64 * w8 + lane] = row_start(st_reg, w8, (u0 + i) * 64 + lane < s.valid, p.scale);
+    if (w8 < 2) stat[128 * (i & 1) + 64 * w8 + lane] = row_start(st_reg, w8, (u0 + i) * 64 + lane < s.valid, p.inv_scale);
     if (i > 0) partner_update(i - 1);
     __syncthreads();
     if (i + 1 < n_tiles) prefetch();
@@ -1001,18 +1194,19 @@ __global__ void __launch_bounds__(256) cross_dkv_join_kernel(const CrossArgs p) 
 // operand tiles, or the epilogue's staging of every wave's 32 x d block, whichever is larger
 constexpr int max_i(int a, int b) { return a > b ? a : b; }
 constexpr int fwd_smem_bytes(int d, int nw) { return max_i((nw >= 8 ? 2 : 1) * (64 * (d + 8) + 64 * (d + 32)), nw * 32 * (d + 8)) * 2; }
+constexpr int step_smem_bytes(int d, int nc) { return max_i(4 * 32 * tile_ld(d) * 2, 8 * 16 * nc * 4 + 4 * 16 * nc * (d + 4) * 4); }
 constexpr int dq_smem_bytes(int d, int nw) { return max_i((nw >= 8 ? 2 : 1) * (2 * 64 * tile_ld(d)), nw * 32 * (d + 8)) * 2; }
 constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 512, 4 * 32 * (d + 4) * 4); }
 constexpr int dkv_pair_smem_bytes(int d) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * 4 * 64 * 16 + 1024; }
 
-template <typename K>
-hipError_t launch(K kern, int grid, int threads, int smem, hipStream_t st, const CrossArgs& p) {
+template <typename K, typename... More>
+hipError_t launch(K kern, int grid, int threads, int smem, hipStream_t st, const CrossArgs& p, More... more) {
   // (a host-side table entry, not a stream operation: allowed while a graph is captured)
   if (smem > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != hipSuccess) return e;
   }
-  RP_LAUNCH(kern, dim3(grid), dim3(threads), smem, st, p);
+  RP_LAUNCH(kern, dim3(grid), dim3(threads), smem, st, p, more...);
   return hipGetLastError();
 }
 
@@ -1030,20 +1224,36 @@ long row_count(const CrossArgs& p) { return (long)(p.a / p.kh) * p.seq_q; }
 size_t row_part_bytes(const CrossArgs& p, int d) { return (size_t)p.kh * p.batch * row_count(p) * (d + 2) * 4; }      // o or dq, and (m, l)
 size_t key_part_bytes(const CrossArgs& p, int d) { return (size_t)2 * p.batch * p.seq_kv * p.kh * d * 4; }
 int row_splits(const CrossArgs& p, int d, size_t bytes) { return splits_for((long)ceil_div(row_count(p), 128) * p.kh * p.batch, ceil_div(p.seq_kv, 64), row_part_bytes(p, d), bytes); }
+// Few rows: 32-key steps, four at a time; slices of eight steps and more, for two workgroups per CU.
+bool few_rows(const CrossArgs& p) { return row_count(p) <= 32; }
+int step_splits(const CrossArgs& p, int d, size_t bytes) {
+  const long nhb = (long)p.kh * p.batch;
+  long n = nhb ? 512 / nhb : 1;
+  if (n > ceil_div(p.seq_kv, 256)) n = ceil_div(p.seq_kv, 256);
+  const size_t each = row_part_bytes(p, d);
+  if (each && n > (long)(bytes / each)) n = (long)(bytes / each);
+  return n < 2 ? 1 : (int)n;
+}
 int key_splits(const CrossArgs& p, int d, size_t bytes) { return splits_for((long)ceil_div(p.seq_kv, 128) * p.kh * p.batch, ceil_div(row_count(p), 64), key_part_bytes(p, d), bytes); }
 
 template <int D>
 hipError_t fwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   const int nhb = p.kh * p.batch;
   const long rows = row_count(p);
-  p.splits = row_splits(p, D, bytes);
-  if (p.splits > 1) {
-    p.part = static_cast<float*>(scratch);
-    p.part_ml = reinterpret_cast<float2*>(p.part + (size_t)p.splits * nhb * rows * D);
-    const hipError_t e = launch(cross_fwd_kernel<D, 4, true>, ceil_div(rows, 128) * nhb * p.splits, 256, fwd_smem_bytes(D, 4), st, p);
-    if (e != hipSuccess) return e;
-    return launch(cross_fwd_join_kernel<D>, ceil_div(nhb * rows * (D / 8), 256), 256, 0, st, p);
+  const bool few = few_rows(p);
+  p.splits = few ? step_splits(p, D, bytes) : row_splits(p, D, bytes);
+  p.part = static_cast<float*>(scratch);
+  p.part_ml = reinterpret_cast<float2*>(p.part + (size_t)p.splits * nhb * rows * D);
+  hipError_t e = hipSuccess;
+  if (few) {
+    const int grid = nhb * p.splits;
+    if (rows <= 16) e = p.splits > 1 ? launch(cross_step_kernel<D, 1, true>, grid, 256, step_smem_bytes(D, 1), st, p) : launch(cross_step_kernel<D, 1, false>, grid, 256, step_smem_bytes(D, 1), st, p);
+    else e = p.splits > 1 ? launch(cross_step_kernel<D, 2, true>, grid, 256, step_smem_bytes(D, 2), st, p) : launch(cross_step_kernel<D, 2, false>, grid, 256, step_smem_bytes(D, 2), st, p);
+  } else if (p.splits > 1) {
+    e = launch(cross_fwd_kernel<D, 4, true>, ceil_div(rows, 128) * nhb * p.splits, 256, fwd_smem_bytes(D, 4), st, p);
   }
+  if (p.splits > 1 && e == hipSuccess) e = launch(cross_fwd_join_kernel<D>, ceil_div(nhb * rows, 4), 256, 0, st, p, few ? 32 : 64);
+  if (few || p.splits > 1) return e;
   if (D == 128 && (long)ceil_div(rows, 256) * nhb >= 1024)
     return launch(cross_fwd_kernel<D, 8, false>, ceil_div(rows, 256) * nhb, 512, fwd_smem_bytes(D, 8), st, p);
   return launch(cross_fwd_kernel<D, 4, false>, ceil_div(rows, 128) * nhb, 256, fwd_smem_bytes(D, 4), st, p);
@@ -1081,9 +1291,9 @@ hipError_t bwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
 // ------------------------------------------------------------------------------------------------ launchers
 void k_cross_attn_scratch(const CrossArgs& p, int d, size_t* fwd_bytes, size_t* bwd_bytes) {
   const size_t all = ~(size_t)0;
-  const int rs = row_splits(p, d, all), ks = key_splits(p, d, all);
+  const int fs = few_rows(p) ? step_splits(p, d, all) : row_splits(p, d, all), rs = row_splits(p, d, all), ks = key_splits(p, d, all);
   const size_t r = rs > 1 ? rs * row_part_bytes(p, d) : 0, k = ks > 1 ? ks * key_part_bytes(p, d) : 0;
-  *fwd_bytes = r;
+  *fwd_bytes = fs > 1 ? fs * row_part_bytes(p, d) : 0;
   *bwd_bytes = r > k ? r : k;
 }
 

@@ -47,7 +47,7 @@ struct CrossArgs {
   long ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv;
   const int *q_len, *kv_len;       // [batch] or NULL
   int batch, seq_q, seq_kv, a, kh;
-  float scale, scale_log2e;
+  float scale, scale_log2e, inv_scale;
   float* part;                     // from here on set by the launcher
   float2* part_ml;
   int splits;

@@ -1354,13 +1354,14 @@ rp_status rp_op_rope(void* stream, int bwd, int layout, int d, int rot, const vo
 namespace {
 // Sizes that the cross attention's kernels cover; fills what they share.
 bool cross_args(CrossArgs& p, int batch, int seq_q, int seq_kv, int a, int kh, int d, float scale) {
-  if (batch < 0 || seq_q < 0 || seq_kv < 0 || a <= 0 || kh <= 0 || a % kh || (d != 64 && d != 128) || !(scale > 0.f) || !isfinite(scale)) return false;
+  if (batch < 0 || seq_q < 0 || seq_kv < 0 || a <= 0 || kh <= 0 || a % kh || (d != 64 && d != 128) || !(scale >= 1e-30f && scale <= 1e30f)) return false;
   // rows of a key head, and workgroups and threads of every launch (up to 256 slices of 128 rows or keys, 16 threads a row), are counted in 31 bits
   const double rows = (double)(a / kh) * seq_q, nhb = (double)kh * batch;
   if (rows > 1.0e9 || seq_kv > 1000000000 || rows * nhb * (d / 8) > 2.0e9 || 2.0 * nhb * seq_kv * (d / 8) > 256.0 * 2.0e9) return false;
   p.batch = batch; p.seq_q = seq_q; p.seq_kv = seq_kv; p.a = a; p.kh = kh;
   p.scale = scale;
   p.scale_log2e = scale * 1.4426950408889634f;
+  p.inv_scale = 1.f / scale;
   return true;
 }
 }  // namespace
