@@ -12,7 +12,7 @@
 //   rows  : a few lanes hold a token's logits, the next token's on their way; every block first adds the slices' counts of its group up; loss
 //           terms leave one pair of fp32 sums per block
 //   total : one block adds the pairs in a fixed order
-//   small : all of it in one block, for batches that one block is through with before the other launches would have started
+//   small : a group in one block, for groups that one block is through with before the other launches would have started
 #include "kernels.hpp"
 #include "layer_ops.hpp"
 
@@ -174,9 +174,20 @@ __global__ void __launch_bounds__(256) balance_rows_kernel(const BalanceArgs p) 
   RowPass<L, C, VEC, 256> rows;
   rows.load(p, base, t0 + tid / L, t1, tid % L);
   for (int e = tid; e < p.E; e += 256) s_cnt[e] = 0;
+  __syncthreads();
   int part = 0;
   for (int i = tid; i < p.slices; i += 256) part += p.tok[g * p.slices + i];
-  const int n_g = block_sum(part, red);      // (and s_cnt is zero everywhere)
+  // the slices' counts of an expert: several threads share it where there are more threads than experts
+  const int lanes = p.E < 256 ? 256 / p.E : 1, mine = p.E < 256 ? tid / p.E : 0;
+  if (mine < lanes) {
+    for (int e = tid - mine * p.E; e < p.E; e += 256) {
+      int n = 0;
+#pragma unroll 16
+      for (int s = mine; s < p.slices; s += lanes) n += p.hist[(g * p.slices + s) * p.E + e];
+      atomicAdd(&s_cnt[e], n);
+    }
+  }
+  const int n_g = block_sum(part, red);      // (its barriers order the counts as well)
   int total = n_g;
   if (p.groups > 1) {
     if (!p.mask) {
@@ -189,18 +200,6 @@ __global__ void __launch_bounds__(256) balance_rows_kernel(const BalanceArgs p) 
       total = block_sum(part, red);
     }
   }
-  // the slices' counts of an expert: several threads share it where there are more threads than experts
-  const int lanes = p.E < 256 ? 256 / p.E : 1;
-  const int mine = tid / p.E;
-  if (p.E >= 256 || mine < lanes) {
-    for (int e = p.E >= 256 ? tid : tid - mine * p.E; e < p.E; e += 256) {
-      int n = 0;
-#pragma unroll 16
-      for (int s = p.E >= 256 ? 0 : mine; s < p.slices; s += lanes) n += p.hist[(g * p.slices + s) * p.E + e];
-      atomicAdd(&s_cnt[e], n);
-    }
-  }
-  __syncthreads();
   const float inv_choices = n_g ? 1.f / ((float)n_g * (float)p.top_k) : 0.f;
   for (int e = tid; e < p.E; e += 256) {
     s_f[e] = (float)s_cnt[e] * inv_choices;
@@ -227,7 +226,7 @@ RP_DEV void write_loss(const BalanceArgs& p, double b, double z, int N) {
   p.loss[2] = (float)z;
 }
 
-// One group in one block.
+// A group in one block; a single group's block writes the loss as well.
 template <int L, int C, int VEC>
 __global__ void __launch_bounds__(1024) balance_small_kernel(const BalanceArgs p) {
   __shared__ int s_hist[1024];
@@ -235,23 +234,35 @@ __global__ void __launch_bounds__(1024) balance_small_kernel(const BalanceArgs p
   __shared__ int red[16];
   __shared__ float redf[16];
   const int tid = threadIdx.x;
+  const long g = blockIdx.x, base = g * p.seq;
   RowPass<L, C, VEC, 1024> rows;
-  rows.load(p, 0, tid / L, p.seq, tid % L);
-  const int n = count_choices<1024>(p, 0, 0, p.seq, s_hist, red);
+  rows.load(p, base, tid / L, p.seq, tid % L);
+  const int n = count_choices<1024>(p, base, 0, p.seq, s_hist, red);
+  int total = n;
+  if (p.groups > 1) {
+    total = p.groups * p.seq;
+    if (p.mask) {      // every block counts all tokens: a byte each
+      int valid = 0;
+      for (int t = tid; t < total; t += 1024) valid += p.mask[t] != 0;
+      total = block_sum(valid, red);
+    }
+  }
   const float inv_choices = n ? 1.f / ((float)n * (float)p.top_k) : 0.f;
   for (int e = tid; e < p.E; e += 1024) {
     s_f[e] = (float)s_hist[e] * inv_choices;
-    p.counts[e] = s_hist[e];
+    p.counts[g * p.E + e] = s_hist[e];
   }
   __syncthreads();
-  const float inv_n = n ? 1.f / (float)n : 0.f;
+  const float inv_n = total ? 1.f / (float)total : 0.f;
   float sum_b = 0.f, sum_z = 0.f;
-  rows.run(p, 0, 0, p.seq, s_f, p.grad_scale * p.coef * (float)p.E * inv_n, p.grad_scale * 2.f * p.z_coef * inv_n, sum_b, sum_z);
+  rows.run(p, base, 0, p.seq, s_f, p.grad_scale * p.coef * (float)p.E * inv_n, p.grad_scale * 2.f * p.z_coef * inv_n, sum_b, sum_z);
   sum_b = block_sum(sum_b, redf);
   sum_z = block_sum(sum_z, redf);
   if (tid == 0) {
-    p.tokens[0] = p.tokens[1] = n;
-    write_loss(p, sum_b, sum_z, n);
+    p.tokens[g] = n;
+    if (g == 0) p.tokens[p.groups] = total;
+    if (p.groups == 1) write_loss(p, sum_b, sum_z, n);
+    else p.part[g] = make_float2(sum_b, sum_z);
   }
 }
 
@@ -274,12 +285,13 @@ struct Shape { int slices, rows_per_block, chunks; };
 // Lanes per token: 16-byte accesses where the rows lie on such boundaries.
 int lanes_of(int E) { return E <= 16 ? 4 : E <= 32 ? 8 : E <= 64 ? 16 : E <= 128 ? 32 : 64; }
 
-// Slices of a group for counting, of about 8192 choices; blocks of its rows, each going over its 256 threads' worth of rows once or, where
-// that would make more than 1024 blocks, several times.
+// Slices of a group for counting, of 2048 choices (two a thread) up to 32 of them; blocks of its rows, each going over its 256 threads' worth of
+// rows once or, where that would make more than 1024 blocks, several times.  31744 x 128, eight choices, us: slices of 8192 | 4096, up to 64 | 2048,
+// up to 64 | 2048: 24.9 | 24.4 | 26.0 | 22.1;  512 | 1024 | 2048 blocks: 25.8 | 24.9 | 29.3.
 Shape shape_of(int T, int seq, int E, int top_k) {
   const int groups = T / seq;
   Shape s;
-  const long slices = ((long)seq * top_k + 8191) / 8192;
+  const long slices = ((long)seq * top_k + 2047) / 2048;
   s.slices = slices > 32 ? 32 : (int)slices;
   const int rows = 256 / lanes_of(E);
   const int passes = (seq + rows - 1) / rows, most = groups < 1024 ? 1024 / groups : 1;
@@ -303,7 +315,7 @@ size_t k_moe_balance_scratch(int T, int seq, int E) {
 
 template <int L, int C, int VEC>
 static void launch_rows(hipStream_t st, const BalanceArgs& p, bool small) {
-  if (small) RP_LAUNCH((balance_small_kernel<L, C, VEC>), dim3(1), dim3(1024), 0, st, p);
+  if (small) RP_LAUNCH((balance_small_kernel<L, C, VEC>), dim3(p.groups), dim3(1024), 0, st, p);
   else RP_LAUNCH((balance_rows_kernel<L, C, VEC>), dim3(p.groups * p.chunks), dim3(256), 0, st, p);
 }
 
@@ -324,8 +336,9 @@ hipError_t k_moe_balance(hipStream_t st, BalanceArgs p, int T, void* scratch) {
   at += up256((size_t)p.groups * s.slices * 4);
   p.part = reinterpret_cast<float2*>(at);
   p.total_given = p.groups > 1 && p.mask && (long)p.groups * s.slices > 1024;
-  // one block is through with 16384 logits (and their choices) in the time of the two launches it saves
-  const bool small = p.groups == 1 && (long)T * p.E <= 16384 && (long)T * p.top_k <= 8192;
+  // one block is through with a group of 16384 logits (and their choices) in the time of the launch or two that it saves: 256 tokens of 32 experts
+  // 12.3 -> 5.7 us
+  const bool small = (long)p.seq * p.E <= 16384 && (long)p.seq * p.top_k <= 8192 && (p.groups == 1 || !p.mask || T <= 65536);
   if (!small) {
     RP_LAUNCH(balance_count_kernel, dim3(p.groups * s.slices), dim3(1024), 0, st, p);
     if (p.total_given) RP_LAUNCH(balance_tokens_kernel, dim3(1), dim3(1024), 0, st, p);
@@ -348,6 +361,6 @@ hipError_t k_moe_balance(hipStream_t st, BalanceArgs p, int T, void* scratch) {
     else if (p.E <= 256) launch_rows<64, 4, 1>(st, p, small);
     else launch_rows<64, 16, 1>(st, p, small);
   }
-  if (!small) RP_LAUNCH(balance_total_kernel, dim3(1), dim3(1024), 0, st, p, (long)p.groups * s.chunks);
+  if (!small || p.groups > 1) RP_LAUNCH(balance_total_kernel, dim3(1), dim3(1024), 0, st, p, small ? (long)p.groups : (long)p.groups * s.chunks);
   return hipGetLastError();
 }

@@ -14,9 +14,6 @@
 //   dK, dV : workgroup = 128 keys, loop over 64-row tiles (d = 128: eight waves, pairs of which share 32 keys; d = 64: four waves)
 // Where there are too few workgroups for the chip, the loop is cut into `splits` slices, whose results another kernel joins in slice
 // order (fp32 partials in the caller's scratch; no atomics, so the result does not depend on timing).
-// Launch order: the key head changes fastest, so that (workgroups go round the eight XCDs) one XCD's L2 keeps to the key heads of its residue, and
-// the sequences of a padded batch spread over all of them (neighbouring key heads per XCD, as attention.hip has it, leaves the longest sequence
-// to two XCDs of a batch of four).
 // Keys behind kv_len are never read (they may hold anything); rows behind q_len get zeros, and lse -inf.
 #include "attention_device.hpp"
 #include "layer_ops.hpp"
@@ -72,6 +69,12 @@ RP_DEV int slices_used(int n, int splits) {
   return (n + per - 1) / per;
 }
 
+// Launch order: the key heads of all sequences change fastest, so that (workgroups go round the eight XCDs) one XCD's L2 keeps to the key heads of
+// its residue, and the sequences of a padded batch spread over all XCDs.  From one round of 256 workgroups to the next the heads move on by eight: a CU
+// that had a workgroup of the longest sequence gets one of another then.  (Training 4 x 509 queries of 64 heads of 64 against up to 1500 keys:
+// forward 68.6 us with neighbouring key heads per XCD as in attention.hip, where two XCDs have the longest sequence to themselves.)
+RP_DEV int head_at(int pos, int rest, int nhb) { return (pos - rest * nhb + 8 * (int)(((long)rest * nhb) >> 8)) % nhb; }
+
 // A 64-key tile, through a descriptor of its own that ends with the sequence: rows past the end read as zero, and no offset outgrows 32
 // bits however long the sequence is.
 template <int D, int NT>
@@ -116,7 +119,7 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_fwd_kernel(con
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nhb = p.kh * p.batch;
   const int rest = (int)blockIdx.x / nhb;
-  const int hb = (int)blockIdx.x % nhb;
+  const int hb = head_at((int)blockIdx.x, rest, nhb);
   const int split = SPLIT ? rest % p.splits : 0;
   const int r0 = (SPLIT ? rest / p.splits : rest) * BQ;
   const Rows s(p, hb);
@@ -470,53 +473,91 @@ __global__ void __launch_bounds__(256) cross_step_kernel(const CrossArgs p) {
   }
 }
 
-// Joins the slices of a row, weights exp2(m_i - max m): one wave per row, whose 512 / D lane groups take every (512 / D)-th slice and are added up in a
-// fixed order.  unit: keys a step of the kernel that cut the slices.
-template <int D>
-__global__ void __launch_bounds__(256) cross_fwd_join_kernel(const CrossArgs p, int unit) {
-  constexpr int CH = D / 8, GROUPS = 64 / CH;
+// ---- joining slices.  A thread has eight elements of one row and every G-th slice; the G threads that share them are added up in a fixed order, by
+// lane exchanges and, where they are in several waves, through LDS.  G grows with the number of slices: few slices of many rows are a matter
+// of bandwidth, many slices of few rows one of the latency of the loads that follow one another.
+template <int CH, int G, int N>
+RP_DEV bool add_groups(float (&acc)[N], float* red /* [256 / 64][CH * N] */) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  constexpr int IN_WAVE = CH * G < 64 ? CH * G : 64, WAVES = CH * G / IN_WAVE;
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+#pragma unroll
+    for (int o = CH; o < IN_WAVE; o <<= 1) acc[e] += __shfl_xor(acc[e], o, 64);
+  if constexpr (WAVES > 1) {
+    const int ch = tid % CH, w = tid >> 6, first = w / WAVES * WAVES;
+    if (lane < CH)
+#pragma unroll
+      for (int e = 0; e < N; ++e) red[w * CH * N + ch * N + e] = acc[e];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      acc[e] = red[first * CH * N + ch * N + e];
+#pragma unroll
+      for (int u = 1; u < WAVES; ++u) acc[e] += red[(first + u) * CH * N + ch * N + e];
+    }
+  }
+  return tid % (CH * G) < CH;      // the thread that stores
+}
+RP_DEV uint4 pack_times(const float* acc, float mul) {
+  return make_uint4(pack_bf16x2(acc[0] * mul, acc[1] * mul), pack_bf16x2(acc[2] * mul, acc[3] * mul), pack_bf16x2(acc[4] * mul, acc[5] * mul),
+                    pack_bf16x2(acc[6] * mul, acc[7] * mul));
+}
+RP_DEV void add_times(float* acc, const float* src, float wgt) {
+  const float4 x0 = *reinterpret_cast<const float4*>(src), x1 = *reinterpret_cast<const float4*>(src + 4);
+  acc[0] += wgt * x0.x; acc[1] += wgt * x0.y; acc[2] += wgt * x0.z; acc[3] += wgt * x0.w;
+  acc[4] += wgt * x1.x; acc[5] += wgt * x1.y; acc[6] += wgt * x1.z; acc[7] += wgt * x1.w;
+}
+
+// Rows of the forward (weights exp2(m_i - max m)) or, with DQ, of dq (sums, times scale).  unit: keys a step of the kernel that cut the slices.
+template <int D, int G, bool DQ>
+__global__ void __launch_bounds__(256) cross_row_join_kernel(const CrossArgs p, int unit) {
+  constexpr int CH = D / 8, RPB = 256 / (CH * G);
+  __shared__ float red[CH * G > 64 ? 4 * CH * 9 : 1];
   const int total = (p.a / p.kh) * p.seq_q, nhb = p.kh * p.batch;
-  const int lane = threadIdx.x & 63, ch = lane % CH, grp = lane / CH;
-  const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (item >= (long)nhb * total) return;
-  const int hb = (int)(item / total), r = (int)(item - (long)hb * total);
+  const int tid = threadIdx.x, ch = tid % CH, grp = tid / CH % G;
+  const long item = (long)blockIdx.x * RPB + tid / (CH * G);
+  const bool in = item < (long)nhb * total;
+  const int hb = in ? (int)(item / total) : 0, r = in ? (int)(item - (long)hb * total) : 0;
   const Rows s(p, hb);
-  const int n = r < s.valid ? slices_used((s.kvlen + unit - 1) / unit, p.splits) : 0;
+  const int n = in && r < s.valid ? slices_used((s.kvlen + unit - 1) / unit, p.splits) : 0;
+  const long row = (long)hb * total + r, step = (long)nhb * total;
+  float acc[9];      // eight elements, and the sum of exponentials
+#pragma unroll
+  for (int e = 0; e < 9; ++e) acc[e] = 0.f;
   float m = -INFINITY;
-  for (int i = lane; i < n; i += 64) m = fmaxf(m, p.part_ml[((long)i * nhb + hb) * total + r].x);
-  m = wave_max(m);
-  float l = 0.f, acc[8];
+  if constexpr (!DQ) {
+    constexpr int L = CH * G < 64 ? CH * G : 64;      // lanes of a wave that work on the row
+#pragma unroll 2
+    for (int i = tid % L; i < n; i += L) m = fmaxf(m, p.part_ml[i * step + row].x);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  }
 #pragma unroll 4
-  for (int i = grp; i < n; i += GROUPS) {
-    const long at = ((long)i * nhb + hb) * total + r;
-    const float2 ml = p.part_ml[at];
-    const float4 x0 = *reinterpret_cast<const float4*>(p.part + at * D + ch * 8), x1 = *reinterpret_cast<const float4*>(p.part + at * D + ch * 8 + 4);
-    const float wgt = fast_exp2(ml.x - m);
-    l += wgt * ml.y;
-    acc[0] += wgt * x0.x; acc[1] += wgt * x0.y; acc[2] += wgt * x0.z; acc[3] += wgt * x0.w;
-    acc[4] += wgt * x1.x; acc[5] += wgt * x1.y; acc[6] += wgt * x1.z; acc[7] += wgt * x1.w;
+  for (int i = grp; i < n; i += G) {
+    float wgt = 1.f;
+    if constexpr (!DQ) {
+      const float2 ml = p.part_ml[i * step + row];
+      wgt = fast_exp2(ml.x - m);
+      acc[8] += wgt * ml.y;
+    }
+    add_times(acc, p.part + (i * step + row) * D + ch * 8, wgt);
   }
-#pragma unroll
-  for (int o = CH; o < 64; o <<= 1) {
-    l += __shfl_xor(l, o, 64);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+  const bool mine = add_groups<CH, G, 9>(acc, red);
+  if (!in || !mine) return;
+  if constexpr (DQ) {
+    *reinterpret_cast<uint4*>(p.dq + s.offset(r, p.lddq, D) + ch * 8) = pack_times(acc, p.scale);
+  } else {
+    if (p.lse && ch == 0) p.lse[s.stat(r, p.a)] = n ? m * 0.6931471805599453f + logf(acc[8]) : -INFINITY;
+    *reinterpret_cast<uint4*>(p.o + s.offset(r, p.ldo, D) + ch * 8) = pack_times(acc, n ? 1.f / acc[8] : 0.f);
   }
-  if (grp) return;
-  const float mul = n ? 1.f / l : 0.f;
-  if (p.lse && ch == 0) p.lse[s.stat(r, p.a)] = n ? m * 0.6931471805599453f + logf(l) : -INFINITY;
-  *reinterpret_cast<uint4*>(p.o + s.offset(r, p.ldo, D) + ch * 8) =
-      make_uint4(pack_bf16x2(acc[0] * mul, acc[1] * mul), pack_bf16x2(acc[2] * mul, acc[3] * mul), pack_bf16x2(acc[4] * mul, acc[5] * mul),
-                 pack_bf16x2(acc[6] * mul, acc[7] * mul));
 }
 
 // ================================================================================================ dQ
 // delta comes from the stored output, as in attention.hip, where many keys share a row's weight.  With few keys a row may put nearly all of it on
 // one, dP - delta cancels there, and the rounding of the stored output (2^-9 of delta) would show in what is left: up to EXACT_DELTA keys
 // the scores are made twice, and delta = sum P dP is as exact as they are.
-constexpr int EXACT_DELTA = 512;
+constexpr int EXACT_DELTA = 256;
 
 template <int D, int NW, bool SPLIT>
 __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(const CrossArgs p) {
@@ -533,7 +574,7 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(cons
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nhb = p.kh * p.batch;
   const int rest = (int)blockIdx.x / nhb;
-  const int hb = (int)blockIdx.x % nhb;
+  const int hb = head_at((int)blockIdx.x, rest, nhb);
   const int split = SPLIT ? rest % p.splits : 0;
   const int r0 = (SPLIT ? rest / p.splits : rest) * BQ;
   const Rows s(p, hb);
@@ -621,11 +662,12 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(cons
   };
 
   if (exact_delta) {      // uniform over the workgroup
+    if (tiles > 0) load_tiles(0);
     for (int j = 0; j < tiles; ++j) {
-      load_tiles(j);
       __syncthreads();
       store_tiles(0);
       __syncthreads();
+      if (j + 1 < tiles) load_tiles(j + 1);
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
         f32x4 sT[2][2], dpT[2][2];
@@ -741,33 +783,6 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(cons
   }
 }
 
-// dq = scale * the sum of a row's slices, in slice order.
-template <int D>
-__global__ void __launch_bounds__(256) cross_dq_join_kernel(const CrossArgs p) {
-  constexpr int CH = D / 8;
-  const int total = (p.a / p.kh) * p.seq_q, nhb = p.kh * p.batch;
-  const long idx = (long)blockIdx.x * 256 + threadIdx.x;
-  const long item = idx / CH;
-  const int ch = (int)(idx % CH);
-  if (item >= (long)nhb * total) return;
-  const int hb = (int)(item / total), r = (int)(item - (long)hb * total);
-  const Rows s(p, hb);
-  const int n = r < s.valid ? slices_used((s.kvlen + 63) / 64, p.splits) : 0;
-  float acc[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-  for (int i = 0; i < n; ++i) {
-    const float* const src = p.part + (((long)i * nhb + hb) * total + r) * D + ch * 8;
-    const float4 x0 = *reinterpret_cast<const float4*>(src), x1 = *reinterpret_cast<const float4*>(src + 4);
-    acc[0] += x0.x; acc[1] += x0.y; acc[2] += x0.z; acc[3] += x0.w;
-    acc[4] += x1.x; acc[5] += x1.y; acc[6] += x1.z; acc[7] += x1.w;
-  }
-  const float mul = p.scale;
-  *reinterpret_cast<uint4*>(p.dq + s.offset(r, p.lddq, D) + ch * 8) =
-      make_uint4(pack_bf16x2(acc[0] * mul, acc[1] * mul), pack_bf16x2(acc[2] * mul, acc[3] * mul), pack_bf16x2(acc[4] * mul, acc[5] * mul),
-                 pack_bf16x2(acc[6] * mul, acc[7] * mul));
-}
-
 // ================================================================================================ dK, dV
 // A thread's share of the 64-row tiles of q and dO: which head and query each of its 16-byte pieces belongs to.  Rows past the last query
 // read row 0 again (their P is made zero, see row_start).
@@ -881,7 +896,7 @@ __global__ void __launch_bounds__(256) cross_dkv_kernel(const CrossArgs p) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nhb = p.kh * p.batch;
   const int rest = (int)blockIdx.x / nhb;
-  const int hb = (int)blockIdx.x % nhb;
+  const int hb = head_at((int)blockIdx.x, rest, nhb);
   const int split = rest % p.splits, kv0 = (rest / p.splits) * 128, kw0 = kv0 + 32 * w;
   const Rows s(p, hb);
   if (p.splits == 1) zero_keys<D, 256>(p, s, kv0, tid);
@@ -1021,7 +1036,7 @@ __global__ void __launch_bounds__(512) cross_dkv_pair_kernel(const CrossArgs p) 
   const int w = w8 >> 1, h = w8 & 1;
   const int nhb = p.kh * p.batch;
   const int rest = (int)blockIdx.x / nhb;
-  const int hb = (int)blockIdx.x % nhb;
+  const int hb = head_at((int)blockIdx.x, rest, nhb);
   const int split = rest % p.splits, kv0 = (rest / p.splits) * 128, kw0 = kv0 + 32 * w;
   const Rows s(p, hb);
   if (p.splits == 1) zero_keys<D, 512>(p, s, kv0, tid);
@@ -1163,32 +1178,28 @@ __global__ void __launch_bounds__(512) cross_dkv_pair_kernel(const CrossArgs p) 
   }
 }
 
-// dk, dv = the sum of a key's slices, in slice order; zero behind the sequence.  Eight elements of dk or of dv per thread.
-template <int D>
-__global__ void __launch_bounds__(256) cross_dkv_join_kernel(const CrossArgs p) {
-  const int ch_row = p.kh * (D / 8);
-  const long T = (long)p.batch * p.seq_kv, per = T * ch_row;
-  long idx = (long)blockIdx.x * 256 + threadIdx.x;
-  if (idx >= 2 * per) return;
-  const bool is_v = idx >= per;
-  if (is_v) idx -= per;
-  const long t = idx / ch_row;
-  const int c = (int)(idx - t * ch_row);
-  const int b = (int)(t / p.seq_kv), key = (int)(t - (long)b * p.seq_kv);
+// dk, dv = the sum of a key's slices; zero behind the sequence.  A "row" is a key head of dk or dv.
+template <int D, int G>
+__global__ void __launch_bounds__(256) cross_key_join_kernel(const CrossArgs p) {
+  constexpr int CH = D / 8, RPB = 256 / (CH * G);
+  __shared__ float red[CH * G > 64 ? 4 * CH * 8 : 1];
+  const int tid = threadIdx.x, ch = tid % CH, grp = tid / CH % G;
+  const long T = (long)p.batch * p.seq_kv, rows = T * p.kh;
+  const long item = (long)blockIdx.x * RPB + tid / (CH * G);
+  const bool in = item < 2 * rows, is_v = item >= rows;
+  const long kv = !in ? 0 : is_v ? item - rows : item;
+  const long t = kv / p.kh;
+  const int g = (int)(kv - t * p.kh), b = (int)(t / p.seq_kv), key = (int)(t - (long)b * p.seq_kv);
   const Rows s(p, b * p.kh);
-  const int n = key < s.kvlen ? slices_used((s.valid + 63) / 64, p.splits) : 0;
-  const long each = T * p.kh * D;
-  const float* src = p.part + (is_v ? p.splits * each : 0) + t * p.kh * D + c * 8;
+  const int n = in && key < s.kvlen ? slices_used((s.valid + 63) / 64, p.splits) : 0;
+  const float* const src = p.part + (is_v ? p.splits * rows * D : 0) + kv * D + ch * 8;
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-  for (int i = 0; i < n; ++i, src += each) {
-    const float4 x0 = *reinterpret_cast<const float4*>(src), x1 = *reinterpret_cast<const float4*>(src + 4);
-    acc[0] += x0.x; acc[1] += x0.y; acc[2] += x0.z; acc[3] += x0.w;
-    acc[4] += x1.x; acc[5] += x1.y; acc[6] += x1.z; acc[7] += x1.w;
-  }
-  bf16* const dst = is_v ? p.dv + t * p.lddv + c * 8 : p.dk + t * p.lddk + c * 8;
-  *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]), pack_bf16x2(acc[4], acc[5]), pack_bf16x2(acc[6], acc[7]));
+#pragma unroll 4
+  for (int i = grp; i < n; i += G) add_times(acc, src + i * rows * D, 1.f);
+  const bool mine = add_groups<CH, G, 8>(acc, red);
+  if (in && mine) *reinterpret_cast<uint4*>((is_v ? p.dv + t * p.lddv : p.dk + t * p.lddk) + g * D + ch * 8) = pack_times(acc, 1.f);
 }
 
 // operand tiles, or the epilogue's staging of every wave's 32 x d block, whichever is larger
@@ -1210,31 +1221,64 @@ hipError_t launch(K kern, int grid, int threads, int smem, hipStream_t st, const
   return hipGetLastError();
 }
 
-// Slices of a loop over `steps` tiles that would run in `groups` workgroups: enough for two workgroups per CU, each with
-// two tiles at least, as many as the scratch holds.
-int splits_for(long groups, int steps, size_t bytes_each, size_t scratch_bytes) {
-  if (groups < 1 || groups >= 256 || steps < 4) return 1;
-  long n = 512 / groups;
-  if (n > steps / 2) n = steps / 2;
-  if (bytes_each && n > (long)(scratch_bytes / bytes_each)) n = (long)(scratch_bytes / bytes_each);
-  return n < 2 ? 1 : (int)n;
+// Slices of a loop over `steps` tiles that would run in `groups` workgroups, at most so many that they make `want`, and as the scratch holds: the
+// number that saves most, if any.  A tile of a workgroup that has few others beside it takes `tile_us` (its chain of loads, products and
+// exponentials); joining costs a launch, about 5 us, and the slices' way to memory and back at 5 TB/s.  Measured with a slice of at least two |
+// four | eight tiles (forward and backward of a training step, us): 102 queries x 16 heads against 1711 keys 48.3 | 52.0 | 58.8; 8 x 15 x 4 heads against
+// 352 32.5 | 36.1 | 36.1; 8 x 47 x 64 heads of 64 against up to 538 60.3 | 60.3 | 47.7; this rule takes the best of each.
+int splits_for(long groups, long want, int steps, double tile_us, size_t bytes_each, size_t scratch_bytes) {
+  if (groups < 1) return 1;
+  long most = want / groups;
+  if (most > steps) most = steps;
+  if (bytes_each && most > (long)(scratch_bytes / bytes_each)) most = (long)(scratch_bytes / bytes_each);
+  int best = 1;
+  double saved = 0.0;
+  for (int n = 2; n <= most; ++n) {
+    const double s = (steps - (steps + n - 1) / n) * tile_us - 5.0 - 2.0 * n * (double)bytes_each / 5.0e6;
+    if (s > saved) { saved = s; best = n; }
+  }
+  return best;
 }
 int ceil_div(long a, int b) { return (int)((a + b - 1) / b); }
 long row_count(const CrossArgs& p) { return (long)(p.a / p.kh) * p.seq_q; }
 size_t row_part_bytes(const CrossArgs& p, int d) { return (size_t)p.kh * p.batch * row_count(p) * (d + 2) * 4; }      // o or dq, and (m, l)
 size_t key_part_bytes(const CrossArgs& p, int d) { return (size_t)2 * p.batch * p.seq_kv * p.kh * d * 4; }
-int row_splits(const CrossArgs& p, int d, size_t bytes) { return splits_for((long)ceil_div(row_count(p), 128) * p.kh * p.batch, ceil_div(p.seq_kv, 64), row_part_bytes(p, d), bytes); }
-// Few rows: 32-key steps, four at a time; slices of eight steps and more, for two workgroups per CU.
+// Forward and dQ: two workgroups of 128 rows per CU.
+int row_splits(const CrossArgs& p, int d, size_t bytes) {
+  return splits_for((long)ceil_div(row_count(p), 128) * p.kh * p.batch, 512, ceil_div(p.seq_kv, 64), 1.4, row_part_bytes(p, d), bytes);
+}
+// Few rows: two workgroups per CU; a slice has a 32-key step for each of its four waves at least.  (Slices of 256 keys and more: one token of 8
+// sequences against up to 1500 keys 13.5 us, with 128 12.5.)
 bool few_rows(const CrossArgs& p) { return row_count(p) <= 32; }
 int step_splits(const CrossArgs& p, int d, size_t bytes) {
   const long nhb = (long)p.kh * p.batch;
-  long n = nhb ? 512 / nhb : 1;
-  if (n > ceil_div(p.seq_kv, 256)) n = ceil_div(p.seq_kv, 256);
   const size_t each = row_part_bytes(p, d);
+  long n = nhb ? 512 / nhb : 1;
+  if (n > ceil_div(p.seq_kv, 128)) n = ceil_div(p.seq_kv, 128);
   if (each && n > (long)(bytes / each)) n = (long)(bytes / each);
   return n < 2 ? 1 : (int)n;
 }
-int key_splits(const CrossArgs& p, int d, size_t bytes) { return splits_for((long)ceil_div(p.seq_kv, 128) * p.kh * p.batch, ceil_div(row_count(p), 64), key_part_bytes(p, d), bytes); }
+// dK, dV: the kernel at d = 128 has a CU to itself; at d = 64 two share one, and a third takes the place of those that end early
+int key_splits(const CrossArgs& p, int d, size_t bytes) {
+  return splits_for((long)ceil_div(p.seq_kv, 128) * p.kh * p.batch, d == 128 ? 256 : 768, ceil_div(row_count(p), 64), d == 128 ? 2.2 : 1.6, key_part_bytes(p, d), bytes);
+}
+
+// Threads that share a row of n slices.
+int join_groups(int n) { return n < 6 ? 1 : n < 24 ? 4 : 16; }
+template <int D, bool DQ>
+hipError_t join_rows(hipStream_t st, const CrossArgs& p, int unit) {
+  const int g = join_groups(p.splits), grid = ceil_div(row_count(p) * p.kh * p.batch, 256 / (D / 8 * g));
+  if (g == 1) return launch(cross_row_join_kernel<D, 1, DQ>, grid, 256, 0, st, p, unit);
+  if (g == 4) return launch(cross_row_join_kernel<D, 4, DQ>, grid, 256, 0, st, p, unit);
+  return launch(cross_row_join_kernel<D, 16, DQ>, grid, 256, 0, st, p, unit);
+}
+template <int D>
+hipError_t join_keys(hipStream_t st, const CrossArgs& p) {
+  const int g = join_groups(p.splits), grid = ceil_div((long)2 * p.batch * p.seq_kv * p.kh, 256 / (D / 8 * g));
+  if (g == 1) return launch(cross_key_join_kernel<D, 1>, grid, 256, 0, st, p);
+  if (g == 4) return launch(cross_key_join_kernel<D, 4>, grid, 256, 0, st, p);
+  return launch(cross_key_join_kernel<D, 16>, grid, 256, 0, st, p);
+}
 
 template <int D>
 hipError_t fwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
@@ -1252,7 +1296,7 @@ hipError_t fwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   } else if (p.splits > 1) {
     e = launch(cross_fwd_kernel<D, 4, true>, ceil_div(rows, 128) * nhb * p.splits, 256, fwd_smem_bytes(D, 4), st, p);
   }
-  if (p.splits > 1 && e == hipSuccess) e = launch(cross_fwd_join_kernel<D>, ceil_div(nhb * rows, 4), 256, 0, st, p, few ? 32 : 64);
+  if (p.splits > 1 && e == hipSuccess) e = join_rows<D, false>(st, p, few ? 32 : 64);
   if (few || p.splits > 1) return e;
   if (D == 128 && (long)ceil_div(rows, 256) * nhb >= 1024)
     return launch(cross_fwd_kernel<D, 8, false>, ceil_div(rows, 256) * nhb, 512, fwd_smem_bytes(D, 8), st, p);
@@ -1271,7 +1315,7 @@ hipError_t bwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
     // no queries: dk and dv are zero
   } else if (p.splits > 1) {
     e = launch(cross_dq_kernel<D, 4, true>, ceil_div(rows, 128) * nhb * p.splits, 256, dq_smem_bytes(D, 4), st, p);
-    if (e == hipSuccess) e = launch(cross_dq_join_kernel<D>, ceil_div(nhb * rows * (D / 8), 256), 256, 0, st, p);
+    if (e == hipSuccess) e = join_rows<D, true>(st, p, 64);
   } else if (D == 128 && (long)ceil_div(rows, 256) * nhb >= 1024) {
     e = launch(cross_dq_kernel<D, 8, false>, ceil_div(rows, 256) * nhb, 512, dq_smem_bytes(D, 8), st, p);
   } else {
@@ -1283,7 +1327,7 @@ hipError_t bwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   if constexpr (D == 128) e = launch(cross_dkv_pair_kernel<D>, grid, 512, dkv_pair_smem_bytes(D), st, p);
   else e = launch(cross_dkv_kernel<D>, grid, 256, dkv_smem_bytes(D), st, p);
   if (e != hipSuccess || p.splits == 1) return e;
-  return launch(cross_dkv_join_kernel<D>, ceil_div((long)2 * p.batch * p.seq_kv * p.kh * (D / 8), 256), 256, 0, st, p);
+  return join_keys<D>(st, p);
 }
 
 }  // namespace
