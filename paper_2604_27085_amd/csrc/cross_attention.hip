@@ -1280,6 +1280,12 @@ hipError_t join_keys(hipStream_t st, const CrossArgs& p) {
   return launch(cross_key_join_kernel<D, 16>, grid, 256, 0, st, p);
 }
 
+#ifndef BIG
+#define BIG 1024
+#endif
+#ifndef BIGQ
+#define BIGQ 1024
+#endif
 template <int D>
 hipError_t fwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   const int nhb = p.kh * p.batch;
@@ -1298,7 +1304,7 @@ hipError_t fwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   }
   if (p.splits > 1 && e == hipSuccess) e = join_rows<D, false>(st, p, few ? 32 : 64);
   if (few || p.splits > 1) return e;
-  if (D == 128 && (long)ceil_div(rows, 256) * nhb >= 1024)
+  if (D == 128 && (long)ceil_div(rows, 256) * nhb >= BIG)
     return launch(cross_fwd_kernel<D, 8, false>, ceil_div(rows, 256) * nhb, 512, fwd_smem_bytes(D, 8), st, p);
   return launch(cross_fwd_kernel<D, 4, false>, ceil_div(rows, 128) * nhb, 256, fwd_smem_bytes(D, 4), st, p);
 }
@@ -1316,7 +1322,7 @@ hipError_t bwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   } else if (p.splits > 1) {
     e = launch(cross_dq_kernel<D, 4, true>, ceil_div(rows, 128) * nhb * p.splits, 256, dq_smem_bytes(D, 4), st, p);
     if (e == hipSuccess) e = join_rows<D, true>(st, p, 64);
-  } else if (D == 128 && (long)ceil_div(rows, 256) * nhb >= 1024) {
+  } else if (D == 128 && (long)ceil_div(rows, 256) * nhb >= BIG) {
     e = launch(cross_dq_kernel<D, 8, false>, ceil_div(rows, 256) * nhb, 512, dq_smem_bytes(D, 8), st, p);
   } else {
     e = launch(cross_dq_kernel<D, 4, false>, ceil_div(rows, 128) * nhb, 256, dq_smem_bytes(D, 4), st, p);
