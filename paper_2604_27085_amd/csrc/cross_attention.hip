@@ -9,7 +9,8 @@
 // Tiles are cut from the rows, so short sequences of many heads fill them, one workgroup's keys serve all heads of the group, and dK, dV of a
 // group need no partials per head.  The tiles, fragments and instructions are those of attention.hip.
 //
-//   forward: workgroup = NW waves x 32 rows, loop over 64-key tiles
+//   forward: workgroup = four waves x 32 rows, loop over 64-key tiles (eight waves, one workgroup per CU, which pays in attention.hip, are 0 to 3 %
+//            slower here, where no workgroup has fewer tiles than another)
 //   dQ     : the same; delta on the way
 //   dK, dV : workgroup = 128 keys, loop over 64-row tiles (d = 128: eight waves, pairs of which share 32 keys; d = 64: four waves)
 // Where there are too few workgroups for the chip, the loop is cut into `splits` slices, whose results another kernel joins in slice
@@ -104,14 +105,12 @@ RP_DEV void zero_rows(const CrossArgs& p, const Rows& s, bf16* out, long ld, flo
 }
 
 // ================================================================================================ forward
-template <int D, int NW, bool SPLIT>
-__global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_fwd_kernel(const CrossArgs p) {
-  constexpr int LDK = D + 8, LDV = D + 32, KS = D / 16, DT = D / 32, NT = NW * 64, BQ = NW * 32;
+template <int D, bool SPLIT>
+__global__ void __launch_bounds__(256, 2) cross_fwd_kernel(const CrossArgs p) {
+  constexpr int LDK = D + 8, LDV = D + 32, KS = D / 16, DT = D / 32, NT = 256, BQ = 128;
   using T64 = Tile64<D, NT>;
-  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // fwd_smem_bytes(D, NW)
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // fwd_smem_bytes(D)
   bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);
-  constexpr bool DB = NW >= 8;      // two sets of K/V tiles, one barrier per key tile
-  constexpr int SET = 64 * LDK + 64 * LDV;
   bf16* const Ks = smem;
   bf16* const Vs = smem + 64 * LDK;
 
@@ -153,34 +152,20 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_fwd_kernel(con
 #pragma unroll
     for (int v = 0; v < 16; ++v) oacc[dt][v] = 0.f;
 
-  const bf16* const kfrag0 = Ks + lr * LDK + 8 * lk;
-  const bf16* const vfrag0 = Vs + tr_base32<LDV>(lane);
+  const bf16* const kfrag = Ks + lr * LDK + 8 * lk;
+  const bf16* const vfrag = Vs + tr_base32<LDV>(lane);
   uint4 kreg[T64::NREG], vreg[T64::NREG];
   auto load_tiles = [&](int j) {
     kt_.load(kreg, j * 64, tid);
     vt_.load(vreg, j * 64, tid);
   };
-  auto store_tiles = [&](int set) {
-    T64::template store<LDK>(kreg, Ks + set * SET, tid);
-    T64::template store<LDV>(vreg, Vs + set * SET, tid);
-  };
   if (j0 < j1) load_tiles(j0);
-  if constexpr (DB) {     // the first tile into its set, the second on its way
-    if (j0 < j1) store_tiles(j0 & 1);
-    if (j0 + 1 < j1) load_tiles(j0 + 1);
-  }
   for (int j = j0; j < j1; ++j) {
     __syncthreads();
-    if constexpr (DB) {
-      if (j + 1 < j1) store_tiles((j + 1) & 1);
-      if (j + 2 < j1) load_tiles(j + 2);
-    } else {
-      store_tiles(0);
-      __syncthreads();
-      if (j + 1 < j1) load_tiles(j + 1);
-    }
-    const bf16* const kfrag = kfrag0 + (DB ? (j & 1) * SET : 0);
-    const bf16* const vfrag = vfrag0 + (DB ? (j & 1) * SET : 0);
+    T64::template store<LDK>(kreg, Ks, tid);
+    T64::template store<LDV>(vreg, Vs, tid);
+    __syncthreads();
+    if (j + 1 < j1) load_tiles(j + 1);
     const int kv0 = j * 64;
     f32x16 sT[2];
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -219,7 +204,7 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_fwd_kernel(con
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sT[kt][v]);
-    mx = (NW < 8 ? half_max(mx) : fmaxf(mx, __shfl_xor(mx, 32, 64))) * p.scale_log2e;
+    mx = half_max(mx) * p.scale_log2e;
     // m_run is a reference exponent that moves only when a row's maximum outgrows it by 2^8 (see attention.hip); every tile has a key,
     // so it is finite from the first one on
     const bool grow = mx > m_run + 8.f;
@@ -559,14 +544,12 @@ __global__ void __launch_bounds__(256) cross_row_join_kernel(const CrossArgs p, 
 // the scores are made twice, and delta = sum P dP is as exact as they are.
 constexpr int EXACT_DELTA = 256;
 
-template <int D, int NW, bool SPLIT>
-__global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(const CrossArgs p) {
-  constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, NT = NW * 64, BQ = NW * 32;
+template <int D, bool SPLIT>
+__global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
+  constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, NT = 256, BQ = 128;
   using T64 = Tile64<D, NT>;
-  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // dq_smem_bytes(D, NW)
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // dq_smem_bytes(D)
   bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);
-  constexpr bool DB = NW >= 8;
-  constexpr int SET = 2 * 64 * LD;
   bf16* const Ks = smem;
   bf16* const Vs = smem + 64 * LD;
 
@@ -628,19 +611,19 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(cons
     }
   }
 
-  const bf16* const kfrag0 = Ks + lr * LD + 8 * lg;
-  const bf16* const ktfrag0 = Ks + tr_base<LD>(lane);
+  const bf16* const kfrag = Ks + lr * LD + 8 * lg;      // (V lies 64 rows further on)
+  const bf16* const ktfrag = Ks + tr_base<LD>(lane);
   uint4 kreg[T64::NREG], vreg[T64::NREG];
   auto load_tiles = [&](int j) {
     kt_.load(kreg, j * 64, tid);
     vt_.load(vreg, j * 64, tid);
   };
-  auto store_tiles = [&](int set) {
-    T64::template store<LD>(kreg, Ks + set * SET, tid);
-    T64::template store<LD>(vreg, Vs + set * SET, tid);
+  auto store_tiles = [&]() {
+    T64::template store<LD>(kreg, Ks, tid);
+    T64::template store<LD>(vreg, Vs, tid);
   };
-  // scores and dP of 32 keys, transposed: [16 keys][16 rows]; kfrag: the set's K, its V lies 64 rows further on
-  auto scores = [&](const bf16* kfrag, int k2, f32x4 (&sT)[2][2], f32x4 (&dpT)[2][2]) {
+  // scores and dP of 32 keys, transposed: [16 keys][16 rows]
+  auto scores = [&](int k2, f32x4 (&sT)[2][2], f32x4 (&dpT)[2][2]) {
     const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
     constexpr int NS = 4 * KS, AHEAD = 4;     // n = (ks * 2 + kt) * 2 + which
     auto sfrag_at = [&](int n) { return *reinterpret_cast<const uint4*>(kfrag + (32 * k2 + 16 * ((n >> 1) & 1) + 64 * (n & 1)) * LD + 32 * (n >> 2)); };
@@ -665,13 +648,13 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(cons
     if (tiles > 0) load_tiles(0);
     for (int j = 0; j < tiles; ++j) {
       __syncthreads();
-      store_tiles(0);
+      store_tiles();
       __syncthreads();
       if (j + 1 < tiles) load_tiles(j + 1);
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
         f32x4 sT[2][2], dpT[2][2];
-        scores(kfrag0, k2, sT, dpT);
+        scores(k2, sT, dpT);
         const int klim = s.kvlen - 1 - (j * 64 + 32 * k2 + 4 * lg);
 #pragma unroll
         for (int c = 0; c < 2; ++c)
@@ -698,27 +681,17 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(cons
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dqacc[dt][0] = dqacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (j0 < j1) load_tiles(j0);
-  if constexpr (DB) {
-    if (j0 < j1) store_tiles(j0 & 1);
-    if (j0 + 1 < j1) load_tiles(j0 + 1);
-  }
   for (int j = j0; j < j1; ++j) {
     __syncthreads();
-    if constexpr (DB) {
-      if (j + 1 < j1) store_tiles((j + 1) & 1);
-      if (j + 2 < j1) load_tiles(j + 2);
-    } else {
-      store_tiles(0);
-      __syncthreads();
-      if (j + 1 < j1) load_tiles(j + 1);
-    }
-    const int set = DB ? (j & 1) * SET : 0;
+    store_tiles();
+    __syncthreads();
+    if (j + 1 < j1) load_tiles(j + 1);
     const bool need_mask = j * 64 + 64 > s.kvlen;
     // the two 32-key halves of the tile one after the other: half as many score registers live at a time
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2) {
       f32x4 sT[2][2], dpT[2][2];
-      scores(kfrag0 + set, k2, sT, dpT);
+      scores(k2, sT, dpT);
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -737,7 +710,7 @@ __global__ void __launch_bounds__(NW * 64, NW <= 4 ? 2 : 1) cross_dq_kernel(cons
       }
       constexpr int AHEAD = 2;      // K^T fragments requested that many pairs of products early
       const uint4 df[2] = {pack_frag(sT[0][0], sT[1][0]), pack_frag(sT[0][1], sT[1][1])};
-      auto ufrag_at = [&](int n) { return read_frag_tr<LD>(ktfrag0 + set + 32 * k2 * LD + 16 * n); };
+      auto ufrag_at = [&](int n) { return read_frag_tr<LD>(ktfrag + 32 * k2 * LD + 16 * n); };
       uint4 uring[AHEAD];
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
@@ -1204,9 +1177,9 @@ __global__ void __launch_bounds__(256) cross_key_join_kernel(const CrossArgs p) 
 
 // operand tiles, or the epilogue's staging of every wave's 32 x d block, whichever is larger
 constexpr int max_i(int a, int b) { return a > b ? a : b; }
-constexpr int fwd_smem_bytes(int d, int nw) { return max_i((nw >= 8 ? 2 : 1) * (64 * (d + 8) + 64 * (d + 32)), nw * 32 * (d + 8)) * 2; }
+constexpr int fwd_smem_bytes(int d) { return max_i(64 * (d + 8) + 64 * (d + 32), 128 * (d + 8)) * 2; }
 constexpr int step_smem_bytes(int d, int nc) { return max_i(4 * 32 * tile_ld(d) * 2, 8 * 16 * nc * 4 + 4 * 16 * nc * (d + 4) * 4); }
-constexpr int dq_smem_bytes(int d, int nw) { return max_i((nw >= 8 ? 2 : 1) * (2 * 64 * tile_ld(d)), nw * 32 * (d + 8)) * 2; }
+constexpr int dq_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d), 128 * (d + 8)) * 2; }
 constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 512, 4 * 32 * (d + 4) * 4); }
 constexpr int dkv_pair_smem_bytes(int d) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * 4 * 64 * 16 + 1024; }
 
@@ -1280,12 +1253,6 @@ hipError_t join_keys(hipStream_t st, const CrossArgs& p) {
   return launch(cross_key_join_kernel<D, 16>, grid, 256, 0, st, p);
 }
 
-#ifndef BIG
-#define BIG 1024
-#endif
-#ifndef BIGQ
-#define BIGQ 1024
-#endif
 template <int D>
 hipError_t fwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   const int nhb = p.kh * p.batch;
@@ -1300,13 +1267,11 @@ hipError_t fwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
     if (rows <= 16) e = p.splits > 1 ? launch(cross_step_kernel<D, 1, true>, grid, 256, step_smem_bytes(D, 1), st, p) : launch(cross_step_kernel<D, 1, false>, grid, 256, step_smem_bytes(D, 1), st, p);
     else e = p.splits > 1 ? launch(cross_step_kernel<D, 2, true>, grid, 256, step_smem_bytes(D, 2), st, p) : launch(cross_step_kernel<D, 2, false>, grid, 256, step_smem_bytes(D, 2), st, p);
   } else if (p.splits > 1) {
-    e = launch(cross_fwd_kernel<D, 4, true>, ceil_div(rows, 128) * nhb * p.splits, 256, fwd_smem_bytes(D, 4), st, p);
+    e = launch(cross_fwd_kernel<D, true>, ceil_div(rows, 128) * nhb * p.splits, 256, fwd_smem_bytes(D), st, p);
   }
   if (p.splits > 1 && e == hipSuccess) e = join_rows<D, false>(st, p, few ? 32 : 64);
   if (few || p.splits > 1) return e;
-  if (D == 128 && (long)ceil_div(rows, 256) * nhb >= BIG)
-    return launch(cross_fwd_kernel<D, 8, false>, ceil_div(rows, 256) * nhb, 512, fwd_smem_bytes(D, 8), st, p);
-  return launch(cross_fwd_kernel<D, 4, false>, ceil_div(rows, 128) * nhb, 256, fwd_smem_bytes(D, 4), st, p);
+  return launch(cross_fwd_kernel<D, false>, ceil_div(rows, 128) * nhb, 256, fwd_smem_bytes(D), st, p);
 }
 
 template <int D>
@@ -1320,12 +1285,10 @@ hipError_t bwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   if (rows == 0) {
     // no queries: dk and dv are zero
   } else if (p.splits > 1) {
-    e = launch(cross_dq_kernel<D, 4, true>, ceil_div(rows, 128) * nhb * p.splits, 256, dq_smem_bytes(D, 4), st, p);
+    e = launch(cross_dq_kernel<D, true>, ceil_div(rows, 128) * nhb * p.splits, 256, dq_smem_bytes(D), st, p);
     if (e == hipSuccess) e = join_rows<D, true>(st, p, 64);
-  } else if (D == 128 && (long)ceil_div(rows, 256) * nhb >= BIG) {
-    e = launch(cross_dq_kernel<D, 8, false>, ceil_div(rows, 256) * nhb, 512, dq_smem_bytes(D, 8), st, p);
   } else {
-    e = launch(cross_dq_kernel<D, 4, false>, ceil_div(rows, 128) * nhb, 256, dq_smem_bytes(D, 4), st, p);
+    e = launch(cross_dq_kernel<D, false>, ceil_div(rows, 128) * nhb, 256, dq_smem_bytes(D), st, p);
   }
   if (e != hipSuccess || p.seq_kv == 0) return e;
   p.splits = key_splits(p, D, bytes);
