@@ -72,14 +72,13 @@ __global__ void __launch_bounds__(256) rope_table_scaled_kernel(float2* __restri
 }
 
 // ------------------------------------------------------------------------------------------------ rotation
-template <int V> struct Words;
-template <> struct Words<8> { typedef uint4 type; };
-template <> struct Words<4> { typedef uint2 type; };
-template <> struct Words<2> { typedef uint32_t type; };
-template <> struct Words<1> { typedef unsigned short type; };
-
+template <int V> struct Piece;      // V elements on a boundary of their own size
+template <> struct Piece<8> { typedef uint4 type; };
+template <> struct Piece<4> { typedef uint2 type; };
+template <> struct Piece<2> { typedef uint32_t type; };
+template <> struct Piece<1> { typedef unsigned short type; };
 template <int V>
-RP_DEV void unpack(const typename Words<V>::type& w, float (&f)[V]) {
+RP_DEV void unpack(const typename Piece<V>::type& w, float (&f)[V]) {
   if constexpr (V == 1) {
     f[0] = bf16_bits_to_f32(w);
   } else {
@@ -89,8 +88,8 @@ RP_DEV void unpack(const typename Words<V>::type& w, float (&f)[V]) {
   }
 }
 template <int V>
-RP_DEV typename Words<V>::type pack(const float (&f)[V]) {
-  typename Words<V>::type w;
+RP_DEV typename Piece<V>::type pack(const float (&f)[V]) {
+  typename Piece<V>::type w;
   if constexpr (V == 1) {
     w = (unsigned short)f32_to_bf16_bits(f[0]);
   } else {
@@ -101,17 +100,40 @@ RP_DEV typename Words<V>::type pack(const float (&f)[V]) {
   return w;
 }
 
-// A thread owns the same V elements of NH heads of one token, so that what it reads of the table serves all of them, and has their loads
-// in flight together.  Half-split pairs (PAIRS false): V pairs, elements u V .. of both halves of the rotated part; neighbouring pairs:
-// V / 2 pairs.  Units past the rotated part carry the rest of the head over (none when the call is in place: nunits leaves them out).
-// Bound by memory: every element is read and written once.  Each thread reads all it changes before it writes, so in == out is fine.
-template <int V, bool PAIRS, int NH>
+// Eight elements at any even address: an access that crosses a line costs a second one, far less than two bytes at a time would.
+struct __attribute__((packed, aligned(2))) Any8 { uint32_t x, y, z, w; };
+template <int V, bool ANY>
+RP_DEV typename Piece<V>::type load(const bf16* p) {
+  if constexpr (ANY) {
+    const Any8 v = *reinterpret_cast<const Any8*>(p);
+    return make_uint4(v.x, v.y, v.z, v.w);
+  } else {
+    return *reinterpret_cast<const typename Piece<V>::type*>(p);
+  }
+}
+template <int V, bool ANY>
+RP_DEV void store(bf16* p, const typename Piece<V>::type& v) {
+  if constexpr (ANY) *reinterpret_cast<Any8*>(p) = Any8{v.x, v.y, v.z, v.w};
+  else *reinterpret_cast<typename Piece<V>::type*>(p) = v;
+}
+
+// How the units of a head are cut.  HALVES: V pairs, elements u V .. of both halves of the rotated part, V the largest power of two that divides
+// rot / 2, and V elements to carry over.  WINDOWS: the same with eight elements at any even address, the last window of the pairs and of what is
+// carried over pushed back to where it ends, so that some elements are written twice, with the same value: not for calls in place.  PAIRS: 16-byte
+// pieces of four neighbouring pairs.  PAIRS_CUT: the same where the rotated part ends inside a piece.
+enum Cut { HALVES, WINDOWS, PAIRS, PAIRS_CUT };
+
+// A thread owns the same unit of NH heads of one token, so that what it reads of the table serves all of them, and has their loads in flight
+// together.  In place, what is only carried over is left out.  Each thread reads all it changes before it writes, and (but for WINDOWS) no two share
+// an element.  All units go one way through the code: a path of their own for the carried pieces doubles the time where a wave has both.
+// Bound by memory: 16384 tokens of 72 heads of 128 in 114 us, 5.37 TB/s, where a large copy reaches 5.16.
+template <int V, Cut CUT, int NH>
 __global__ void __launch_bounds__(256) rope_kernel(const RotateArgs p) {
-  constexpr int NCS = PAIRS ? (V + 1) / 2 : V;
-  typedef typename Words<V>::type word;
+  constexpr bool ANY = CUT == WINDOWS, NEAR = CUT == PAIRS || CUT == PAIRS_CUT;
+  constexpr int NCS = NEAR ? V / 2 : V;
+  typedef typename Piece<V>::type piece;
   const int heads = p.a + p.k, nhg = (heads + NH - 1) / NH;
-  const int per = nhg * p.nunits;
-  const int nrot = PAIRS ? p.rot / V : p.rot / (2 * V);     // units of the rotated part
+  const int per = nhg * p.nunits, half = p.rot / 2, nrot = p.nrot;
   const int tl = (int)threadIdx.x / per;
   const int t = (int)blockIdx.x * p.tokens_per_block + (p.tokens_per_block > 1 ? tl : 0);
   if (t >= p.T || (p.tokens_per_block > 1 && tl >= p.tokens_per_block)) return;
@@ -120,25 +142,27 @@ __global__ void __launch_bounds__(256) rope_kernel(const RotateArgs p) {
   for (int it = p.tokens_per_block > 1 ? (int)threadIdx.x - tl * per : (int)threadIdx.x; it < per; it += 256) {
     const int u = it % p.nunits, h0 = it / p.nunits;
     const bool turn = u < nrot;
-    const int x0 = turn ? u * V : p.rot + (u - nrot) * V;
+    int x0 = turn || NEAR ? u * V : p.rot + (u - nrot) * V;
+    if (ANY) x0 = turn ? min(x0, half - V) : min(x0, p.d - V);
     float co[NCS], si[NCS];
     if (turn) {
-      const float2* row = p.cs + (long)pos * (p.rot / 2) + u * NCS;
+      const int i0 = NEAR ? u * NCS : x0;
+      const float2* const row = p.cs + (long)pos * half + i0;
 #pragma unroll
       for (int e = 0; e < NCS; ++e) {
-        const float2 v = in_table ? row[e] : make_float2(NAN, NAN);
+        const float2 v = in_table && (CUT != PAIRS_CUT || i0 + e < half) ? row[e] : make_float2(NAN, NAN);
         co[e] = v.x;
         si[e] = p.bwd ? -v.y : v.y;
       }
     }
-    word w0[NH], w1[NH];
+    piece w0[NH], w1[NH];
 #pragma unroll
     for (int i = 0; i < NH; ++i) {
       const int head = h0 + i * nhg;
       if (head >= heads) break;
       const bf16* src = head < p.a ? p.in_q + (long)t * p.ld_in_q + (long)head * p.d : p.in_k + (long)t * p.ld_in_k + (long)(head - p.a) * p.d;
-      w0[i] = *reinterpret_cast<const word*>(src + x0);
-      if (!PAIRS && turn) w1[i] = *reinterpret_cast<const word*>(src + x0 + p.rot / 2);
+      w0[i] = load<V, ANY>(src + x0);
+      if (!NEAR && turn) w1[i] = load<V, ANY>(src + x0 + half);
     }
 #pragma unroll
     for (int i = 0; i < NH; ++i) {
@@ -148,12 +172,13 @@ __global__ void __launch_bounds__(256) rope_kernel(const RotateArgs p) {
       if (turn) {
         float x[V];
         unpack<V>(w0[i], x);
-        if constexpr (PAIRS) {
+        if constexpr (NEAR) {
 #pragma unroll
           for (int e = 0; e < V / 2; ++e) {
             const float a = x[2 * e], b = x[2 * e + 1];
-            x[2 * e] = a * co[e] - b * si[e];
-            x[2 * e + 1] = b * co[e] + a * si[e];
+            const bool on = CUT != PAIRS_CUT || u * NCS + e < half;
+            x[2 * e] = on ? a * co[e] - b * si[e] : a;
+            x[2 * e + 1] = on ? b * co[e] + a * si[e] : b;
           }
         } else {
           float y[V], z[V];
@@ -163,24 +188,30 @@ __global__ void __launch_bounds__(256) rope_kernel(const RotateArgs p) {
             z[e] = y[e] * co[e] + x[e] * si[e];
             x[e] = x[e] * co[e] - y[e] * si[e];
           }
-          *reinterpret_cast<word*>(dst + x0 + p.rot / 2) = pack<V>(z);
+          store<V, ANY>(dst + x0 + half, pack<V>(z));
         }
         w0[i] = pack<V>(x);
       }
-      *reinterpret_cast<word*>(dst + x0) = w0[i];
+      store<V, ANY>(dst + x0, w0[i]);
     }
   }
 }
 
-template <int V, bool PAIRS>
+template <int V, Cut CUT>
 hipError_t launch_rope(hipStream_t st, RotateArgs p, bool in_place) {
   constexpr int NH = 4;
   const int heads = p.a + p.k;
-  p.nunits = (PAIRS ? p.rot / V : p.rot / (2 * V)) + (in_place ? 0 : (p.d - p.rot) / V);
+  if (CUT == PAIRS || CUT == PAIRS_CUT) {
+    p.nrot = (p.rot + 7) / 8;
+    p.nunits = in_place ? p.nrot : p.d / 8;
+  } else {
+    p.nrot = (p.rot / 2 + V - 1) / V;
+    p.nunits = p.nrot + (in_place ? 0 : (p.d - p.rot + V - 1) / V);
+  }
   const int per = ((heads + NH - 1) / NH) * p.nunits;
   p.tokens_per_block = per < 256 ? 256 / per : 1;
   const int blocks = (int)(((long)p.T + p.tokens_per_block - 1) / p.tokens_per_block);
-  RP_LAUNCH((rope_kernel<V, PAIRS, NH>), dim3(blocks), dim3(256), 0, st, p);
+  RP_LAUNCH((rope_kernel<V, CUT, NH>), dim3(blocks), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 
@@ -199,18 +230,17 @@ hipError_t k_rope_table_scaled(hipStream_t st, float2* cs, int n_pos, int rot, c
   return hipGetLastError();
 }
 
-// Elements per access: the widest power of two that divides the rotated part (its half, for half-split pairs) is right for every row,
-// whose starts are multiples of 16 bytes.
 hipError_t k_rope(hipStream_t st, int layout, const RotateArgs& p) {
   if (p.T == 0 || p.a + p.k == 0) return hipSuccess;
-  const bool in_place = p.in_q == p.out_q && (p.k == 0 || p.in_k == p.out_k);
-  if (layout) {
-    if (p.rot % 8 == 0) return launch_rope<8, true>(st, p, in_place);
-    return launch_rope<2, true>(st, p, in_place);
-  }
-  const int half = p.rot / 2;
-  if (half % 8 == 0) return launch_rope<8, false>(st, p, in_place);
-  if (half % 4 == 0) return launch_rope<4, false>(st, p, in_place);
-  if (half % 2 == 0) return launch_rope<2, false>(st, p, in_place);
-  return launch_rope<1, false>(st, p, in_place);
+  const bool in_place = (p.a == 0 || p.in_q == p.out_q) && (p.k == 0 || p.in_k == p.out_k);
+  if (layout) return p.rot % 8 == 0 ? launch_rope<8, PAIRS>(st, p, in_place) : launch_rope<8, PAIRS_CUT>(st, p, in_place);
+  const int half = p.rot / 2, rest = p.d - p.rot;
+  if (half % 8 == 0) return launch_rope<8, HALVES>(st, p, in_place);
+  if (half % 4 == 0) return launch_rope<4, HALVES>(st, p, in_place);
+  // Windows touch elements twice: no part of a call may be in place.  84166 tokens of 6 heads of 256, rot 234: one element an access 224 us, windows
+  // 127;  where four elements an access do, either is ahead by some per cent (rot 24 of 96: 63 | 58, 60 of 128: 42 | 44).
+  const bool apart = (p.a == 0 || p.in_q != p.out_q) && (p.k == 0 || p.in_k != p.out_k);
+  if (apart && half >= 8 && (rest == 0 || rest >= 8)) return launch_rope<8, WINDOWS>(st, p, in_place);
+  if (half % 2 == 0) return launch_rope<2, HALVES>(st, p, in_place);
+  return launch_rope<1, HALVES>(st, p, in_place);
 }
