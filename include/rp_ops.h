@@ -135,7 +135,7 @@ RP_API rp_status rp_op_rope_table_scaled(void* stream, void* cs, const rp_rope_s
 /* Rotation of a query heads and k key heads of d elements (a multiple of 8, up to 512), the first rot of them (even), the rest carried over.
  * layout 0: half-split pairs (i, i + rot/2);  1: neighbouring pairs (2i, 2i + 1).  bwd 1: in_* are gradients of the rotated heads, out_* the
  * gradients of the heads (the transpose).  pos [dev] int32 [T]: a token's row of cs; NULL: t % seq.  A position outside 0 .. n_pos - 1 has no
- * row: the rotated part of such a token becomes NaN.  Row strides ld_* in elements; T any number; out_* is in_* with the same stride (in place) or
+ * row: the rotated part of such a token becomes NaN.  Row strides ld_* in elements; T up to 2^30; out_* is in_* with the same stride (in place) or
  * does not overlap it; a or k 0: its pointers are not used. */
 RP_API rp_status rp_op_rope(void* stream, int bwd, int layout, int d, int rot, const void* in_q, const void* in_k, long ld_in_q, long ld_in_k,
                      void* out_q, void* out_k, long ld_out_q, long ld_out_k, const void* cs, int n_pos, const int* pos, int T, int seq, int a,

@@ -1333,7 +1333,7 @@ rp_status rp_op_rope_table_scaled(void* stream, void* cs, const rp_rope_scaling*
 
 rp_status rp_op_rope(void* stream, int bwd, int layout, int d, int rot, const void* in_q, const void* in_k, long ld_in_q, long ld_in_k, void* out_q,
                      void* out_k, long ld_out_q, long ld_out_k, const void* cs, int n_pos, const int* pos, int T, int seq, int a, int k) {
-  if (T < 0 || a < 0 || k < 0 || layout < 0 || layout > 1 || d < 8 || d > 512 || d % 8 || rot < 2 || rot > d || rot % 2 || n_pos < 0 || (n_pos && !cs) ||
+  if (T < 0 || T > (1 << 30) || a < 0 || k < 0 || layout < 0 || layout > 1 || d < 8 || d > 512 || d % 8 || rot < 2 || rot > d || rot % 2 || n_pos < 0 || (n_pos && !cs) ||
       reinterpret_cast<uintptr_t>(cs) % 8 || (!pos && (seq <= 0 || n_pos < (T < seq ? T : seq))))
     return fail(nullptr, RP_EINVAL, "rp_op_rope: bad arguments");
   if ((a && (bad_heads(in_q, T, a, d, ld_in_q) || bad_heads(out_q, T, a, d, ld_out_q))) ||

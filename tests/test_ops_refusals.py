@@ -53,7 +53,7 @@ GOOD_ROPE = dict(bwd=0, layout=0, d=64, rot=64, in_q=P, in_k=P, ld_in_q=256, ld_
 
 @pytest.mark.parametrize("bad", [dict(layout=2), dict(layout=-1), dict(d=60), dict(d=0), dict(d=520, rot=64), dict(rot=0), dict(rot=63), dict(rot=66), dict(in_q=None),
                                  dict(in_k=None), dict(out_q=None), dict(out_k=P + 8), dict(in_q=P + 2), dict(ld_in_q=252), dict(ld_in_q=248), dict(ld_out_k=120),
-                                 dict(ld_out_q=1 << 24), dict(cs=None), dict(cs=P + 4), dict(n_pos=7), dict(n_pos=-1), dict(T_=-1), dict(seq=0), dict(a=-1), dict(k=-1),
+                                 dict(ld_out_q=1 << 24), dict(cs=None), dict(cs=P + 4), dict(n_pos=7), dict(n_pos=-1), dict(T_=-1), dict(T_=(1 << 30) + 1, pos=P), dict(seq=0), dict(a=-1), dict(k=-1),
                                  dict(ld_out_q=264)])
 def test_rope_refuses(bad):
     refused(B.rp_op_rope, None, **dict(GOOD_ROPE, **bad))
