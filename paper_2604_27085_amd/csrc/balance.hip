@@ -323,7 +323,11 @@ Shape shape_of(int T, int seq, int E, int top_k) {
   s.slices = slices > 32 ? 32 : (int)slices;
   const int rows = 256 / lanes_of(E);
   const int passes = (seq + rows - 1) / rows, most = groups < 1024 ? 1024 / groups : 1;
-  s.rows_per_block = rows * ((passes + most - 1) / most);
+  int each = (passes + most - 1) / most;
+  // a block of four rows spends as long on the counts of more than 512 experts as on them: twice as many where 256 blocks and more are left
+  // (1024 experts, 3968 tokens 26.3 -> 21.5 us, 353 tokens 12.8 -> 14.1)
+  if (E > 512 && each < 2 && (long)groups * passes >= 512) each = 2;
+  s.rows_per_block = rows * each;
   s.chunks = (seq + s.rows_per_block - 1) / s.rows_per_block;
   return s;
 }
