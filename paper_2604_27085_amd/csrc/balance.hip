@@ -102,8 +102,8 @@ __global__ void __launch_bounds__(1024) balance_tokens_kernel(const BalanceArgs 
   if (threadIdx.x == 0) p.tokens[p.groups] = n;
 }
 
-// A block's share of the rows: L lanes per token, C accesses of VEC logits a lane, element (lane + L i) VEC + v.
-template <int L, int C, int VEC, int NT>
+// A block's share of the rows: L lanes per token, C accesses of VEC logits a lane, element (lane + L i) VEC + v.  FULL: E = L C VEC, no lane is left over.
+template <int L, int C, int VEC, bool FULL, int NT>
 struct RowPass {
   typedef float fvec __attribute__((ext_vector_type(VEC)));
   static constexpr int ROWS = NT / L;
@@ -120,7 +120,7 @@ struct RowPass {
       const int e0 = (sub + L * c) * VEC;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) { x[c][v] = -INFINITY; given[c][v] = 0.f; }
-      if (in && e0 < p.E) {
+      if (in && (FULL || e0 < p.E)) {
         x[c] = *reinterpret_cast<const fvec*>(p.logits + row * p.E + e0);
         if (p.dlogits_in) given[c] = *reinterpret_cast<const fvec*>(p.dlogits_in + row * p.E + e0);
       }
@@ -136,7 +136,7 @@ struct RowPass {
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         const int e = (sub + L * c) * VEC + v;
-        f[c][v] = e < p.E ? s_f[e] : 0.f;
+        f[c][v] = FULL || e < p.E ? s_f[e] : 0.f;
       }
     for (int t = t0 + row_in; t - row_in < t1; t += ROWS) {
       fvec y[C], was[C];
@@ -174,7 +174,7 @@ struct RowPass {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           const int e0 = (sub + L * c) * VEC;
-          if (e0 < p.E) {
+          if (FULL || e0 < p.E) {
             fvec d;
 #pragma unroll
             for (int v = 0; v < VEC; ++v) d[v] = was[c][v] + (live ? y[c][v] * inv_l * (kb * f[c][v] + shift) : 0.f);
@@ -186,7 +186,7 @@ struct RowPass {
   }
 };
 
-template <int L, int C, int VEC>
+template <int L, int C, int VEC, bool FULL>
 __global__ void __launch_bounds__(256) balance_rows_kernel(const BalanceArgs p) {
   __shared__ int s_cnt[1024];
   __shared__ float s_f[1024];
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(256) balance_rows_kernel(const BalanceArgs p) 
   const int tid = threadIdx.x, chunk = (int)blockIdx.x % p.chunks;
   const long g = (int)blockIdx.x / p.chunks, base = g * p.seq;
   const int t0 = chunk * p.rows_per_block, t1 = min(p.seq, t0 + p.rows_per_block);
-  RowPass<L, C, VEC, 256> rows;
+  RowPass<L, C, VEC, FULL, 256> rows;
   rows.load(p, base, t0 + tid / L, t1, tid % L);
   for (int e = tid; e < p.E; e += 256) s_cnt[e] = 0;
   __syncthreads();
@@ -251,7 +251,7 @@ RP_DEV void write_loss(const BalanceArgs& p, double b, double z, int N) {
 }
 
 // A group in one block; a single group's block writes the loss as well.
-template <int L, int C, int VEC>
+template <int L, int C, int VEC, bool FULL>
 __global__ void __launch_bounds__(1024) balance_small_kernel(const BalanceArgs p) {
   __shared__ int s_hist[1024];
   __shared__ float s_f[1024];
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(1024) balance_small_kernel(const BalanceArgs p
   __shared__ float redf[16];
   const int tid = threadIdx.x;
   const long g = blockIdx.x, base = g * p.seq;
-  RowPass<L, C, VEC, 1024> rows;
+  RowPass<L, C, VEC, FULL, 1024> rows;
   rows.load(p, base, tid / L, p.seq, tid % L);
   const int n = count_choices<1024>(p, base, 0, p.seq, s_hist, red);
   int total = n;
@@ -345,10 +345,15 @@ size_t k_moe_balance_scratch(int T, int seq, int E) {
   return up256(groups * s.slices * E * 4) + up256(groups * s.slices * 4) + up256(groups * s.chunks * 8);
 }
 
+template <int L, int C, int VEC, bool FULL>
+static void launch_rows_as(hipStream_t st, const BalanceArgs& p, bool small) {
+  if (small) RP_LAUNCH((balance_small_kernel<L, C, VEC, FULL>), dim3(p.groups), dim3(1024), 0, st, p);
+  else RP_LAUNCH((balance_rows_kernel<L, C, VEC, FULL>), dim3(p.groups * p.chunks), dim3(256), 0, st, p);
+}
 template <int L, int C, int VEC>
 static void launch_rows(hipStream_t st, const BalanceArgs& p, bool small) {
-  if (small) RP_LAUNCH((balance_small_kernel<L, C, VEC>), dim3(p.groups), dim3(1024), 0, st, p);
-  else RP_LAUNCH((balance_rows_kernel<L, C, VEC>), dim3(p.groups * p.chunks), dim3(256), 0, st, p);
+  if (VEC == 4 && p.E == L * C * VEC) launch_rows_as<L, C, VEC, VEC == 4>(st, p, small);
+  else launch_rows_as<L, C, VEC, false>(st, p, small);
 }
 
 hipError_t k_moe_balance(hipStream_t st, BalanceArgs p, int T, void* scratch) {
