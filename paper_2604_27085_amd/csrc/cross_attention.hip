@@ -281,13 +281,13 @@ __global__ void __launch_bounds__(256, 2) cross_fwd_kernel(const CrossArgs p) {
 
 // ---- few rows: the step of a generation -----------------------------------------------------------------------
 // At most 16 NC rows per key head (the queries of a step times the heads of the group).  Bound by reading K and V once, so a wave works alone, without
-// barriers: the four waves of a workgroup take its 32-key steps in turn, K goes from memory straight into the fragments of the matrix
+// barriers: the waves of a workgroup take its 32-key steps in turn, K goes from memory straight into the fragments of the matrix
 // instruction (16 rows x 64 bytes a load: a whole row is used by one wave), V through a piece of LDS of the wave's own, since its
 // reduction runs over the keys.  The next step's K and V are on their way during a step.  At the end the waves join in LDS.
-template <int D, int NC, bool SPLIT>
-__global__ void __launch_bounds__(256) cross_step_kernel(const CrossArgs p) {
+template <int D, int NC, int NW, bool SPLIT>
+__global__ void __launch_bounds__(64 * NW) cross_step_kernel(const CrossArgs p) {
   constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, CH = D / 8, NV = 32 * CH / 64;
-  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // step_smem_bytes(D, NC)
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // step_smem_bytes(D, NC, NW)
   typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(256) cross_step_kernel(const CrossArgs p) {
   };
   if (j0 + w < j1) load_step(j0 + w);
   const bf16* const vfrag = Vs + tr_base<LD>(lane);
-  for (int j = j0 + w; j < j1; j += 4) {
+  for (int j = j0 + w; j < j1; j += NW) {
     f32x4 sT[2][NC];      // [16 keys][16 rows]
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(256) cross_step_kernel(const CrossArgs p) {
       const int c = 64 * i + lane;
       *reinterpret_cast<u32x4*>(Vs + (c / CH) * LD + (c % CH) * 8) = vreg[i];
     }
-    if (j + 4 < j1) load_step(j + 4);
+    if (j + NW < j1) load_step(j + NW);
     if (32 * j + 32 > s.kvlen) {      // uniform: the last step
       const int klim = s.kvlen - 1 - (32 * j + 4 * lg);
 #pragma unroll
@@ -409,8 +409,8 @@ __global__ void __launch_bounds__(256) cross_step_kernel(const CrossArgs p) {
   }
 
   // the waves join: wave w's reference exponent and sum of every row, then its rows of O^T
-  float* const ml = reinterpret_cast<float*>(dyn_smem);      // [4][2][16 NC]
-  float* const os = ml + 8 * 16 * NC;                        // [4][16 NC][D + 4]
+  float* const ml = reinterpret_cast<float*>(dyn_smem);      // [NW][2][16 NC]
+  float* const os = ml + 2 * NW * 16 * NC;                   // [NW][16 NC][D + 4]
   __syncthreads();
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -424,18 +424,18 @@ __global__ void __launch_bounds__(256) cross_step_kernel(const CrossArgs p) {
       *reinterpret_cast<f32x4*>(os + (w * 16 * NC + 16 * c + lr) * (D + 4) + 16 * dt + 4 * lg) = oacc[dt][c];
   }
   __syncthreads();
-  for (int i = tid; i < 16 * NC * CH; i += 256) {
+  for (int i = tid; i < 16 * NC * CH; i += 64 * NW) {
     const int row = i / CH, ch = i % CH;
     if (row >= s.total) break;
     const bool live = row < s.valid && j0 < j1;
     if (SPLIT && !live) continue;
     float m = -INFINITY, l = 0.f, acc[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) m = fmaxf(m, ml[2 * u * 16 * NC + row]);
+    for (int u = 0; u < NW; ++u) m = fmaxf(m, ml[2 * u * 16 * NC + row]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < NW; ++u) {
       const float mu = ml[2 * u * 16 * NC + row];
       const float wgt = mu == -INFINITY ? 0.f : fast_exp2(mu - m);      // (a wave without a step)
       l += wgt * ml[(2 * u + 1) * 16 * NC + row];
@@ -1178,7 +1178,7 @@ __global__ void __launch_bounds__(256) cross_key_join_kernel(const CrossArgs p) 
 // operand tiles, or the epilogue's staging of every wave's 32 x d block, whichever is larger
 constexpr int max_i(int a, int b) { return a > b ? a : b; }
 constexpr int fwd_smem_bytes(int d) { return max_i(64 * (d + 8) + 64 * (d + 32), 128 * (d + 8)) * 2; }
-constexpr int step_smem_bytes(int d, int nc) { return max_i(4 * 32 * tile_ld(d) * 2, 8 * 16 * nc * 4 + 4 * 16 * nc * (d + 4) * 4); }
+constexpr int step_smem_bytes(int d, int nc, int nw) { return nw * max_i(32 * tile_ld(d) * 2, 16 * nc * (2 + d + 4) * 4); }
 constexpr int dq_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d), 128 * (d + 8)) * 2; }
 constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 512, 4 * 32 * (d + 4) * 4); }
 constexpr int dkv_pair_smem_bytes(int d) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * 4 * 64 * 16 + 1024; }
@@ -1220,16 +1220,27 @@ size_t key_part_bytes(const CrossArgs& p, int d) { return (size_t)2 * p.batch * 
 int row_splits(const CrossArgs& p, int d, size_t bytes) {
   return splits_for((long)ceil_div(row_count(p), 128) * p.kh * p.batch, 512, ceil_div(p.seq_kv, 64), 1.4, row_part_bytes(p, d), bytes);
 }
-// Few rows: two workgroups per CU; a slice has a 32-key step for each of its four waves at least.  (Slices of 256 keys and more: one token of 8
-// sequences against up to 1500 keys 13.5 us, with 128 12.5.)
+// Few rows: slices for two workgroups of four waves per CU, with a 32-key step for each wave at least -- or one workgroup of eight waves, without slices,
+// where its waves are through with their steps (2.1 us each, one after the other: a CU fetches 60 GB/s) before the slices would have been joined (a
+// second launch, 3 us).  One token against d = 128, us, slices | eight waves: 8 sequences of 1500 keys, 8 key heads 14.6 | 17.2, 1 of 700 9.0 | 10.0,
+// 32 of 1000 30.1 | 25.6; 2 of 300, 16 key heads of 64 8.1 | 5.7.
 bool few_rows(const CrossArgs& p) { return row_count(p) <= 32; }
 int step_splits(const CrossArgs& p, int d, size_t bytes) {
   const long nhb = (long)p.kh * p.batch;
   const size_t each = row_part_bytes(p, d);
+  const int steps = ceil_div(p.seq_kv, 32);
   long n = nhb ? 512 / nhb : 1;
-  if (n > ceil_div(p.seq_kv, 128)) n = ceil_div(p.seq_kv, 128);
+  if (n > ceil_div(steps, 4)) n = ceil_div(steps, 4);
   if (each && n > (long)(bytes / each)) n = (long)(bytes / each);
-  return n < 2 ? 1 : (int)n;
+  if (n < 2 || ceil_div(steps, 8) * 2.1 <= ceil_div(ceil_div(steps, (int)n), 4) * 2.1 + 3.0) return 1;
+  return (int)n;
+}
+template <int D, int NC>
+hipError_t launch_step(hipStream_t st, const CrossArgs& p) {
+  const int nhb = p.kh * p.batch;
+  if (p.splits > 1) return launch(cross_step_kernel<D, NC, 4, true>, nhb * p.splits, 256, step_smem_bytes(D, NC, 4), st, p);
+  if (p.seq_kv > 128 && nhb < 512) return launch(cross_step_kernel<D, NC, 8, false>, nhb, 512, step_smem_bytes(D, NC, 8), st, p);
+  return launch(cross_step_kernel<D, NC, 4, false>, nhb, 256, step_smem_bytes(D, NC, 4), st, p);
 }
 // dK, dV: the kernel at d = 128 has a CU to itself; at d = 64 two share one, and a third takes the place of those that end early
 int key_splits(const CrossArgs& p, int d, size_t bytes) {
@@ -1263,9 +1274,7 @@ hipError_t fwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   p.part_ml = reinterpret_cast<float2*>(p.part + (size_t)p.splits * nhb * rows * D);
   hipError_t e = hipSuccess;
   if (few) {
-    const int grid = nhb * p.splits;
-    if (rows <= 16) e = p.splits > 1 ? launch(cross_step_kernel<D, 1, true>, grid, 256, step_smem_bytes(D, 1), st, p) : launch(cross_step_kernel<D, 1, false>, grid, 256, step_smem_bytes(D, 1), st, p);
-    else e = p.splits > 1 ? launch(cross_step_kernel<D, 2, true>, grid, 256, step_smem_bytes(D, 2), st, p) : launch(cross_step_kernel<D, 2, false>, grid, 256, step_smem_bytes(D, 2), st, p);
+    e = rows <= 16 ? launch_step<D, 1>(st, p) : launch_step<D, 2>(st, p);
   } else if (p.splits > 1) {
     e = launch(cross_fwd_kernel<D, true>, ceil_div(rows, 128) * nhb * p.splits, 256, fwd_smem_bytes(D), st, p);
   }

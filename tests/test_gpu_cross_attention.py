@@ -103,6 +103,8 @@ SHAPES = [
     (8, 1, 1500, 16, 8, 128, None, [1500, 3, 0, 700, 64, 65, 1, 1499]), (1, 1, 9000, 8, 8, 128, None, None), (2, 3, 5000, 32, 4, 64, [3, 2], [5000, 129]),
     (1, 640, 640, 8, 8, 128, None, None), (1, 4000, 100, 8, 2, 128, None, None), (2, 1500, 70, 8, 2, 64, [1500, 611], [70, 5]), (1, 513, 31, 16, 16, 64, None, None),
     (5, 17, 515, 4, 2, 128, [17, 1, 16, 9, 0], [515, 512, 513, 0, 200]), (1, 31, 513, 5, 5, 64, None, None), (2, 16, 2048, 64, 4, 128, None, [2048, 1025]),
+    # one workgroup of eight waves a key head
+    (3, 2, 300, 32, 2, 128, [2, 1, 2], [300, 0, 131]), (2, 1, 300, 16, 16, 64, None, [257, 300]), (2, 5, 290, 12, 2, 64, [5, 4], [290, 33]),
 ]
 
 
