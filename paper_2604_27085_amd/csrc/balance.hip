@@ -13,6 +13,9 @@
 //           terms leave one pair of fp32 sums per block
 //   total : one block adds the pairs in a fixed order
 //   small : a group in one block, for groups that one block is through with before the other launches would have started
+//
+// Bound by launches that wait for one another: 31744 tokens, eight of 128 experts, with a gradient to add to 19.6 us (count 5, rows 12, total 3) where its 50 MB
+// take 9.6; 4 x 1001 x 256 13.7.
 #include "kernels.hpp"
 #include "layer_ops.hpp"
 

@@ -51,6 +51,7 @@ RP_DEV void cos_sin_turns(double turns, double& co, double& si) {
 // Thread = one pair index and every `rows`-th of the block's positions.  Only the first of them and the step between them are worked out
 // from their angles; from there on the pair is turned by the step, in 64 bits (4 products a position where the polynomials and the angle take
 // 30, which would bound the kernel: 131072 x 64 pairs 20.9 us).  32 steps at most: they multiply the polynomials' error to 3e-10.
+// Now bound by its writes: 131072 x 64 pairs 11.7 us, 5.7 TB/s (a fill reaches 6.9).
 __global__ void __launch_bounds__(256) rope_table_scaled_kernel(float2* __restrict__ cs, int n_pos, int half, int rows, int per_block, const RopeScale r) {
   const int i0 = (int)threadIdx.x % half, lane_row = (int)threadIdx.x / half;      // (half <= 256)
   if (lane_row >= rows) return;
