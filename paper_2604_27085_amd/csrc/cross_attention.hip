@@ -21,8 +21,8 @@
 // matrix pipe busy 58, 58 and 50 %, vector issue 48, 43 and 41 %, memory nothing to speak of: the exponentials and conversions beside the
 // products, and the clock that the power allows, as in attention.hip.  At d = 64 (64 heads, 4 x 512 queries against 1536 keys) 68, 90 and 121 us: the
 // vector instructions of a tile are the same for half the products.  A padded batch adds what its longest sequence's workgroups last longer.
-// P and dS are rounded to bf16, as the matrix instruction takes them (2^-9 a term at most on the average of many); scores, statistics, dP - delta and every
-// sum are fp32.
+// P, and dS for dK, are rounded to bf16, as the matrix instruction takes them (2^-9 a term at most); dS for dQ is taken in two parts; scores, statistics,
+// dP - delta and every sum are fp32.
 #include "attention_device.hpp"
 #include "layer_ops.hpp"
 
@@ -533,12 +533,15 @@ __global__ void __launch_bounds__(256) cross_row_join_kernel(const CrossArgs p, 
       const float2 ml = p.part_ml[i * step + row];
       wgt = fast_exp2(ml.x - m);
       acc[8] += wgt * ml.y;
+    } else {
+      acc[8] += p.part_ml[i * step + row].x;
     }
     add_times(acc, p.part + (i * step + row) * D + ch * 8, wgt);
   }
   const bool mine = add_groups<CH, G, 9>(acc, red);
   if (!in || !mine) return;
   if constexpr (DQ) {
+    if (ch == 0 && n) p.delta[s.stat(r, p.a)] += acc[8];
     *reinterpret_cast<uint4*>(p.dq + s.offset(r, p.lddq, D) + ch * 8) = pack_times(acc, p.scale);
   } else {
     if (p.lse && ch == 0) p.lse[s.stat(r, p.a)] = n ? m * 0.6931471805599453f + logf(acc[8]) : -INFINITY;
@@ -549,8 +552,12 @@ __global__ void __launch_bounds__(256) cross_row_join_kernel(const CrossArgs p, 
 // ================================================================================================ dQ
 // delta comes from the stored output, as in attention.hip, where many keys share a row's weight.  With few keys a row may put nearly all of it on
 // one, dP - delta cancels there, and the rounding of the stored output (2^-9 of delta) would show in what is left: up to EXACT_DELTA keys
-// the scores are made twice, and delta = sum P dP is as exact as they are.
-constexpr int EXACT_DELTA = 256;
+// the scores are made twice, and delta = sum P dP is as exact as they are.  Above, the rows of dS, which sum up to zero, tell at the end what delta
+// was off by; dK, dV take the corrected one.
+// dS goes into its product in two parts, its bf16 and the bf16 of what that left over: K^T's fragments serve both, and dq is off by little more than its
+// own rounding.  Distance to 64 bits, 10^-3 (one rounding of the exact result: 1.66), without | with the second part and the corrected delta: dq 2.4 to 2.7 |
+// 1.7 to 2.2, dk 2.2 to 2.6 | 2.2 to 2.4; time, forward and backward: 4096 queries of 32 heads of 128 against 8192 keys 2165 | 2350 us, a few us of the short ones.
+constexpr int EXACT_DELTA = 128;
 
 template <int D, bool SPLIT>
 __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
@@ -679,15 +686,10 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
     dl[1] = column_sum(dl[1]);
     __syncthreads();      // the tiles are stored anew below
   }
-  if (split == 0 && lg == 0) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-      if (r0 + 32 * w + 16 * c + lr < s.valid) p.delta[stat[c]] = dl[c];
-  }
-
   f32x4 dqacc[DT][2];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dqacc[dt][0] = dqacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float row_sum[2] = {0.f, 0.f};
   if (j0 < j1) load_tiles(j0);
   for (int j = j0; j < j1; ++j) {
     __syncthreads();
@@ -716,8 +718,21 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) sT[kt][c][e] = 16 * kt + e > klim ? 0.f : sT[kt][c][e];
       }
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) row_sum[c] += sT[kt][c][e];
       constexpr int AHEAD = 2;      // K^T fragments requested that many pairs of products early
-      const uint4 df[2] = {pack_frag(sT[0][0], sT[1][0]), pack_frag(sT[0][1], sT[1][1])};
+      uint4 df[2], low[2];          // dS in bf16, and what the rounding left over
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        df[c] = pack_frag(sT[0][c], sT[1][c]);
+        sT[0][c] -= f32x4{bf16_lo(df[c].x), bf16_hi(df[c].x), bf16_lo(df[c].y), bf16_hi(df[c].y)};
+        sT[1][c] -= f32x4{bf16_lo(df[c].z), bf16_hi(df[c].z), bf16_lo(df[c].w), bf16_hi(df[c].w)};
+        low[c] = pack_frag(sT[0][c], sT[1][c]);
+      }
       auto ufrag_at = [&](int n) { return read_frag_tr<LD>(ktfrag + 32 * k2 * LD + 16 * n); };
       uint4 uring[AHEAD];
 #pragma unroll
@@ -728,7 +743,23 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
         if (n + AHEAD < DT) uring[n % AHEAD] = ufrag_at(n + AHEAD);
 #pragma unroll
         for (int c = 0; c < 2; ++c) dqacc[n][c] = mfma16(a, df[c], dqacc[n][c]);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) dqacc[n][c] = mfma16(a, low[c], dqacc[n][c]);
         __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  // the rows of dS sum up to zero: what they do sum up to is what delta was off by
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const float off = column_sum(row_sum[c]);
+    const int row = r0 + 32 * w + 16 * c + lr;
+    if (lg == 0 && row < s.valid) {
+      if constexpr (SPLIT) {      // joined with the slices
+        if (split == 0) p.delta[stat[c]] = dl[c];
+        if (j0 < j1) p.part_ml[((long)split * nhb + hb) * s.total + row] = make_float2(off, 0.f);
+      } else {
+        p.delta[stat[c]] = dl[c] + off;
       }
     }
   }
@@ -1298,6 +1329,7 @@ hipError_t bwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   p.part = static_cast<float*>(scratch);
   // dQ first: it works out delta, which dK/dV reads
   p.splits = row_splits(p, D, bytes);
+  p.part_ml = reinterpret_cast<float2*>(p.part + (size_t)p.splits * nhb * rows * D);
   hipError_t e = hipSuccess;
   if (rows == 0) {
     // no queries: dk and dv are zero

@@ -7,7 +7,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 DEV = "cuda:0"
 BF16 = torch.bfloat16
-EXACT_DELTA = 256      # keys up to which the backward takes delta from the scores
+EXACT_DELTA = 128      # keys up to which the backward takes delta from the scores
 
 
 @pytest.fixture(scope="module")
