@@ -11,7 +11,7 @@
 //
 //   forward: workgroup = four waves x 32 rows, loop over 64-key tiles (eight waves, one workgroup per CU, which pays in attention.hip, are 0 to 3 %
 //            slower here, where no workgroup has fewer tiles than another)
-//   dQ     : the same; delta on the way
+//   dQ     : the same; delta on the way (with the loop in slices, in a launch before)
 //   dK, dV : workgroup = 128 keys, loop over 64-row tiles (d = 128: eight waves, pairs of which share 32 keys; d = 64: four waves)
 // Where there are too few workgroups for the chip, the loop is cut into `splits` slices, whose results another kernel joins in slice
 // order (fp32 partials in the caller's scratch; no atomics, so the result does not depend on timing).
@@ -21,7 +21,7 @@
 // part, see cross_dq_kernel), dK/dV 1090 (1.01); matrix pipe busy 58, 61 and 50 %, vector issue 48, 51 and 41 %, memory nothing to speak of: the exponentials and conversions beside the
 // products, and the clock that the power allows, as in attention.hip.  At d = 64 (64 heads, 4 x 512 queries against 1536 keys) 68, 118 and 117 us: the
 // vector instructions of a tile are the same for half the products.  A padded batch adds what its longest sequence's workgroups last longer.
-// P, and dS for dK, are rounded to bf16, as the matrix instruction takes them (2^-9 a term at most); dS for dQ is taken in two parts; scores, statistics,
+// P, and dS for dK, are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most); dS for dQ is taken in two parts; scores, statistics,
 // dP - delta and every sum are fp32.
 #include "attention_device.hpp"
 #include "layer_ops.hpp"
@@ -82,6 +82,13 @@ RP_DEV int slices_used(int n, int splits) {
 // that had a workgroup of the longest sequence gets one of another then.  (Training 4 x 509 queries of 64 heads of 64 against up to 1500 keys:
 // forward 68.6 us with neighbouring key heads per XCD as in attention.hip, where two XCDs have the longest sequence to themselves.)
 RP_DEV int head_at(int pos, int rest, int nhb) { return (pos - rest * nhb + 8 * (int)(((long)rest * nhb) >> 8)) % nhb; }
+
+// Between a wave's stores to LDS and its lanes' reads of one another's (and the other way round): LDS works in order for a wave, so this is for the compiler.
+RP_DEV void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 // A 64-key tile, through a descriptor of its own that ends with the sequence: rows past the end read as zero, and no offset outgrows 32
 // bits however long the sequence is.
@@ -515,9 +522,10 @@ __global__ void __launch_bounds__(256) cross_row_join_kernel(const CrossArgs p, 
   const Rows s(p, hb);
   const int n = in && r < s.valid ? slices_used((s.kvlen + unit - 1) / unit, p.splits) : 0;
   const long row = (long)hb * total + r, step = (long)nhb * total;
-  float acc[9];      // eight elements, and the sum of exponentials
+  constexpr int N = DQ ? 8 : 9;      // eight elements, and the forward's sum of exponentials
+  float acc[N];
 #pragma unroll
-  for (int e = 0; e < 9; ++e) acc[e] = 0.f;
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
   float m = -INFINITY;
   if constexpr (!DQ) {
     constexpr int L = CH * G < 64 ? CH * G : 64;      // lanes of a wave that work on the row
@@ -533,15 +541,12 @@ __global__ void __launch_bounds__(256) cross_row_join_kernel(const CrossArgs p, 
       const float2 ml = p.part_ml[i * step + row];
       wgt = fast_exp2(ml.x - m);
       acc[8] += wgt * ml.y;
-    } else {
-      acc[8] += p.part_ml[i * step + row].x;
     }
     add_times(acc, p.part + (i * step + row) * D + ch * 8, wgt);
   }
-  const bool mine = add_groups<CH, G, 9>(acc, red);
+  const bool mine = add_groups<CH, G, N>(acc, red);
   if (!in || !mine) return;
   if constexpr (DQ) {
-    if (ch == 0 && n) p.delta[s.stat(r, p.a)] += acc[8];
     *reinterpret_cast<uint4*>(p.dq + s.offset(r, p.lddq, D) + ch * 8) = pack_times(acc, p.scale);
   } else {
     if (p.lse && ch == 0) p.lse[s.stat(r, p.a)] = n ? m * 0.6931471805599453f + logf(acc[8]) : -INFINITY;
@@ -550,17 +555,116 @@ __global__ void __launch_bounds__(256) cross_row_join_kernel(const CrossArgs p, 
 }
 
 // ================================================================================================ dQ
-// delta comes from the stored output, as in attention.hip, where many keys share a row's weight.  With few keys a row may put nearly all of it on
-// one, dP - delta cancels there, and the rounding of the stored output (2^-9 of delta) would show in what is left: up to EXACT_DELTA keys
-// the scores are made twice, and delta = sum P dP is as exact as they are.  Above, the rows of dS, which sum up to zero, tell at the end what delta
-// was off by; dK, dV take the corrected one.
+// dP - delta cancels where a row puts nearly all of its weight on one key, and a delta from the stored output, dO.o, carries that one's rounding (2^-8 at most):
+// rows on one of 129 keys had dq off by 0.06 to 0.16 of its norm.  So delta has to be as exact as the scores where it matters:
+//   up to EXACT_DELTA keys, unless cut into slices, the scores are made twice, the first time for delta = sum P dP / sum P;
+//   with the key loop in slices a launch of its own (DELTA) makes those two sums of every slice;
+//   else delta starts as dO.o, and the rows of dS, which sum up to zero, tell at the end what it was off by.  Rows where that is more than FAR sum |dS|, more
+//   than a rounding of every dS to bf16 could do, get dq - off sum P K (mean_keys; of rows whose scores have standard deviation 2
+//   one in 10000 against 8192 keys, one in 1500 against 1500 and one in 240 against 300).  dK, dV take the corrected one in any case.
 // dS goes into its product in two parts, its bf16 and the bf16 of what that left over: K^T's fragments serve both, and dq is off by little more than its
-// own rounding.  Distance to 64 bits, 10^-3 (one rounding of the exact result: 1.66), without | with the second part and the corrected delta: dq 2.4 to 2.7 |
-// 1.7 to 2.2, dk 2.2 to 2.6 | 2.2 to 2.4; time, forward and backward: 4096 queries of 32 heads of 128 against 8192 keys 2165 | 2350 us, a few us of the short ones.
-constexpr int EXACT_DELTA = 128;
+// own rounding (relative 2-norm 1.7e-3 with delta from the scores; in one part 2.4e-3).
+constexpr int EXACT_DELTA = 256;
+constexpr float FAR = 1.f / 256.f;
+// WHOLE: a workgroup's rows against all keys; EXACT: the same where no sequence has more than EXACT_DELTA keys; SLICE, DELTA: a slice of them
+enum DqPass { WHOLE, EXACT, SLICE, DELTA };
 
-template <int D, bool SPLIT>
+// Two score tiles as pack_frag gives them, and what that rounding left over.  (a, b are used up.)
+RP_DEV void two_parts(f32x4& a, f32x4& b, uint4& high, uint4& low) {
+  high = pack_frag(a, b);
+  a -= f32x4{bf16_lo(high.x), bf16_hi(high.x), bf16_lo(high.y), bf16_hi(high.y)};
+  b -= f32x4{bf16_lo(high.z), bf16_hi(high.z), bf16_lo(high.w), bf16_hi(high.w)};
+  low = pack_frag(a, b);
+}
+
+constexpr int dq_tile_bytes(int d) { return 2 * 64 * tile_ld(d) * 2; }
+
+// sum[i][..] = sum_k P K of rows list[i], i < n <= 16, of a workgroup's 128.  There are few of them, so the waves share their keys: a wave takes every fourth
+// step of 32 keys by itself, K from memory straight into fragments for the scores, three steps ahead, and through a piece of LDS of its own for the product
+// whose reduction runs over the keys; in the end the waves' parts are added in order.  All threads; smem is free before and holds the sums, rows D + 4
+// apart, behind.  Training step of 2 x 1024 queries of 16 heads against 1024 keys, where each workgroup is alone on its CU and half of them have such
+// a row: 118 us without, 131 with (32 rows at a time, one step ahead: 134).
+template <int D>
+RP_DEV void mean_keys(const CrossArgs& p, const Rows& s, int r0, const int* list, int n, bf16* smem, int tid) {
+  constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, AHEAD = 3;
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  const int lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  bf16* const Ks = smem + w * 32 * LD;
+  const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
+  u32x4 kreg[AHEAD][2][KS];
+  auto load_step = [&](u32x4 (&r)[2][KS], int k0) {      // rows past the end read as zero
+    const int left = min(32, s.kvlen - k0);
+    const rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(kb + (long)k0 * p.ldk), 0, (int)(((long)(left - 1) * p.ldk + D) * 2), 0x00020000);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        r[kt][ks] = __builtin_amdgcn_raw_buffer_load_b128(rk, (int)(((16 * kt + lr) * (int)p.ldk + 32 * ks + 8 * lg) * 2), 0, 0);
+  };
+  const int k_first = 32 * w;
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (k_first + 128 * i < s.kvlen) load_step(kreg[i], k_first + 128 * i);
+  const bool ok = lr < n;
+  const int row = r0 + list[ok ? lr : 0];
+  const bf16* const qr = p.q + s.offset(row, p.ldq, D) + 8 * lg;
+  uint4 qf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const uint4*>(qr + 32 * ks);
+  const float lse2 = ok ? p.lse_in[s.stat(row, p.a)] * 1.4426950408889634f : INFINITY;      // P = 0
+  f32x4 acc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int k0 = k_first; k0 < s.kvlen; k0 += 128 * AHEAD) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int k = k0 + 128 * i;
+      if (k >= s.kvlen) break;
+      f32x4 sT[2];      // [16 keys][16 rows]
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) sT[kt] = mfma16(__builtin_bit_cast(uint4, kreg[i][kt][ks]), qf[ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sT[kt]);
+      wave_lds_order();      // the last step's K has been read
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) *reinterpret_cast<u32x4*>(Ks + (16 * kt + lr) * LD + 32 * ks + 8 * lg) = kreg[i][kt][ks];
+      wave_lds_order();
+      if (k + 128 * AHEAD < s.kvlen) load_step(kreg[i], k + 128 * AHEAD);
+      const int klim = s.kvlen - 1 - (k + 4 * lg);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sT[kt][e] = 16 * kt + e > klim ? 0.f : fast_exp2(__builtin_fmaf(sT[kt][e], p.scale_log2e, -lse2));
+      uint4 high, low;
+      two_parts(sT[0], sT[1], high, low);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint4 a = read_frag_tr<LD>(Ks + tr_base<LD>(lane) + 16 * dt);
+        acc[dt] = mfma16(a, high, acc[dt]);
+        acc[dt] = mfma16(a, low, acc[dt]);
+      }
+    }
+  }
+  float* const sum = reinterpret_cast<float*>(smem) + lr * (D + 4) + 4 * lg;
+  for (int u = 0; u < 4; ++u) {
+    __syncthreads();
+    if (w == u) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        f32x4* const at = reinterpret_cast<f32x4*>(sum + 16 * dt);
+        *at = u ? *at + acc[dt] : acc[dt];
+      }
+    }
+  }
+  __syncthreads();
+}
+
+template <int D, DqPass PASS>
 __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
+  constexpr bool SPLIT = PASS == SLICE || PASS == DELTA;
   constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, NT = 256, BQ = 128;
   using T64 = Tile64<D, NT>;
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // dq_smem_bytes(D)
@@ -586,12 +690,12 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
     slice_of(tiles, p.splits, split, j0, j1);
     if (j0 >= j1 && split > 0) return;
   }
-  const bool exact_delta = s.kvlen <= EXACT_DELTA;
+  if (PASS == DELTA && j0 >= j1) return;      // uniform, before any barrier
+  const bool exact_delta = PASS == EXACT || (PASS == WHOLE && s.kvlen <= EXACT_DELTA);
   const KeyTile<D, NT> kt_(p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D, p.ldk, s.kvlen), vt_(p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D, p.ldv, s.kvlen);
 
   uint4 qf[2][KS], dof[2][KS];     // a lane's rows: column tiles c = 0, 1
   float lse2[2], dl[2];
-  long stat[2];
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
     const int row = r0 + 32 * w + 16 * c + lr;
@@ -608,10 +712,22 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
         dof[c][ks] = *reinterpret_cast<const uint4*>(dor + 32 * ks);
       }
     }
-    stat[c] = s.stat(rc, p.a);
-    lse2[c] = ok ? p.lse_in[stat[c]] * 1.4426950408889634f : INFINITY;   // rows past the end get P = 0
+    lse2[c] = ok ? p.lse_in[s.stat(rc, p.a)] * 1.4426950408889634f : INFINITY;   // rows past the end get P = 0
     dl[c] = 0.f;
-    if (!exact_delta) {
+    if (PASS == SLICE) {      // the slices' sums, every fourth by one of the four lanes of a row
+      float sum = 0.f, mass = 0.f;
+      const int n = slices_used(tiles, p.splits);
+#pragma unroll 8
+      for (int i = lg; i < n; i += 4) {
+        const float2 v = ok ? p.part_ml[((long)i * nhb + hb) * s.total + row] : make_float2(0.f, 0.f);
+        sum += v.x;
+        mass += v.y;
+      }
+      sum = column_sum(sum);
+      mass = column_sum(mass);
+      dl[c] = ok && n ? sum / mass : 0.f;
+    }
+    if (PASS == WHOLE && !exact_delta) {
       float sum = 0.f;
       if (ok) {
         const bf16* const orow = p.o_in + s.offset(rc, p.ldo, D) + 8 * lg;
@@ -659,13 +775,15 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
     }
   };
 
-  if (exact_delta) {      // uniform over the workgroup
-    if (tiles > 0) load_tiles(0);
-    for (int j = 0; j < tiles; ++j) {
+  if (PASS == DELTA || exact_delta) {      // uniform over the workgroup
+    const int first = PASS == DELTA ? j0 : 0, last = PASS == DELTA ? j1 : tiles;
+    float mass[2] = {0.f, 0.f};
+    if (first < last) load_tiles(first);
+    for (int j = first; j < last; ++j) {
       __syncthreads();
       store_tiles();
       __syncthreads();
-      if (j + 1 < tiles) load_tiles(j + 1);
+      if (j + 1 < last) load_tiles(j + 1);
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
         f32x4 sT[2][2], dpT[2][2];
@@ -677,19 +795,31 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
           for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float pr = fast_exp2(__builtin_fmaf(sT[kt][c][e], p.scale_log2e, -lse2[c]));
-              dl[c] += 16 * kt + e > klim ? 0.f : pr * dpT[kt][c][e];
+              const bool in = 16 * kt + e <= klim;
+              const float pr = in ? fast_exp2(__builtin_fmaf(sT[kt][c][e], p.scale_log2e, -lse2[c])) : 0.f;
+              mass[c] += pr;
+              dl[c] += in ? pr * dpT[kt][c][e] : 0.f;
             }
       }
     }
-    dl[0] = column_sum(dl[0]);
-    dl[1] = column_sum(dl[1]);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int row = r0 + 32 * w + 16 * c + lr;
+      dl[c] = column_sum(dl[c]);
+      mass[c] = column_sum(mass[c]);
+      if constexpr (PASS == DELTA) {
+        if (lg == 0 && row < s.valid) p.part_ml[((long)split * nhb + hb) * s.total + row] = make_float2(dl[c], mass[c]);
+      } else {
+        dl[c] = row < s.valid && tiles > 0 ? dl[c] / mass[c] : 0.f;
+      }
+    }
+    if (PASS == DELTA) return;
     __syncthreads();      // the tiles are stored anew below
   }
   f32x4 dqacc[DT][2];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dqacc[dt][0] = dqacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float row_sum[2] = {0.f, 0.f};
+  float row_sum[2] = {0.f, 0.f}, row_size[2] = {0.f, 0.f};      // of dS: its sum, and that of its absolute values
   if (j0 < j1) load_tiles(j0);
   for (int j = j0; j < j1; ++j) {
     __syncthreads();
@@ -718,21 +848,21 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) sT[kt][c][e] = 16 * kt + e > klim ? 0.f : sT[kt][c][e];
       }
+      if (PASS == WHOLE) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+          for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) row_sum[c] += sT[kt][c][e];
-      constexpr int AHEAD = 2;      // K^T fragments requested that many pairs of products early
-      uint4 df[2], low[2];          // dS in bf16, and what the rounding left over
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        df[c] = pack_frag(sT[0][c], sT[1][c]);
-        sT[0][c] -= f32x4{bf16_lo(df[c].x), bf16_hi(df[c].x), bf16_lo(df[c].y), bf16_hi(df[c].y)};
-        sT[1][c] -= f32x4{bf16_lo(df[c].z), bf16_hi(df[c].z), bf16_lo(df[c].w), bf16_hi(df[c].w)};
-        low[c] = pack_frag(sT[0][c], sT[1][c]);
+            for (int e = 0; e < 4; ++e) {
+              row_sum[c] += sT[kt][c][e];
+              row_size[c] += fabsf(sT[kt][c][e]);
+            }
       }
+      constexpr int AHEAD = 2;      // K^T fragments requested that many pairs of products early
+      uint4 df[2], low[2];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) two_parts(sT[0][c], sT[1][c], df[c], low[c]);
       auto ufrag_at = [&](int n) { return read_frag_tr<LD>(ktfrag + 32 * k2 * LD + 16 * n); };
       uint4 uring[AHEAD];
 #pragma unroll
@@ -749,19 +879,61 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
       }
     }
   }
-  // the rows of dS sum up to zero: what they do sum up to is what delta was off by
+  // the rows of dS sum up to zero: what they do sum up to is what delta was off by, and dq by that times sum P K
+  if constexpr (PASS == WHOLE) {
+    float off[2];
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const float off = column_sum(row_sum[c]);
-    const int row = r0 + 32 * w + 16 * c + lr;
-    if (lg == 0 && row < s.valid) {
-      if constexpr (SPLIT) {      // joined with the slices
-        if (split == 0) p.delta[stat[c]] = dl[c];
-        if (j0 < j1) p.part_ml[((long)split * nhb + hb) * s.total + row] = make_float2(off, 0.f);
-      } else {
-        p.delta[stat[c]] = dl[c] + off;
+    for (int c = 0; c < 2; ++c) {
+      off[c] = column_sum(row_sum[c]);
+      dl[c] += off[c];
+    }
+    if (!exact_delta) {
+      int* const marks = reinterpret_cast<int*>(dyn_smem + dq_tile_bytes(D));      // the four waves' column tiles: a bit a row
+      int* const list = marks + 8;                                                 // the rows that are off, in order
+      bool far[2];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        far[c] = fabsf(off[c]) > FAR * column_sum(row_size[c]);
+        const int mark = (int)(__builtin_amdgcn_ballot_w64(far[c]) & 0xffffull);      // (the four lanes of a row agree)
+        if (lane == 0) marks[2 * w + c] = mark;
+      }
+      __syncthreads();      // (the last tile has been read as well)
+      int count = 0, at[2] = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int n = __popc(marks[i]);
+        at[0] += i < 2 * w ? n : 0;
+        at[1] += i < 2 * w + 1 ? n : 0;
+        count += n;
+      }
+      count = __builtin_amdgcn_readfirstlane(count);
+      if (count) {      // uniform over the workgroup
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          at[c] += __popc(marks[2 * w + c] & ((1 << lr) - 1));
+          if (lg == 0 && far[c]) list[at[c]] = 32 * w + 16 * c + lr;
+        }
+        __syncthreads();
+        for (int first = 0; first < count; first += 16) {
+          mean_keys<D>(p, s, r0, list + first, min(16, count - first), smem, tid);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const int i = at[c] - first;
+            if (far[c] && i >= 0 && i < 16) {
+              const float* const mean = reinterpret_cast<const float*>(smem) + i * (D + 4) + 4 * lg;
+#pragma unroll
+              for (int dt = 0; dt < DT; ++dt) dqacc[dt][c] -= off[c] * *reinterpret_cast<const f32x4*>(mean + 16 * dt);
+            }
+          }
+          __syncthreads();
+        }
       }
     }
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int row = r0 + 32 * w + 16 * c + lr;
+    if (lg == 0 && row < s.valid && (!SPLIT || split == 0)) p.delta[s.stat(row, p.a)] = dl[c];
   }
   if constexpr (SPLIT) {
     if (j0 >= j1) return;
@@ -1218,7 +1390,7 @@ __global__ void __launch_bounds__(256) cross_key_join_kernel(const CrossArgs p) 
 constexpr int max_i(int a, int b) { return a > b ? a : b; }
 constexpr int fwd_smem_bytes(int d) { return max_i(64 * (d + 8) + 64 * (d + 32), 128 * (d + 8)) * 2; }
 constexpr int step_smem_bytes(int d, int nc, int nw) { return nw * max_i(32 * tile_ld(d) * 2, 16 * nc * (2 + d + 4) * 4); }
-constexpr int dq_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d), 128 * (d + 8)) * 2; }
+constexpr int dq_smem_bytes(int d) { return max_i(dq_tile_bytes(d), 128 * (d + 8) * 2) + (8 + 128) * 4; }
 constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 512, 4 * 32 * (d + 4) * 4); }
 constexpr int dkv_pair_smem_bytes(int d) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * 4 * 64 * 16 + 1024; }
 
@@ -1334,10 +1506,14 @@ hipError_t bwd(hipStream_t st, CrossArgs p, void* scratch, size_t bytes) {
   if (rows == 0) {
     // no queries: dk and dv are zero
   } else if (p.splits > 1) {
-    e = launch(cross_dq_kernel<D, true>, ceil_div(rows, 128) * nhb * p.splits, 256, dq_smem_bytes(D), st, p);
+    const int grid = ceil_div(rows, 128) * nhb * p.splits;
+    e = launch(cross_dq_kernel<D, DELTA>, grid, 256, dq_smem_bytes(D), st, p);
+    if (e == hipSuccess) e = launch(cross_dq_kernel<D, SLICE>, grid, 256, dq_smem_bytes(D), st, p);
     if (e == hipSuccess) e = join_rows<D, true>(st, p, 64);
   } else {
-    e = launch(cross_dq_kernel<D, false>, ceil_div(rows, 128) * nhb, 256, dq_smem_bytes(D), st, p);
+    const int grid = ceil_div(rows, 128) * nhb;
+    e = p.seq_kv <= EXACT_DELTA ? launch(cross_dq_kernel<D, EXACT>, grid, 256, dq_smem_bytes(D), st, p)
+                                : launch(cross_dq_kernel<D, WHOLE>, grid, 256, dq_smem_bytes(D), st, p);
   }
   if (e != hipSuccess || p.seq_kv == 0) return e;
   p.splits = key_splits(p, D, bytes);
