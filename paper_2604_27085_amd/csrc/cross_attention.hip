@@ -367,11 +367,13 @@ __global__ void __launch_bounds__(64 * NW) cross_step_kernel(const CrossArgs p) 
 #pragma unroll
         for (int c = 0; c < NC; ++c)
           sT[kt][c] = mfma16(__builtin_bit_cast(uint4, kreg[kt][ks]), qf[c][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sT[kt][c]);
+    wave_lds_order();      // the last step's V has been read
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = 64 * i + lane;
       *reinterpret_cast<u32x4*>(Vs + (c / CH) * LD + (c % CH) * 8) = vreg[i];
     }
+    wave_lds_order();
     if (j + NW < j1) load_step(j + NW);
     if (32 * j + 32 > s.kvlen) {      // uniform: the last step
       const int klim = s.kvlen - 1 - (32 * j + 4 * lg);
