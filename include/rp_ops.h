@@ -146,6 +146,8 @@ RP_API rp_status rp_op_rope(void* stream, int bwd, int layout, int d, int rot, c
  * on.  q_len, kv_len [dev] int32 [batch], or NULL for full sequences: how many rows of a padded sequence are in use.  Keys behind kv_len
  * are not read; rows of o behind q_len, and all rows where kv_len is 0, become 0.  scale (1e-30 to 1e30) multiplies q.k.  lse fp32 [batch, a, seq_q]
  * (natural log; -inf for the rows that become 0), or NULL.
+ * At most 2^24 - 1 blocks of 128 rows, ceil((a / kh) seq_q / 128) batch kh, and for the backward call as many blocks of 128 keys, ceil(seq_kv / 128) batch kh
+ * (d = 128: 2^23 - 1).
  * scratch [dev, scratch_bytes] or NULL: where there are few rows, the keys are cut into slices that are joined in order, as many as its size
  * allows (rp_op_cross_attn_scratch: what the calls make use of).  It holds nothing between calls; two calls that may run at the same time need
  * one each.  No output may overlap an input, the scratch or another output (columns of one array beside each other do not). */

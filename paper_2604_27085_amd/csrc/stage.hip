@@ -1353,11 +1353,13 @@ rp_status rp_op_rope(void* stream, int bwd, int layout, int d, int rot, const vo
 
 namespace {
 // Sizes that the cross attention's kernels cover; fills what they share.
-bool cross_args(CrossArgs& p, int batch, int seq_q, int seq_kv, int a, int kh, int d, float scale) {
+bool cross_args(CrossArgs& p, int batch, int seq_q, int seq_kv, int a, int kh, int d, float scale, bool backward) {
   if (batch < 0 || seq_q < 0 || seq_kv < 0 || a <= 0 || kh <= 0 || a % kh || (d != 64 && d != 128) || !(scale >= 1e-30f && scale <= 1e30f)) return false;
-  // rows of a key head, and workgroups and threads of every launch (up to 256 slices of 128 rows or keys, 16 threads a row), are counted in 31 bits
+  // rows of a key head are counted in 31 bits, and a launch has fewer than 2^32 threads: 256 for 128 rows of a key head (or fewer, there is a block for them all
+  // the same); backward 512 for 128 keys at d = 128, 256 at d = 64.  (Cut into slices, a launch has 768 blocks at most, and those that join them 2^25 threads.)
   const double rows = (double)(a / kh) * seq_q, nhb = (double)kh * batch;
   if (rows > 1.0e9 || seq_kv > 1000000000 || rows * nhb * (d / 8) > 2.0e9 || 2.0 * nhb * seq_kv * (d / 8) > 256.0 * 2.0e9) return false;
+  if (ceil(rows / 128) * nhb * 256 >= 4294967296.0 || (backward && ceil(seq_kv / 128.0) * nhb * (d == 128 ? 512 : 256) >= 4294967296.0)) return false;
   p.batch = batch; p.seq_q = seq_q; p.seq_kv = seq_kv; p.a = a; p.kh = kh;
   p.scale = scale;
   p.scale_log2e = scale * 1.4426950408889634f;
@@ -1368,7 +1370,7 @@ bool cross_args(CrossArgs& p, int batch, int seq_q, int seq_kv, int a, int kh, i
 
 rp_status rp_op_cross_attn_scratch(int batch, int seq_q, int seq_kv, int a, int kh, int d, size_t* fwd_bytes, size_t* bwd_bytes) {
   CrossArgs p{};
-  if (!cross_args(p, batch, seq_q, seq_kv, a, kh, d, 1.f)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_scratch: bad arguments");
+  if (!cross_args(p, batch, seq_q, seq_kv, a, kh, d, 1.f, false)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_scratch: bad arguments");
   size_t f = 0, b = 0;
   k_cross_attn_scratch(p, d, &f, &b);
   if (fwd_bytes) *fwd_bytes = f;
@@ -1380,7 +1382,7 @@ rp_status rp_op_cross_attn_fwd(void* stream, const void* q, const void* k, const
                                const int* q_len, const int* kv_len, int batch, int seq_q, int seq_kv, int a, int kh, int d, float scale, void* scratch,
                                size_t scratch_bytes) {
   CrossArgs p{};
-  if (!cross_args(p, batch, seq_q, seq_kv, a, kh, d, scale)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_fwd: bad sizes or scale");
+  if (!cross_args(p, batch, seq_q, seq_kv, a, kh, d, scale, false)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_fwd: bad sizes or scale");
   const long tq = (long)batch * seq_q, tk = (long)batch * seq_kv;
   if (bad_heads(q, tq, a, d, ldq) || bad_heads(o, tq, a, d, ldo) || bad_heads(k, tk, kh, d, ldk) || bad_heads(v, tk, kh, d, ldv))
     return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_fwd: tensors missing, not on 16-byte boundaries, or bad strides");
@@ -1398,7 +1400,7 @@ rp_status rp_op_cross_attn_bwd(void* stream, const void* q, const void* k, const
                                const int* q_len, const int* kv_len, int batch, int seq_q, int seq_kv, int a, int kh, int d, float scale, void* scratch,
                                size_t scratch_bytes) {
   CrossArgs p{};
-  if (!cross_args(p, batch, seq_q, seq_kv, a, kh, d, scale)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_bwd: bad sizes or scale");
+  if (!cross_args(p, batch, seq_q, seq_kv, a, kh, d, scale, true)) return fail(nullptr, RP_EINVAL, "rp_op_cross_attn_bwd: bad sizes or scale");
   const long tq = (long)batch * seq_q, tk = (long)batch * seq_kv;
   if (bad_heads(q, tq, a, d, ldq) || bad_heads(o, tq, a, d, ldo) || bad_heads(dout, tq, a, d, lddo) || bad_heads(dq, tq, a, d, lddq) ||
       bad_heads(k, tk, kh, d, ldk) || bad_heads(v, tk, kh, d, ldv) || bad_heads(dk, tk, kh, d, lddk) || bad_heads(dv, tk, kh, d, lddv) ||
