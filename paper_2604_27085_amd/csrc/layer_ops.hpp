@@ -14,7 +14,7 @@ struct RotateArgs {
   const float2* cs;
   const int* pos;                  // [T] or NULL: t % seq
   int n_pos, T, seq, a, k, d, rot, bwd;
-  int nunits, nrot, tokens_per_block;    // set by the launcher
+  int nunits, nrot, tokens_per_block, first;    // set by the launcher; first: the launch's first token
 };
 // layout 0: pairs (i, i + rot/2);  1: pairs (2i, 2i+1).
 hipError_t k_rope(hipStream_t st, int layout, const RotateArgs& p);

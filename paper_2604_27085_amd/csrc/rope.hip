@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(256) rope_kernel(const RotateArgs p) {
   const int heads = p.a + p.k, nhg = (heads + NH - 1) / NH;
   const int per = nhg * p.nunits, half = p.rot / 2, nrot = p.nrot;
   const int tl = (int)threadIdx.x / per;
-  const int t = (int)blockIdx.x * p.tokens_per_block + (p.tokens_per_block > 1 ? tl : 0);
+  const int t = p.first + (int)blockIdx.x * p.tokens_per_block + (p.tokens_per_block > 1 ? tl : 0);
   if (t >= p.T || (p.tokens_per_block > 1 && tl >= p.tokens_per_block)) return;
   const int pos = p.pos ? p.pos[t] : t % p.seq;
   const bool in_table = pos >= 0 && pos < p.n_pos;
@@ -211,9 +211,15 @@ hipError_t launch_rope(hipStream_t st, RotateArgs p, bool in_place) {
   }
   const int per = ((heads + NH - 1) / NH) * p.nunits;
   p.tokens_per_block = per < 256 ? 256 / per : 1;
-  const int blocks = (int)(((long)p.T + p.tokens_per_block - 1) / p.tokens_per_block);
-  RP_LAUNCH((rope_kernel<V, CUT, NH>), dim3(blocks), dim3(256), 0, st, p);
-  return hipGetLastError();
+  // a launch has fewer than 2^32 threads: 2^31 in one, and as many launches as it takes
+  const long blocks = ((long)p.T + p.tokens_per_block - 1) / p.tokens_per_block, most = 1l << 23;
+  for (long b = 0; b < blocks; b += most) {
+    p.first = (int)(b * p.tokens_per_block);
+    RP_LAUNCH((rope_kernel<V, CUT, NH>), dim3((unsigned)(blocks - b < most ? blocks - b : most)), dim3(256), 0, st, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
