@@ -163,7 +163,7 @@ RP_API rp_status rp_op_cross_attn_bwd(void* stream, const void* q, const void* k
                                float scale, void* scratch, size_t scratch_bytes);
 
 /* Balance loss of a router, forward and backward in one call.  The T tokens are groups of `seq` (T for one group; a sequence each to balance
- * every sequence); mask [dev] uint8 [T], 0 for padding, or NULL.  logits [dev] fp32 [T, E], E <= 1024; idx [dev] int32 [T, top_k]: the experts of every token
+ * every sequence), T up to 2^30; mask [dev] uint8 [T], 0 for padding, or NULL.  logits [dev] fp32 [T, E], E <= 1024; idx [dev] int32 [T, top_k]: the experts of every token
  * (rp_op_moe_route_plan's; numbers outside 0 .. E - 1 are not counted).  Over the N valid tokens, with p = softmax(logits) over all experts
  * and f_ge = counts_ge / (n_g top_k):
  *   loss_balance = E / N sum_t sum_e f_ge p_te;   loss_z = 1 / N sum_t (log sum_e exp logits_te)^2;   loss = coef loss_balance + z_coef loss_z

@@ -87,13 +87,13 @@ __global__ void __launch_bounds__(1024) balance_count_kernel(const BalanceArgs p
   __shared__ int s_hist[1024];
   __shared__ int red[16];
   const int tid = threadIdx.x, slice = (int)blockIdx.x % p.slices;
-  const long g = (int)blockIdx.x / p.slices;
+  const long g = p.first + (int)blockIdx.x / p.slices, out_at = g * p.slices + slice;
   const int per = (p.seq + p.slices - 1) / p.slices;
   const int t0 = min(slice * per, p.seq), t1 = min(t0 + per, p.seq);
   const int valid = count_choices<1024>(p, g * p.seq, t0, t1, s_hist, red);
-  int* const out = p.hist + (long)blockIdx.x * p.E;
+  int* const out = p.hist + out_at * p.E;
   for (int e = tid; e < p.E; e += 1024) out[e] = s_hist[e];
-  if (tid == 0) p.tok[blockIdx.x] = valid;
+  if (tid == 0) p.tok[out_at] = valid;
 }
 
 // Tokens of all groups, for masked batches of many groups (else the rows' blocks add them up themselves).
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(256) balance_rows_kernel(const BalanceArgs p) 
   __shared__ int red[4];
   __shared__ float redf[4];
   const int tid = threadIdx.x, chunk = (int)blockIdx.x % p.chunks;
-  const long g = (int)blockIdx.x / p.chunks, base = g * p.seq;
+  const long g = p.first + (int)blockIdx.x / p.chunks, base = g * p.seq;
   const int t0 = chunk * p.rows_per_block, t1 = min(p.seq, t0 + p.rows_per_block);
   RowPass<L, C, VEC, FULL, 256> rows;
   rows.load(p, base, t0 + tid / L, t1, tid % L);
@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(256) balance_rows_kernel(const BalanceArgs p) 
   float sum_b = 0.f, sum_z = 0.f;
   rows.run(p, base, t0, t1, s_f, p.grad_scale * p.coef * (float)p.E * inv_n, p.grad_scale * 2.f * p.z_coef * inv_n, sum_b, sum_z);
   const float tb = block_sum(sum_b, redf), tz = block_sum(sum_z, redf);
-  if (tid == 0) p.part[blockIdx.x] = make_float2(tb, tz);
+  if (tid == 0) p.part[g * p.chunks + chunk] = make_float2(tb, tz);
 }
 
 RP_DEV void write_loss(const BalanceArgs& p, double b, double z, int N) {
@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(1024) balance_small_kernel(const BalanceArgs p
   __shared__ int red[16];
   __shared__ float redf[16];
   const int tid = threadIdx.x;
-  const long g = blockIdx.x, base = g * p.seq;
+  const long g = p.first + (int)blockIdx.x, base = g * p.seq;
   RowPass<L, C, VEC, FULL, 1024> rows;
   rows.load(p, base, tid / L, p.seq, tid % L);
   const int n = count_choices<1024>(p, base, 0, p.seq, s_hist, red);
@@ -348,10 +348,20 @@ size_t k_moe_balance_scratch(int T, int seq, int E) {
   return up256(groups * s.slices * E * 4) + up256(groups * s.slices * 4) + up256(groups * s.chunks * 8);
 }
 
+// Launches over all groups, `each` blocks a group: a launch has fewer than 2^32 threads, 2^21 blocks of 1024 at most here.
+template <typename K>
+static void launch_groups(K kern, int each, int threads, hipStream_t st, BalanceArgs p) {
+  const int most = (1 << 21) / each;
+  for (long first = 0; first < p.groups; first += most) {
+    p.first = (int)first;
+    const int n = p.groups - (int)first < most ? p.groups - (int)first : most;
+    RP_LAUNCH(kern, dim3(n * each), dim3(threads), 0, st, p);
+  }
+}
 template <int L, int C, int VEC, bool FULL>
 static void launch_rows_as(hipStream_t st, const BalanceArgs& p, bool small) {
-  if (small) RP_LAUNCH((balance_small_kernel<L, C, VEC, FULL>), dim3(p.groups), dim3(1024), 0, st, p);
-  else RP_LAUNCH((balance_rows_kernel<L, C, VEC, FULL>), dim3(p.groups * p.chunks), dim3(256), 0, st, p);
+  if (small) launch_groups(balance_small_kernel<L, C, VEC, FULL>, 1, 1024, st, p);
+  else launch_groups(balance_rows_kernel<L, C, VEC, FULL>, p.chunks, 256, st, p);
 }
 template <int L, int C, int VEC>
 static void launch_rows(hipStream_t st, const BalanceArgs& p, bool small) {
@@ -380,7 +390,7 @@ hipError_t k_moe_balance(hipStream_t st, BalanceArgs p, int T, void* scratch) {
   // 12.3 -> 5.7 us
   const bool small = (long)p.seq * p.E <= 16384 && (long)p.seq * p.top_k <= 8192 && (p.groups == 1 || !p.mask || T <= 65536);
   if (!small) {
-    RP_LAUNCH(balance_count_kernel, dim3(p.groups * s.slices), dim3(1024), 0, st, p);
+    launch_groups(balance_count_kernel, s.slices, 1024, st, p);
     if (p.total_given) RP_LAUNCH(balance_tokens_kernel, dim3(1), dim3(1024), 0, st, p);
   }
   const uintptr_t at16 = reinterpret_cast<uintptr_t>(p.logits) | reinterpret_cast<uintptr_t>(p.dlogits) | reinterpret_cast<uintptr_t>(p.dlogits_in);

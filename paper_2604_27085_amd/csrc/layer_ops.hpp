@@ -32,7 +32,7 @@ struct BalanceArgs {
   float coef, z_coef, grad_scale;
   int *hist, *tok;                 // from here on set by the launcher
   float2* part;
-  int groups, slices, chunks, rows_per_block, total_given;
+  int groups, slices, chunks, rows_per_block, total_given, first;    // first: the launch's first group
 };
 size_t k_moe_balance_scratch(int T, int seq, int E);
 hipError_t k_moe_balance(hipStream_t st, BalanceArgs p, int T, void* scratch);

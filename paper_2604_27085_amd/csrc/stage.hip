@@ -1418,7 +1418,7 @@ rp_status rp_op_cross_attn_bwd(void* stream, const void* q, const void* k, const
 }
 
 rp_status rp_op_moe_balance_scratch(int T, int seq, int E, size_t* scratch_bytes) {
-  if (!scratch_bytes || T < 0 || seq <= 0 || T % seq || E <= 0 || E > 1024) return fail(nullptr, RP_EINVAL, "rp_op_moe_balance_scratch: bad arguments");
+  if (!scratch_bytes || T < 0 || T > (1 << 30) || seq <= 0 || T % seq || E <= 0 || E > 1024) return fail(nullptr, RP_EINVAL, "rp_op_moe_balance_scratch: bad arguments");
   *scratch_bytes = k_moe_balance_scratch(T, seq, E);
   return RP_OK;
 }
@@ -1426,7 +1426,7 @@ rp_status rp_op_moe_balance_scratch(int T, int seq, int E, size_t* scratch_bytes
 rp_status rp_op_moe_balance(void* stream, const float* logits, const int* idx, const unsigned char* mask, int T, int seq, int E, int top_k, float coef,
                             float z_coef, float grad_scale, int* counts, int* tokens, float* loss_out, const float* dlogits_in, float* dlogits,
                             void* scratch, size_t scratch_bytes) {
-  if (T < 0 || seq <= 0 || T % seq || E <= 0 || E > 1024 || top_k <= 0 || top_k > E || !tokens || !loss_out || (T && (!logits || !idx || !counts)) ||
+  if (T < 0 || T > (1 << 30) || seq <= 0 || T % seq || E <= 0 || E > 1024 || top_k <= 0 || top_k > E || !tokens || !loss_out || (T && (!logits || !idx || !counts)) ||
       (dlogits_in && !dlogits))
     return fail(nullptr, RP_EINVAL, "rp_op_moe_balance: bad arguments");
   if (T && (!scratch || off16(scratch) || scratch_bytes < k_moe_balance_scratch(T, seq, E)))

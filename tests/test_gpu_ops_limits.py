@@ -40,3 +40,22 @@ def test_a_rotation_of_more_than_two_to_the_32_threads(B):
     for part in x[:whole].view(-1, n, d).split(256):
         assert bool((part.view(torch.int16) == few.view(torch.int16)).all())
     assert torch.equal(x[whole:], few[:T - whole])
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_a_balance_loss_of_more_than_two_to_the_22_groups(B, masked):
+    """A group a token: what is chosen has all of the group's weight, f = 1 / top_k on it."""
+    from test_gpu_balance import check, run
+    T, E, k = (1 << 22) + 3, 8, 2
+    g = torch.Generator(device=DEV).manual_seed(2)
+    x = 2.0 * torch.randn((T, E), generator=g, device=DEV)
+    idx = x.topk(k, 1).indices.to(torch.int32)
+    mask = (torch.rand(T, generator=g, device=DEV) < 0.7).to(torch.uint8) if masked else None
+    keep = mask.bool() if masked else torch.ones(T, dtype=torch.bool, device=DEV)
+    counts = torch.zeros((T, E), dtype=torch.float64, device=DEV).scatter_(1, idx.long(), 1.0) * keep[:, None]
+    f, p, N = counts / k, x.double().softmax(1) * keep[:, None], int(keep.sum())
+    dot, lse = (f * p).sum(1, keepdim=True), torch.where(keep, torch.logsumexp(x.double(), 1), 0.0)
+    bal, z = E / N * dot.sum(), lse.square().sum() / N
+    part = lambda sign: 0.5 * p * (0.2 * E / N * (f + sign * dot) + 0.1 * 2 / N * (lse if sign < 0 else lse.abs())[:, None])  # noqa: E731
+    want = (counts.long(), torch.cat((keep, keep.sum()[None])), torch.stack((0.2 * bal + 0.1 * z, bal, z)), part(-1), part(1))
+    check(run(B, x, idx, mask, 1, k, 0.2, 0.1, 0.5), want)

@@ -32,3 +32,14 @@ def test_cross_attention_scratch_goes_as_far_as_the_forward():
     assert B.rp_op_cross_attn_scratch((1 << 24) - 1, 1, 1, 1, 1, 64) == (0, 0)
     with pytest.raises(B.RpError):
         B.rp_op_cross_attn_scratch(1 << 24, 1, 1, 1, 1, 64)
+
+
+def test_balance_counts_tokens_up_to_two_to_the_30():
+    """Token numbers, and the sums of one and a block's step, stay inside 31 bits."""
+    args = [None, P, P, None, 1 << 30, 1, 16, 2, 0.1, 0.0, 1.0, P, P, P, None, P, P, 1 << 62]
+    assert B.rp_op_moe_balance_scratch(1 << 30, 1 << 30, 16) > 0
+    for T in ((1 << 30) + 1, 2 ** 31 - 1):
+        args[4] = T
+        assert B.lib.rp_op_moe_balance(*args) == B.RP_EINVAL
+        with pytest.raises(B.RpError):
+            B.rp_op_moe_balance_scratch(T, 1, 16)
