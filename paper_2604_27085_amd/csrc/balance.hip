@@ -350,23 +350,26 @@ size_t k_moe_balance_scratch(int T, int seq, int E) {
 
 // Launches over all groups, `each` blocks a group: a launch has fewer than 2^32 threads, 2^21 blocks of 1024 at most here.
 template <typename K>
-static void launch_groups(K kern, int each, int threads, hipStream_t st, BalanceArgs p) {
+static hipError_t launch_groups(K kern, int each, int threads, hipStream_t st, BalanceArgs p) {
   const int most = (1 << 21) / each;
   for (long first = 0; first < p.groups; first += most) {
     p.first = (int)first;
     const int n = p.groups - (int)first < most ? p.groups - (int)first : most;
     RP_LAUNCH(kern, dim3(n * each), dim3(threads), 0, st, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
+  return hipSuccess;
 }
 template <int L, int C, int VEC, bool FULL>
-static void launch_rows_as(hipStream_t st, const BalanceArgs& p, bool small) {
-  if (small) launch_groups(balance_small_kernel<L, C, VEC, FULL>, 1, 1024, st, p);
-  else launch_groups(balance_rows_kernel<L, C, VEC, FULL>, p.chunks, 256, st, p);
+static hipError_t launch_rows_as(hipStream_t st, const BalanceArgs& p, bool small) {
+  if (small) return launch_groups(balance_small_kernel<L, C, VEC, FULL>, 1, 1024, st, p);
+  return launch_groups(balance_rows_kernel<L, C, VEC, FULL>, p.chunks, 256, st, p);
 }
 template <int L, int C, int VEC>
-static void launch_rows(hipStream_t st, const BalanceArgs& p, bool small) {
-  if (VEC == 4 && p.E == L * C * VEC) launch_rows_as<L, C, VEC, VEC == 4>(st, p, small);
-  else launch_rows_as<L, C, VEC, false>(st, p, small);
+static hipError_t launch_rows(hipStream_t st, const BalanceArgs& p, bool small) {
+  if (VEC == 4 && p.E == L * C * VEC) return launch_rows_as<L, C, VEC, VEC == 4>(st, p, small);
+  return launch_rows_as<L, C, VEC, false>(st, p, small);
 }
 
 hipError_t k_moe_balance(hipStream_t st, BalanceArgs p, int T, void* scratch) {
@@ -389,26 +392,32 @@ hipError_t k_moe_balance(hipStream_t st, BalanceArgs p, int T, void* scratch) {
   // one block is through with a group of 16384 logits (and their choices) in the time of the launch or two that it saves: 256 tokens of 32 experts
   // 12.3 -> 5.7 us
   const bool small = (long)p.seq * p.E <= 16384 && (long)p.seq * p.top_k <= 8192 && (p.groups == 1 || !p.mask || T <= 65536);
+  hipError_t e = hipSuccess;      // (RP_LAUNCH forgets what the launch before it left: each is asked for)
   if (!small) {
-    launch_groups(balance_count_kernel, s.slices, 1024, st, p);
-    if (p.total_given) RP_LAUNCH(balance_tokens_kernel, dim3(1), dim3(1024), 0, st, p);
+    e = launch_groups(balance_count_kernel, s.slices, 1024, st, p);
+    if (e == hipSuccess && p.total_given) {
+      RP_LAUNCH(balance_tokens_kernel, dim3(1), dim3(1024), 0, st, p);
+      e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
   }
   const uintptr_t at16 = reinterpret_cast<uintptr_t>(p.logits) | reinterpret_cast<uintptr_t>(p.dlogits) | reinterpret_cast<uintptr_t>(p.dlogits_in);
   if (p.E % 4 == 0 && at16 % 16 == 0) {      // rows on 16-byte boundaries: 16-byte accesses
-    if (p.E <= 8) launch_rows<2, 1, 4>(st, p, small);
-    else if (p.E <= 16) launch_rows<4, 1, 4>(st, p, small);
-    else if (p.E <= 32) launch_rows<4, 2, 4>(st, p, small);
-    else if (p.E <= 64) launch_rows<8, 2, 4>(st, p, small);
-    else if (p.E <= 128) launch_rows<16, 2, 4>(st, p, small);
-    else if (p.E <= 256) launch_rows<32, 2, 4>(st, p, small);
-    else if (p.E <= 512) launch_rows<64, 2, 4>(st, p, small);
-    else launch_rows<64, 4, 4>(st, p, small);
+    if (p.E <= 8) e = launch_rows<2, 1, 4>(st, p, small);
+    else if (p.E <= 16) e = launch_rows<4, 1, 4>(st, p, small);
+    else if (p.E <= 32) e = launch_rows<4, 2, 4>(st, p, small);
+    else if (p.E <= 64) e = launch_rows<8, 2, 4>(st, p, small);
+    else if (p.E <= 128) e = launch_rows<16, 2, 4>(st, p, small);
+    else if (p.E <= 256) e = launch_rows<32, 2, 4>(st, p, small);
+    else if (p.E <= 512) e = launch_rows<64, 2, 4>(st, p, small);
+    else e = launch_rows<64, 4, 4>(st, p, small);
   } else {
-    if (p.E <= 16) launch_rows<16, 1, 1>(st, p, small);
-    else if (p.E <= 64) launch_rows<64, 1, 1>(st, p, small);
-    else if (p.E <= 256) launch_rows<64, 4, 1>(st, p, small);
-    else launch_rows<64, 16, 1>(st, p, small);
+    if (p.E <= 16) e = launch_rows<16, 1, 1>(st, p, small);
+    else if (p.E <= 64) e = launch_rows<64, 1, 1>(st, p, small);
+    else if (p.E <= 256) e = launch_rows<64, 4, 1>(st, p, small);
+    else e = launch_rows<64, 16, 1>(st, p, small);
   }
-  if (!small || p.groups > 1) RP_LAUNCH(balance_total_kernel, dim3(1), dim3(256), 0, st, p, small ? p.groups : p.groups * s.chunks);
+  if (e != hipSuccess || (small && p.groups == 1)) return e;
+  RP_LAUNCH(balance_total_kernel, dim3(1), dim3(256), 0, st, p, small ? p.groups : p.groups * s.chunks);
   return hipGetLastError();
 }
