@@ -156,8 +156,7 @@ struct RowPass {
       }
       if (t - row_in + ROWS < t1) load(p, base, t + ROWS, t1, sub);
       m = over_lanes<L>(m, Max());
-      const bool some = m != -INFINITY;      // a row of -inf has no probabilities
-      const float ref = some ? m : 0.f;
+      const float ref = m != -INFINITY ? m : 0.f;
       float l = 0.f, dot = 0.f;
 #pragma unroll
       for (int c = 0; c < C; ++c)
@@ -169,7 +168,8 @@ struct RowPass {
         }
       l = over_lanes<L>(l, Add());
       dot = over_lanes<L>(dot, Add());
-      const float inv_l = some ? 1.f / l : 0.f, lse = some ? m + logf(l) : 0.f;
+      const bool some = l != 0.f;      // a row of -inf has no probabilities; one of NaN, which the maximum passes over, has NaN here
+      const float inv_l = some ? 1.f / l : 0.f, lse = some ? ref + logf(l) : 0.f;
       dot *= inv_l;
       if (sub == 0) { sum_b += dot; sum_z += lse * lse; }
       if (t < t1 && p.dlogits) {
