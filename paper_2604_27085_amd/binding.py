@@ -146,6 +146,8 @@ def _ptr(t):
     try:
         return t.data_ptr()      # (asked for its type first, a tensor takes twice as long)
     except AttributeError:
+        if not isinstance(t, int):      # (bytes and text would pass as addresses of host memory)
+            raise
         return t
 
 
