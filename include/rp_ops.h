@@ -1,6 +1,6 @@
 /*
- * rp_ops.h -- kernel-level entry points of the same library, one per hot-path kernel, so that each kernel can be
- * compared with the CPU oracle on its own.  Same conventions as rp.h: plain C types, all data pointers are device
+ * rp_ops.h -- kernel-level entry points of the same library: the kernels of the hot path one by one, so that each can be
+ * compared with the CPU oracle on its own, and what a decoder layer other than the stage's is built from.  Same conventions as rp.h: plain C types, all data pointers are device
  * pointers, bf16 row-major unless stated, `stream` is a hipStream_t, calls only enqueue.  Errors: RP_EINVAL for
  * arguments the kernels do not cover, RP_EHIP for launch failures.
  */
@@ -169,7 +169,8 @@ RP_API rp_status rp_op_cross_attn_bwd(void* stream, const void* q, const void* k
  *   loss_balance = E / N sum_t sum_e f_ge p_te;   loss_z = 1 / N sum_t (log sum_e exp logits_te)^2;   loss = coef loss_balance + z_coef loss_z
  * counts [dev] int32 [T / seq, E], tokens [dev] int32 [T / seq + 1] (n_g, then N); loss_out [dev] fp32 [3]: loss, loss_balance, loss_z (all 0 for N = 0).
  * dlogits [dev] fp32 [T, E] or NULL = grad_scale * the gradient of the loss (the counts are constants) + dlogits_in, the gradient the layer has
- * left (rp_stage_backward's d_router_logits), or NULL; dlogits may be dlogits_in.  Padding, and a token whose logits are all -inf, adds nothing to
+ * left, or NULL; dlogits may be dlogits_in.  (rp_stage_backward's d_router_logits where the caller supplies the logits and takes their gradient on to a router
+ * of its own.  With moe_router 1 the stage has taken its router's gradient on within the call: nothing added afterwards gets there.)  Padding, and a token whose logits are all -inf, adds nothing to
  * the losses and gets no gradient.  scratch [dev, scratch_bytes], rp_op_moe_balance_scratch bytes; a call of its own each. */
 RP_API rp_status rp_op_moe_balance_scratch(int T, int seq, int E, size_t* scratch_bytes);
 RP_API rp_status rp_op_moe_balance(void* stream, const float* logits, const int* idx, const unsigned char* mask, int T, int seq, int E, int top_k,
