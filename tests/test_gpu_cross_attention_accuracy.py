@@ -72,3 +72,23 @@ def test_sharp_rows(B, gain, d, n, sliced):
     x = inputs(200, n, 4, 2, d, gain * math.sqrt(128.0 / d))
     exact = sliced or n <= EXACT_DELTA
     check(gradients(B, *x, sliced), A.gradients(*x, d ** -0.5, exact), [("dq", A.DQ_SHARP_EXACT if exact else A.DQ_SHARP), ("dk", A.DK_SHARP)])
+
+
+@pytest.mark.parametrize("scratch", ["none", "full"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_sharp_rows_of_a_padded_batch(B, d, scratch):
+    """Sequences of different lengths, as columns of larger arrays, whose unused rows hold NaN: each row's own place, query and delta."""
+    from test_gpu_cross_attention import Case
+    c = Case(3, 200, 700, 6, 2, d, [200, 77, 5], [700, 300, 257], pad=8)
+    b, nq, nk, a, kh, _ = c.shape
+    g = torch.Generator().manual_seed(d)
+    q, k, v, do = [c.view(t, n) for t, n in ((c.q, nq), (c.k, nk), (c.v, nk), (c.do, nq))]
+    for i in range(b):
+        q[i, :c.ql[i]] = A.sharp_queries(k[i, :c.kl[i]].float().cpu(), a, c.ql[i], 1.1 * math.sqrt(128.0 / d), g).to(DEV)
+    c.run(B, scratch)
+    got = c.got()
+    for i in range(b):
+        m, n = c.ql[i], c.kl[i]
+        want = A.gradients(*[t.cpu() for t in (q[i, :m], k[i, :n], v[i, :n], do[i, :m])], c.scale, False)
+        check({"dq": got["dq"][i, :m].cpu(), "dk": got["dk"][i, :n].cpu()}, want, [("dq", A.DQ_SHARP), ("dk", A.DK_SHARP)])
+        assert float(got["dq"][i, m:].abs().sum()) == 0.0 and float(got["dk"][i, n:].abs().sum()) == 0.0
