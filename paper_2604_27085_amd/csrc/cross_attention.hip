@@ -17,9 +17,10 @@
 // order (fp32 partials in the caller's scratch; no atomics, so the result does not depend on timing).
 // Keys behind kv_len are never read (they may hold anything); rows behind q_len get zeros, and lse -inf.
 //
-// What bounds them, at 4096 queries of 32 heads of 128 against 8192 keys of 8 heads: forward 530 us (1.04 PFLOP/s), dQ 928 (1.18 with the product's second
-// part, see cross_dq_kernel), dK/dV 1090 (1.01); matrix pipe busy 58, 61 and 50 %, vector issue 48, 51 and 41 %, memory nothing to speak of: the exponentials and conversions beside the
-// products, and the clock that the power allows, as in attention.hip.  At d = 64 (64 heads, 4 x 512 queries against 1536 keys) 68, 118 and 117 us: the
+// What bounds them, at 4096 queries of 32 heads of 128 against 8192 keys of 8 heads (kernels alone, medians of 60 passes): forward 536 us (1.03 PFLOP/s), dQ 940 (1.17
+// with the product's second part, see cross_dq_kernel), dK/dV 988 (1.11); matrix pipe busy 58, 58 and 50 %, vector issue 48, 52 and 41 %, memory nothing to speak of: the
+// exponentials and conversions beside the products, and the clock that the power allows, as in attention.hip.  At d = 64 (64 heads, 4 x 512 queries against 1536 keys)
+// 71, 140 and 124 us: the
 // vector instructions of a tile are the same for half the products.  A padded batch adds what its longest sequence's workgroups last longer.
 // P, and dS for dK, are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most); dS for dQ is taken in two parts; scores, statistics,
 // dP - delta and every sum are fp32.
@@ -244,7 +245,7 @@ __global__ void __launch_bounds__(256, 2) cross_fwd_kernel(const CrossArgs p) {
       }
     l_run += psum;
     {
-      uint4 pf[4];      // P in bf16, as the matrix instruction takes it: relative 2^-9 a term, on sums held in fp32
+      uint4 pf[4];      // P in bf16, as the matrix instruction takes it: relative 2^-8 a term, on sums held in fp32
 #pragma unroll
       for (int gk = 0; gk < 4; ++gk) pf[gk] = pack_frag32(sT[gk >> 1], 8 * (gk & 1));
       MFMA_PHASE_BEGIN();
