@@ -100,8 +100,8 @@ def distance(x, y):
 DQ_ORDINARY = 2.1e-3
 # dq of sharp rows: c = |off| / sum |dS| of the rows that are not taken again is spread over 0 .. TAU, TAU / sqrt(3) in the mean square; a row on one key has
 #   sum |dS| = 2 |dS_top|, so its dq is off by 2 c; with the result's own rounding sqrt((2 TAU / sqrt(3))^2 + 1.66e-3^2) = 4.8e-3.
-DQ_SHARP = math.sqrt((2 * TAU) ** 2 / 3 + ONE_ROUNDING ** 2) * 1.03
+DQ_SHARP = math.sqrt((2 * TAU) ** 2 / 3 + ONE_ROUNDING ** 2)
 # the same with delta from the scores: its own rounding, and the fp32 of dP - delta
 DQ_SHARP_EXACT = 2.1e-3
-# dk: dS and the result are rounded, sqrt(2) * 1.66e-3; rows of one key add up with equal signs now and then
+# dk: dS and the result are rounded, sqrt(2) * 1.66e-3 = 2.35e-3, and a quarter more where a key's few terms, which have either sign, cancel
 DK_SHARP = 3.0e-3
