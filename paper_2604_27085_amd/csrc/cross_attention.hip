@@ -564,7 +564,8 @@ __global__ void __launch_bounds__(256) cross_row_join_kernel(const CrossArgs p, 
 //   with the key loop in slices a launch of its own (DELTA) makes those two sums of every slice;
 //   else delta starts as dO.o, and the rows of dS, which sum up to zero, tell at the end what it was off by.  Rows where that is more than FAR sum |dS|, more
 //   than a rounding of every dS to bf16 could do, get dq - off sum P K (mean_keys; of rows whose scores have standard deviation 2
-//   one in 10000 against 8192 keys, one in 1500 against 1500 and one in 240 against 300).  dK, dV take the corrected one in any case.
+//   one in 10000 against 8192 keys, one in 1500 against 1500 and one in 240 against 300), the others dq - off times the mean of 64 keys: that takes out what a
+//   part that all keys share would add (three times their spread: dq off by 1.9e-3 instead of 8e-3).  dK, dV take the corrected delta in any case.
 // dS goes into its product in two parts, its bf16 and the bf16 of what that left over: K^T's fragments serve both, and dq is off by little more than its
 // own rounding (relative 2-norm 1.7e-3 with delta from the scores; in one part 2.4e-3).
 constexpr int EXACT_DELTA = 256;
@@ -823,12 +824,12 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dqacc[dt][0] = dqacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
   float row_sum[2] = {0.f, 0.f}, row_size[2] = {0.f, 0.f};      // of dS: its sum, and that of its absolute values
-  if (j0 < j1) load_tiles(j0);
-  for (int j = j0; j < j1; ++j) {
+  if (j0 < j1) load_tiles(j1 - 1);
+  for (int j = j1 - 1; j >= j0; --j) {      // the first tile last: it is full, and its keys are averaged below
     __syncthreads();
     store_tiles();
     __syncthreads();
-    if (j + 1 < j1) load_tiles(j + 1);
+    if (j > j0) load_tiles(j - 1);
     const bool need_mask = j * 64 + 64 > s.kvlen;
     // the two 32-key halves of the tile one after the other: half as many score registers live at a time
 #pragma unroll
@@ -901,6 +902,23 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
         if (lane == 0) marks[2 * w + c] = mark;
       }
       __syncthreads();      // (the last tile has been read as well)
+      // the other rows: the mean of 64 keys in the place of sum P K, which is what all keys share of it
+      float* const mean = reinterpret_cast<float*>(Vs);      // [NT / D][D]
+      {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 64 * D / NT; ++i) sum += (float)Ks[((tid / D) * (64 * D / NT) + i) * LD + tid % D];
+        mean[tid] = sum * (1.f / 64.f);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        f32x4 m = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NT / D; ++i) m += *reinterpret_cast<const f32x4*>(mean + i * D + 16 * dt + 4 * lg);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) dqacc[dt][c] -= (far[c] ? 0.f : off[c]) * m;
+      }
       int count = 0, at[2] = {0, 0};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -923,9 +941,9 @@ __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs p) {
           for (int c = 0; c < 2; ++c) {
             const int i = at[c] - first;
             if (far[c] && i >= 0 && i < 16) {
-              const float* const mean = reinterpret_cast<const float*>(smem) + i * (D + 4) + 4 * lg;
+              const float* const sum = reinterpret_cast<const float*>(smem) + i * (D + 4) + 4 * lg;
 #pragma unroll
-              for (int dt = 0; dt < DT; ++dt) dqacc[dt][c] -= off[c] * *reinterpret_cast<const f32x4*>(mean + 16 * dt);
+              for (int dt = 0; dt < DT; ++dt) dqacc[dt][c] -= off[c] * *reinterpret_cast<const f32x4*>(sum + 16 * dt);
             }
           }
           __syncthreads();

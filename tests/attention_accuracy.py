@@ -2,7 +2,9 @@
 shows what the limits tell apart.
 
   dq     is rounded once (H); dS goes into its product as two bf16 numbers, off by H^2;  delta is off by no more than TAU sum_k |dS_k| of its row, by
-         nothing where it comes from the scores themselves (up to 256 keys, or with the key loop in slices)
+         nothing where it comes from the scores themselves (up to 256 keys, or with the key loop in slices).  With delta off by x, dS is off by P x and sums up
+         to x over a row (sum P = 1), which the kernel sees and takes off again with M, the mean of the first 64 keys:  sum (dS + P x) K - x M
+         = sum dS K + x sum P (K - M), so dq is off by x sum P |K - M| at most, element by element
   dk     is rounded once, its dS once; the delta it takes is always the corrected one
   fp32   a product of d terms adds up d / 32 + 32 roundings at most, E = 40 * 2^-24 of the terms' absolute values; an exponent that is off by e takes its
          exponential e off, and a row's log-sum-exp is off by what its exponents are
@@ -46,11 +48,12 @@ def gradients(q, k, v, do, scale, exact_delta):
         dp_abs = dh.abs() @ vx.abs().t()
         size = ds.abs().sum(1, keepdim=True)
         noise = e * (ds.abs() + p * size) + E * p * (dp_abs + (p * dp_abs).sum(1, keepdim=True))
-        for name, rounded, delta, other in (("dq", H * H, 0.0 if exact_delta else TAU / (1 - TAU), kx), ("dk", H, 0.0, qh)):
-            err = rounded * ds.abs() + noise + delta * size * p
+        for name, rounded, other in (("dq", H * H, kx), ("dk", H, qh)):
+            err = rounded * ds.abs() + noise
             if name == "dq":
+                far = 0.0 if exact_delta else TAU / (1 - TAU) * size * (p @ (kx - kx[:64].mean(0)).abs())
                 out[name][0][:, h] = scale * ds @ other
-                out[name][1][:, h] = scale * (1 + H) * (err @ other.abs())
+                out[name][1][:, h] = scale * (1 + H) * (err @ other.abs() + far)
             else:
                 out[name][0][:, g] += scale * ds.t() @ other
                 out[name][1][:, g] += scale * (1 + H) * (err.t() @ other.abs())
@@ -64,8 +67,8 @@ def bf16(t):
 
 
 def as_the_kernels_round(q, k, v, do, scale, exact_delta, parts=2, repeat=True, correct=True):
-    """dq and dk as the kernels make them but for fp32: dS in `parts` bf16 parts for dq, a delta that is off by more than TAU sum |dS| taken again with its
-    correction (repeat), and the corrected delta for dk (correct)."""
+    """dq and dk as the kernels make them but for fp32: dS in `parts` bf16 parts for dq, which is corrected by what delta was off by times sum P K where that is more
+    than TAU sum |dS|, else times the mean of 64 keys (repeat), and the corrected delta for dk (correct)."""
     q, k, v, do = [t.to(F64) for t in (q, k, v, do)]
     a, kh = q.shape[1], k.shape[1]
     dq, dk = torch.zeros_like(q), torch.zeros_like(k)
@@ -78,12 +81,13 @@ def as_the_kernels_round(q, k, v, do, scale, exact_delta, parts=2, repeat=True, 
         delta = (p * dp).sum(1, keepdim=True) if exact_delta else stored
         ds = p * (dp - delta)
         off = ds.sum(1, keepdim=True)
-        if repeat:
-            ds = torch.where(off.abs() > TAU * ds.abs().sum(1, keepdim=True), p * (dp - delta - off), ds)
         x = bf16(ds)
         if parts == 2:
             x = x + bf16(ds - x)
-        dq[:, h] = bf16(scale * x @ kx)
+        got = x @ kx
+        if repeat and not exact_delta:
+            got = got - off * torch.where(off.abs() > TAU * ds.abs().sum(1, keepdim=True), p @ kx, kx[:64].mean(0))
+        dq[:, h] = bf16(scale * got)
         dk[:, g] += scale * bf16(p * (dp - delta - (off if correct else 0.0))).t() @ qh
     return {"dq": dq, "dk": bf16(dk)}
 

@@ -55,3 +55,14 @@ def test_sharp_rows(n, d, gain):
     got, want = run(x, d, True)
     assert A.distance(got["dq"], want["dq"][0]) < A.DQ_SHARP_EXACT
     assert inside(got, want, "dq") and inside(got, want, "dk")
+
+
+@pytest.mark.parametrize("share", [1.0, 3.0])
+@pytest.mark.parametrize("n,d", [(300, 128), (705, 64)])
+def test_keys_that_share_a_part(n, d, share):
+    q, k, v, do = inputs(400, n, d, std=1.0)
+    k = (k.float() + share * torch.randn((1, 1, d), generator=torch.Generator().manual_seed(n))).to(torch.bfloat16)
+    got, want = run((q, k, v, do), d)
+    assert A.distance(got["dq"], want["dq"][0]) < A.DQ_ORDINARY and inside(got, want, "dq")
+    bad, _ = run((q, k, v, do), d, repeat=False)
+    assert A.distance(bad["dq"], want["dq"][0]) > A.DQ_ORDINARY

@@ -64,6 +64,19 @@ def test_ordinary_rows(B, d, n, sliced, std):
     check(gradients(B, *x, sliced), A.gradients(*x, d ** -0.5, sliced or n <= EXACT_DELTA), [("dq", A.DQ_ORDINARY)])
 
 
+@pytest.mark.parametrize("n,sliced", LOOPS + [(300, False), (705, False)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("share", [1.0, 3.0])
+def test_keys_that_share_a_part(B, share, d, n, sliced):
+    """A part that all keys have in common (a bias) adds the same to every score of a row and nothing to dq, since a row of dS sums up to zero; what delta is off by
+    times it would show.  Against the mean of 64 keys 1 / 64 of the centred keys' square is left besides sum P^2: sqrt(2) u sqrt(0.03 + 1 / 64) = 0.3 u
+    beside dq's own rounding u, 1.74e-3."""
+    q, k, v, do = inputs(200, n, 4, 2, d, std=1.0)
+    k = (k.float() + share * torch.randn((1, 2, d), generator=torch.Generator().manual_seed(n))).to(torch.bfloat16)
+    x = (q, k, v, do)
+    check(gradients(B, *x, sliced), A.gradients(*x, d ** -0.5, sliced or n <= EXACT_DELTA), [("dq", A.DQ_ORDINARY)])
+
+
 @pytest.mark.parametrize("n,sliced", LOOPS)
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("gain", [1.0, 1.2])
