@@ -177,6 +177,76 @@ RP_API rp_status rp_op_moe_balance(void* stream, const float* logits, const int*
                             float coef, float z_coef, float grad_scale, int* counts, int* tokens, float* loss_out, const float* dlogits_in,
                             float* dlogits, void* scratch, size_t scratch_bytes);
 
+/* ---- training on packed documents: the plan of a packed row, attention with a span of keys for every query, a gated linear recurrence, the embedding, dropout ----
+ * These calls find the device of `stream` themselves, as those above. */
+
+/* What the documents of packed rows make of every token.  The T tokens are rows of `seq`; starts [dev] int32 [n_docs + 1], not descending: document i is the
+ * tokens starts[i] .. starts[i + 1] - 1 (an empty one has none); tokens before starts[0] and from starts[n_docs] on are padding.  A document that a row's
+ * end cuts does not see beyond it.  Each output may be NULL.
+ *   span [dev] int32 [T, 2]  the keys that the token sees, first and last + 1, counted from its row's first token (rp_op_span_attn_fwd): its document up to itself; the last
+ *                            `window` of those where window > 0; and, where prefix [dev] int32 [n_docs] is given, its document's first prefix[i] tokens, which see one
+ *                            another both ways.  Padding sees nothing.
+ *   pos [dev] int32 [T]      place within the document (rp_op_rope); 0 for padding
+ *   first [dev] uint8 [T]    1 where a document begins, and for padding (rp_op_scan_fwd) */
+RP_API rp_status rp_op_pack_plan(void* stream, const int* starts, const int* prefix, int n_docs, int window, int T, int seq, int* span, int* pos,
+                          unsigned char* first);
+
+/* Grouped-query attention in which every query sees a span of the keys: documents of a packed row, sliding windows, prefixes, padding, or caches of different lengths
+ * (with few queries, the step of a generation), flash style.  q, o [batch * seq_q, a, d]; k, v [batch * seq_kv, kh, d], d 64 or 128; row strides ld* in elements; any lengths
+ * from 0 on.  span [dev] int32 [batch, seq_q, 2]: query t of a sequence sees that sequence's keys span[t][0] <= j < span[t][1] (cut to 0 .. seq_kv).  With z = scale q.k:
+ *   s = z, or cap tanh(z / cap) where cap > 0 (1e-3 to 1e3);  minus slopes[h] |p - j| where slopes [dev] fp32 [a] is given, p = q_pos [dev] int32 [batch, seq_q],
+ *   or t + seq_kv - seq_q where q_pos is NULL;  lse = log sum exp s;  o = sum exp(s - lse) v.
+ * scale 1e-30 to 1e30.  lse fp32 [batch, a, seq_q] (natural log), or NULL.  A query that sees nothing has o = 0, lse = -inf, and gives and gets no gradient.  What a
+ * query does not see does not reach it, also where it is infinite or NaN; a key that it sees with an infinity or NaN in v makes its whole row NaN where only some
+ * queries near it see that key.
+ * o_rest bf16, laid out as o, or NULL: what o's rounding left over (o + o_rest is good to 2^-16).  The backward call makes sum_j P dP from both; without it that is as exact as o.
+ * scratch [dev, scratch_bytes]: the forward call cuts the keys of few rows into as many slices as it allows, and does without (NULL); the backward call needs the
+ * smaller number, least_bytes, and cuts with more.  It holds nothing between calls; two calls that may run at the same time need one each.  No output may
+ * overlap an input, the scratch or another output (columns of one array beside each other do not). */
+RP_API rp_status rp_op_span_attn_scratch(int batch, int seq_q, int seq_kv, int a, int kh, int d, size_t* fwd_bytes, size_t* bwd_bytes, size_t* least_bytes);
+RP_API rp_status rp_op_span_attn_fwd(void* stream, const void* q, const void* k, const void* v, void* o, void* o_rest, float* lse, long ldq, long ldk, long ldv,
+                              long ldo, const int* span, const int* q_pos, const float* slopes, float cap, int batch, int seq_q, int seq_kv, int a, int kh,
+                              int d, float scale, void* scratch, size_t scratch_bytes);
+/* o, o_rest, lse: the forward's.  delta fp32 [batch, a, seq_q] is scratch.  dq [batch * seq_q, a, d], dk, dv [batch * seq_kv, kh, d] overwritten; keys that nothing sees
+ * get 0.  The slopes are constants. */
+RP_API rp_status rp_op_span_attn_bwd(void* stream, const void* q, const void* k, const void* v, const void* o, const void* o_rest, const void* dout,
+                              const float* lse, float* delta, void* dq, void* dk, void* dv, long ldq, long ldk, long ldv, long ldo, long lddo, long lddq,
+                              long lddk, long lddv, const int* span, const int* q_pos, const float* slopes, float cap, int batch, int seq_q, int seq_kv, int a,
+                              int kh, int d, float scale, void* scratch, size_t scratch_bytes);
+
+/* Gated linear recurrence, every channel by itself:  h_t = f_t h_(t-1) + w(f_t) x_t,  f_t = sigmoid(g_t),  y_t = h_t.
+ * x, g, y bf16 [batch * seq, c], c a multiple of 8, row strides ld* in elements.  h0, last fp32 [batch, c] or NULL: the state before the first token (else 0) and
+ * behind the last (last may be h0: the step of a generation).  first [dev] uint8 [batch * seq] or NULL: where not 0 a document begins, and the state before counts for
+ * nothing.  len [dev] int32 [batch] or NULL: how many tokens of a padded sequence are in use; y behind them becomes 0, last is the state at their end.
+ * states [dev] or NULL: for the backward call, state_bytes of rp_op_scan_sizes.  scratch [dev, scratch_bytes]: a call of its own each. */
+enum { RP_SCAN_PLAIN = 0, RP_SCAN_MEAN = 1, RP_SCAN_ENERGY = 2 };      /* w: 1, 1 - f, sqrt(1 - f^2) */
+RP_API rp_status rp_op_scan_sizes(int batch, int seq, int c, size_t* state_bytes, size_t* scratch_bytes);
+RP_API rp_status rp_op_scan_fwd(void* stream, int weight, const void* x, const void* g, void* y, long ldx, long ldg, long ldy, const unsigned char* first,
+                         const int* len, const float* h0, float* last, float* states, int batch, int seq, int c, void* scratch, size_t scratch_bytes);
+/* dy bf16 [batch * seq, c]; dlast fp32 [batch, c] or NULL: the gradient of the last state.  dx, dg bf16 overwritten (0 behind len; dx may be dy or x, dg may be g, with the
+ * same stride); dh0 fp32 [batch, c] or NULL. */
+RP_API rp_status rp_op_scan_bwd(void* stream, int weight, const void* x, const void* g, const void* dy, void* dx, void* dg, long ldx, long ldg, long lddy,
+                         long lddx, long lddg, const unsigned char* first, const int* len, const float* states, const float* dlast, float* dh0, int batch,
+                         int seq, int c, void* scratch, size_t scratch_bytes);
+
+/* Embedding: x_t = scale E[ids_t].  table bf16 [V, h] (V < 2^20), ids [dev] int32 [T] (T < 2^24), x bf16 [T, h]; h a multiple of 8, at most 65536; row strides ld* in
+ * elements.  A token outside 0 .. V - 1 (padding) has the row 0. */
+RP_API rp_status rp_op_embed_fwd(void* stream, const void* table, long ldt, const int* ids, float scale, void* x, long ldx, int T, int V, int h);
+/* Its gradient: dtable fp32 [V, h] = (+= where accumulate) scale times the sums of dx's rows (bf16) over the tokens of every number, in ascending order of the tokens
+ * (the same bits every time).  Accumulating leaves the rows of other numbers alone; it may go on top of the head's gradient where the two share their weights.
+ * scratch [dev, scratch_bytes], rp_op_embed_scratch bytes; a call of its own each. */
+RP_API rp_status rp_op_embed_scratch(int T, int V, int h, size_t* scratch_bytes);
+RP_API rp_status rp_op_embed_bwd(void* stream, const void* dx, long lddx, const int* ids, float scale, float* dtable, long lddt, int accumulate, int T, int V,
+                          int h, void* scratch, size_t scratch_bytes);
+
+/* Dropout onto a residual: y = res + x / share where an element stays, res where it does not (res NULL: 0).  x, res, y bf16 [T, n], n a multiple of 8, row strides ld* in
+ * elements; y may be x or res with the same stride.  Element i = t n + column stays where 16 bits of a counter-based generator are below keep = round(65536 (1 - p)),
+ * 0 <= p <= 1; share = keep / 65536.  The bits: with words w[0..3] = Philox 4x32-10 of the counter {i / 8 (64 bits), offset + *step (64 bits)} under the key seed, element i has
+ * the low (even i) or high (odd) half of w[i % 8 / 2].  The mask is stored nowhere: the backward call is the same one with the gradient in x's place (and the one it adds to in
+ * res's).  step [dev] uint64 or NULL: read when the call runs, so that every replay of a captured call can have a mask of its own. */
+RP_API rp_status rp_op_dropout(void* stream, const void* x, long ldx, const void* res, long ldr, void* y, long ldy, int T, int n, float p,
+                        unsigned long long seed, unsigned long long offset, const unsigned long long* step);
+
 /* Per-kernel timeline of the stage calls on a ctx (measurement aid; the only calls that synchronise).
  * rp_trace_start: from now on every kernel a stage/head call enqueues is preceded by a timing event (at most
  * max_records ops are recorded).  rp_trace_stop: waits for the compute stream, writes up to cap records

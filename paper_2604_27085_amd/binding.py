@@ -15,6 +15,7 @@ IGNORE_INDEX = -100
 LORA_BITS = {"q": 1, "k": 2, "v": 4, "o": 8, "gate": 16, "up": 32, "down": 64}
 GEMM_NT, GEMM_NN, GEMM_TN = 0, 1, 2
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = range(4)
+SCAN_PLAIN, SCAN_MEAN, SCAN_ENERGY = range(3)
 PHASE_RECOMPUTE, PHASE_BACKWARD, PHASE_BOTH = 1, 2, 3
 
 TENSOR_IDS = ["G1", "WQKV", "GQ", "GK", "WO", "G2", "WGU", "WD", "WR", "LA_Q", "LA_K", "LA_V", "LB_Q", "LB_K", "LB_V",
@@ -129,6 +130,18 @@ _SIGS = {
                              _i, _i, _f, _vp, _sz],
     "rp_op_moe_balance_scratch": [_i, _i, _i, _psz],
     "rp_op_moe_balance": [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _f, _f, _f, _vp, _vp, _vp, _vp, _vp, _vp, _sz],
+    "rp_op_pack_plan": [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp],
+    "rp_op_span_attn_scratch": [_i, _i, _i, _i, _i, _i, _psz, _psz, _psz],
+    "rp_op_span_attn_fwd": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _l, _l, _l, _l, _vp, _vp, _vp, _f, _i, _i, _i, _i, _i, _i, _f, _vp, _sz],
+    "rp_op_span_attn_bwd": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _l, _l, _l, _l, _l, _l, _l, _l, _vp, _vp, _vp, _f, _i, _i, _i,
+                            _i, _i, _i, _f, _vp, _sz],
+    "rp_op_scan_sizes": [_i, _i, _i, _psz, _psz],
+    "rp_op_scan_fwd": [_vp, _i, _vp, _vp, _vp, _l, _l, _l, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _sz],
+    "rp_op_scan_bwd": [_vp, _i, _vp, _vp, _vp, _vp, _vp, _l, _l, _l, _l, _l, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _sz],
+    "rp_op_embed_scratch": [_i, _i, _i, _psz],
+    "rp_op_embed_fwd": [_vp, _vp, _l, _vp, _f, _vp, _l, _i, _i, _i],
+    "rp_op_embed_bwd": [_vp, _vp, _l, _vp, _f, _vp, _l, _i, _i, _i, _i, _vp, _sz],
+    "rp_op_dropout": [_vp, _vp, _l, _vp, _l, _vp, _l, _i, _i, _f, C.c_ulonglong, C.c_ulonglong, _vp],
 }
 EXPORTS = sorted(list(_SIGS) + ["rp_last_error"])
 for _name, _args in _SIGS.items():
@@ -443,3 +456,61 @@ def rp_op_moe_balance(stream, logits, idx, mask, T_, seq, E, top_k, coef, z_coef
                       scratch):
     _check(lib.rp_op_moe_balance(stream, _ptr(logits), _ptr(idx), _ptr(mask), T_, seq, E, top_k, coef, z_coef, grad_scale, _ptr(counts),
                                  _ptr(tokens), _ptr(loss), _ptr(dlogits_in), _ptr(dlogits), _ptr(scratch), _bytes(scratch)))
+
+
+def rp_op_pack_plan(stream, starts, prefix, n_docs, window, T_, seq, span=None, pos=None, first=None):
+    _check(lib.rp_op_pack_plan(stream, _ptr(starts), _ptr(prefix), n_docs, window, T_, seq, _ptr(span), _ptr(pos), _ptr(first)))
+
+
+def rp_op_span_attn_scratch(batch, seq_q, seq_kv, a, kh, d):
+    """Returns the bytes of scratch that the forward and the backward call make use of, and the least that the backward call needs."""
+    f, b, least = C.c_size_t(), C.c_size_t(), C.c_size_t()
+    _check(lib.rp_op_span_attn_scratch(batch, seq_q, seq_kv, a, kh, d, C.byref(f), C.byref(b), C.byref(least)))
+    return f.value, b.value, least.value
+
+
+def rp_op_span_attn_fwd(stream, q, k, v, o, o_rest, lse, ldq, ldk, ldv, ldo, span, q_pos, slopes, cap, batch, seq_q, seq_kv, a, kh, d, scale, scratch=None):
+    _check(lib.rp_op_span_attn_fwd(stream, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(o_rest), _ptr(lse), ldq, ldk, ldv, ldo, _ptr(span), _ptr(q_pos),
+                                   _ptr(slopes), cap, batch, seq_q, seq_kv, a, kh, d, scale, _ptr(scratch), _bytes(scratch)))
+
+
+def rp_op_span_attn_bwd(stream, q, k, v, o, o_rest, dout, lse, delta, dq, dk, dv, ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv, span, q_pos, slopes, cap,
+                        batch, seq_q, seq_kv, a, kh, d, scale, scratch):
+    _check(lib.rp_op_span_attn_bwd(stream, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(o_rest), _ptr(dout), _ptr(lse), _ptr(delta), _ptr(dq), _ptr(dk),
+                                   _ptr(dv), ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv, _ptr(span), _ptr(q_pos), _ptr(slopes), cap, batch, seq_q, seq_kv,
+                                   a, kh, d, scale, _ptr(scratch), _bytes(scratch)))
+
+
+def rp_op_scan_sizes(batch, seq, c):
+    """Returns the bytes of the states that the forward call leaves for the backward one, and of scratch."""
+    n, s = C.c_size_t(), C.c_size_t()
+    _check(lib.rp_op_scan_sizes(batch, seq, c, C.byref(n), C.byref(s)))
+    return n.value, s.value
+
+
+def rp_op_scan_fwd(stream, weight, x, g, y, ldx, ldg, ldy, first, len_, h0, last, states, batch, seq, c, scratch=None):
+    _check(lib.rp_op_scan_fwd(stream, weight, _ptr(x), _ptr(g), _ptr(y), ldx, ldg, ldy, _ptr(first), _ptr(len_), _ptr(h0), _ptr(last), _ptr(states), batch,
+                              seq, c, _ptr(scratch), _bytes(scratch)))
+
+
+def rp_op_scan_bwd(stream, weight, x, g, dy, dx, dg, ldx, ldg, lddy, lddx, lddg, first, len_, states, dlast, dh0, batch, seq, c, scratch=None):
+    _check(lib.rp_op_scan_bwd(stream, weight, _ptr(x), _ptr(g), _ptr(dy), _ptr(dx), _ptr(dg), ldx, ldg, lddy, lddx, lddg, _ptr(first), _ptr(len_),
+                              _ptr(states), _ptr(dlast), _ptr(dh0), batch, seq, c, _ptr(scratch), _bytes(scratch)))
+
+
+def rp_op_embed_scratch(T_, V, h):
+    n = C.c_size_t()
+    _check(lib.rp_op_embed_scratch(T_, V, h, C.byref(n)))
+    return n.value
+
+
+def rp_op_embed_fwd(stream, table, ldt, ids, scale, x, ldx, T_, V, h):
+    _check(lib.rp_op_embed_fwd(stream, _ptr(table), ldt, _ptr(ids), scale, _ptr(x), ldx, T_, V, h))
+
+
+def rp_op_embed_bwd(stream, dx, lddx, ids, scale, dtable, lddt, accumulate, T_, V, h, scratch=None):
+    _check(lib.rp_op_embed_bwd(stream, _ptr(dx), lddx, _ptr(ids), scale, _ptr(dtable), lddt, accumulate, T_, V, h, _ptr(scratch), _bytes(scratch)))
+
+
+def rp_op_dropout(stream, x, ldx, res, ldr, y, ldy, T_, n, p, seed, offset=0, step=None):
+    _check(lib.rp_op_dropout(stream, _ptr(x), ldx, _ptr(res), ldr, _ptr(y), ldy, T_, n, p, seed, offset, _ptr(step)))

@@ -1,0 +1,424 @@
+// Embedding: rows of a table by token, and the table's gradient.
+//
+//   x_t = scale E[id_t];   dE[v] (+)= scale sum over the tokens t with id_t = v, in ascending order, of dx_t
+//
+// A token whose number is outside 0 .. V - 1 (padding) has the row zero and adds nothing.
+//
+// The gradient sorts the tokens by their number (stably, so equal ones stay in order), cuts the sorted tokens into chunks of equal length and adds up runs of equal
+// numbers within them: however often a token comes, the work is spread evenly, and no sum depends on timing.  A run that goes on into the next chunk leaves its part in scratch; a second
+// kernel adds those up in order.  Sums are fp32.
+#include "pack_ops.hpp"
+
+namespace {
+
+constexpr int NT = 256;
+constexpr int SMALL = 1024;                 // tokens that one block sorts by comparing all pairs
+constexpr int BATCH = 1024;                 // tokens of a radix step
+constexpr int MOST_BLOCKS = 64;             // of the radix sort: each reads all blocks' counts
+constexpr int MOST_DIGITS = 1024;
+
+// ------------------------------------------------------------------------------------------------ rows
+// `lanes` threads take a row's 16-byte pieces; lanes is a power of two.
+__global__ void __launch_bounds__(NT) embed_rows_kernel(const bf16* table, long ldt, const int* ids, float scale, bf16* x, long ldx, int T, int V, int h8, int lanes) {
+  const int lane = threadIdx.x & (lanes - 1);
+  const long t = (long)blockIdx.x * (NT / lanes) + threadIdx.x / lanes;
+  if (t >= T) return;
+  const int id = ids[t];
+  const bool in = (unsigned)id < (unsigned)V;
+  const uint4* const src = reinterpret_cast<const uint4*>(table + (long)(in ? id : 0) * ldt);
+  uint4* const dst = reinterpret_cast<uint4*>(x + t * ldx);
+#pragma unroll 4
+  for (int c = lane; c < h8; c += lanes) {
+    const uint4 u = src[c];
+    uint4 y = make_uint4(pack_bf16x2(bf16_lo(u.x) * scale, bf16_hi(u.x) * scale), pack_bf16x2(bf16_lo(u.y) * scale, bf16_hi(u.y) * scale),
+                         pack_bf16x2(bf16_lo(u.z) * scale, bf16_hi(u.z) * scale), pack_bf16x2(bf16_lo(u.w) * scale, bf16_hi(u.w) * scale));
+    dst[c] = in ? y : make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ sorting
+RP_DEV uint32_t key_of(int id, int V) { return (unsigned)id < (unsigned)V ? (uint32_t)id : (uint32_t)V; }
+
+// Up to 1024 tokens, one block: a token's place is the number of those before it in the order, found by comparing it with all of them in LDS.  Also marks the
+// rows that have tokens, where the others are to be cleared.
+__global__ void __launch_bounds__(SMALL) embed_sort_small_kernel(const int* ids, int T, int V, uint2* sorted, uint32_t* marks) {
+  __shared__ uint32_t keys[SMALL];
+  const int i = threadIdx.x;
+  const uint32_t mine = i < T ? key_of(ids[i], V) : 0xffffffffu;
+  keys[i] = mine;
+  if (marks)
+    for (int w = i; w < (V + 31) / 32; w += SMALL) marks[w] = 0u;
+  __threadfence();      // the words are clear before a bit is set
+  __syncthreads();
+  if (i >= T) return;
+  if (marks && mine < (uint32_t)V) atomicOr(marks + (mine >> 5), 1u << (mine & 31));
+  int place = 0;
+#pragma unroll 8
+  for (int j = 0; j < (T + 3) / 4; ++j) {      // (behind T: the largest number, at higher places)
+    const uint4 u = *reinterpret_cast<const uint4*>(keys + 4 * j);
+    place += (u.x < mine || (u.x == mine && 4 * j < i)) + (u.y < mine || (u.y == mine && 4 * j + 1 < i)) + (u.z < mine || (u.z == mine && 4 * j + 2 < i)) +
+             (u.w < mine || (u.w == mine && 4 * j + 3 < i));
+  }
+  sorted[place] = make_uint2(mine, (uint32_t)i);
+}
+
+// More: radix sort by two digits (one where one is enough).  Every block has a run of `run` tokens; counts[digit pass][block][digit].
+struct SortArgs {
+  const int* ids;
+  uint2 *from, *to;                // {key, token}; the first pass reads ids
+  int* counts;                     // [2][blocks][digits]
+  uint32_t* marks;                 // [ceil(V / 32)] or NULL
+  int T, V, run, blocks, shift, bits, pass, passes;
+};
+
+__global__ void __launch_bounds__(NT) embed_count_kernel(const SortArgs p) {
+  __shared__ int hist[MOST_DIGITS];
+  const int digits = 1 << p.bits, tid = threadIdx.x;
+  for (int d = tid; d < digits; d += NT) hist[d] = 0;
+  __syncthreads();
+  const long first = (long)blockIdx.x * p.run, last = min(first + p.run, (long)p.T);
+  for (long i = first + tid; i < last; i += NT) atomicAdd(hist + (key_of(p.ids[i], p.V) & (digits - 1)), 1);
+  __syncthreads();
+  int* const mine = p.counts + (long)blockIdx.x * digits;
+  for (int d = tid; d < digits; d += NT) {
+    mine[d] = hist[d];
+    if (p.passes > 1) mine[(long)p.blocks * digits + d] = 0;      // the second pass's, which the first adds up
+  }
+  if (p.marks)
+    for (int w = blockIdx.x * NT + tid; w < (p.V + 31) / 32; w += p.blocks * NT) p.marks[w] = 0u;
+}
+
+__global__ void __launch_bounds__(NT) embed_scatter_kernel(const SortArgs p) {
+  __shared__ int base[MOST_DIGITS];            // where the block's next token of a digit goes
+  __shared__ int count[NT / 64][MOST_DIGITS];  // a wave's, then where its first goes
+  __shared__ int wave_total[NT / 64];
+  const int digits = 1 << p.bits, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int* const counts = p.counts + (long)p.pass * p.blocks * digits;
+  // places before a digit: all smaller digits, and this one in the blocks before
+  int before_chunk = 0;
+  for (int d0 = 0; d0 < digits; d0 += NT) {
+    const int d = d0 + tid;
+    int total = 0, before = 0;
+    if (d < digits) {
+#pragma unroll 8
+      for (int b = 0; b < p.blocks; ++b) {
+        const int n = counts[(long)b * digits + d];
+        before += b < (int)blockIdx.x ? n : 0;
+        total += n;
+      }
+    }
+    int sum = total;      // inclusive over the wave
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int n = __shfl_up(sum, o, 64);
+      if (lane >= o) sum += n;
+    }
+    if (lane == 63) wave_total[w] = sum;
+    __syncthreads();
+    int smaller = before_chunk;
+    for (int u = 0; u < NT / 64; ++u) {
+      if (u < w) smaller += wave_total[u];
+      before_chunk += wave_total[u];
+    }
+    if (d < digits) base[d] = smaller + sum - total + before;
+    __syncthreads();
+  }
+  const long first = (long)blockIdx.x * p.run, last = min(first + p.run, (long)p.T);
+  for (long i0 = first; i0 < last; i0 += BATCH) {
+    for (int d = tid; d < digits; d += NT)
+#pragma unroll
+      for (int u = 0; u < NT / 64; ++u) count[u][d] = 0;
+    __syncthreads();
+    uint32_t key[4], tok[4];
+    int digit[4], rank[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const long i = i0 + 256 * w + 64 * j + lane;
+      const bool in = i < last;
+      key[j] = tok[j] = 0u;
+      if (in) {
+        if (p.pass == 0) {
+          key[j] = key_of(p.ids[i], p.V);
+          tok[j] = (uint32_t)i;
+        } else {
+          const uint2 e = p.from[i];
+          key[j] = e.x;
+          tok[j] = e.y;
+        }
+      }
+      digit[j] = (int)(key[j] >> p.shift) & (digits - 1);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool in = i0 + 256 * w + 64 * j + lane < last;
+      unsigned long long same = __ballot(in);      // the lanes with this one's digit
+      for (int b = 0; b < p.bits; ++b) {
+        const unsigned long long set = __ballot((digit[j] >> b) & 1);
+        same &= (digit[j] >> b) & 1 ? set : ~set;
+      }
+      const int ahead = __popcll(same & ((1ull << lane) - 1ull));
+      // all lanes read before the first one of each digit adds (LDS works in order for a wave, so the fences are for the compiler)
+      rank[j] = count[w][digit[j]] + ahead;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      if (in && ahead == 0) count[w][digit[j]] += __popcll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    for (int d = tid; d < digits; d += NT) {
+      int at = base[d];
+#pragma unroll
+      for (int u = 0; u < NT / 64; ++u) {
+        const int n = count[u][d];
+        count[u][d] = at;
+        at += n;
+      }
+      base[d] = at;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i0 + 256 * w + 64 * j + lane < last) {
+        const int at = count[w][digit[j]] + rank[j];
+        p.to[at] = make_uint2(key[j], tok[j]);
+        if (p.pass == 0) {
+          if (p.passes > 1) atomicAdd(p.counts + ((long)p.blocks + at / p.run) * digits + ((key[j] >> p.bits) & (digits - 1)), 1);
+          if (p.marks && key[j] < (uint32_t)p.V) atomicOr(p.marks + (key[j] >> 5), 1u << (key[j] & 31));
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Zeros for the rows without tokens, 16 bytes a thread and step.
+__global__ void __launch_bounds__(NT) embed_clear_kernel(const EmbedGrad p, const uint32_t* marks) {
+  const int h4 = p.h / 4;
+  for (int v = blockIdx.x; v < p.V; v += gridDim.x) {
+    if (marks[v >> 5] >> (v & 31) & 1u) continue;
+    float4* const row = reinterpret_cast<float4*>(p.dtable + (long)v * p.ldt);
+    for (int c = threadIdx.x; c < h4; c += NT) row[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ sums
+struct SumArgs {
+  EmbedGrad g;
+  const uint2* sorted;
+  float* part;      // [2][chunks][h]: a chunk's run that began before it, and its run that goes on behind it
+  int chunk, chunks, slices, width, lanes;      // width: 8-element pieces of a slice
+};
+
+struct Sum8 {
+  float v[8];
+  RP_DEV void clear() {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+  }
+  RP_DEV void add(const uint4& u) {
+    v[0] += bf16_lo(u.x); v[1] += bf16_hi(u.x); v[2] += bf16_lo(u.y); v[3] += bf16_hi(u.y);
+    v[4] += bf16_lo(u.z); v[5] += bf16_hi(u.z); v[6] += bf16_lo(u.w); v[7] += bf16_hi(u.w);
+  }
+  RP_DEV void add(const float* src) {
+    const float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
+    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+  }
+  RP_DEV void store(float* dst) const {
+    *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(dst + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  // to the table
+  RP_DEV void finish(const EmbedGrad& p, uint32_t key, int col) const {
+    float* const row = p.dtable + (long)key * p.ldt + col;
+    Sum8 r;
+    r.clear();
+    if (p.accumulate) r.add(row);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.v[e] += p.scale * v[e];
+    r.store(row);
+  }
+};
+
+// `lanes` threads take a chunk of the sorted tokens and a slice of the columns.  The rows of eight tokens are on their way at a time.
+__global__ void __launch_bounds__(NT) embed_sum_kernel(const SumArgs p) {
+  constexpr int AHEAD = 8;
+  const int lane = threadIdx.x & (p.lanes - 1);
+  const long unit = (long)blockIdx.x * (NT / p.lanes) + threadIdx.x / p.lanes;
+  const int chunk = (int)(unit / p.slices), slice = (int)(unit - (long)chunk * p.slices);
+  const int piece = slice * p.width + lane, col = 8 * piece;
+  if (chunk >= p.chunks || lane >= p.width || col >= p.g.h) return;
+  const int first = chunk * p.chunk, last = min(first + p.chunk, p.g.T);
+  const uint32_t none = (uint32_t)p.g.V;
+  const uint32_t prev = first > 0 ? p.sorted[first - 1].x : 0xffffffffu, next = last < p.g.T ? p.sorted[last].x : 0xffffffffu;
+  Sum8 sum;
+  sum.clear();
+  uint32_t now = p.sorted[first].x;
+  bool began = now != prev;      // the present run began in this chunk
+  for (int i0 = first; i0 < last; i0 += AHEAD) {
+    uint4 row[AHEAD];
+    uint32_t key[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const uint2 e = p.sorted[min(i0 + j, last - 1)];
+      key[j] = i0 + j < last ? e.x : none;
+      row[j] = make_uint4(0u, 0u, 0u, 0u);
+      if (key[j] != none) row[j] = *reinterpret_cast<const uint4*>(p.g.dx + (long)e.y * p.g.lddx + col);
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (i0 + j >= last) break;
+      if (key[j] != now) {
+        if (now != none) {
+          if (began) sum.finish(p.g, now, col);
+          else sum.store(p.part + (long)chunk * p.g.h + col);
+        }
+        sum.clear();
+        now = key[j];
+        began = true;
+      }
+      sum.add(row[j]);
+    }
+  }
+  if (now == none) return;
+  if (!began) sum.store(p.part + (long)chunk * p.g.h + col);                              // also a run through the whole chunk
+  else if (now == next) sum.store(p.part + ((long)p.chunks + chunk) * p.g.h + col);
+  else sum.finish(p.g, now, col);
+}
+
+// The runs over several chunks, at the chunk that they begin in: its last part and the first ones of the chunks behind it.  32 threads take 256 columns,
+// eight such groups every eighth part.
+__global__ void __launch_bounds__(NT) embed_join_kernel(const SumArgs p) {
+  __shared__ float red[8][256];
+  __shared__ int parts;
+  const int slices = (p.g.h + 255) / 256;
+  const int chunk = (int)(blockIdx.x / slices), slice = (int)(blockIdx.x - (unsigned)chunk * slices);
+  const int first = chunk * p.chunk, last = first + p.chunk;      // (the last chunk of all has no block)
+  const uint32_t v = p.sorted[last - 1].x;
+  if (v != p.sorted[last].x || v == (uint32_t)p.g.V) return;                                          // no run goes on
+  if (first > 0 && p.sorted[first - 1].x == v && p.sorted[first].x == v) return;                      // it began earlier
+  const int tid = threadIdx.x;
+  if (tid < 64) {      // chunks behind that begin with it
+    int n = 0;
+    for (;;) {
+      const long at = last + (long)(n + tid) * p.chunk;
+      const bool more = at < p.g.T && p.sorted[at].x == v;
+      const unsigned long long m = __ballot(more);
+      if (~m) {
+        n += __builtin_ctzll(~m);
+        break;
+      }
+      n += 64;
+    }
+    if (tid == 0) parts = n;
+  }
+  __syncthreads();
+  const int grp = tid >> 5, lane = tid & 31, col = slice * 256 + 8 * lane;
+  const bool in = col < p.g.h;
+  Sum8 sum;
+  sum.clear();
+  if (in) {
+    if (grp == 0) sum.add(p.part + ((long)p.chunks + chunk) * p.g.h + col);
+#pragma unroll 4
+    for (int i = grp; i < parts; i += 8) sum.add(p.part + (long)(chunk + 1 + i) * p.g.h + col);
+  }
+  sum.store(&red[grp][8 * lane]);
+  __syncthreads();
+  if (grp || !in) return;
+#pragma unroll
+  for (int u = 1; u < 8; ++u) sum.add(&red[u][8 * lane]);
+  sum.finish(p.g, v, col);
+}
+
+int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
+size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
+
+// Digits: the numbers 0 .. V in one pass of up to 10 bits, or in two.
+struct SortPlan {
+  int bits, passes, blocks, run;
+  SortPlan(int T, int V) {
+    int all = 1;
+    while ((1l << all) <= V) ++all;
+    passes = all > 10 ? 2 : 1;
+    bits = (all + passes - 1) / passes;
+    blocks = ceil_div(T, BATCH);
+    if (blocks > MOST_BLOCKS) blocks = MOST_BLOCKS;
+    if (blocks < 1) blocks = 1;
+    run = ceil_div(ceil_div(T, blocks), BATCH) * BATCH;
+    blocks = T ? ceil_div(T, run) : 1;
+  }
+};
+// Sorted tokens that a group of threads adds up.
+int chunk_length(int T) { return T >= 8192 ? 32 : T >= 2048 ? 16 : 8; }
+
+struct Places {      // of the scratch memory
+  size_t sorted, other, counts, marks, part, end;
+  Places(int T, int V, int h) {
+    const SortPlan s(T, V);
+    sorted = 0;
+    other = round16((size_t)T * 8);
+    counts = other + (T > SMALL && s.passes > 1 ? round16((size_t)T * 8) : 0);
+    marks = counts + (T > SMALL ? (size_t)2 * s.blocks * (4 << s.bits) : 0);
+    part = marks + round16((size_t)((V + 31) / 32) * 4);
+    end = part + (size_t)2 * ceil_div(T, chunk_length(T)) * h * 4;
+  }
+};
+
+}  // namespace
+
+hipError_t k_embed_fwd(hipStream_t st, const bf16* table, long ldt, const int* ids, float scale, bf16* x, long ldx, int T, int V, int h) {
+  if (T == 0 || h == 0) return hipSuccess;
+  int lanes = 1;
+  while (lanes < NT && lanes < h / 8) lanes <<= 1;
+  RP_LAUNCH(embed_rows_kernel, dim3(ceil_div(T, NT / lanes)), dim3(NT), 0, st, table, ldt, ids, scale, x, ldx, T, V, h / 8, lanes);
+  return hipGetLastError();
+}
+
+size_t k_embed_scratch(int T, int V, int h) { return Places(T, V, h).end; }
+
+hipError_t k_embed_bwd(hipStream_t st, const EmbedGrad& g, void* scratch) {
+  if (g.h == 0 || g.V == 0 || (g.T == 0 && g.accumulate)) return hipSuccess;
+  hipError_t e = hipSuccess;
+  const int clear_blocks = g.V < 4096 ? g.V : 4096;
+  char* const mem = static_cast<char*>(scratch);
+  const Places at(g.T, g.V, g.h);
+  const SortPlan s(g.T, g.V);
+  uint32_t* const marks = g.accumulate ? nullptr : reinterpret_cast<uint32_t*>(mem + at.marks);
+  uint2* const sorted = reinterpret_cast<uint2*>(mem + at.sorted);
+  if (g.T <= SMALL) {
+    RP_LAUNCH(embed_sort_small_kernel, dim3(1), dim3(SMALL), 0, st, g.ids, g.T, g.V, sorted, marks);
+    e = hipGetLastError();
+  } else {
+    uint2* const other = reinterpret_cast<uint2*>(mem + at.other);
+    SortArgs a{g.ids, nullptr, s.passes > 1 ? other : sorted, reinterpret_cast<int*>(mem + at.counts), marks, g.T, g.V, s.run, s.blocks, 0, s.bits, 0, s.passes};
+    RP_LAUNCH(embed_count_kernel, dim3(s.blocks), dim3(NT), 0, st, a);
+    e = hipGetLastError();
+    for (int pass = 0; pass < s.passes && e == hipSuccess; ++pass) {
+      a.pass = pass;
+      a.shift = pass * s.bits;
+      if (pass == 1) { a.from = other; a.to = sorted; }
+      RP_LAUNCH(embed_scatter_kernel, dim3(s.blocks), dim3(NT), 0, st, a);
+      e = hipGetLastError();
+    }
+  }
+  if (e == hipSuccess && marks) {
+    RP_LAUNCH(embed_clear_kernel, dim3(clear_blocks), dim3(NT), 0, st, g, marks);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || g.T == 0) return e;
+  SumArgs a{};
+  a.g = g;
+  a.sorted = sorted;
+  a.part = reinterpret_cast<float*>(mem + at.part);
+  a.chunk = chunk_length(g.T);
+  a.chunks = ceil_div(g.T, a.chunk);
+  a.slices = ceil_div(g.h / 8, NT);
+  a.width = ceil_div(g.h / 8, a.slices);
+  a.lanes = 1;
+  while (a.lanes < a.width) a.lanes <<= 1;
+  RP_LAUNCH(embed_sum_kernel, dim3(ceil_div((long)a.chunks * a.slices, NT / a.lanes)), dim3(NT), 0, st, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || a.chunks < 2) return e;
+  RP_LAUNCH(embed_join_kernel, dim3((unsigned)(a.chunks - 1) * ((g.h + 255) / 256)), dim3(NT), 0, st, a);
+  return hipGetLastError();
+}

@@ -1,0 +1,1266 @@
+// Attention in which every query sees a span of the keys, lo_t <= j < hi_t: documents of a packed row, windows, prefixes, padding, caches of different lengths.
+//
+//   z = scale q k^T;  c = cap tanh(z / cap) (or z);  S = c - slope |p_t - j| (or c);  lse = log sum exp S;  P = exp(S - lse);  o = P v
+//   dV = P^T dO;  dP = dO V^T;  delta = rowsum(P dP) = rowsum(dO o);  dS = P (dP - delta) (1 - (c / cap)^2);  dQ = scale dS K;  dK = scale dS^T Q
+//
+// The span belongs to the query, so the query heads of a key head's group share it: row r of a key head is query r / grp of head r % grp, and a tile of 128 rows holds 128 / grp
+// neighbouring queries with all their heads.  Their spans nearly agree: the keys that a tile needs are those that any of its queries sees, tiles of keys that every
+// query sees take no mask, and dK, dV of a group need no partials per head.
+//
+//   forward, dQ: workgroup = four waves x 32 rows, loop over the 64-key tiles that any row sees, the last rows first (causal rows at the end see most)
+//   dK, dV     : workgroup = 128 keys, loop over the 64-row tiles that see any of them (d = 128: eight waves, pairs of which share 32 keys; d = 64: four); what each row
+//                tile sees in all is left behind by dQ, which runs before
+// Where there are too few workgroups for the chip, the loop is cut into `splits` slices, whose results another kernel joins in slice order (fp32 partials in the caller's
+// scratch; no atomics, so the result does not depend on timing).
+//
+// In a tile that some rows do not see, scores are replaced, and what the products sum over (V; K of dQ; Q and dO) has its infinities and NaN taken out, since 0 times those would
+// reach the rows beside them: a document is not touched by what is in another.  (Forward: a row that does see such a value of v becomes NaN as a whole.  Backward: lse and
+// delta of such rows are NaN by then.)
+//
+// P (for P v and dV) and dS are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most); scores, statistics, dP - delta and every sum are
+// fp32.  The forward divides by the sum of the rounded P: what all terms of a row were rounded by alike drops out, and where a row lies on one key o is that key's v.  o goes out in two
+// parts, its bf16 and that of what the rounding left over, so that delta = dO.(o + rest) does not carry o's rounding, which would be as large as dP - delta in such rows.
+#include <type_traits>
+
+#include "attention_slices.hpp"
+#include "pack_ops.hpp"
+
+namespace {
+
+// operand tiles, or the epilogue's staging of every wave's 32 x d block, whichever is larger
+constexpr int fwd_tile_bytes(int d) { return max_i(64 * (d + 8) + 64 * (d + 32), 128 * (d + 8)) * 2; }
+constexpr int dq_tile_bytes(int d) { return max_i(2 * 64 * tile_ld(d), 128 * (d + 8)) * 2; }
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+// Sizes of one sequence and key head.
+struct Rows {
+  int b, g, grp, total, seq_q;
+  unsigned inv;      // 2^32 / grp, rounded up
+  RP_DEV Rows(const SpanArgs& p, int hb) {
+    b = hb / p.kh;
+    g = hb - b * p.kh;
+    grp = p.a / p.kh;
+    seq_q = p.seq_q;
+    total = grp * seq_q;
+    inv = grp > 1 ? 0xffffffffu / (unsigned)grp + 1u : 0u;
+  }
+  // query and head within the group of row r: r inv / 2^32 is at most one too large
+  RP_DEV void at(int r, int& q, int& h) const {
+    q = grp > 1 ? (int)__umulhi((unsigned)r, inv) : r;
+    h = r - q * grp;
+    if (h < 0) { --q; h += grp; }
+  }
+  // offset of row r in a [T, heads, d] tensor of row stride ld, from its first element
+  RP_DEV long offset(int r, long ld, int d) const {
+    int q, h;
+    at(r, q, h);
+    return ((long)b * seq_q + q) * ld + (long)(g * grp + h) * d;
+  }
+  RP_DEV long stat(int r, int a) const {   // in a [batch, a, seq_q] array
+    int q, h;
+    at(r, q, h);
+    return ((long)b * a + g * grp + h) * seq_q + q;
+  }
+};
+
+// What a row sees; nothing: 0, 0.  Rows behind the last one see nothing either.
+RP_DEV int2 span_of(const SpanArgs& p, const Rows& s, int r) {
+  if (r >= s.total) return make_int2(0, 0);
+  int q, h;
+  s.at(r, q, h);
+  const int2 v = p.span[(long)s.b * p.seq_q + q];
+  const int lo = max(v.x, 0), hi = min(v.y, p.seq_kv);
+  return hi > lo ? make_int2(lo, hi) : make_int2(0, 0);
+}
+
+// Of several rows: the keys that any of them sees, [lo, hi), and those that all of them see, [all_lo, all_hi).
+struct Seen {
+  int lo, hi, all_lo, all_hi;
+  RP_DEV void start(const int2& v, bool row) {
+    lo = v.y > v.x ? v.x : 0x7fffffff;
+    hi = v.y;
+    all_lo = row ? v.x : 0;
+    all_hi = row ? v.y : 0x7fffffff;
+  }
+  RP_DEV void add(int a, int b, int c, int d) {
+    lo = min(lo, a);
+    hi = max(hi, b);
+    all_lo = max(all_lo, c);
+    all_hi = min(all_hi, d);
+  }
+  // over the lanes l ^ from, l ^ 2 from, .. below `to`; then the same in all lanes
+  RP_DEV void lanes(int from, int to) {
+    for (int o = from; o < to; o <<= 1) add(__shfl_xor(lo, o, 64), __shfl_xor(hi, o, 64), __shfl_xor(all_lo, o, 64), __shfl_xor(all_hi, o, 64));
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+  }
+  RP_DEV bool any(int k0, int k1) const { return k0 < hi && k1 > lo; }
+  RP_DEV bool all(int k0, int k1) const { return all_lo <= k0 && all_hi >= k1; }
+};
+// The four waves' rows together, through LDS [4]; all threads.
+RP_DEV Seen seen_by_all(const Seen& mine, int4* lds, int w, int lane) {
+  if (lane == 0) lds[w] = make_int4(mine.lo, mine.hi, mine.all_lo, mine.all_hi);
+  __syncthreads();
+  Seen s = mine;
+  for (int u = 0; u < 4; ++u) {
+    const int4 v = lds[u];
+    s.add(v.x, v.y, v.z, v.w);
+  }
+  s.lanes(64, 64);
+  return s;
+}
+
+// Scores as exponents of two: k1 z' for plain ones, z' = q.k; capped ones from e = 2^(k1 z') = exp(2 z / cap): tanh = 1 - 2 r, r = 1 / (1 + e).
+struct Score {
+  float k1, k2;      // plain: scale log2(e);  capped: 2 scale log2(e) / cap, cap log2(e)
+  RP_DEV explicit Score(const SpanArgs& p) {
+    k1 = p.cap > 0.f ? 2.f * p.scale * LOG2E / p.cap : p.scale * LOG2E;
+    k2 = p.cap * LOG2E;
+  }
+};
+// (absolute error cap 2^-23 or so, from 1 + e)
+RP_DEV float cap_r(float z, const Score& c) { return __builtin_amdgcn_rcpf(1.f + fast_exp2(z * c.k1)); }
+template <bool CAP>
+RP_DEV float score2(float z, const Score& c) { return CAP ? __builtin_fmaf(-2.f * c.k2, cap_r(z, c), c.k2) : z * c.k1; }
+
+// 16 bytes with infinities and NaN made zero; `bad` where there was one.
+RP_DEV uint32_t finite2(uint32_t u, bool& bad) {
+  const bool lo = (u & 0x7f80u) == 0x7f80u, hi = (u & 0x7f800000u) == 0x7f800000u;
+  bad = bad || lo || hi;
+  return (lo ? 0u : u & 0xffffu) | (hi ? 0u : u & 0xffff0000u);
+}
+RP_DEV uint4 finite8(const uint4& u, bool& bad) { return make_uint4(finite2(u.x, bad), finite2(u.y, bad), finite2(u.z, bad), finite2(u.w, bad)); }
+template <int N>
+RP_DEV void make_finite(uint4 (&r)[N]) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = finite8(r[i], bad);
+}
+
+RP_DEV float sum2(uint32_t pair, float acc) {      // the two bf16 of a register, added up in fp32
+  typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2, pair), __builtin_bit_cast(v2, 0x3f803f80u), acc, false);
+}
+
+constexpr float FLOOR = -1.0e37f;      // the reference exponent of rows that have seen nothing yet: finite, so that exp2(-inf - FLOOR) = 0
+
+// ================================================================================================ forward
+template <int D, bool SPLIT, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256, 2) span_fwd_kernel(const SpanArgs p) {
+  constexpr int LDK = D + 8, LDV = D + 32, KS = D / 16, DT = D / 32, NT = 256, BQ = 128, CH = D / 8;
+  using T64 = Tile64<D, NT>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // fwd_smem_bytes(D)
+  bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);
+  bf16* const Ks = smem;
+  bf16* const Vs = smem + 64 * LDK;
+  int4* const seen_lds = reinterpret_cast<int4*>(dyn_smem + fwd_tile_bytes(D));       // [4]
+  unsigned* const bad_keys = reinterpret_cast<unsigned*>(seen_lds + 4);               // [2 tiles][2]: a bit a key
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, lk = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nhb = p.kh * p.batch;
+  const int rest = (int)blockIdx.x / nhb;
+  const int hb = head_at((int)blockIdx.x, rest, nhb);
+  const int split = SPLIT ? rest % p.splits : 0;
+  const Rows s(p, hb);
+  const int blocks = (s.total + BQ - 1) / BQ;
+  const int r0 = (blocks - 1 - (SPLIT ? rest / p.splits : rest)) * BQ;
+  const Score sc(p);
+
+  const int row = r0 + 32 * w + lr;     // the lane's row
+  const bool live = row < s.total;
+  const int2 span = span_of(p, s, row);
+  Seen mine;
+  mine.start(span, live);
+  mine.lanes(1, 32);
+  if (tid < 4) bad_keys[tid] = 0u;
+  const Seen block = seen_by_all(mine, seen_lds, w, lane);
+  int j0 = 0, j1 = 0;
+  if (block.hi > block.lo) {
+    j0 = block.lo / 64;
+    j1 = (block.hi + 63) / 64;
+  }
+  if (SPLIT) {
+    int first, last;
+    slice_of(j1 - j0, p.splits, split, first, last);
+    j1 = j0 + last;
+    j0 += first;
+  }
+  const KeyTile<D, NT> kt_(p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D, p.ldk, p.seq_kv), vt_(p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D, p.ldv, p.seq_kv);
+
+  uint4 qf[KS];
+  float slope2 = 0.f;
+  int pos = 0;
+  {
+    int q, h;
+    s.at(live ? row : 0, q, h);
+    const bf16* const qr = p.q + ((long)s.b * p.seq_q + q) * p.ldq + (long)(s.g * s.grp + h) * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (live) qf[ks] = *reinterpret_cast<const uint4*>(qr + 16 * ks + 8 * lk);
+    }
+    if (BIAS && live) {
+      slope2 = p.slopes[s.g * s.grp + h] * LOG2E;
+      pos = p.q_pos ? p.q_pos[(long)s.b * p.seq_q + q] : q + p.seq_kv - p.seq_q;
+    }
+  }
+
+  float m_run = FLOOR, l_run = 0.f, lt_run = 0.f;      // lt: the sum of the rounded P
+  f32x16 oacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) oacc[dt][v] = 0.f;
+
+  const bf16* const kfrag = Ks + lr * LDK + 8 * lk;
+  const bf16* const vfrag = Vs + tr_base32<LDV>(lane);
+  uint4 kreg[T64::NREG], vreg[T64::NREG];
+  auto load_tiles = [&](int j) {
+    kt_.load(kreg, j * 64, tid);
+    vt_.load(vreg, j * 64, tid);
+  };
+  if (j0 < j1) load_tiles(j0);
+  for (int j = j0; j < j1; ++j) {
+    const int kv0 = j * 64;
+    const bool whole = block.all(kv0, kv0 + 64);      // uniform over the workgroup
+    __syncthreads();
+    if (!whole) {
+#pragma unroll
+      for (int it = 0; it < T64::NREG; ++it) {
+        bool bad = false;
+        vreg[it] = finite8(vreg[it], bad);
+        const int key = (it * NT + tid) / CH;
+        if (bad) atomicOr(bad_keys + 2 * (j & 1) + (key >> 5), 1u << (key & 31));
+      }
+    }
+    T64::template store<LDK>(kreg, Ks, tid);
+    T64::template store<LDV>(vreg, Vs, tid);
+    __syncthreads();
+    if (j + 1 < j1) load_tiles(j + 1);
+    if (tid < 2) bad_keys[2 * ((j + 1) & 1) + tid] = 0u;      // (last read before the barriers above, next written behind the next one)
+    if (!mine.any(kv0, kv0 + 64)) continue;                   // uniform over the wave
+    f32x16 sT[2];
+    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    constexpr int AHEAD = 3;      // LDS fragments are requested that many products early
+    {
+      constexpr int NS = 2 * KS;
+      auto sfrag_at = [&](int n) { return *reinterpret_cast<const uint4*>(kfrag + 32 * (n & 1) * LDK + 16 * (n >> 1)); };
+      uint4 ring[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) ring[n] = sfrag_at(n);
+      MFMA_PHASE_BEGIN();
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        const uint4 a = ring[n % AHEAD];
+        if (n + AHEAD < NS) ring[n % AHEAD] = sfrag_at(n + AHEAD);
+        sT[n & 1] = mfma32(a, qf[n >> 1], n < 2 ? zero16 : sT[n & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      MFMA_PHASE_END();
+    }
+    constexpr int NU = 4 * DT;
+    auto ufrag_at = [&](int n) { return read_frag_tr32<LDV>(vfrag, n / DT, 32 * (n % DT)); };
+    uint4 uring[AHEAD];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (CAP) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sT[kt][v] = score2<true>(sT[kt][v], sc);
+    }
+    if constexpr (BIAS) {
+      const float from = (float)(pos - (kv0 + 4 * lk));
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          sT[kt][v] = __builtin_fmaf(-slope2, fabsf(from - (float)(32 * kt + 8 * (v >> 2) + (v & 3))), CAP ? sT[kt][v] : sT[kt][v] * sc.k1);
+    }
+    constexpr bool DONE = CAP || BIAS;      // scores are exponents already
+    if (!whole) {
+      const int lo = span.x - (kv0 + 4 * lk);
+      const unsigned n = (unsigned)(span.y - span.x);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sT[kt][v] = (unsigned)(32 * kt + 8 * (v >> 2) + (v & 3) - lo) < n ? sT[kt][v] : -INFINITY;
+      const unsigned b0 = __builtin_amdgcn_readfirstlane(bad_keys[2 * (j & 1)]), b1 = __builtin_amdgcn_readfirstlane(bad_keys[2 * (j & 1) + 1]);
+      if (b0 | b1) {      // does the row see one of the keys whose v was not finite?
+        const unsigned long long bad = b0 | (unsigned long long)b1 << 32;
+        const int from = max(span.x - kv0, 0), to = min(span.y - kv0, 64);
+        if (to > from && (bad >> from & (to - from == 64 ? ~0ull : (1ull << (to - from)) - 1ull))) lt_run = NAN;
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sT[kt][v]);
+    mx = DONE ? half_max(mx) : half_max(mx) * sc.k1;
+    // m_run is a reference exponent that moves only when a row's maximum outgrows it by 2^8 (see attention.hip)
+    const bool grow = mx > m_run + 8.f;
+    if (__builtin_amdgcn_ballot_w64(grow) != 0ull) {
+      const float m_new = grow ? mx : m_run;
+      float alpha = fast_exp2(m_run - m_new);
+      asm volatile("" : "+v"(alpha));
+      l_run *= alpha;
+      lt_run *= alpha;
+      m_run = m_new;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
+    }
+    float psum = 0.f;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float e = fast_exp2(DONE ? sT[kt][v] - m_run : __builtin_fmaf(sT[kt][v], sc.k1, -m_run));
+        sT[kt][v] = e;
+        psum += e;
+      }
+    l_run += psum;
+    {
+      uint4 pf[4];
+      float rsum = 0.f;
+#pragma unroll
+      for (int gk = 0; gk < 4; ++gk) {
+        pf[gk] = pack_frag32(sT[gk >> 1], 8 * (gk & 1));
+        rsum = sum2(pf[gk].x, sum2(pf[gk].y, sum2(pf[gk].z, sum2(pf[gk].w, rsum))));
+      }
+      lt_run += rsum;
+      MFMA_PHASE_BEGIN();
+#pragma unroll
+      for (int n = 0; n < NU; ++n) {
+        const uint4 a = uring[n % AHEAD];
+        if (n + AHEAD < NU) uring[n % AHEAD] = ufrag_at(n + AHEAD);
+        oacc[n % DT] = mfma32(a, pf[n / DT], oacc[n % DT]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      MFMA_PHASE_END();
+    }
+  }
+
+  const float l_tot = l_run + __shfl_xor(l_run, 32, 64), lt_tot = lt_run + __shfl_xor(lt_run, 32, 64);
+  if constexpr (SPLIT) {
+    const long at = ((long)split * nhb + hb) * s.total + row;
+    if (live) {
+      if (lk == 0) p.part_ml[at] = make_float4(m_run, l_tot, lt_tot, 0.f);
+      if (j0 < j1)      // (of a slice without keys the sum is 0, and its part is not read)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int vg = 0; vg < 4; ++vg)
+            *reinterpret_cast<float4*>(p.part + at * D + 32 * dt + 8 * vg + 4 * lk) =
+                make_float4(oacc[dt][4 * vg], oacc[dt][4 * vg + 1], oacc[dt][4 * vg + 2], oacc[dt][4 * vg + 3]);
+    }
+  } else {
+    const bool some = live && span.y > span.x;      // a row that sees nothing: o = 0, lse = -inf
+    const float mul = some ? 1.f / lt_tot : 0.f;
+    if (p.lse && lk == 0 && live) p.lse[s.stat(row, p.a)] = some ? m_run * 0.6931471805599453f + logf(l_tot) : -INFINITY;
+    bf16* const stage = smem + w * 32 * LDK;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {      // o, then what its rounding left over
+      bf16* const dst = part ? p.rest : p.o;
+      if (!dst) continue;
+      __syncthreads();
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int vg = 0; vg < 4; ++vg) {
+          float y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            y[e] = some ? oacc[dt][4 * vg + e] * mul : 0.f;
+            if (part) y[e] -= (float)(bf16)y[e];
+          }
+          *reinterpret_cast<uint2*>(stage + lr * LDK + 32 * dt + 8 * vg + 4 * lk) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+        }
+      __syncthreads();
+#pragma unroll
+      for (int it = 0; it < (32 * CH) / 64; ++it) {
+        const int idx = it * 64 + lane, rr = idx / CH, ch = idx % CH, r = r0 + 32 * w + rr;
+        if (r < s.total) *reinterpret_cast<uint4*>(dst + s.offset(r, p.ldo, D) + ch * 8) = *reinterpret_cast<const uint4*>(stage + rr * LDK + ch * 8);
+      }
+    }
+  }
+}
+
+// Rows of the forward (weights exp2(m_i - max m)) or, with DQ, of dq (sums).
+template <int D, int G, bool DQ>
+__global__ void __launch_bounds__(256) span_row_join_kernel(const SpanArgs p) {
+  constexpr int CH = D / 8, RPB = 256 / (CH * G), N = DQ ? 8 : 10;      // eight elements, and the forward's two sums
+  __shared__ float red[CH * G > 64 ? 4 * CH * N : 1];
+  const int total = (p.a / p.kh) * p.seq_q, nhb = p.kh * p.batch;
+  const int tid = threadIdx.x, ch = tid % CH, grp = tid / CH % G;
+  const long item = (long)blockIdx.x * RPB + tid / (CH * G);
+  const bool in = item < (long)nhb * total;
+  const int hb = in ? (int)(item / total) : 0, r = in ? (int)(item - (long)hb * total) : 0;
+  const Rows s(p, hb);
+  const int n = in ? p.splits : 0;
+  const long row = (long)hb * total + r, step = (long)nhb * total;
+  float acc[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
+  float m = -INFINITY;
+  if constexpr (!DQ) {
+    constexpr int L = CH * G < 64 ? CH * G : 64;      // lanes of a wave that work on the row
+#pragma unroll 2
+    for (int i = tid % L; i < n; i += L) m = fmaxf(m, p.part_ml[i * step + row].x);
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  }
+#pragma unroll 4
+  for (int i = grp; i < n; i += G) {
+    if constexpr (DQ) {
+      add_times(acc, p.part + (i * step + row) * D + ch * 8, 1.f);
+    } else {
+      const float4 ml = p.part_ml[i * step + row];
+      if (ml.y != 0.f) {      // the slice has keys that the row sees
+        const float wgt = fast_exp2(ml.x - m);
+        acc[8] += wgt * ml.y;
+        acc[9] += wgt * ml.z;
+        add_times(acc, p.part + (i * step + row) * D + ch * 8, wgt);
+      }
+    }
+  }
+  const bool store = add_groups<CH, G, N>(acc, red);
+  if (!in || !store) return;
+  if constexpr (DQ) {
+    *reinterpret_cast<uint4*>(p.dq + s.offset(r, p.lddq, D) + ch * 8) = pack_times(acc, p.scale);
+  } else {
+    const int2 span = span_of(p, s, r);
+    const bool some = span.y > span.x;
+    if (p.lse && ch == 0) p.lse[s.stat(r, p.a)] = some ? m * 0.6931471805599453f + logf(acc[8]) : -INFINITY;
+    const float mul = some ? 1.f / acc[9] : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = some ? acc[e] * mul : 0.f;
+    const long at = s.offset(r, p.ldo, D) + ch * 8;
+    *reinterpret_cast<uint4*>(p.o + at) = pack_times(acc, 1.f);
+    if (p.rest) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] -= (float)(bf16)acc[e];
+      *reinterpret_cast<uint4*>(p.rest + at) = pack_times(acc, 1.f);
+    }
+  }
+}
+
+// ================================================================================================ dQ
+template <int D, bool SPLIT, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256, 2) span_dq_kernel(const SpanArgs p) {
+  constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, NT = 256, BQ = 128;
+  using T64 = Tile64<D, NT>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // dq_smem_bytes(D)
+  bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);
+  bf16* const Ks = smem;
+  bf16* const Vs = smem + 64 * LD;
+  int4* const seen_lds = reinterpret_cast<int4*>(dyn_smem + dq_tile_bytes(D));       // [4]
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nhb = p.kh * p.batch;
+  const int rest = (int)blockIdx.x / nhb;
+  const int hb = head_at((int)blockIdx.x, rest, nhb);
+  const int split = SPLIT ? rest % p.splits : 0;
+  const Rows s(p, hb);
+  const int blocks = (s.total + BQ - 1) / BQ;
+  const int r0 = (blocks - 1 - (SPLIT ? rest / p.splits : rest)) * BQ;
+  const Score sc(p);
+
+  int2 span[2];
+  Seen mine;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int row = r0 + 32 * w + 16 * c + lr;
+    span[c] = span_of(p, s, row);
+    Seen v;
+    v.start(span[c], row < s.total);
+    if (c == 0) mine = v;
+    else mine.add(v.lo, v.hi, v.all_lo, v.all_hi);
+  }
+  mine.lanes(1, 16);
+  const Seen block = seen_by_all(mine, seen_lds, w, lane);
+  // what dK, dV have to know of the two tiles of 64 rows
+  if (s.g == 0 && split == 0 && (tid & 127) == 0 && r0 + 32 * w < s.total) {
+    const int4 x = seen_lds[w], y = seen_lds[w + 1];
+    p.tiles[(long)s.b * ((s.total + 63) / 64) + r0 / 64 + w / 2] = make_int4(min(x.x, y.x), max(x.y, y.y), max(x.z, y.z), min(x.w, y.w));
+  }
+  int j0 = 0, j1 = 0;
+  if (block.hi > block.lo) {
+    j0 = block.lo / 64;
+    j1 = (block.hi + 63) / 64;
+  }
+  if (SPLIT) {
+    int first, last;
+    slice_of(j1 - j0, p.splits, split, first, last);
+    j1 = j0 + last;
+    j0 += first;
+  }
+  const KeyTile<D, NT> kt_(p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D, p.ldk, p.seq_kv), vt_(p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D, p.ldv, p.seq_kv);
+
+  uint4 qf[2][KS], dof[2][KS];     // a lane's rows: column tiles c = 0, 1
+  float lse2[2], dl[2], slope2[2] = {0.f, 0.f};
+  int pos[2] = {0, 0};
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int row = r0 + 32 * w + 16 * c + lr;
+    const bool ok = row < s.total;
+    const int rc = ok ? row : 0;
+    const bf16* const qr = p.q + s.offset(rc, p.ldq, D) + 8 * lg;
+    const bf16* const dor = p.dout + s.offset(rc, p.lddo, D) + 8 * lg;
+    const long at_o = s.offset(rc, p.ldo, D) + 8 * lg;
+    float sum = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      dof[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (ok) {
+        qf[c][ks] = *reinterpret_cast<const uint4*>(qr + 32 * ks);
+        dof[c][ks] = *reinterpret_cast<const uint4*>(dor + 32 * ks);
+        uint4 o[2];
+        o[0] = *reinterpret_cast<const uint4*>(p.o_in + at_o + 32 * ks);
+        o[1] = make_uint4(0u, 0u, 0u, 0u);
+        if (p.rest_in) o[1] = *reinterpret_cast<const uint4*>(p.rest_in + at_o + 32 * ks);
+        const uint4 d = dof[c][ks];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          sum += bf16_lo(o[i].x) * bf16_lo(d.x) + bf16_hi(o[i].x) * bf16_hi(d.x) + bf16_lo(o[i].y) * bf16_lo(d.y) + bf16_hi(o[i].y) * bf16_hi(d.y) +
+                 bf16_lo(o[i].z) * bf16_lo(d.z) + bf16_hi(o[i].z) * bf16_hi(d.z) + bf16_lo(o[i].w) * bf16_lo(d.w) + bf16_hi(o[i].w) * bf16_hi(d.w);
+      }
+    }
+    const bool some = span[c].y > span[c].x;
+    lse2[c] = some ? p.lse_in[s.stat(rc, p.a)] * LOG2E : INFINITY;      // rows that see nothing get P = 0
+    sum = column_sum(sum);
+    dl[c] = some ? sum : 0.f;
+    if (BIAS) {
+      int q, h;
+      s.at(rc, q, h);
+      slope2[c] = p.slopes[s.g * s.grp + h] * LOG2E;
+      pos[c] = p.q_pos ? p.q_pos[(long)s.b * p.seq_q + q] : q + p.seq_kv - p.seq_q;
+    }
+    if (lg == 0 && ok && split == 0) p.delta[s.stat(row, p.a)] = dl[c];
+  }
+
+  const bf16* const kfrag = Ks + lr * LD + 8 * lg;      // (V lies 64 rows further on)
+  const bf16* const ktfrag = Ks + tr_base<LD>(lane);
+  uint4 kreg[T64::NREG], vreg[T64::NREG];
+  auto load_tiles = [&](int j) {
+    kt_.load(kreg, j * 64, tid);
+    vt_.load(vreg, j * 64, tid);
+  };
+  f32x4 dqacc[DT][2];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) dqacc[dt][0] = dqacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (j0 < j1) load_tiles(j0);
+  for (int j = j0; j < j1; ++j) {
+    const bool whole = block.all(j * 64, j * 64 + 64);      // uniform over the workgroup
+    __syncthreads();
+    if (!whole) make_finite(kreg);
+    T64::template store<LD>(kreg, Ks, tid);
+    T64::template store<LD>(vreg, Vs, tid);
+    __syncthreads();
+    if (j + 1 < j1) load_tiles(j + 1);
+    // the two 32-key halves of the tile one after the other: half as many score registers live at a time
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) {
+      const int k0 = j * 64 + 32 * k2;
+      if (!mine.any(k0, k0 + 32)) continue;      // uniform over the wave
+      f32x4 sT[2][2], dpT[2][2];      // [16 keys][16 rows]
+      const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
+      {
+        constexpr int NS = 4 * KS, AHEAD = 4;     // n = (ks * 2 + kt) * 2 + which
+        auto sfrag_at = [&](int n) { return *reinterpret_cast<const uint4*>(kfrag + (32 * k2 + 16 * ((n >> 1) & 1) + 64 * (n & 1)) * LD + 32 * (n >> 2)); };
+        uint4 ring[AHEAD];
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) ring[n] = sfrag_at(n);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          const uint4 a = ring[n % AHEAD];
+          if (n + AHEAD < NS) ring[n % AHEAD] = sfrag_at(n + AHEAD);
+          const int ks = n >> 2, kt = (n >> 1) & 1;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (n & 1) dpT[kt][c] = mfma16(a, dof[c][ks], ks == 0 ? zero4 : dpT[kt][c]);
+            else sT[kt][c] = mfma16(a, qf[c][ks], ks == 0 ? zero4 : sT[kt][c]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float from = BIAS ? (float)(pos[c] - (k0 + 4 * lg)) : 0.f;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float z = sT[kt][c][e], r = CAP ? cap_r(z, sc) : 0.f;
+            float x;      // exponent of P
+            if constexpr (CAP || BIAS) {
+              x = CAP ? __builtin_fmaf(-2.f * sc.k2, r, sc.k2) : z * sc.k1;
+              if (BIAS) x = __builtin_fmaf(-slope2[c], fabsf(from - (float)(16 * kt + e)), x);
+              x -= lse2[c];
+            } else {
+              x = __builtin_fmaf(z, sc.k1, -lse2[c]);
+            }
+            float ds = fast_exp2(x) * (dpT[kt][c][e] - dl[c]);
+            if (CAP) ds *= 4.f * r * (1.f - r);
+            sT[kt][c][e] = ds;   // dS^T
+          }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int lo = span[c].x - (k0 + 4 * lg);
+          const unsigned n = (unsigned)(span[c].y - span[c].x);
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sT[kt][c][e] = (unsigned)(16 * kt + e - lo) < n ? sT[kt][c][e] : 0.f;
+        }
+      }
+      constexpr int AHEAD = 4;      // K^T fragments requested that many pairs of products early
+      const uint4 df[2] = {pack_frag(sT[0][0], sT[1][0]), pack_frag(sT[0][1], sT[1][1])};
+      auto ufrag_at = [&](int n) { return read_frag_tr<LD>(ktfrag + 32 * k2 * LD + 16 * n); };
+      uint4 uring[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
+#pragma unroll
+      for (int n = 0; n < DT; ++n) {
+        const uint4 a = uring[n % AHEAD];
+        if (n + AHEAD < DT) uring[n % AHEAD] = ufrag_at(n + AHEAD);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) dqacc[n][c] = mfma16(a, df[c], dqacc[n][c]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  if constexpr (SPLIT) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int row = r0 + 32 * w + 16 * c + lr;
+      if (row < s.total) {
+        float* const out = p.part + (((long)split * nhb + hb) * s.total + row) * D + 4 * lg;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          *reinterpret_cast<float4*>(out + 16 * dt) = make_float4(dqacc[dt][c][0], dqacc[dt][c][1], dqacc[dt][c][2], dqacc[dt][c][3]);
+      }
+    }
+  } else {
+    __syncthreads();
+    bf16* const stage = smem + w * 32 * (D + 8);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        *reinterpret_cast<uint2*>(stage + (16 * c + lr) * (D + 8) + 16 * dt + 4 * lg) =
+            make_uint2(pack_bf16x2(dqacc[dt][c][0] * p.scale, dqacc[dt][c][1] * p.scale), pack_bf16x2(dqacc[dt][c][2] * p.scale, dqacc[dt][c][3] * p.scale));
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < (32 * (D / 8)) / 64; ++it) {
+      const int idx = it * 64 + lane, rr = idx / (D / 8), ch = idx % (D / 8), r = r0 + 32 * w + rr;
+      if (r < s.total) *reinterpret_cast<uint4*>(p.dq + s.offset(r, p.lddq, D) + ch * 8) = *reinterpret_cast<const uint4*>(stage + rr * (D + 8) + ch * 8);
+    }
+  }
+}
+
+// ================================================================================================ dK, dV
+// A thread's share of a 64-row tile of q and dO, zero behind the last row.
+template <int D, int NT>
+struct RowTile {
+  static constexpr int CH = D / 8, NREG = 64 * CH / NT;
+  // base: the group's first head of the sequence's first query
+  static RP_DEV void load(uint4 (&q_reg)[NREG], uint4 (&do_reg)[NREG], const Rows& s, const bf16* qb, long ldq, const bf16* dob, long lddo, int row0, int tid) {
+#pragma unroll
+    for (int it = 0; it < NREG; ++it) {
+      typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));      // (copied as a struct, the pieces would live in scratch memory)
+      const int r = row0 + (it * NT + tid) / CH;
+      int q, h;
+      s.at(r < s.total ? r : 0, q, h);
+      const int in_row = h * D + ((it * NT + tid) % CH) * 8;
+      const u32x4 x = *reinterpret_cast<const u32x4*>(qb + (long)q * ldq + in_row), y = *reinterpret_cast<const u32x4*>(dob + (long)q * lddo + in_row);
+      const unsigned in = r < s.total ? 0xffffffffu : 0u;      // zero behind the last row: 0 times what the first one holds may be NaN
+      q_reg[it] = make_uint4(x.x & in, x.y & in, x.z & in, x.w & in);
+      do_reg[it] = make_uint4(y.x & in, y.y & in, y.z & in, y.w & in);
+    }
+  }
+};
+
+// What there is to know of the rows of a 64-row tile, a row per lane of waves 0 to 3, in LDS as six arrays of 64: what the score starts from, -delta, first key and
+// number of keys seen, position from the tile's first key, slope.  Rows that see nothing, and rows behind the last: P = exp(-inf) = 0.
+template <bool CAP, bool BIAS>
+struct RowStat {
+  static constexpr int FLOATS = 64 * 6;
+  float x, y;
+  // The loads are only issued here; the values are put in LDS a tile later.
+  RP_DEV void load(const SpanArgs& p, const Rows& s, int row0, int lane, int w) {
+    const int r = row0 + lane;
+    const bool in = r < s.total;
+    int q, h;
+    s.at(in ? r : 0, q, h);
+    const long stat = ((long)s.b * p.a + s.g * s.grp + h) * p.seq_q + q;
+    if (w == 0) x = in ? p.lse_in[stat] : -INFINITY;
+    if (w == 1) x = in ? p.delta[stat] : 0.f;
+    if (w == 2) {
+      const int2 v = span_of(p, s, r);
+      x = __int_as_float(v.x);
+      y = __int_as_float(v.y - v.x);
+    }
+    if (BIAS && w == 3) {
+      x = __int_as_float(p.q_pos ? p.q_pos[(long)s.b * p.seq_q + q] : q + p.seq_kv - p.seq_q);
+      y = p.slopes[s.g * s.grp + h] * LOG2E;
+    }
+  }
+  RP_DEV void store(float* lds, const SpanArgs& p, int kv0, int lane, int w) const {
+    // plain scores: the product starts from -lse / scale, so that it comes out as z - lse; a capped or biased one is taken off after
+    if (w == 0) lds[lane] = x == -INFINITY ? -INFINITY : CAP || BIAS ? -x * LOG2E : -x / p.scale;
+    if (w == 1) lds[64 + lane] = -x;
+    if (w == 2) {
+      lds[128 + lane] = x;
+      lds[192 + lane] = y;
+    }
+    if (BIAS && w == 3) {
+      lds[256 + lane] = (float)(__float_as_int(x) - kv0);
+      lds[320 + lane] = y;
+    }
+  }
+};
+
+// P and dS of 2 x 16 rows by 2 x 16 keys, in place of the scores and dP - delta.  lds: RowStat's, from the first of the rows on; key: the lane's first key, from kv0.
+template <bool CAP, bool BIAS>
+RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, const float* lds, int lg, int key, int kv0, bool whole) {
+#pragma unroll
+  for (int qt = 0; qt < 2; ++qt) {
+    const float* const at = lds + 16 * qt + 4 * lg;
+    f32x4 start, pos, slope;
+    if (CAP || BIAS) start = *reinterpret_cast<const f32x4*>(at);
+    if (BIAS) {
+      pos = *reinterpret_cast<const f32x4*>(at + 256);
+      slope = *reinterpret_cast<const f32x4*>(at + 320);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float z = s[qt][t][e], r = CAP ? cap_r(z, c) : 0.f;
+        float x = CAP ? __builtin_fmaf(-2.f * c.k2, r, c.k2) : z * c.k1;
+        if (BIAS) x = __builtin_fmaf(-slope[e], fabsf(pos[e] - (float)(key + 16 * t)), x);
+        if (CAP || BIAS) x += start[e];
+        const float pr = fast_exp2(x);
+        s[qt][t][e] = pr;
+        dp[qt][t][e] = pr * dp[qt][t][e];
+        if (CAP) dp[qt][t][e] *= 4.f * r * (1.f - r);
+      }
+  }
+  if (!whole) {
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      const int4 lo = *reinterpret_cast<const int4*>(lds + 128 + 16 * qt + 4 * lg), n = *reinterpret_cast<const int4*>(lds + 192 + 16 * qt + 4 * lg);
+      const int first[4] = {lo.x, lo.y, lo.z, lo.w};
+      const int count[4] = {n.x, n.y, n.z, n.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const bool seen = (unsigned)(kv0 + key + 16 * t - first[e]) < (unsigned)count[e];
+          s[qt][t][e] = seen ? s[qt][t][e] : 0.f;
+          dp[qt][t][e] = seen ? dp[qt][t][e] : 0.f;
+        }
+    }
+  }
+}
+
+// The row tiles that see any of a workgroup's keys: which they are (tiles between the first and the last may see none), found by all threads together.
+struct RowRange {
+  const int4* tiles;
+  int k0, k1, first, last;      // [first, last)
+  RP_DEV bool any(int u) const {
+    const int4 v = tiles[u];
+    return k0 < v.y && k1 > v.x;
+  }
+  RP_DEV bool all(int u) const {
+    const int4 v = tiles[u];
+    return v.z <= k0 && v.w >= k1;
+  }
+  template <int NT>
+  RP_DEV void find(const SpanArgs& p, const Rows& s, int key0, int* lds /* [2 NT / 64] */, int tid) {
+    const int n = (s.total + 63) / 64;
+    tiles = p.tiles + (long)s.b * n;
+    k0 = key0;
+    k1 = min(key0 + 128, p.seq_kv);
+    int lo = 0x7fffffff, hi = 0;
+    for (int u = tid; u < n; u += NT)
+      if (any(u)) {
+        lo = min(lo, u);
+        hi = u + 1;
+      }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      lo = min(lo, __shfl_xor(lo, o, 64));
+      hi = max(hi, __shfl_xor(hi, o, 64));
+    }
+    if ((tid & 63) == 0) {
+      lds[2 * (tid >> 6)] = lo;
+      lds[2 * (tid >> 6) + 1] = hi;
+    }
+    __syncthreads();
+    for (int w = 0; w < NT / 64; ++w) {
+      lo = min(lo, lds[2 * w]);
+      hi = max(hi, lds[2 * w + 1]);
+    }
+    __syncthreads();
+    first = __builtin_amdgcn_readfirstlane(hi > 0 ? lo : 0);
+    last = __builtin_amdgcn_readfirstlane(hi);
+  }
+  // the next tile from u on that sees any key, or `end`
+  RP_DEV int next(int u, int end) const {
+    while (u < end && !any(u)) ++u;
+    return u;
+  }
+};
+
+// The keys of a workgroup do not mix: a column of the score tiles is a key's own.
+template <int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
+  constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16;
+  using T64 = Tile64<D, 256>;
+  using Stat = RowStat<CAP, BIAS>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];
+  bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);             // Q | dO | the rows' numbers
+  bf16* const Qs = smem;
+  bf16* const dOs = smem + 64 * LD;
+  float* const stat = reinterpret_cast<float*>(smem + 2 * 64 * LD);
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nhb = p.kh * p.batch;
+  const int rest = (int)blockIdx.x / nhb;
+  const int hb = head_at((int)blockIdx.x, rest, nhb);
+  const int split = rest % p.splits, kv0 = (rest / p.splits) * 128, kw0 = kv0 + 32 * w;
+  const Rows s(p, hb);
+  const Score sc(p);
+  RowRange range;
+  range.find<256>(p, s, kv0, reinterpret_cast<int*>(stat), tid);
+  int u0, u1;
+  slice_of(range.last - range.first, p.splits, split, u0, u1);
+  u0 += range.first;
+  u1 += range.first;
+  const int kpos[2] = {kw0 + lr, kw0 + 16 + lr};
+  const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
+  const bf16* const vb = p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D;
+
+  uint4 kf[2][KS], vf[2][KS];
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      vf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (kpos[c] < p.seq_kv) {
+        kf[c][ks] = *reinterpret_cast<const uint4*>(kb + (long)kpos[c] * p.ldk + 32 * ks + 8 * lg);
+        vf[c][ks] = *reinterpret_cast<const uint4*>(vb + (long)kpos[c] * p.ldv + 32 * ks + 8 * lg);
+      }
+    }
+  f32x4 dkacc[DT][2], dvacc[DT][2];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) dkacc[dt][0] = dkacc[dt][1] = dvacc[dt][0] = dvacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const bf16* qfrag = Qs + lr * LD + 8 * lg;
+  const bf16* dofrag = dOs + lr * LD + 8 * lg;
+  const bf16* qtfrag = Qs + tr_base<LD>(lane);
+  const bf16* dotfrag = dOs + tr_base<LD>(lane);
+
+  const bf16* const qb = p.q + (long)s.b * p.seq_q * p.ldq + (long)s.g * s.grp * D;
+  const bf16* const dob = p.dout + (long)s.b * p.seq_q * p.lddo + (long)s.g * s.grp * D;
+  uint4 qreg[T64::NREG], doreg[T64::NREG];
+  Stat rstat;
+  auto prefetch = [&](int u) {
+    RowTile<D, 256>::load(qreg, doreg, s, qb, p.ldq, dob, p.lddo, u * 64, tid);
+    rstat.load(p, s, u * 64, lane, w);
+  };
+  int u = range.next(u0, u1);
+  if (u < u1) prefetch(u);
+  while (u < u1) {
+    const bool whole = range.all(u);
+    const int after = range.next(u + 1, u1);
+    __syncthreads();
+    if (!whole) {
+      make_finite(qreg);
+      make_finite(doreg);
+    }
+    T64::template store<LD>(qreg, Qs, tid);
+    T64::template store<LD>(doreg, dOs, tid);
+    rstat.store(stat, p, kv0, lane, w);
+    __syncthreads();
+    if (after < u1) prefetch(after);
+    // the two 32-row halves of the tile one after the other: half as many score registers live at a time
+#pragma unroll
+    for (int t2 = 0; t2 < 2; ++t2) {
+      f32x4 z[2][2], dp[2][2], z0[2], dp0[2];     // [16 rows][16 keys]; what they start from
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt) {
+        z0[qt] = CAP || BIAS ? f32x4{0.f, 0.f, 0.f, 0.f} : *reinterpret_cast<const f32x4*>(stat + 32 * t2 + 16 * qt + 4 * lg);
+        dp0[qt] = *reinterpret_cast<const f32x4*>(stat + 64 + 32 * t2 + 16 * qt + 4 * lg);
+      }
+      constexpr int AHEAD = 4;
+      {
+        constexpr int NS = 4 * KS;     // n = (ks * 2 + qt) * 2 + which
+        auto sfrag_at = [&](int n) { return *reinterpret_cast<const uint4*>(((n & 1) ? dofrag : qfrag) + (32 * t2 + 16 * ((n >> 1) & 1)) * LD + 32 * (n >> 2)); };
+        uint4 ring[AHEAD];
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) ring[n] = sfrag_at(n);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          const uint4 a = ring[n % AHEAD];
+          if (n + AHEAD < NS) ring[n % AHEAD] = sfrag_at(n + AHEAD);
+          const int ks = n >> 2, qt = (n >> 1) & 1;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (n & 1) dp[qt][c] = mfma16(a, vf[c][ks], ks == 0 ? dp0[qt] : dp[qt][c]);
+            else z[qt][c] = mfma16(a, kf[c][ks], ks == 0 ? z0[qt] : z[qt][c]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      constexpr int NU = 2 * DT;
+      auto ufrag_at = [&](int n) { return read_frag_tr<LD>(((n & 1) ? qtfrag : dotfrag) + 32 * t2 * LD + 16 * (n >> 1)); };
+      uint4 uring[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
+      __builtin_amdgcn_sched_barrier(0);
+      probabilities<CAP, BIAS>(z, dp, sc, stat + 32 * t2, lg, 32 * w + lr, kv0, whole);
+      {
+        const uint4 pfg[2] = {pack_frag(z[0][0], z[1][0]), pack_frag(z[0][1], z[1][1])};
+        const uint4 dfg[2] = {pack_frag(dp[0][0], dp[1][0]), pack_frag(dp[0][1], dp[1][1])};
+#pragma unroll
+        for (int n = 0; n < NU; ++n) {
+          const uint4 a = uring[n % AHEAD];
+          if (n + AHEAD < NU) uring[n % AHEAD] = ufrag_at(n + AHEAD);
+          const int dt = n >> 1;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (n & 1) dkacc[dt][c] = mfma16(a, dfg[c], dkacc[dt][c]);
+            else dvacc[dt][c] = mfma16(a, pfg[c], dvacc[dt][c]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    u = after;
+  }
+  __syncthreads();
+  const long tok0 = (long)s.b * p.seq_kv;
+  if (p.splits == 1) {
+    store_acc_T<D>(dkacc, p.scale, smem + w * 32 * (D + 8), p.dk + tok0 * p.lddk + s.g * D, p.lddk, kw0, p.seq_kv, lane);
+    store_acc_T<D>(dvacc, 1.f, smem + w * 32 * (D + 8), p.dv + tok0 * p.lddv + s.g * D, p.lddv, kw0, p.seq_kv, lane);
+  } else {
+    float* const stage = reinterpret_cast<float*>(smem) + w * 32 * (D + 4);
+    const long ldp = (long)p.kh * D, each = (long)p.batch * p.seq_kv * ldp;
+    float* const out = p.part + split * each + tok0 * ldp + s.g * D;
+    store_acc_T_f32<D>(dkacc, p.scale, stage, out, ldp, kw0, p.seq_kv, lane);
+    store_acc_T_f32<D>(dvacc, 1.f, stage, out + p.splits * each, ldp, kw0, p.seq_kv, lane);
+  }
+}
+
+// Two waves per SIMD at d = 128 (see attn_bwd_dkv_pair_kernel in attention.hip): the 32 keys of a pair of waves are shared, wave h of it keeps
+// the accumulators of half h of the head dimension, makes the scores of rows 32 h .. of each tile and hands P and dS to its partner through LDS.
+template <int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
+  constexpr int LD = tile_ld(D), KS = D / 32, DH = D / 32;
+  using T64 = Tile64<D, 512>;
+  using Stat = RowStat<CAP, BIAS>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];
+  bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);             // two sets (tile parity) of Q | dO, then the exchange
+  constexpr int TSET = 2 * 64 * LD;
+  uint4* const exch = reinterpret_cast<uint4*>(smem + 2 * TSET);    // [8 waves][4 fragments][64 lanes]
+  float* const stat = reinterpret_cast<float*>(exch + 8 * 4 * 64);  // [2 sets]
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w = w8 >> 1, h = w8 & 1;
+  const int nhb = p.kh * p.batch;
+  const int rest = (int)blockIdx.x / nhb;
+  const int hb = head_at((int)blockIdx.x, rest, nhb);
+  const int split = rest % p.splits, kv0 = (rest / p.splits) * 128, kw0 = kv0 + 32 * w;
+  const Rows s(p, hb);
+  const Score sc(p);
+  RowRange range;
+  range.find<512>(p, s, kv0, reinterpret_cast<int*>(stat), tid);
+  int u0, u1;
+  slice_of(range.last - range.first, p.splits, split, u0, u1);
+  u0 += range.first;
+  u1 += range.first;
+  const int kpos[2] = {kw0 + lr, kw0 + 16 + lr};
+  const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
+  const bf16* const vb = p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D;
+
+  uint4 kf[2][KS], vf[2][KS];
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      vf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (kpos[c] < p.seq_kv) {
+        kf[c][ks] = *reinterpret_cast<const uint4*>(kb + (long)kpos[c] * p.ldk + 32 * ks + 8 * lg);
+        vf[c][ks] = *reinterpret_cast<const uint4*>(vb + (long)kpos[c] * p.ldv + 32 * ks + 8 * lg);
+      }
+    }
+  f32x4 dkacc[DH][2], dvacc[DH][2];
+#pragma unroll
+  for (int dt = 0; dt < DH; ++dt) dkacc[dt][0] = dkacc[dt][1] = dvacc[dt][0] = dvacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const bf16* qfrag = smem + (32 * h + lr) * LD + 8 * lg;           // this wave's 32 rows of a tile
+  const bf16* dofrag = qfrag + 64 * LD;
+  const bf16* qtfrag = smem + tr_base<LD>(lane) + 16 * DH * h;      // its half of the head dimension
+  const bf16* dotfrag = qtfrag + 64 * LD;
+  uint4* const ex_mine = exch + (w8 * 4) * 64 + lane;
+  const uint4* const ex_theirs = exch + ((w8 ^ 1) * 4) * 64 + lane;
+
+  const bf16* const qb = p.q + (long)s.b * p.seq_q * p.ldq + (long)s.g * s.grp * D;
+  const bf16* const dob = p.dout + (long)s.b * p.seq_q * p.lddo + (long)s.g * s.grp * D;
+  uint4 qreg[T64::NREG], doreg[T64::NREG];
+  Stat rstat;
+  auto prefetch = [&](int u) {
+    RowTile<D, 512>::load(qreg, doreg, s, qb, p.ldq, dob, p.lddo, u * 64, tid);
+    rstat.load(p, s, u * 64, lane, w8);
+  };
+  int u = range.next(u0, u1);
+  if (u < u1) prefetch(u);
+
+  constexpr int AHEAD = 2;     // two waves per SIMD cover each other's LDS latency: a short ring is enough
+  auto update_half = [&](int set, int t2, const uint4 (&pf)[2], const uint4 (&df)[2]) {
+    constexpr int NU = 2 * DH;     // n = dt * 2 + which
+    auto ufrag_at = [&](int n) { return read_frag_tr<LD>(((n & 1) ? qtfrag : dotfrag) + set * TSET + 32 * t2 * LD + 16 * (n >> 1)); };
+    uint4 uring[AHEAD];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
+    MFMA_PHASE_BEGIN();
+#pragma unroll
+    for (int n = 0; n < NU; ++n) {
+      const uint4 a = uring[n % AHEAD];
+      if (n + AHEAD < NU) uring[n % AHEAD] = ufrag_at(n + AHEAD);
+      const int dt = n >> 1;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        if (n & 1) dkacc[dt][c] = mfma16(a, df[c], dkacc[dt][c]);
+        else dvacc[dt][c] = mfma16(a, pf[c], dvacc[dt][c]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    MFMA_PHASE_END();
+  };
+  // Two barriers per tile.  After the first one every wave is done with the previous tile's scores and has published its fragments: the
+  // new tile is stored (into the other set) while the accumulators take the partner's half of the PREVIOUS tile.
+  auto partner_update = [&](int prev) {
+    const uint4 ppf[2] = {ex_theirs[0], ex_theirs[64]};
+    const uint4 pdf[2] = {ex_theirs[128], ex_theirs[192]};
+    update_half(prev & 1, h ^ 1, ppf, pdf);
+  };
+  int i = 0;
+  for (; u < u1; ++i) {
+    const bool whole = range.all(u);
+    const int after = range.next(u + 1, u1);
+    __syncthreads();
+    bf16* const q_set = smem + (i & 1) * TSET;
+    float* const st_set = stat + (i & 1) * Stat::FLOATS;
+    if (!whole) {
+      make_finite(qreg);
+      make_finite(doreg);
+    }
+    T64::template store<LD>(qreg, q_set, tid);
+    T64::template store<LD>(doreg, q_set + 64 * LD, tid);
+    rstat.store(st_set, p, kv0, lane, w8);
+    if (i > 0) partner_update(i - 1);
+    __syncthreads();
+    if (after < u1) prefetch(after);
+    f32x4 z[2][2], dp[2][2], z0[2], dp0[2];      // [16 rows][16 keys]; what they start from
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      z0[qt] = CAP || BIAS ? f32x4{0.f, 0.f, 0.f, 0.f} : *reinterpret_cast<const f32x4*>(st_set + 32 * h + 16 * qt + 4 * lg);
+      dp0[qt] = *reinterpret_cast<const f32x4*>(st_set + 64 + 32 * h + 16 * qt + 4 * lg);
+    }
+    {
+      constexpr int NS = 4 * KS;     // n = (ks * 2 + qt) * 2 + which
+      auto sfrag_at = [&](int n) { return *reinterpret_cast<const uint4*>(((n & 1) ? dofrag : qfrag) + (i & 1) * TSET + 16 * ((n >> 1) & 1) * LD + 32 * (n >> 2)); };
+      uint4 ring[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) ring[n] = sfrag_at(n);
+      MFMA_PHASE_BEGIN();
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        const uint4 a = ring[n % AHEAD];
+        if (n + AHEAD < NS) ring[n % AHEAD] = sfrag_at(n + AHEAD);
+        const int ks = n >> 2, qt = (n >> 1) & 1;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if (n & 1) dp[qt][c] = mfma16(a, vf[c][ks], ks == 0 ? dp0[qt] : dp[qt][c]);
+          else z[qt][c] = mfma16(a, kf[c][ks], ks == 0 ? z0[qt] : z[qt][c]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      MFMA_PHASE_END();
+    }
+    probabilities<CAP, BIAS>(z, dp, sc, st_set + 32 * h, lg, 32 * w + lr, kv0, whole);
+    const uint4 pfg[2] = {pack_frag(z[0][0], z[1][0]), pack_frag(z[0][1], z[1][1])};
+    const uint4 dfg[2] = {pack_frag(dp[0][0], dp[1][0]), pack_frag(dp[0][1], dp[1][1])};
+    // the partner read last tile's fragments before the barrier above: the slots are free
+    ex_mine[0] = pfg[0]; ex_mine[64] = pfg[1]; ex_mine[128] = dfg[0]; ex_mine[192] = dfg[1];
+    update_half(i & 1, h, pfg, dfg);
+    u = after;
+  }
+  __syncthreads();
+  if (i > 0) partner_update(i - 1);
+  __syncthreads();
+  const long tok0 = (long)s.b * p.seq_kv;
+  const int d0 = s.g * D + h * (D / 2);
+  if (p.splits == 1) {
+    bf16* const stage = smem + w8 * 32 * (D / 2 + 8);
+    store_acc_T<D / 2>(dkacc, p.scale, stage, p.dk + tok0 * p.lddk + d0, p.lddk, kw0, p.seq_kv, lane);
+    store_acc_T<D / 2>(dvacc, 1.f, stage, p.dv + tok0 * p.lddv + d0, p.lddv, kw0, p.seq_kv, lane);
+  } else {
+    float* const stage = reinterpret_cast<float*>(smem) + w8 * 32 * (D / 2 + 4);
+    const long ldp = (long)p.kh * D, each = (long)p.batch * p.seq_kv * ldp;
+    float* const out = p.part + split * each + tok0 * ldp + d0;
+    store_acc_T_f32<D / 2>(dkacc, p.scale, stage, out, ldp, kw0, p.seq_kv, lane);
+    store_acc_T_f32<D / 2>(dvacc, 1.f, stage, out + p.splits * each, ldp, kw0, p.seq_kv, lane);
+  }
+}
+
+// dk, dv = the sum of a key's slices.  A "row" is a key head of dk or dv.
+template <int D, int G>
+__global__ void __launch_bounds__(256) span_key_join_kernel(const SpanArgs p) {
+  constexpr int CH = D / 8, RPB = 256 / (CH * G);
+  __shared__ float red[CH * G > 64 ? 4 * CH * 8 : 1];
+  const int tid = threadIdx.x, ch = tid % CH, grp = tid / CH % G;
+  const long T = (long)p.batch * p.seq_kv, rows = T * p.kh;
+  const long item = (long)blockIdx.x * RPB + tid / (CH * G);
+  const bool in = item < 2 * rows, is_v = item >= rows;
+  const long kv = !in ? 0 : is_v ? item - rows : item;
+  const long t = kv / p.kh;
+  const int g = (int)(kv - t * p.kh);
+  const int n = in ? p.splits : 0;
+  const float* const src = p.part + (is_v ? p.splits * rows * D : 0) + kv * D + ch * 8;
+  float acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+#pragma unroll 4
+  for (int i = grp; i < n; i += G) add_times(acc, src + i * rows * D, 1.f);
+  const bool store = add_groups<CH, G, 8>(acc, red);
+  if (in && store) *reinterpret_cast<uint4*>((is_v ? p.dv + t * p.lddv : p.dk + t * p.lddk) + g * D + ch * 8) = pack_times(acc, 1.f);
+}
+
+constexpr int fwd_smem_bytes(int d) { return fwd_tile_bytes(d) + 64 + 16; }
+constexpr int dq_smem_bytes(int d) { return dq_tile_bytes(d) + 64; }
+constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 6 * 64 * 4, 4 * 32 * (d + 4) * 4); }
+constexpr int dkv_pair_smem_bytes(int d) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * 4 * 64 * 16 + 2 * 6 * 64 * 4; }
+
+long row_count(const SpanArgs& p) { return (long)(p.a / p.kh) * p.seq_q; }
+size_t row_part_bytes(const SpanArgs& p, int d) { return (size_t)p.kh * p.batch * row_count(p) * (d + 4) * 4; }      // o or dq, and (m, l, lt)
+size_t key_part_bytes(const SpanArgs& p, int d) { return (size_t)2 * p.batch * p.seq_kv * p.kh * d * 4; }
+size_t tiles_bytes(const SpanArgs& p) { return (size_t)p.batch * ceil_div(row_count(p), 64) * 16; }
+// Forward and dQ: two workgroups of 128 rows per CU.
+int row_splits(const SpanArgs& p, int d, size_t bytes) {
+  return splits_for((long)ceil_div(row_count(p), 128) * p.kh * p.batch, 512, ceil_div(p.seq_kv, 64), 1.4, row_part_bytes(p, d), bytes);
+}
+// dK, dV: the kernel at d = 128 has a CU to itself; at d = 64 two share one, and a third takes the place of those that end early
+int key_splits(const SpanArgs& p, int d, size_t bytes) {
+  return splits_for((long)ceil_div(p.seq_kv, 128) * p.kh * p.batch, d == 128 ? 256 : 768, ceil_div(row_count(p), 64), d == 128 ? 2.2 : 1.6, key_part_bytes(p, d), bytes);
+}
+
+template <int D, bool DQ>
+hipError_t join_rows(hipStream_t st, const SpanArgs& p) {
+  const int g = join_groups(p.splits), grid = ceil_div(row_count(p) * p.kh * p.batch, 256 / (D / 8 * g));
+  if (g == 1) return launch(span_row_join_kernel<D, 1, DQ>, grid, 256, 0, st, p);
+  if (g == 4) return launch(span_row_join_kernel<D, 4, DQ>, grid, 256, 0, st, p);
+  return launch(span_row_join_kernel<D, 16, DQ>, grid, 256, 0, st, p);
+}
+template <int D>
+hipError_t join_keys(hipStream_t st, const SpanArgs& p) {
+  const int g = join_groups(p.splits), grid = ceil_div((long)2 * p.batch * p.seq_kv * p.kh, 256 / (D / 8 * g));
+  if (g == 1) return launch(span_key_join_kernel<D, 1>, grid, 256, 0, st, p);
+  if (g == 4) return launch(span_key_join_kernel<D, 4>, grid, 256, 0, st, p);
+  return launch(span_key_join_kernel<D, 16>, grid, 256, 0, st, p);
+}
+
+template <int D, bool CAP, bool BIAS>
+hipError_t fwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
+  const int nhb = p.kh * p.batch;
+  const long rows = row_count(p);
+  p.splits = row_splits(p, D, bytes);
+  p.part = static_cast<float*>(scratch);
+  p.part_ml = reinterpret_cast<float4*>(p.part + (size_t)p.splits * nhb * rows * D);
+  const int grid = ceil_div(rows, 128) * nhb * p.splits;
+  if (p.splits == 1) return launch(span_fwd_kernel<D, false, CAP, BIAS>, grid, 256, fwd_smem_bytes(D), st, p);
+  const hipError_t e = launch(span_fwd_kernel<D, true, CAP, BIAS>, grid, 256, fwd_smem_bytes(D), st, p);
+  return e == hipSuccess ? join_rows<D, false>(st, p) : e;
+}
+
+template <int D, bool CAP, bool BIAS>
+hipError_t bwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
+  const int nhb = p.kh * p.batch;
+  const long rows = row_count(p);
+  const size_t head = tiles_bytes(p);
+  p.tiles = static_cast<int4*>(scratch);
+  p.part = reinterpret_cast<float*>(static_cast<char*>(scratch) + head);
+  bytes -= head;
+  hipError_t e = hipSuccess;
+  // dQ first: it works out delta, and what the row tiles see, which dK/dV read
+  if (rows > 0) {
+    p.splits = row_splits(p, D, bytes);
+    const int grid = ceil_div(rows, 128) * nhb * p.splits;
+    if (p.splits > 1) {
+      e = launch(span_dq_kernel<D, true, CAP, BIAS>, grid, 256, dq_smem_bytes(D), st, p);
+      if (e == hipSuccess) e = join_rows<D, true>(st, p);
+    } else {
+      e = launch(span_dq_kernel<D, false, CAP, BIAS>, grid, 256, dq_smem_bytes(D), st, p);
+    }
+  }
+  if (e != hipSuccess || p.seq_kv == 0) return e;
+  p.splits = key_splits(p, D, bytes);
+  const int grid = ceil_div(p.seq_kv, 128) * nhb * p.splits;
+  if constexpr (D == 128) e = launch(span_dkv_pair_kernel<D, CAP, BIAS>, grid, 512, dkv_pair_smem_bytes(D), st, p);
+  else e = launch(span_dkv_kernel<D, CAP, BIAS>, grid, 256, dkv_smem_bytes(D), st, p);
+  if (e != hipSuccess || p.splits == 1) return e;
+  return join_keys<D>(st, p);
+}
+
+// One of eight: d, cap, bias.
+template <typename F>
+hipError_t with_kind(const SpanArgs& p, int d, F&& f) {
+  typedef std::integral_constant<int, 64> d64;
+  typedef std::integral_constant<int, 128> d128;
+  const auto kind = [&](auto dd) {
+    if (p.cap > 0.f) return p.slopes ? f(dd, std::true_type{}, std::true_type{}) : f(dd, std::true_type{}, std::false_type{});
+    return p.slopes ? f(dd, std::false_type{}, std::true_type{}) : f(dd, std::false_type{}, std::false_type{});
+  };
+  return d == 128 ? kind(d128{}) : kind(d64{});
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------------------ launchers
+void k_span_attn_scratch(const SpanArgs& p, int d, size_t* fwd_bytes, size_t* bwd_bytes) {
+  const size_t all = ~(size_t)0;
+  const int rs = row_splits(p, d, all), ks = key_splits(p, d, all);
+  const size_t r = rs > 1 ? rs * row_part_bytes(p, d) : 0, k = ks > 1 ? ks * key_part_bytes(p, d) : 0;
+  *fwd_bytes = r;
+  *bwd_bytes = tiles_bytes(p) + (r > k ? r : k);
+}
+size_t k_span_attn_least(const SpanArgs& p) { return tiles_bytes(p); }
+
+hipError_t k_span_attn_fwd(hipStream_t st, const SpanArgs& p, int d, void* scratch, size_t bytes) {
+  if (p.batch == 0 || p.seq_q == 0) return hipSuccess;
+  return with_kind(p, d, [&](auto dd, auto cap, auto bias) { return fwd<decltype(dd)::value, decltype(cap)::value, decltype(bias)::value>(st, p, scratch, bytes); });
+}
+
+hipError_t k_span_attn_bwd(hipStream_t st, const SpanArgs& p, int d, void* scratch, size_t bytes) {
+  if (p.batch == 0 || (p.seq_q == 0 && p.seq_kv == 0)) return hipSuccess;
+  return with_kind(p, d, [&](auto dd, auto cap, auto bias) { return bwd<decltype(dd)::value, decltype(cap)::value, decltype(bias)::value>(st, p, scratch, bytes); });
+}

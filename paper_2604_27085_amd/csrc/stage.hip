@@ -13,6 +13,7 @@
 #include "gemm.hpp"
 #include "kernels.hpp"
 #include "layer_ops.hpp"
+#include "pack_ops.hpp"
 #include "layout.hpp"
 #include "transfers.hpp"
 
@@ -1437,6 +1438,207 @@ rp_status rp_op_moe_balance(void* stream, const float* logits, const int* idx, c
   StreamDevice on(reinterpret_cast<hipStream_t>(stream));
   if (on.err != hipSuccess) OP_RET(on.err);
   const hipError_t e = k_moe_balance(reinterpret_cast<hipStream_t>(stream), p, T, scratch);
+  OP_RET(e);
+}
+
+// ---- training on packed documents -----------------------------------------------------------------------------------
+namespace {
+// A [rows, n] tensor of 2- or 4-byte elements with a row stride: present unless it is empty, on 16-byte boundaries, rows apart.
+bool bad_rows(const void* p, long rows, int n, long ld) { return (rows > 0 && n > 0 && !p) || off16(p) || ld % 8 || ld < n || ld > (1l << 23); }
+}  // namespace
+
+rp_status rp_op_pack_plan(void* stream, const int* starts, const int* prefix, int n_docs, int window, int T, int seq, int* span, int* pos, unsigned char* first) {
+  if (n_docs < 0 || n_docs > (1 << 30) || window < 0 || T < 0 || T > (1 << 30) || seq <= 0 || T % seq || (T && !starts) || reinterpret_cast<uintptr_t>(span) % 8)
+    return fail(nullptr, RP_EINVAL, "rp_op_pack_plan: bad arguments");
+  PackArgs p{starts, prefix, reinterpret_cast<int2*>(span), pos, first, n_docs, window, T, seq};
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_pack_plan(reinterpret_cast<hipStream_t>(stream), p);
+  OP_RET(e);
+}
+
+namespace {
+// Sizes that the span attention's kernels cover; fills what they share.
+bool span_args(SpanArgs& p, int batch, int seq_q, int seq_kv, int a, int kh, int d, float scale, float cap, bool backward) {
+  if (batch < 0 || seq_q < 0 || seq_kv < 0 || a <= 0 || kh <= 0 || a % kh || (d != 64 && d != 128) || !(scale >= 1e-30f && scale <= 1e30f) ||
+      !(cap == 0.f || (cap >= 1e-3f && cap <= 1e3f)))
+    return false;
+  // rows of a key head are counted in 31 bits, and a launch has fewer than 2^32 threads: 256 for 128 rows of a key head; backward 512 for 128 keys at
+  // d = 128, 256 at d = 64.  (Cut into slices, a launch has 768 blocks at most, and those that join them 2^25 threads.)
+  const double rows = (double)(a / kh) * seq_q, nhb = (double)kh * batch;
+  if (rows > 1.0e9 || seq_kv > 1000000000 || rows * nhb * (d / 8) > 2.0e9 || 2.0 * nhb * seq_kv * (d / 8) > 256.0 * 2.0e9) return false;
+  if (ceil(rows / 128) * nhb * 256 >= 4294967296.0 || (backward && ceil(seq_kv / 128.0) * nhb * (d == 128 ? 512 : 256) >= 4294967296.0)) return false;
+  p.batch = batch; p.seq_q = seq_q; p.seq_kv = seq_kv; p.a = a; p.kh = kh;
+  p.scale = scale;
+  p.cap = cap;
+  return true;
+}
+bool off8(const void* p) { return reinterpret_cast<uintptr_t>(p) % 8 != 0; }
+}  // namespace
+
+rp_status rp_op_span_attn_scratch(int batch, int seq_q, int seq_kv, int a, int kh, int d, size_t* fwd_bytes, size_t* bwd_bytes, size_t* least_bytes) {
+  SpanArgs p{};
+  if (!span_args(p, batch, seq_q, seq_kv, a, kh, d, 1.f, 0.f, false)) return fail(nullptr, RP_EINVAL, "rp_op_span_attn_scratch: bad arguments");
+  size_t f = 0, b = 0;
+  k_span_attn_scratch(p, d, &f, &b);
+  if (fwd_bytes) *fwd_bytes = f;
+  if (bwd_bytes) *bwd_bytes = b;
+  if (least_bytes) *least_bytes = k_span_attn_least(p);
+  return RP_OK;
+}
+
+rp_status rp_op_span_attn_fwd(void* stream, const void* q, const void* k, const void* v, void* o, void* o_rest, float* lse, long ldq, long ldk, long ldv, long ldo,
+                              const int* span, const int* q_pos, const float* slopes, float cap, int batch, int seq_q, int seq_kv, int a, int kh, int d,
+                              float scale, void* scratch, size_t scratch_bytes) {
+  SpanArgs p{};
+  if (!span_args(p, batch, seq_q, seq_kv, a, kh, d, scale, cap, false)) return fail(nullptr, RP_EINVAL, "rp_op_span_attn_fwd: bad sizes, scale or cap");
+  const long tq = (long)batch * seq_q, tk = (long)batch * seq_kv;
+  if (bad_heads(q, tq, a, d, ldq) || bad_heads(o, tq, a, d, ldo) || off16(o_rest) || bad_heads(k, tk, kh, d, ldk) || bad_heads(v, tk, kh, d, ldv) || (tq && !span) || off8(span))
+    return fail(nullptr, RP_EINVAL, "rp_op_span_attn_fwd: tensors missing, not on 16-byte boundaries, or bad strides");
+  if (off16(scratch) || (scratch_bytes && !scratch)) return fail(nullptr, RP_EINVAL, "rp_op_span_attn_fwd: bad scratch");
+  p.q = static_cast<const bf16*>(q); p.k = static_cast<const bf16*>(k); p.v = static_cast<const bf16*>(v); p.o = static_cast<bf16*>(o);
+  p.rest = static_cast<bf16*>(o_rest); p.lse = lse; p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo;
+  p.span = reinterpret_cast<const int2*>(span); p.q_pos = q_pos; p.slopes = slopes;
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_span_attn_fwd(reinterpret_cast<hipStream_t>(stream), p, d, scratch, scratch_bytes);
+  OP_RET(e);
+}
+
+rp_status rp_op_span_attn_bwd(void* stream, const void* q, const void* k, const void* v, const void* o, const void* o_rest, const void* dout, const float* lse,
+                              float* delta, void* dq, void* dk, void* dv, long ldq, long ldk, long ldv, long ldo, long lddo, long lddq, long lddk, long lddv,
+                              const int* span, const int* q_pos, const float* slopes, float cap, int batch, int seq_q, int seq_kv, int a, int kh, int d,
+                              float scale, void* scratch, size_t scratch_bytes) {
+  SpanArgs p{};
+  if (!span_args(p, batch, seq_q, seq_kv, a, kh, d, scale, cap, true)) return fail(nullptr, RP_EINVAL, "rp_op_span_attn_bwd: bad sizes, scale or cap");
+  const long tq = (long)batch * seq_q, tk = (long)batch * seq_kv;
+  if (bad_heads(q, tq, a, d, ldq) || bad_heads(o, tq, a, d, ldo) || off16(o_rest) || bad_heads(dout, tq, a, d, lddo) || bad_heads(dq, tq, a, d, lddq) ||
+      bad_heads(k, tk, kh, d, ldk) || bad_heads(v, tk, kh, d, ldv) || bad_heads(dk, tk, kh, d, lddk) || bad_heads(dv, tk, kh, d, lddv) ||
+      (tq && (!lse || !delta || !span)) || off8(span))
+    return fail(nullptr, RP_EINVAL, "rp_op_span_attn_bwd: tensors missing, not on 16-byte boundaries, or bad strides");
+  const size_t least = k_span_attn_least(p);
+  if (off16(scratch) || (scratch_bytes && !scratch) || scratch_bytes < least)
+    return fail(nullptr, RP_EINVAL, "rp_op_span_attn_bwd: scratch holds %zu bytes, %zu needed, on a 16-byte boundary", scratch ? scratch_bytes : 0, least);
+  p.q = static_cast<const bf16*>(q); p.k = static_cast<const bf16*>(k); p.v = static_cast<const bf16*>(v); p.o_in = static_cast<const bf16*>(o);
+  p.rest_in = static_cast<const bf16*>(o_rest); p.dout = static_cast<const bf16*>(dout); p.lse_in = lse; p.delta = delta;
+  p.dq = static_cast<bf16*>(dq); p.dk = static_cast<bf16*>(dk); p.dv = static_cast<bf16*>(dv);
+  p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo; p.lddo = lddo; p.lddq = lddq; p.lddk = lddk; p.lddv = lddv;
+  p.span = reinterpret_cast<const int2*>(span); p.q_pos = q_pos; p.slopes = slopes;
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_span_attn_bwd(reinterpret_cast<hipStream_t>(stream), p, d, scratch, scratch_bytes);
+  OP_RET(e);
+}
+
+rp_status rp_op_dropout(void* stream, const void* x, long ldx, const void* res, long ldr, void* y, long ldy, int T, int n, float p, unsigned long long seed,
+                        unsigned long long offset, const unsigned long long* step) {
+  if (T < 0 || n < 0 || n % 8 || !(p >= 0.f && p <= 1.f) || (double)T * n > 137438953472.0 || reinterpret_cast<uintptr_t>(step) % 8)
+    return fail(nullptr, RP_EINVAL, "rp_op_dropout: bad arguments");
+  if (bad_rows(x, T, n, ldx) || bad_rows(y, T, n, ldy) || (res && bad_rows(res, T, n, ldr)) || (y == x && ldy != ldx) || (res && y == res && ldy != ldr))
+    return fail(nullptr, RP_EINVAL, "rp_op_dropout: tensors missing, not on 16-byte boundaries, or bad strides");
+  DropoutArgs a{};
+  a.x = static_cast<const bf16*>(x); a.res = static_cast<const bf16*>(res); a.y = static_cast<bf16*>(y);
+  a.ldx = ldx; a.ldr = ldr; a.ldy = ldy; a.n8 = (uint32_t)(n / 8); a.groups = (long)T * (n / 8);
+  a.step = step; a.seed = seed; a.offset = offset;
+  a.keep = (uint32_t)lrint((1.0 - (double)p) * 65536.0);
+  a.scale = a.keep ? (float)(65536.0 / a.keep) : 0.f;
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_dropout(reinterpret_cast<hipStream_t>(stream), a);
+  OP_RET(e);
+}
+
+namespace {
+// (a launch has fewer than 2^32 threads: 256 for a token, or for 256 columns of eight tokens or more)
+bool bad_embedding(int T, int V, int h) { return T < 0 || T >= (1 << 24) || V < 0 || V >= (1 << 20) || h < 0 || h % 8 || h > 65536 || ((double)T / 8 + 1) * (h / 256 + 1) >= 16777216.0; }
+}  // namespace
+
+rp_status rp_op_embed_fwd(void* stream, const void* table, long ldt, const int* ids, float scale, void* x, long ldx, int T, int V, int h) {
+  if (bad_embedding(T, V, h) || (T && !ids) || !isfinite(scale)) return fail(nullptr, RP_EINVAL, "rp_op_embed_fwd: bad sizes, tokens or scale");
+  if (bad_rows(table, V, h, ldt) || bad_rows(x, T, h, ldx) || (T && h && !table))
+    return fail(nullptr, RP_EINVAL, "rp_op_embed_fwd: tensors missing, not on 16-byte boundaries, or bad strides");
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_embed_fwd(reinterpret_cast<hipStream_t>(stream), static_cast<const bf16*>(table), ldt, ids, scale, static_cast<bf16*>(x), ldx, T, V, h);
+  OP_RET(e);
+}
+
+rp_status rp_op_embed_scratch(int T, int V, int h, size_t* scratch_bytes) {
+  if (!scratch_bytes || bad_embedding(T, V, h)) return fail(nullptr, RP_EINVAL, "rp_op_embed_scratch: bad arguments");
+  *scratch_bytes = k_embed_scratch(T, V, h);
+  return RP_OK;
+}
+
+rp_status rp_op_embed_bwd(void* stream, const void* dx, long lddx, const int* ids, float scale, float* dtable, long lddt, int accumulate, int T, int V, int h,
+                          void* scratch, size_t scratch_bytes) {
+  if (bad_embedding(T, V, h) || (T && !ids) || !isfinite(scale)) return fail(nullptr, RP_EINVAL, "rp_op_embed_bwd: bad sizes, tokens or scale");
+  if (bad_rows(dx, T, h, lddx) || bad_rows(dtable, V, h, lddt)) return fail(nullptr, RP_EINVAL, "rp_op_embed_bwd: tensors missing, not on 16-byte boundaries, or bad strides");
+  const size_t need = V && h && (T || !accumulate) ? k_embed_scratch(T, V, h) : 0;
+  if (need && (!scratch || off16(scratch) || scratch_bytes < need))
+    return fail(nullptr, RP_EINVAL, "rp_op_embed_bwd: scratch holds %zu bytes, %zu needed, on a 16-byte boundary", scratch ? scratch_bytes : 0, need);
+  EmbedGrad p{static_cast<const bf16*>(dx), ids, dtable, lddx, lddt, scale, accumulate != 0, T, V, h};
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_embed_bwd(reinterpret_cast<hipStream_t>(stream), p, scratch);
+  OP_RET(e);
+}
+
+namespace {
+// (512 threads for 64 tokens of 256 channels)
+bool bad_scan(int batch, int seq, int c) {
+  return batch < 0 || seq < 0 || seq > (1 << 30) || c < 0 || c % 8 || c > (1 << 23) || (double)batch * ((double)seq / 64 + 1) * (c / 256 + 1) >= 8388608.0 ||
+         (double)batch * c >= 4294967296.0;
+}
+bool bad_state(const void* p) { return off16(p); }
+}  // namespace
+
+rp_status rp_op_scan_sizes(int batch, int seq, int c, size_t* state_bytes, size_t* scratch_bytes) {
+  if (bad_scan(batch, seq, c)) return fail(nullptr, RP_EINVAL, "rp_op_scan_sizes: bad arguments");
+  size_t n = 0, s = 0;
+  k_scan_sizes(batch, seq, c, &n, &s);
+  if (state_bytes) *state_bytes = n;
+  if (scratch_bytes) *scratch_bytes = s;
+  return RP_OK;
+}
+
+rp_status rp_op_scan_fwd(void* stream, int weight, const void* x, const void* g, void* y, long ldx, long ldg, long ldy, const unsigned char* first, const int* len,
+                         const float* h0, float* last, float* states, int batch, int seq, int c, void* scratch, size_t scratch_bytes) {
+  if (bad_scan(batch, seq, c) || weight < RP_SCAN_PLAIN || weight > RP_SCAN_ENERGY) return fail(nullptr, RP_EINVAL, "rp_op_scan_fwd: bad sizes or weight");
+  const long T = (long)batch * seq;
+  if (bad_rows(x, T, c, ldx) || bad_rows(g, T, c, ldg) || bad_rows(y, T, c, ldy) || bad_state(h0) || bad_state(last) || bad_state(states))
+    return fail(nullptr, RP_EINVAL, "rp_op_scan_fwd: tensors missing, not on 16-byte boundaries, or bad strides");
+  size_t n = 0, need = 0;
+  k_scan_sizes(batch, seq, c, &n, &need);
+  if (need && (!scratch || off16(scratch) || scratch_bytes < need))
+    return fail(nullptr, RP_EINVAL, "rp_op_scan_fwd: scratch holds %zu bytes, %zu needed, on a 16-byte boundary", scratch ? scratch_bytes : 0, need);
+  ScanArgs p{};
+  p.x = static_cast<const bf16*>(x); p.g = static_cast<const bf16*>(g); p.y = static_cast<bf16*>(y); p.ldx = ldx; p.ldg = ldg; p.ldy = ldy;
+  p.first = first; p.len = len; p.h0 = h0; p.last = last; p.states = states; p.batch = batch; p.seq = seq; p.c = c;
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_scan_fwd(reinterpret_cast<hipStream_t>(stream), weight, p, scratch);
+  OP_RET(e);
+}
+
+rp_status rp_op_scan_bwd(void* stream, int weight, const void* x, const void* g, const void* dy, void* dx, void* dg, long ldx, long ldg, long lddy, long lddx,
+                         long lddg, const unsigned char* first, const int* len, const float* states, const float* dlast, float* dh0, int batch, int seq, int c,
+                         void* scratch, size_t scratch_bytes) {
+  if (bad_scan(batch, seq, c) || weight < RP_SCAN_PLAIN || weight > RP_SCAN_ENERGY) return fail(nullptr, RP_EINVAL, "rp_op_scan_bwd: bad sizes or weight");
+  const long T = (long)batch * seq;
+  if (bad_rows(x, T, c, ldx) || bad_rows(g, T, c, ldg) || bad_rows(dy, T, c, lddy) || bad_rows(dx, T, c, lddx) || bad_rows(dg, T, c, lddg) ||
+      (T && c && !states) || bad_state(states) || bad_state(dlast) || bad_state(dh0))
+    return fail(nullptr, RP_EINVAL, "rp_op_scan_bwd: tensors missing, not on 16-byte boundaries, or bad strides");
+  size_t n = 0, need = 0;
+  k_scan_sizes(batch, seq, c, &n, &need);
+  if (need && (!scratch || off16(scratch) || scratch_bytes < need))
+    return fail(nullptr, RP_EINVAL, "rp_op_scan_bwd: scratch holds %zu bytes, %zu needed, on a 16-byte boundary", scratch ? scratch_bytes : 0, need);
+  ScanArgs p{};
+  p.x = static_cast<const bf16*>(x); p.g = static_cast<const bf16*>(g); p.dy = static_cast<const bf16*>(dy); p.dx = static_cast<bf16*>(dx); p.dg = static_cast<bf16*>(dg);
+  p.ldx = ldx; p.ldg = ldg; p.lddy = lddy; p.lddx = lddx; p.lddg = lddg;
+  p.first = first; p.len = len; p.states = const_cast<float*>(states); p.dlast = dlast; p.dh0 = dh0; p.batch = batch; p.seq = seq; p.c = c;
+  StreamDevice on(reinterpret_cast<hipStream_t>(stream));
+  if (on.err != hipSuccess) OP_RET(on.err);
+  const hipError_t e = k_scan_bwd(reinterpret_cast<hipStream_t>(stream), weight, p, scratch);
   OP_RET(e);
 }
 
