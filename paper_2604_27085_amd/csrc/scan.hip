@@ -61,6 +61,11 @@ RP_DEV void load_rows(const bf16* base, long ld, const Place& s, int seq, uint2 
     if (s.in && s.t0 + i < s.len) r[i] = *reinterpret_cast<const uint2*>(src + i * ld);
   }
 }
+// The gates are made again from g for every use: kept from one to the next they would be the registers of half of the waves (244 instead of 110 for the backward kernel).
+RP_DEV void forget(uint2 (&r)[TOK]) {
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) asm volatile("" : "+v"(r[i].x), "+v"(r[i].y));
+}
 // bit i: token t0 + i begins a document
 RP_DEV uint32_t load_first(const ScanArgs& p, const Place& s) {
   uint32_t m = 0;
@@ -73,27 +78,24 @@ RP_DEV uint32_t load_first(const ScanArgs& p, const Place& s) {
   return m;
 }
 
-// The map of a wave's eight tokens, forwards (state) or backwards (mu).
+// The map of a wave's eight tokens, forwards (state) or backwards (mu).  A token behind the length has the map (1, 0); what decides is the same in all lanes, so the
+// selects cost less than branches around the registers that the tokens are in.
 template <int W>
 RP_DEV void wave_map(const uint2 (&gr)[TOK], const uint2 (&xr)[TOK], uint32_t first, const Place& s, f4& A, f4& B) {
   A = f4{1.f, 1.f, 1.f, 1.f};
   B = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
-    if (s.t0 + i >= s.len) break;      // uniform
+    const bool live = s.t0 + i < s.len, begins = first >> i & 1;
     const f4 g = unpack(gr[i]), x = unpack(xr[i]);
 #pragma unroll
     for (int e = 0; e < LANES; ++e) {
       float f, r;
       gates(g[e], f, r);
       const float u = weight<W>(f, r) * x[e];
-      if (first >> i & 1) {
-        A[e] = 0.f;
-        B[e] = u;
-      } else {
-        A[e] *= f;
-        B[e] = __builtin_fmaf(f, B[e], u);
-      }
+      const float a = begins ? 0.f : A[e] * f, b = begins ? u : __builtin_fmaf(f, B[e], u);
+      A[e] = live ? a : A[e];
+      B[e] = live ? b : B[e];
     }
   }
 }
@@ -101,19 +103,17 @@ RP_DEV void wave_map_back(const uint2 (&gr)[TOK], const uint2 (&dyr)[TOK], uint3
   A = f4{1.f, 1.f, 1.f, 1.f};
   B = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = TOK - 1; i >= 0; --i) {
-    if (s.t0 + i >= s.len) continue;      // uniform
+  for (int j = 0; j < TOK; ++j) {
+    const int i = TOK - 1 - j;
+    const bool live = s.t0 + i < s.len, begins = first >> i & 1;
     const f4 g = unpack(gr[i]), dy = unpack(dyr[i]);
 #pragma unroll
     for (int e = 0; e < LANES; ++e) {
       float f, r;
       gates(g[e], f, r);
-      if (first >> i & 1) {
-        A[e] = B[e] = 0.f;
-      } else {
-        A[e] *= f;
-        B[e] = f * (dy[e] + B[e]);
-      }
+      const float a = begins ? 0.f : A[e] * f, b = begins ? 0.f : f * (dy[e] + B[e]);
+      A[e] = live ? a : A[e];
+      B[e] = live ? b : B[e];
     }
   }
 }
@@ -227,26 +227,23 @@ __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p, con
   bf16* const out = p.y + ((long)s.b * p.seq + s.t0) * p.ldy + s.ch;
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
-    if (s.t0 + i >= p.seq) break;      // uniform
-    uint2 y = make_uint2(0u, 0u);
-    if (s.t0 + i < s.len) {
-      const f4 g = unpack(gr[i]), x = unpack(xr[i]);
+    const bool live = s.t0 + i < s.len, begins = first >> i & 1;
+    const f4 g = unpack(gr[i]), x = unpack(xr[i]);
 #pragma unroll
-      for (int e = 0; e < LANES; ++e) {
-        float f, r;
-        gates(g[e], f, r);
-        const float u = weight<W>(f, r) * x[e];
-        h[e] = first >> i & 1 ? u : __builtin_fmaf(f, h[e], u);
-      }
-      y = pack(h);
+    for (int e = 0; e < LANES; ++e) {
+      float f, r;
+      gates(g[e], f, r);
+      const float u = weight<W>(f, r) * x[e];
+      const float next = begins ? u : __builtin_fmaf(f, h[e], u);
+      h[e] = live ? next : h[e];
     }
-    if (s.in) *reinterpret_cast<uint2*>(out + i * p.ldy) = y;
+    if (s.in && s.t0 + i < p.seq) *reinterpret_cast<uint2*>(out + i * p.ldy) = live ? pack(h) : make_uint2(0u, 0u);
   }
   if (ONE && p.last && s.w == NW - 1 && s.in) *reinterpret_cast<f4*>(p.last + (long)s.b * p.c + s.ch) = h;      // (waves without tokens pass the state on)
 }
 
 template <int W, bool ONE>
-__global__ void __launch_bounds__(64 * NW) scan_bwd_kernel(const ScanArgs p, const float* carry) {
+__global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p, const float* carry) {
   __shared__ f4 As[NW][64], Bs[NW][64], Ab[NW][64], Bb[NW][64];
   const Place s(p);
   uint2 gr[TOK], xr[TOK], dyr[TOK];
@@ -260,46 +257,49 @@ __global__ void __launch_bounds__(64 * NW) scan_bwd_kernel(const ScanArgs p, con
   wave_map<W>(gr, xr, first, s, A, B);
   As[s.w][s.lane] = A;
   Bs[s.w][s.lane] = B;
+  forget(gr);
   wave_map_back(gr, dyr, first, s, A, B);
   Ab[s.w][s.lane] = A;
   Bb[s.w][s.lane] = B;
   __syncthreads();
   h = enter<false>(As, Bs, s, h);
   mu = enter<true>(Ab, Bb, s, mu);
+  forget(gr);
   f4 before[TOK];      // h_(t-1), 0 where a document begins
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
-    before[i] = f4{0.f, 0.f, 0.f, 0.f};
-    if (s.t0 + i >= s.len) continue;
+    const bool live = s.t0 + i < s.len, begins = first >> i & 1;
     const f4 g = unpack(gr[i]), x = unpack(xr[i]);
 #pragma unroll
     for (int e = 0; e < LANES; ++e) {
       float f, r;
       gates(g[e], f, r);
       const float u = weight<W>(f, r) * x[e];
-      before[i][e] = first >> i & 1 ? 0.f : h[e];
-      h[e] = first >> i & 1 ? u : __builtin_fmaf(f, h[e], u);
+      before[i][e] = begins ? 0.f : h[e];
+      const float next = begins ? u : __builtin_fmaf(f, h[e], u);
+      h[e] = live ? next : h[e];
     }
   }
+  forget(gr);
   bf16* const dx = p.dx + ((long)s.b * p.seq + s.t0) * p.lddx + s.ch;
   bf16* const dg = p.dg + ((long)s.b * p.seq + s.t0) * p.lddg + s.ch;
 #pragma unroll
-  for (int i = TOK - 1; i >= 0; --i) {
-    if (s.t0 + i >= p.seq) continue;      // uniform
-    f4 gx = {0.f, 0.f, 0.f, 0.f}, gg = gx;
-    if (s.t0 + i < s.len) {
-      const f4 g = unpack(gr[i]), x = unpack(xr[i]), dy = unpack(dyr[i]);
+  for (int j = 0; j < TOK; ++j) {
+    const int i = TOK - 1 - j;
+    const bool live = s.t0 + i < s.len, begins = first >> i & 1;
+    const f4 g = unpack(gr[i]), x = unpack(xr[i]), dy = unpack(dyr[i]);
+    f4 gx, gg;
 #pragma unroll
-      for (int e = 0; e < LANES; ++e) {
-        float f, r;
-        gates(g[e], f, r);
-        const float lam = dy[e] + mu[e];
-        gx[e] = weight<W>(f, r) * lam;
-        gg[e] = lam * (before[i][e] * (f * r) + x[e] * weight_slope<W>(f, r));
-        mu[e] = first >> i & 1 ? 0.f : f * lam;
-      }
+    for (int e = 0; e < LANES; ++e) {
+      float f, r;
+      gates(g[e], f, r);
+      const float lam = dy[e] + mu[e];
+      gx[e] = live ? weight<W>(f, r) * lam : 0.f;
+      gg[e] = live ? lam * (before[i][e] * (f * r) + x[e] * weight_slope<W>(f, r)) : 0.f;
+      const float next = begins ? 0.f : f * lam;
+      mu[e] = live ? next : mu[e];
     }
-    if (s.in) {
+    if (s.in && s.t0 + i < p.seq) {
       *reinterpret_cast<uint2*>(dx + i * p.lddx) = pack(gx);
       *reinterpret_cast<uint2*>(dg + i * p.lddg) = pack(gg);
     }

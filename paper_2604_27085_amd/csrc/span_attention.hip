@@ -776,18 +776,13 @@ RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, c
   }
 }
 
-// The row tiles that see any of a workgroup's keys: which they are (tiles between the first and the last may see none), found by all threads together.
+// The row tiles that see any of a workgroup's keys, one after the other (tiles between the first and the last may see none).  What 64 neighbouring tiles see is asked for at
+// once, a tile a lane, and kept as two masks: a load on the way to every tile would be waited for.
 struct RowRange {
   const int4* tiles;
   int k0, k1, first, last;      // [first, last)
-  RP_DEV bool any(int u) const {
-    const int4 v = tiles[u];
-    return k0 < v.y && k1 > v.x;
-  }
-  RP_DEV bool all(int u) const {
-    const int4 v = tiles[u];
-    return v.z <= k0 && v.w >= k1;
-  }
+  int base, u, end;             // the masks' first tile; the present tile
+  unsigned long long any, all;
   template <int NT>
   RP_DEV void find(const SpanArgs& p, const Rows& s, int key0, int* lds /* [2 NT / 64] */, int tid) {
     const int n = (s.total + 63) / 64;
@@ -795,11 +790,13 @@ struct RowRange {
     k0 = key0;
     k1 = min(key0 + 128, p.seq_kv);
     int lo = 0x7fffffff, hi = 0;
-    for (int u = tid; u < n; u += NT)
-      if (any(u)) {
-        lo = min(lo, u);
-        hi = u + 1;
+    for (int t = tid; t < n; t += NT) {
+      const int4 v = tiles[t];
+      if (k0 < v.y && k1 > v.x) {
+        lo = min(lo, t);
+        hi = t + 1;
       }
+    }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       lo = min(lo, __shfl_xor(lo, o, 64));
@@ -818,10 +815,37 @@ struct RowRange {
     first = __builtin_amdgcn_readfirstlane(hi > 0 ? lo : 0);
     last = __builtin_amdgcn_readfirstlane(hi);
   }
-  // the next tile from u on that sees any key, or `end`
-  RP_DEV int next(int u, int end) const {
-    while (u < end && !any(u)) ++u;
-    return u;
+  RP_DEV void look(int from, int lane) {
+    base = from;
+    const int t = min(from + lane, end - 1);
+    const int4 v = tiles[t];
+    any = __ballot(from + lane < end && k0 < v.y && k1 > v.x);
+    all = __ballot(v.z <= k0 && v.w >= k1);
+  }
+  RP_DEV void settle(int lane) {      // to the present tile or the next one that sees any key; u = end: no more
+    while (u < end) {
+      if (u >= base + 64) look(u, lane);
+      const unsigned long long m = any >> (u - base);
+      if (m) {
+        u += __builtin_ctzll(m);
+        return;
+      }
+      u = base + 64;
+    }
+    u = end;
+  }
+  RP_DEV void start(int from, int to, int lane) {      // [from, to)
+    u = from;
+    end = to;
+    base = from - 64;
+    any = all = 0;
+    settle(lane);
+  }
+  RP_DEV bool more() const { return u < end; }
+  RP_DEV bool whole() const { return all >> (u - base) & 1; }      // every row of the present tile sees all of the keys
+  RP_DEV void next(int lane) {
+    ++u;
+    settle(lane);
   }
 };
 
@@ -884,11 +908,10 @@ __global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
     RowTile<D, 256>::load(qreg, doreg, s, qb, p.ldq, dob, p.lddo, u * 64, tid);
     rstat.load(p, s, u * 64, lane, w);
   };
-  int u = range.next(u0, u1);
-  if (u < u1) prefetch(u);
-  while (u < u1) {
-    const bool whole = range.all(u);
-    const int after = range.next(u + 1, u1);
+  range.start(u0, u1, lane);
+  if (range.more()) prefetch(range.u);
+  while (range.more()) {
+    const bool whole = range.whole();
     __syncthreads();
     if (!whole) {
       make_finite(qreg);
@@ -898,7 +921,8 @@ __global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
     T64::template store<LD>(doreg, dOs, tid);
     rstat.store(stat, p, kv0, lane, w);
     __syncthreads();
-    if (after < u1) prefetch(after);
+    range.next(lane);
+    if (range.more()) prefetch(range.u);
     // the two 32-row halves of the tile one after the other: half as many score registers live at a time
 #pragma unroll
     for (int t2 = 0; t2 < 2; ++t2) {
@@ -952,7 +976,6 @@ __global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
         }
       }
     }
-    u = after;
   }
   __syncthreads();
   const long tok0 = (long)s.b * p.seq_kv;
@@ -1031,8 +1054,8 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
     RowTile<D, 512>::load(qreg, doreg, s, qb, p.ldq, dob, p.lddo, u * 64, tid);
     rstat.load(p, s, u * 64, lane, w8);
   };
-  int u = range.next(u0, u1);
-  if (u < u1) prefetch(u);
+  range.start(u0, u1, lane);
+  if (range.more()) prefetch(range.u);
 
   constexpr int AHEAD = 2;     // two waves per SIMD cover each other's LDS latency: a short ring is enough
   auto update_half = [&](int set, int t2, const uint4 (&pf)[2], const uint4 (&df)[2]) {
@@ -1064,9 +1087,8 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
     update_half(prev & 1, h ^ 1, ppf, pdf);
   };
   int i = 0;
-  for (; u < u1; ++i) {
-    const bool whole = range.all(u);
-    const int after = range.next(u + 1, u1);
+  for (; range.more(); ++i) {
+    const bool whole = range.whole();
     __syncthreads();
     bf16* const q_set = smem + (i & 1) * TSET;
     float* const st_set = stat + (i & 1) * Stat::FLOATS;
@@ -1079,7 +1101,8 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
     rstat.store(st_set, p, kv0, lane, w8);
     if (i > 0) partner_update(i - 1);
     __syncthreads();
-    if (after < u1) prefetch(after);
+    range.next(lane);
+    if (range.more()) prefetch(range.u);
     f32x4 z[2][2], dp[2][2], z0[2], dp0[2];      // [16 rows][16 keys]; what they start from
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
@@ -1113,7 +1136,6 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
     // the partner read last tile's fragments before the barrier above: the slots are free
     ex_mine[0] = pfg[0]; ex_mine[64] = pfg[1]; ex_mine[128] = dfg[0]; ex_mine[192] = dfg[1];
     update_half(i & 1, h, pfg, dfg);
-    u = after;
   }
   __syncthreads();
   if (i > 0) partner_update(i - 1);
