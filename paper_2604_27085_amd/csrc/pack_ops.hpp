@@ -50,8 +50,8 @@ struct ScanArgs {
   float* states;                   // [batch, chunks, c]: the state that every chunk starts from; written by the forward call, or NULL
   int batch, seq, c;
   int chunks, blocks;              // from here on set by the launcher; blocks: of channels
-  float2* agg;
-  float* carry;
+  unsigned* counter;
+  unsigned long long* words;       // [batch, chunks, c]
 };
 void k_scan_sizes(int batch, int seq, int c, size_t* states, size_t* scratch);
 hipError_t k_scan_fwd(hipStream_t st, int weight, const ScanArgs& p, void* scratch);

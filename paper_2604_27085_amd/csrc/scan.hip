@@ -7,9 +7,12 @@
 // 1 - f is taken as sigmoid(-g): a gate near one keeps its distance from it.
 //
 // h_t = a_t h_(t-1) + b_t is a scan over the maps (a, b), which compose as (a2, b2) after (a1, b1) = (a2 a1, a2 b1 + b2).  Chunks of 64 tokens by 256 channels; a wave
-// has eight tokens, a lane four channels, all in registers.  One launch makes every chunk's map, one the state that each starts from, one the outputs.  The backward
-// pass is the same from behind; h_(t-1) is made again from the states that the forward pass left, in fp32 (4 bytes for 64 tokens), not from y, which is rounded.
-// States, sums and products are fp32 throughout.
+// has eight tokens, a lane four channels, all in registers, so every input is read once: a workgroup makes its chunk's map, publishes it, finds out what its chunk starts from, and writes
+// the outputs.  That it finds by looking back over the chunks before: from the nearest one whose end state is there, through the maps of those in between.  Workgroups take their
+// chunks in order of time by a counter, so whoever waits waits for workgroups that have started and that wait only for earlier ones; the first waits for none.  A
+// chunk's end state is the same sequence of operations wherever the looking ended: the results do not depend on timing.
+// The backward pass is the same from behind; h_(t-1) is made again from the states that the forward pass left, in fp32 (4 bytes for 64 tokens), not from y, which is
+// rounded.  States, sums and products are fp32 throughout.
 #include "pack_ops.hpp"
 
 namespace {
@@ -34,17 +37,18 @@ RP_DEV float weight(float f, float r) { return W == 0 ? 1.f : W == 1 ? r : __bui
 template <int W>
 RP_DEV float weight_slope(float f, float r) { return W == 0 ? 0.f : W == 1 ? -f * r : -f * f * __builtin_amdgcn_sqrtf(r * __builtin_amdgcn_rcpf(1.f + f)); }
 
-// A workgroup's place: the channels change fastest, so that workgroups side by side read neighbouring pieces of the same rows.
+// A workgroup's place: the channels change fastest, so that workgroups side by side read neighbouring pieces of the same rows, and time slowest.
 struct Place {
   int b, chunk, ch, tid, lane, w, t0, len;      // t0: the wave's first token
   bool in;
-  RP_DEV Place(const ScanArgs& p) {
+  RP_DEV Place(const ScanArgs& p, int id, bool back) {
     tid = threadIdx.x;
     lane = tid & 63;
     w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int rest = (int)(blockIdx.x / (unsigned)p.blocks), cb = (int)blockIdx.x - rest * p.blocks;
-    b = rest / p.chunks;
-    chunk = rest - b * p.chunks;
+    const int rest = id / p.blocks, cb = id - rest * p.blocks;
+    chunk = rest / p.batch;
+    b = rest - chunk * p.batch;
+    if (back) chunk = p.chunks - 1 - chunk;
     ch = cb * BLOCK_CH + LANES * lane;
     in = ch < p.c;
     t0 = chunk * CHUNK + w * TOK;
@@ -122,70 +126,105 @@ RP_DEV void wave_map_back(const uint2 (&gr)[TOK], const uint2 (&dyr)[TOK], uint3
 // reach every document behind it.
 RP_DEV float through(float a, float b, float h) { return a == 0.f ? b : __builtin_fmaf(a, h, b); }
 
-// ------------------------------------------------------------------------------------------------ the chunks' maps
-template <int W, bool BACK>
-__global__ void __launch_bounds__(64 * NW) scan_map_kernel(const ScanArgs p) {
-  __shared__ f4 As[NW][64], Bs[NW][64];
-  const Place s(p);
-  uint2 gr[TOK], xr[TOK];
-  load_rows(p.g, p.ldg, s, p.seq, gr);
-  if (BACK) load_rows(p.dy, p.lddy, s, p.seq, xr);
-  else load_rows(p.x, p.ldx, s, p.seq, xr);
-  const uint32_t first = load_first(p, s);
-  f4 A, B;
-  if (BACK) wave_map_back(gr, xr, first, s, A, B);
-  else wave_map<W>(gr, xr, first, s, A, B);
-  As[s.w][s.lane] = A;
-  Bs[s.w][s.lane] = B;
-  __syncthreads();
-  if (s.w != 0 || !s.in) return;
-#pragma unroll
-  for (int i = 1; i < NW; ++i) {
-    const int u = BACK ? NW - 1 - i : i;
-    if (i == 1) {
-      A = As[BACK ? NW - 1 : 0][s.lane];
-      B = Bs[BACK ? NW - 1 : 0][s.lane];
-    }
-    const f4 a = As[u][s.lane], b = Bs[u][s.lane];
-#pragma unroll
-    for (int e = 0; e < LANES; ++e) {
-      A[e] = a[e] == 0.f ? 0.f : A[e] * a[e];
-      B[e] = through(a[e], b[e], B[e]);
-    }
-  }
-  float4* const out = reinterpret_cast<float4*>(p.agg + s.at(p));
-  out[0] = make_float4(A[0], B[0], A[1], B[1]);
-  out[1] = make_float4(A[2], B[2], A[3], B[3]);
-}
+// ------------------------------------------------------------------------------------------------ between chunks
+// What a chunk tells the ones behind it of a channel, 64 bits that are written and read at once: nothing yet (0); its map: b, and a (0 .. 1, or NaN) with the sign bit
+// set; or its end state, with all bits set above it.
+typedef unsigned long long word_t;
+constexpr uint32_t STATE = 0xffffffffu;
+RP_DEV word_t map_word(float a, float b) { return (word_t)((a != a ? 0x7fc00000u : __float_as_uint(a)) | 0x80000000u) << 32 | __float_as_uint(b); }
+RP_DEV word_t state_word(float h) { return (word_t)STATE << 32 | __float_as_uint(h); }
+RP_DEV void publish(word_t* at, word_t w) { __hip_atomic_store(at, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+RP_DEV word_t look(const word_t* at) { return __hip_atomic_load(const_cast<word_t*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// What every chunk starts from: a thread takes a channel, chunk by chunk.
+// What a chunk starts from, for all waves of its workgroup.  Wave 0 publishes the chunk's map; every wave then waits for one of the eight chunks before and puts what it says into
+// LDS, and all of them go from the nearest end state through the maps behind it.  Where none of the eight has its end state yet, they look again.
+// `given`: the state before the first chunk (behind the last one, BACK); end: wave 0's, the chunk's own end state.
+struct Looks {
+  f4 a[NW][64], b[NW][64];
+  int state[NW];
+};
 template <bool BACK>
-__global__ void __launch_bounds__(64) scan_carry_kernel(const ScanArgs p, float* carry) {
-  constexpr int AHEAD = 16;
-  const long i = (long)blockIdx.x * 64 + threadIdx.x;
-  if (i >= (long)p.batch * p.c) return;
-  const int b = (int)(i / p.c), ch = (int)(i - (long)b * p.c);
-  const float* const start = BACK ? p.dlast : p.h0;
-  float h = start ? start[i] : 0.f;
-  const long base = (long)b * p.chunks * p.c + ch;
-  for (int k0 = 0; k0 < p.chunks; k0 += AHEAD) {
-    float2 m[AHEAD];
+RP_DEV f4 start_of(const ScanArgs& p, const Place& s, const f4 (&As)[NW][64], const f4 (&Bs)[NW][64], Looks& looks, const f4& given, f4& end) {
+  const int before = BACK ? p.chunks - 1 - s.chunk : s.chunk;
+  word_t* const mine = p.words + (s.in ? s.at(p) : 0);
+  f4 A = As[BACK ? NW - 1 : 0][s.lane], B = Bs[BACK ? NW - 1 : 0][s.lane];
+  if (s.w == 0) {
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      const int k = min(k0 + j, p.chunks - 1);
-      m[j] = p.agg[base + (long)(BACK ? p.chunks - 1 - k : k) * p.c];
+    for (int i = 1; i < NW; ++i) {
+      const int u = BACK ? NW - 1 - i : i;
+      const f4 a = As[u][s.lane], b = Bs[u][s.lane];
+#pragma unroll
+      for (int e = 0; e < LANES; ++e) {
+        A[e] = a[e] == 0.f ? 0.f : A[e] * a[e];
+        B[e] = through(a[e], b[e], B[e]);
+      }
     }
+    if (before > 0 && s.in)
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      const int k = k0 + j;
-      if (k < p.chunks) {
-        carry[base + (long)(BACK ? p.chunks - 1 - k : k) * p.c] = h;
-        h = through(m[j].x, m[j].y, h);
+      for (int e = 0; e < LANES; ++e) publish(mine + e, map_word(A[e], B[e]));
+  }
+  f4 h = given;
+  if (before > 0) {      // uniform over the workgroup
+    const word_t* const theirs = mine + (BACK ? 1 : -1) * (long)(s.w + 1) * p.c;
+    int from;
+    for (;;) {
+      bool state = false;
+      if (s.w < before) {
+        word_t w[LANES];
+        for (;;) {      // ends: that chunk's workgroup took its place before this one
+          bool there = true;
+          state = true;
+#pragma unroll
+          for (int e = 0; e < LANES; ++e) {
+            w[e] = s.in ? look(theirs + e) : state_word(0.f);
+            there = there && (uint32_t)(w[e] >> 32) != 0u;
+            state = state && (uint32_t)(w[e] >> 32) == STATE;
+          }
+          if (__all(there)) break;
+          __builtin_amdgcn_s_sleep(1);
+        }
+        f4 a, b;
+#pragma unroll
+        for (int e = 0; e < LANES; ++e) {
+          a[e] = __uint_as_float((uint32_t)(w[e] >> 32));
+          b[e] = __uint_as_float((uint32_t)w[e]);
+        }
+        looks.a[s.w][s.lane] = a;
+        looks.b[s.w][s.lane] = b;
+        state = __all(state);
+      }
+      if (s.lane == 0) looks.state[s.w] = state;
+      __syncthreads();
+      from = -1;
+#pragma unroll
+      for (int i = NW - 1; i >= 0; --i)
+        if (looks.state[i]) from = i;
+      if (__builtin_amdgcn_readfirstlane(from) >= 0) break;
+      __syncthreads();      // all have seen that there is none
+      __builtin_amdgcn_s_sleep(4);
+    }
+    from = __builtin_amdgcn_readfirstlane(from);
+    for (int i = from; i >= 0; --i) {
+      const f4 a = looks.a[i][s.lane], b = looks.b[i][s.lane];
+#pragma unroll
+      for (int e = 0; e < LANES; ++e) {
+        const uint32_t hi = __float_as_uint(a[e]);
+        h[e] = hi == STATE ? b[e] : through(__uint_as_float(hi & 0x7fffffffu), b[e], h[e]);
       }
     }
   }
-  float* const end = BACK ? p.dh0 : p.last;
-  if (end) end[i] = h;
+  if (s.w == 0) {
+#pragma unroll
+    for (int e = 0; e < LANES; ++e) {
+      end[e] = through(A[e], B[e], h[e]);
+      if (s.in) publish(mine + e, state_word(end[e]));
+    }
+  }
+  return h;
+}
+
+__global__ void __launch_bounds__(256) scan_clear_kernel(uint4* to, long n) {
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) to[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // ------------------------------------------------------------------------------------------------ outputs
@@ -202,29 +241,47 @@ RP_DEV f4 enter(const f4 (&As)[NW][64], const f4 (&Bs)[NW][64], const Place& s, 
 }
 // ONE: a sequence is one chunk, which starts from the call's own state
 template <bool ONE>
-RP_DEV f4 chunk_start(const ScanArgs& p, const Place& s, const float* carry, const float* given) {
-  const float* const src = ONE ? given : carry;
-  if (!src || !s.in) return f4{0.f, 0.f, 0.f, 0.f};
-  return *reinterpret_cast<const f4*>(src + (ONE ? (long)s.b * p.c + s.ch : s.at(p)));
+RP_DEV int take_place(const ScanArgs& p, int* lds) {
+  if (ONE) return (int)blockIdx.x;
+  if (threadIdx.x == 0) *lds = (int)atomicAdd(p.counter, 1u);
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(*lds);
+}
+RP_DEV f4 given_state(const float* src, const ScanArgs& p, const Place& s) {
+  return src && s.in ? *reinterpret_cast<const f4*>(src + (long)s.b * p.c + s.ch) : f4{0.f, 0.f, 0.f, 0.f};
+}
+// What the chunk starts from; the waves have put their maps into LDS.  The state behind the last chunk goes to `last`.
+template <bool ONE, bool BACK>
+RP_DEV f4 chunk_start(const ScanArgs& p, const Place& s, const f4 (&As)[NW][64], const f4 (&Bs)[NW][64], Looks* looks, const float* given, float* last) {
+  f4 h = given_state(given, p, s);
+  if constexpr (!ONE) {
+    f4 end;
+    h = start_of<BACK>(p, s, As, Bs, *looks, h, end);
+    if (last && s.w == 0 && s.in && s.chunk == (BACK ? 0 : p.chunks - 1)) *reinterpret_cast<f4*>(last + (long)s.b * p.c + s.ch) = end;
+  }
+  return h;
 }
 
 template <int W, bool ONE>
-__global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p, const float* carry) {
+__global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p) {
   __shared__ f4 As[NW][64], Bs[NW][64];
-  const Place s(p);
+  __shared__ Looks looks;
+  __shared__ int place;
+  const Place s(p, take_place<ONE>(p, &place), false);
   uint2 gr[TOK], xr[TOK];
   load_rows(p.g, p.ldg, s, p.seq, gr);
   load_rows(p.x, p.ldx, s, p.seq, xr);
   const uint32_t first = load_first(p, s);
-  const f4 start = chunk_start<ONE>(p, s, carry, p.h0);
   f4 A, B;
   wave_map<W>(gr, xr, first, s, A, B);
   As[s.w][s.lane] = A;
   Bs[s.w][s.lane] = B;
   __syncthreads();
+  const f4 start = chunk_start<ONE, false>(p, s, As, Bs, &looks, p.h0, p.last);
   f4 h = enter<false>(As, Bs, s, start);
-  if (ONE && s.in && s.w == 0 && p.states && p.seq > 0) *reinterpret_cast<f4*>(p.states + s.at(p)) = start;
+  if (s.in && s.w == 0 && p.states && p.seq > 0) *reinterpret_cast<f4*>(p.states + s.at(p)) = start;
   bf16* const out = p.y + ((long)s.b * p.seq + s.t0) * p.ldy + s.ch;
+  forget(gr);
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
     const bool live = s.t0 + i < s.len, begins = first >> i & 1;
@@ -243,16 +300,17 @@ __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p, con
 }
 
 template <int W, bool ONE>
-__global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p, const float* carry) {
+__global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p) {
   __shared__ f4 As[NW][64], Bs[NW][64], Ab[NW][64], Bb[NW][64];
-  const Place s(p);
+  __shared__ Looks looks;
+  __shared__ int place;
+  const Place s(p, take_place<ONE>(p, &place), true);
   uint2 gr[TOK], xr[TOK], dyr[TOK];
   load_rows(p.g, p.ldg, s, p.seq, gr);
-  load_rows(p.x, p.ldx, s, p.seq, xr);
   load_rows(p.dy, p.lddy, s, p.seq, dyr);
+  load_rows(p.x, p.ldx, s, p.seq, xr);
   const uint32_t first = load_first(p, s);
   f4 h = s.in && p.seq > 0 ? *reinterpret_cast<const f4*>(p.states + s.at(p)) : f4{0.f, 0.f, 0.f, 0.f};
-  f4 mu = chunk_start<ONE>(p, s, carry, p.dlast);
   f4 A, B;
   wave_map<W>(gr, xr, first, s, A, B);
   As[s.w][s.lane] = A;
@@ -262,9 +320,11 @@ __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p, 
   Ab[s.w][s.lane] = A;
   Bb[s.w][s.lane] = B;
   __syncthreads();
+  f4 mu = chunk_start<ONE, true>(p, s, Ab, Bb, &looks, p.dlast, p.dh0);
   h = enter<false>(As, Bs, s, h);
   mu = enter<true>(Ab, Bb, s, mu);
   forget(gr);
+  forget(xr);
   f4 before[TOK];      // h_(t-1), 0 where a document begins
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
@@ -281,6 +341,8 @@ __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p, 
     }
   }
   forget(gr);
+  forget(xr);
+  forget(dyr);
   bf16* const dx = p.dx + ((long)s.b * p.seq + s.t0) * p.lddx + s.ch;
   bf16* const dg = p.dg + ((long)s.b * p.seq + s.t0) * p.lddg + s.ch;
 #pragma unroll
@@ -308,66 +370,44 @@ __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p, 
 }
 
 int chunks_of(int seq) { return (seq + CHUNK - 1) / CHUNK; }
+// The counter, and a word for every channel of every chunk.
+size_t scratch_bytes(int batch, int chunks, int c) { return chunks > 1 ? 16 + 8 * (size_t)batch * chunks * c : 0; }
 
 template <int W>
-hipError_t fwd(hipStream_t st, const ScanArgs& p, float* carry) {
+void enqueue(hipStream_t st, const ScanArgs& p, bool back) {
   const dim3 grid((unsigned)p.batch * p.chunks * p.blocks), block(64 * NW);
-  if (p.chunks == 1) {
-    RP_LAUNCH((scan_fwd_kernel<W, true>), grid, block, 0, st, p, carry);
-    return hipGetLastError();
+  if (back) {
+    if (p.chunks == 1) RP_LAUNCH((scan_bwd_kernel<W, true>), grid, block, 0, st, p);
+    else RP_LAUNCH((scan_bwd_kernel<W, false>), grid, block, 0, st, p);
+  } else {
+    if (p.chunks == 1) RP_LAUNCH((scan_fwd_kernel<W, true>), grid, block, 0, st, p);
+    else RP_LAUNCH((scan_fwd_kernel<W, false>), grid, block, 0, st, p);
   }
-  RP_LAUNCH((scan_map_kernel<W, false>), grid, block, 0, st, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  RP_LAUNCH((scan_carry_kernel<false>), dim3((unsigned)(((long)p.batch * p.c + 63) / 64)), dim3(64), 0, st, p, carry);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  RP_LAUNCH((scan_fwd_kernel<W, false>), grid, block, 0, st, p, carry);
-  return hipGetLastError();
 }
-template <int W>
-hipError_t bwd(hipStream_t st, const ScanArgs& p, float* carry) {
-  const dim3 grid((unsigned)p.batch * p.chunks * p.blocks), block(64 * NW);
-  if (p.chunks == 1) {
-    RP_LAUNCH((scan_bwd_kernel<W, true>), grid, block, 0, st, p, carry);
-    return hipGetLastError();
+
+hipError_t run(hipStream_t st, int weight, ScanArgs p, void* scratch, bool back) {
+  p.chunks = p.seq ? chunks_of(p.seq) : 1;      // without tokens the state is passed on
+  p.blocks = (p.c + BLOCK_CH - 1) / BLOCK_CH;
+  if (p.batch == 0 || p.c == 0) return hipSuccess;
+  if (p.chunks > 1) {
+    p.counter = static_cast<unsigned*>(scratch);
+    p.words = reinterpret_cast<unsigned long long*>(static_cast<char*>(scratch) + 16);
+    const long n = (long)(scratch_bytes(p.batch, p.chunks, p.c) / 16);      // (c is even)
+    const long blocks = (n + 1023) / 1024;
+    RP_LAUNCH(scan_clear_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, st, static_cast<uint4*>(scratch), n);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  RP_LAUNCH((scan_map_kernel<W, true>), grid, block, 0, st, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  RP_LAUNCH((scan_carry_kernel<true>), dim3((unsigned)(((long)p.batch * p.c + 63) / 64)), dim3(64), 0, st, p, carry);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  RP_LAUNCH((scan_bwd_kernel<W, false>), grid, block, 0, st, p, carry);
+  weight == 0 ? enqueue<0>(st, p, back) : weight == 1 ? enqueue<1>(st, p, back) : enqueue<2>(st, p, back);
   return hipGetLastError();
 }
 
 }  // namespace
 
 void k_scan_sizes(int batch, int seq, int c, size_t* states, size_t* scratch) {
-  const size_t n = (size_t)batch * chunks_of(seq) * c;
-  *states = 4 * n;
-  *scratch = chunks_of(seq) > 1 ? 12 * n : 0;
+  *states = 4 * (size_t)batch * chunks_of(seq) * c;
+  *scratch = scratch_bytes(batch, chunks_of(seq), c);
 }
 
-hipError_t k_scan_fwd(hipStream_t st, int weight, const ScanArgs& args, void* scratch) {
-  ScanArgs p = args;
-  p.chunks = p.seq ? chunks_of(p.seq) : 1;      // without tokens the state is passed on
-  p.blocks = (p.c + BLOCK_CH - 1) / BLOCK_CH;
-  if (p.batch == 0 || p.c == 0) return hipSuccess;
-  const size_t n = (size_t)p.batch * p.chunks * p.c;
-  p.agg = static_cast<float2*>(scratch);
-  float* const carry = p.states ? p.states : reinterpret_cast<float*>(p.agg + n);
-  return weight == 0 ? fwd<0>(st, p, carry) : weight == 1 ? fwd<1>(st, p, carry) : fwd<2>(st, p, carry);
-}
-
-hipError_t k_scan_bwd(hipStream_t st, int weight, const ScanArgs& args, void* scratch) {
-  ScanArgs p = args;
-  p.chunks = p.seq ? chunks_of(p.seq) : 1;
-  p.blocks = (p.c + BLOCK_CH - 1) / BLOCK_CH;
-  if (p.batch == 0 || p.c == 0) return hipSuccess;
-  const size_t n = (size_t)p.batch * p.chunks * p.c;
-  p.agg = static_cast<float2*>(scratch);
-  float* const carry = reinterpret_cast<float*>(p.agg + n);
-  return weight == 0 ? bwd<0>(st, p, carry) : weight == 1 ? bwd<1>(st, p, carry) : bwd<2>(st, p, carry);
-}
+hipError_t k_scan_fwd(hipStream_t st, int weight, const ScanArgs& p, void* scratch) { return run(st, weight, p, scratch, false); }
+hipError_t k_scan_bwd(hipStream_t st, int weight, const ScanArgs& p, void* scratch) { return run(st, weight, p, scratch, true); }
