@@ -6,30 +6,40 @@
 // Where a document starts, f_t of the recurrence is 0 (the state before counts for nothing, and gets no gradient).  Behind a sequence's length the state is kept as it is.
 // 1 - f is taken as sigmoid(-g): a gate near one keeps its distance from it.
 //
-// h_t = a_t h_(t-1) + b_t is a scan over the maps (a, b), which compose as (a2, b2) after (a1, b1) = (a2 a1, a2 b1 + b2).  Chunks of 64 tokens by 256 channels; a wave
-// has eight tokens, a lane four channels, all in registers, so every input is read once: a workgroup makes its chunk's map, publishes it, finds out what its chunk starts from, and writes
+// h_t = a_t h_(t-1) + b_t is a scan over the maps (a, b), which compose as (a2, b2) after (a1, b1) = (a2 a1, a2 b1 + b2).  Chunks of 128 tokens by 128 channels; a wave
+// has 16 tokens, a lane two channels, all in registers, so every input is read once: a workgroup makes its chunk's map, publishes it, finds out what its chunk starts from, and writes
 // the outputs.  That it finds by looking back over the chunks before: from the nearest one whose end state is there, through the maps of those in between.  Workgroups take their
 // chunks in order of time by a counter, so whoever waits waits for workgroups that have started and that wait only for earlier ones; the first waits for none.  A
 // chunk's end state is the same sequence of operations wherever the looking ended: the results do not depend on timing.
-// The backward pass is the same from behind; h_(t-1) is made again from the states that the forward pass left, in fp32 (4 bytes for 64 tokens), not from y, which is
+// The backward pass is the same from behind; h_(t-1) is made again from the states that the forward pass left, in fp32 (4 bytes for 128 tokens), not from y, which is
 // rounded.  States, sums and products are fp32 throughout.
+#include <type_traits>
+
 #include "pack_ops.hpp"
 
 namespace {
 
-constexpr int NW = 8, TOK = 8, CHUNK = NW * TOK, LANES = 4, BLOCK_CH = 64 * LANES;
+constexpr int NW = 8, TOK = 16, CHUNK = NW * TOK, LANES = 2, BLOCK_CH = 64 * LANES;
 
-typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float fch __attribute__((ext_vector_type(LANES)));      // a lane's channels
+typedef uint32_t raw_t;                                          // as they are in memory
 
-RP_DEV f4 unpack(const uint2& u) { return f4{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)}; }
-RP_DEV uint2 pack(const f4& v) { return make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); }
+RP_DEV float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+RP_DEV fch unpack(raw_t u) { return fch{bf16_lo(u), bf16_hi(u)}; }
+RP_DEV raw_t pack(const fch& v) { return pack_bf16x2(v[0], v[1]); }
 
-// sigmoid(g) and sigmoid(-g): the smaller one from an exponential that is at most 1, so that it keeps its relative precision (the exponential's argument is
-// rounded: 2^-22 or so), the larger one as 1 less it, which is then one rounding off.  Errors of f add up over as many tokens as a gate remembers.
-RP_DEV void gates(float g, float& f, float& r) {
-  const float e = __expf(-fabsf(g)), t = e * __builtin_amdgcn_rcpf(1.f + e), s = 1.f - t;      // (NaN stays NaN)
-  f = g >= 0.f ? s : t;
-  r = g >= 0.f ? t : s;
+// sigmoid(g) and sigmoid(-g): the smaller one, t, from an exponential that is at most 1, so that it keeps its relative precision (the exponential's argument is
+// rounded: 2^-22 or so), the larger one as 1 - t, which is then one rounding off.  Errors of f add up over as many tokens as a gate remembers.  Kept between uses: t
+// with g's sign.
+RP_DEV float smaller_gate(float g) {
+  const float e = fast_exp2(fabsf(g) * -1.4426950408889634f);
+  return __builtin_copysignf(e * __builtin_amdgcn_rcpf(1.f + e), g);      // (NaN stays NaN)
+}
+RP_DEV void gates(float ts, float& f, float& r) {
+  const float t = fabsf(ts), s = 1.f - t;
+  const bool below = __float_as_int(ts) < 0;      // (t may be 0)
+  f = below ? t : s;
+  r = below ? s : t;
 }
 template <int W>
 RP_DEV float weight(float f, float r) { return W == 0 ? 1.f : W == 1 ? r : __builtin_amdgcn_sqrtf(r * (1.f + f)); }
@@ -40,35 +50,47 @@ RP_DEV float weight_slope(float f, float r) { return W == 0 ? 0.f : W == 1 ? -f 
 // A workgroup's place: the channels change fastest, so that workgroups side by side read neighbouring pieces of the same rows, and time slowest.
 struct Place {
   int b, chunk, ch, tid, lane, w, t0, len;      // t0: the wave's first token
-  bool in;
+  bool in, full;      // full: all of the wave's tokens are in use
   RP_DEV Place(const ScanArgs& p, int id, bool back) {
     tid = threadIdx.x;
     lane = tid & 63;
     w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int rest = id / p.blocks, cb = id - rest * p.blocks;
-    chunk = rest / p.batch;
+    const int rest = __builtin_amdgcn_readfirstlane(id / p.blocks), cb = id - rest * p.blocks;
+    chunk = __builtin_amdgcn_readfirstlane(rest / p.batch);
     b = rest - chunk * p.batch;
     if (back) chunk = p.chunks - 1 - chunk;
     ch = cb * BLOCK_CH + LANES * lane;
     in = ch < p.c;
     t0 = chunk * CHUNK + w * TOK;
-    len = p.len ? min(max(p.len[b], 0), p.seq) : p.seq;
+    len = __builtin_amdgcn_readfirstlane(p.len ? min(max(p.len[b], 0), p.seq) : p.seq);
+    full = t0 + TOK <= len;
   }
   RP_DEV long at(const ScanArgs& p) const { return ((long)b * p.chunks + chunk) * p.c + ch; }      // in [batch, chunks, c]
 };
-// Tokens t0 .. t0 + 7 of a tensor, zero behind the length.
-RP_DEV void load_rows(const bf16* base, long ld, const Place& s, int seq, uint2 (&r)[TOK]) {
-  const bf16* const src = base + ((long)s.b * seq + s.t0) * ld + s.ch;
-#pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    r[i] = make_uint2(0u, 0u);
-    if (s.in && s.t0 + i < s.len) r[i] = *reinterpret_cast<const uint2*>(src + i * ld);
+// A wave's tokens of a tensor, through a descriptor that begins at the first of them and ends behind the last one in use: the others read as zero, and are not written.
+struct TokenRows {
+  __amdgpu_buffer_rsrc_t rsrc;
+  int lane, step;      // byte offsets of the lane's channels (a lane without channels: out of range), and from token to token
+  RP_DEV TokenRows(const bf16* base, long ld, const Place& s, const ScanArgs& p, int end /* of the sequence's tokens in use */) {
+    const int n = min(max(end - s.t0, 0), TOK);
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base + ((long)s.b * p.seq + s.t0) * ld), 0, n ? (int)(((n - 1) * ld + p.c) * 2) : 0, 0x00020000);
+    lane = s.in ? s.ch * 2 : (int)0x80000000;
+    step = (int)(ld * 2);
   }
-}
-// The gates are made again from g for every use: kept from one to the next they would be the registers of half of the waves (244 instead of 110 for the backward kernel).
-RP_DEV void forget(uint2 (&r)[TOK]) {
+  RP_DEV void load(raw_t (&r)[TOK]) const {
 #pragma unroll
-  for (int i = 0; i < TOK; ++i) asm volatile("" : "+v"(r[i].x), "+v"(r[i].y));
+    for (int i = 0; i < TOK; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, lane, i * step, 0);
+  }
+  RP_DEV void store(int i, raw_t v) const { __builtin_amdgcn_raw_buffer_store_b32(v, rsrc, lane, i * step, 0); }
+};
+// The compiler is not to keep what it has made of these for a later use: it is made again for less than the registers would cost.
+RP_DEV void forget(raw_t (&r)[TOK]) {
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) asm volatile("" : "+v"(r[i]));
+}
+RP_DEV void forget(fch (&r)[TOK]) {
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) asm volatile("" : "+v"(r[i]));
 }
 // bit i: token t0 + i begins a document
 RP_DEV uint32_t load_first(const ScanArgs& p, const Place& s) {
@@ -82,44 +104,59 @@ RP_DEV uint32_t load_first(const ScanArgs& p, const Place& s) {
   return m;
 }
 
-// The map of a wave's eight tokens, forwards (state) or backwards (mu).  A token behind the length has the map (1, 0); what decides is the same in all lanes, so the
-// selects cost less than branches around the registers that the tokens are in.
-template <int W>
-RP_DEV void wave_map(const uint2 (&gr)[TOK], const uint2 (&xr)[TOK], uint32_t first, const Place& s, f4& A, f4& B) {
-  A = f4{1.f, 1.f, 1.f, 1.f};
-  B = f4{0.f, 0.f, 0.f, 0.f};
+// PLAIN: the wave is full and no token begins a document; else selects, by what is the same in all lanes.
+template <int W, bool PLAIN>
+RP_DEV float step(float ts, float x, bool live, bool begins, float h) {      // h_t from h_(t-1)
+  float f, r;
+  gates(ts, f, r);
+  const float u = weight<W>(f, r) * x;
+  const float next = !PLAIN && begins ? u : __builtin_fmaf(f, h, u);
+  return PLAIN || live ? next : h;
+}
+
+// The map of a wave's tokens, forwards (state), with the gates on the way, or backwards (mu).  A token behind the length has the map (1, 0).
+template <int W, bool PLAIN>
+RP_DEV void wave_map(const raw_t (&gr)[TOK], const raw_t (&xr)[TOK], fch (&ts)[TOK], uint32_t first, const Place& s, fch& A, fch& B) {
+  A = fch{1.f, 1.f};
+  B = fch{0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
     const bool live = s.t0 + i < s.len, begins = first >> i & 1;
-    const f4 g = unpack(gr[i]), x = unpack(xr[i]);
+    const fch g = unpack(gr[i]), x = unpack(xr[i]);
 #pragma unroll
     for (int e = 0; e < LANES; ++e) {
+      ts[i][e] = smaller_gate(g[e]);
       float f, r;
-      gates(g[e], f, r);
-      const float u = weight<W>(f, r) * x[e];
-      const float a = begins ? 0.f : A[e] * f, b = begins ? u : __builtin_fmaf(f, B[e], u);
-      A[e] = live ? a : A[e];
-      B[e] = live ? b : B[e];
+      gates(ts[i][e], f, r);
+      const float a = !PLAIN && begins ? 0.f : A[e] * f;
+      A[e] = PLAIN || live ? a : A[e];
+      B[e] = step<W, PLAIN>(ts[i][e], x[e], live, begins, B[e]);
     }
   }
 }
-RP_DEV void wave_map_back(const uint2 (&gr)[TOK], const uint2 (&dyr)[TOK], uint32_t first, const Place& s, f4& A, f4& B) {
-  A = f4{1.f, 1.f, 1.f, 1.f};
-  B = f4{0.f, 0.f, 0.f, 0.f};
+template <bool PLAIN>
+RP_DEV void wave_map_back(const raw_t (&dyr)[TOK], const fch (&ts)[TOK], uint32_t first, const Place& s, fch& A, fch& B) {
+  A = fch{1.f, 1.f};
+  B = fch{0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < TOK; ++j) {
     const int i = TOK - 1 - j;
     const bool live = s.t0 + i < s.len, begins = first >> i & 1;
-    const f4 g = unpack(gr[i]), dy = unpack(dyr[i]);
+    const fch dy = unpack(dyr[i]);
 #pragma unroll
     for (int e = 0; e < LANES; ++e) {
       float f, r;
-      gates(g[e], f, r);
-      const float a = begins ? 0.f : A[e] * f, b = begins ? 0.f : f * (dy[e] + B[e]);
-      A[e] = live ? a : A[e];
-      B[e] = live ? b : B[e];
+      gates(ts[i][e], f, r);
+      const float a = !PLAIN && begins ? 0.f : A[e] * f, b = !PLAIN && begins ? 0.f : f * (dy[e] + B[e]);
+      A[e] = PLAIN || live ? a : A[e];
+      B[e] = PLAIN || live ? b : B[e];
     }
   }
+}
+template <typename F>
+RP_DEV void plain_or_not(const Place& s, uint32_t first, F&& f) {
+  if (s.full && first == 0u) f(std::true_type{});      // uniform
+  else f(std::false_type{});
 }
 
 // What comes out of the map (a, b), and (a, b) after (A, B).  a = 0 where a document begins: what was before is not multiplied by it, or an infinity there would
@@ -140,19 +177,19 @@ RP_DEV word_t look(const word_t* at) { return __hip_atomic_load(const_cast<word_
 // LDS, and all of them go from the nearest end state through the maps behind it.  Where none of the eight has its end state yet, they look again.
 // `given`: the state before the first chunk (behind the last one, BACK); end: wave 0's, the chunk's own end state.
 struct Looks {
-  f4 a[NW][64], b[NW][64];
+  fch a[NW][64], b[NW][64];
   int state[NW];
 };
 template <bool BACK>
-RP_DEV f4 start_of(const ScanArgs& p, const Place& s, const f4 (&As)[NW][64], const f4 (&Bs)[NW][64], Looks& looks, const f4& given, f4& end) {
+RP_DEV fch start_of(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], const fch (&Bs)[NW][64], Looks& looks, const fch& given, fch& end) {
   const int before = BACK ? p.chunks - 1 - s.chunk : s.chunk;
   word_t* const mine = p.words + (s.in ? s.at(p) : 0);
-  f4 A = As[BACK ? NW - 1 : 0][s.lane], B = Bs[BACK ? NW - 1 : 0][s.lane];
+  fch A = As[BACK ? NW - 1 : 0][s.lane], B = Bs[BACK ? NW - 1 : 0][s.lane];
   if (s.w == 0) {
 #pragma unroll
     for (int i = 1; i < NW; ++i) {
       const int u = BACK ? NW - 1 - i : i;
-      const f4 a = As[u][s.lane], b = Bs[u][s.lane];
+      const fch a = As[u][s.lane], b = Bs[u][s.lane];
 #pragma unroll
       for (int e = 0; e < LANES; ++e) {
         A[e] = a[e] == 0.f ? 0.f : A[e] * a[e];
@@ -163,7 +200,7 @@ RP_DEV f4 start_of(const ScanArgs& p, const Place& s, const f4 (&As)[NW][64], co
 #pragma unroll
       for (int e = 0; e < LANES; ++e) publish(mine + e, map_word(A[e], B[e]));
   }
-  f4 h = given;
+  fch h = given;
   if (before > 0) {      // uniform over the workgroup
     const word_t* const theirs = mine + (BACK ? 1 : -1) * (long)(s.w + 1) * p.c;
     int from;
@@ -183,7 +220,7 @@ RP_DEV f4 start_of(const ScanArgs& p, const Place& s, const f4 (&As)[NW][64], co
           if (__all(there)) break;
           __builtin_amdgcn_s_sleep(1);
         }
-        f4 a, b;
+        fch a, b;
 #pragma unroll
         for (int e = 0; e < LANES; ++e) {
           a[e] = __uint_as_float((uint32_t)(w[e] >> 32));
@@ -201,11 +238,10 @@ RP_DEV f4 start_of(const ScanArgs& p, const Place& s, const f4 (&As)[NW][64], co
         if (looks.state[i]) from = i;
       if (__builtin_amdgcn_readfirstlane(from) >= 0) break;
       __syncthreads();      // all have seen that there is none
-      __builtin_amdgcn_s_sleep(4);
     }
     from = __builtin_amdgcn_readfirstlane(from);
     for (int i = from; i >= 0; --i) {
-      const f4 a = looks.a[i][s.lane], b = looks.b[i][s.lane];
+      const fch a = looks.a[i][s.lane], b = looks.b[i][s.lane];
 #pragma unroll
       for (int e = 0; e < LANES; ++e) {
         const uint32_t hi = __float_as_uint(a[e]);
@@ -230,10 +266,10 @@ __global__ void __launch_bounds__(256) scan_clear_kernel(uint4* to, long n) {
 // ------------------------------------------------------------------------------------------------ outputs
 // The maps of the waves before (behind) this one on what the chunk starts from.
 template <bool BACK>
-RP_DEV f4 enter(const f4 (&As)[NW][64], const f4 (&Bs)[NW][64], const Place& s, f4 h) {
+RP_DEV fch enter(const fch (&As)[NW][64], const fch (&Bs)[NW][64], const Place& s, fch h) {
   for (int i = 0; i < (BACK ? NW - 1 - s.w : s.w); ++i) {
     const int u = BACK ? NW - 1 - i : i;
-    const f4 a = As[u][s.lane], b = Bs[u][s.lane];
+    const fch a = As[u][s.lane], b = Bs[u][s.lane];
 #pragma unroll
     for (int e = 0; e < LANES; ++e) h[e] = through(a[e], b[e], h[e]);
   }
@@ -247,126 +283,135 @@ RP_DEV int take_place(const ScanArgs& p, int* lds) {
   __syncthreads();
   return __builtin_amdgcn_readfirstlane(*lds);
 }
-RP_DEV f4 given_state(const float* src, const ScanArgs& p, const Place& s) {
-  return src && s.in ? *reinterpret_cast<const f4*>(src + (long)s.b * p.c + s.ch) : f4{0.f, 0.f, 0.f, 0.f};
+RP_DEV fch given_state(const float* src, const ScanArgs& p, const Place& s) {
+  return src && s.in ? *reinterpret_cast<const fch*>(src + (long)s.b * p.c + s.ch) : fch{0.f, 0.f};
 }
 // What the chunk starts from; the waves have put their maps into LDS.  The state behind the last chunk goes to `last`.
 template <bool ONE, bool BACK>
-RP_DEV f4 chunk_start(const ScanArgs& p, const Place& s, const f4 (&As)[NW][64], const f4 (&Bs)[NW][64], Looks* looks, const float* given, float* last) {
-  f4 h = given_state(given, p, s);
+RP_DEV fch chunk_start(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], const fch (&Bs)[NW][64], Looks* looks, const float* given, float* last) {
+  fch h = given_state(given, p, s);
   if constexpr (!ONE) {
-    f4 end;
+    fch end;
     h = start_of<BACK>(p, s, As, Bs, *looks, h, end);
-    if (last && s.w == 0 && s.in && s.chunk == (BACK ? 0 : p.chunks - 1)) *reinterpret_cast<f4*>(last + (long)s.b * p.c + s.ch) = end;
+    if (last && s.w == 0 && s.in && s.chunk == (BACK ? 0 : p.chunks - 1)) *reinterpret_cast<fch*>(last + (long)s.b * p.c + s.ch) = end;
   }
   return h;
 }
 
 template <int W, bool ONE>
 __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p) {
-  __shared__ f4 As[NW][64], Bs[NW][64];
+  __shared__ fch As[NW][64], Bs[NW][64];
   __shared__ Looks looks;
   __shared__ int place;
   const Place s(p, take_place<ONE>(p, &place), false);
-  uint2 gr[TOK], xr[TOK];
-  load_rows(p.g, p.ldg, s, p.seq, gr);
-  load_rows(p.x, p.ldx, s, p.seq, xr);
+  raw_t gr[TOK], xr[TOK];
+  TokenRows(p.g, p.ldg, s, p, s.len).load(gr);
+  TokenRows(p.x, p.ldx, s, p, s.len).load(xr);
   const uint32_t first = load_first(p, s);
-  f4 A, B;
-  wave_map<W>(gr, xr, first, s, A, B);
-  As[s.w][s.lane] = A;
-  Bs[s.w][s.lane] = B;
-  __syncthreads();
-  const f4 start = chunk_start<ONE, false>(p, s, As, Bs, &looks, p.h0, p.last);
-  f4 h = enter<false>(As, Bs, s, start);
-  if (s.in && s.w == 0 && p.states && p.seq > 0) *reinterpret_cast<f4*>(p.states + s.at(p)) = start;
-  bf16* const out = p.y + ((long)s.b * p.seq + s.t0) * p.ldy + s.ch;
-  forget(gr);
-#pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    const bool live = s.t0 + i < s.len, begins = first >> i & 1;
-    const f4 g = unpack(gr[i]), x = unpack(xr[i]);
-#pragma unroll
-    for (int e = 0; e < LANES; ++e) {
-      float f, r;
-      gates(g[e], f, r);
-      const float u = weight<W>(f, r) * x[e];
-      const float next = begins ? u : __builtin_fmaf(f, h[e], u);
-      h[e] = live ? next : h[e];
-    }
-    if (s.in && s.t0 + i < p.seq) *reinterpret_cast<uint2*>(out + i * p.ldy) = live ? pack(h) : make_uint2(0u, 0u);
+  fch ts[TOK];
+  {
+    fch A, B;
+    plain_or_not(s, first, [&](auto plain) { wave_map<W, decltype(plain)::value>(gr, xr, ts, first, s, A, B); });
+    As[s.w][s.lane] = A;
+    Bs[s.w][s.lane] = B;
   }
-  if (ONE && p.last && s.w == NW - 1 && s.in) *reinterpret_cast<f4*>(p.last + (long)s.b * p.c + s.ch) = h;      // (waves without tokens pass the state on)
+  __syncthreads();
+  const fch start = chunk_start<ONE, false>(p, s, As, Bs, &looks, p.h0, p.last);
+  fch h = enter<false>(As, Bs, s, start);
+  if (s.in && s.w == 0 && p.states && p.seq > 0) *reinterpret_cast<fch*>(p.states + s.at(p)) = start;
+  const TokenRows out(p.y, p.ldy, s, p, p.seq);
+  forget(xr);
+  forget(ts);
+  plain_or_not(s, first, [&](auto plain) {
+    constexpr bool PLAIN = decltype(plain)::value;
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) {
+      const bool live = s.t0 + i < s.len, begins = first >> i & 1;
+      const fch x = unpack(xr[i]);
+#pragma unroll
+      for (int e = 0; e < LANES; ++e) h[e] = step<W, PLAIN>(ts[i][e], x[e], live, begins, h[e]);
+      out.store(i, PLAIN || live ? pack(h) : 0u);
+      }
+  });
+  if (ONE && p.last && s.w == NW - 1 && s.in) *reinterpret_cast<fch*>(p.last + (long)s.b * p.c + s.ch) = h;      // (waves without tokens pass the state on)
 }
 
 template <int W, bool ONE>
 __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p) {
-  __shared__ f4 As[NW][64], Bs[NW][64], Ab[NW][64], Bb[NW][64];
+  __shared__ fch As[NW][64], Bs[NW][64], Ab[NW][64], Bb[NW][64];
   __shared__ Looks looks;
   __shared__ int place;
   const Place s(p, take_place<ONE>(p, &place), true);
-  uint2 gr[TOK], xr[TOK], dyr[TOK];
-  load_rows(p.g, p.ldg, s, p.seq, gr);
-  load_rows(p.dy, p.lddy, s, p.seq, dyr);
-  load_rows(p.x, p.ldx, s, p.seq, xr);
-  const uint32_t first = load_first(p, s);
-  f4 h = s.in && p.seq > 0 ? *reinterpret_cast<const f4*>(p.states + s.at(p)) : f4{0.f, 0.f, 0.f, 0.f};
-  f4 A, B;
-  wave_map<W>(gr, xr, first, s, A, B);
-  As[s.w][s.lane] = A;
-  Bs[s.w][s.lane] = B;
-  forget(gr);
-  wave_map_back(gr, dyr, first, s, A, B);
-  Ab[s.w][s.lane] = A;
-  Bb[s.w][s.lane] = B;
+  raw_t xr[TOK], dyr[TOK];
+  uint32_t first;
+  fch ts[TOK];
+  fch h = s.in && p.seq > 0 ? *reinterpret_cast<const fch*>(p.states + s.at(p)) : fch{0.f, 0.f};
+  {
+    raw_t gr[TOK];
+    TokenRows(p.g, p.ldg, s, p, s.len).load(gr);
+    TokenRows(p.x, p.ldx, s, p, s.len).load(xr);
+    TokenRows(p.dy, p.lddy, s, p, s.len).load(dyr);
+    first = load_first(p, s);
+    plain_or_not(s, first, [&](auto plain) {
+      constexpr bool PLAIN = decltype(plain)::value;
+      fch A, B;
+      wave_map<W, PLAIN>(gr, xr, ts, first, s, A, B);
+      As[s.w][s.lane] = A;
+      Bs[s.w][s.lane] = B;
+      forget(ts);
+      wave_map_back<PLAIN>(dyr, ts, first, s, A, B);
+      Ab[s.w][s.lane] = A;
+      Bb[s.w][s.lane] = B;
+    });
+  }
   __syncthreads();
-  f4 mu = chunk_start<ONE, true>(p, s, Ab, Bb, &looks, p.dlast, p.dh0);
+  fch mu = chunk_start<ONE, true>(p, s, Ab, Bb, &looks, p.dlast, p.dh0);
   h = enter<false>(As, Bs, s, h);
   mu = enter<true>(Ab, Bb, s, mu);
-  forget(gr);
-  forget(xr);
-  f4 before[TOK];      // h_(t-1), 0 where a document begins
-#pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    const bool live = s.t0 + i < s.len, begins = first >> i & 1;
-    const f4 g = unpack(gr[i]), x = unpack(xr[i]);
-#pragma unroll
-    for (int e = 0; e < LANES; ++e) {
-      float f, r;
-      gates(g[e], f, r);
-      const float u = weight<W>(f, r) * x[e];
-      before[i][e] = begins ? 0.f : h[e];
-      const float next = begins ? u : __builtin_fmaf(f, h[e], u);
-      h[e] = live ? next : h[e];
-    }
-  }
-  forget(gr);
   forget(xr);
   forget(dyr);
-  bf16* const dx = p.dx + ((long)s.b * p.seq + s.t0) * p.lddx + s.ch;
-  bf16* const dg = p.dg + ((long)s.b * p.seq + s.t0) * p.lddg + s.ch;
+  forget(ts);
+  const TokenRows dx(p.dx, p.lddx, s, p, p.seq), dg(p.dg, p.lddg, s, p, p.seq);
+  // back through the tokens for lam and dx, then forward for h and dg: dy's registers become lam's
+  plain_or_not(s, first, [&](auto plain) {
+    constexpr bool PLAIN = decltype(plain)::value;
+    fch lam[TOK];
 #pragma unroll
-  for (int j = 0; j < TOK; ++j) {
-    const int i = TOK - 1 - j;
-    const bool live = s.t0 + i < s.len, begins = first >> i & 1;
-    const f4 g = unpack(gr[i]), x = unpack(xr[i]), dy = unpack(dyr[i]);
-    f4 gx, gg;
+    for (int j = 0; j < TOK; ++j) {
+      const int i = TOK - 1 - j;
+      const bool live = s.t0 + i < s.len, begins = first >> i & 1;
+      const fch dy = unpack(dyr[i]);
+      fch gx;
 #pragma unroll
-    for (int e = 0; e < LANES; ++e) {
-      float f, r;
-      gates(g[e], f, r);
-      const float lam = dy[e] + mu[e];
-      gx[e] = live ? weight<W>(f, r) * lam : 0.f;
-      gg[e] = live ? lam * (before[i][e] * (f * r) + x[e] * weight_slope<W>(f, r)) : 0.f;
-      const float next = begins ? 0.f : f * lam;
-      mu[e] = live ? next : mu[e];
-    }
-    if (s.in && s.t0 + i < p.seq) {
-      *reinterpret_cast<uint2*>(dx + i * p.lddx) = pack(gx);
-      *reinterpret_cast<uint2*>(dg + i * p.lddg) = pack(gg);
-    }
-  }
-  if (ONE && p.dh0 && s.w == 0 && s.in) *reinterpret_cast<f4*>(p.dh0 + (long)s.b * p.c + s.ch) = mu;
+      for (int e = 0; e < LANES; ++e) {
+        float f, r;
+        gates(ts[i][e], f, r);
+        lam[i][e] = dy[e] + mu[e];
+        gx[e] = weight<W>(f, r) * lam[i][e];
+        const float next = !PLAIN && begins ? 0.f : f * lam[i][e];
+        mu[e] = PLAIN || live ? next : mu[e];
+      }
+      dx.store(i, PLAIN || live ? pack(gx) : 0u);
+      }
+    forget(ts);
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) {
+      const bool live = s.t0 + i < s.len, begins = first >> i & 1;
+      const fch x = unpack(xr[i]);
+      fch gg;
+#pragma unroll
+      for (int e = 0; e < LANES; ++e) {
+        float f, r;
+        gates(ts[i][e], f, r);
+        const float before = !PLAIN && begins ? 0.f : h[e];
+        // (w = 1 - f: the two terms share f (1 - f))
+        gg[e] = lam[i][e] * (W == 1 ? f * r * (before - x[e]) : before * (f * r) + x[e] * weight_slope<W>(f, r));
+        h[e] = step<W, PLAIN>(ts[i][e], x[e], live, begins, h[e]);
+      }
+      dg.store(i, PLAIN || live ? pack(gg) : 0u);
+      }
+  });
+  if (ONE && p.dh0 && s.w == 0 && s.in) *reinterpret_cast<fch*>(p.dh0 + (long)s.b * p.c + s.ch) = mu;
 }
 
 int chunks_of(int seq) { return (seq + CHUNK - 1) / CHUNK; }
