@@ -74,6 +74,9 @@ struct SpanArgs {
   float* part;
   float4* part_ml;
   int splits;
+  int2* ranges;                    // [batch * key tiles] row tiles that see any of its keys
+  int* sums;                       // [batch * key tiles + 1]
+  int parts;                       // pieces of a key head's (key tile, row tile) pairs, or 0
 };
 void k_span_attn_scratch(const SpanArgs& p, int d, size_t* fwd_bytes, size_t* bwd_bytes);
 size_t k_span_attn_least(const SpanArgs& p);      // what the backward call cannot do without

@@ -31,6 +31,8 @@ namespace {
 constexpr int fwd_tile_bytes(int d) { return max_i(64 * (d + 8) + 64 * (d + 32), 128 * (d + 8)) * 2; }
 constexpr int dq_tile_bytes(int d) { return max_i(2 * 64 * tile_ld(d), 128 * (d + 8)) * 2; }
 
+constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 6 * 64 * 4, 4 * 32 * (d + 4) * 4); }
+constexpr int dkv_pair_smem_bytes(int d) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * 4 * 64 * 16 + 2 * 6 * 64 * 4; }
 constexpr float LOG2E = 1.4426950408889634f;
 
 // Sizes of one sequence and key head.
@@ -148,6 +150,9 @@ RP_DEV float sum2(uint32_t pair, float acc) {      // the two bf16 of a register
   typedef __bf16 v2 __attribute__((ext_vector_type(2)));
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2, pair), __builtin_bit_cast(v2, 0x3f803f80u), acc, false);
 }
+
+// In a branch that is taken for the few tiles at the edge of a span: keeps the compiler from doing the work for every tile and selecting.
+RP_DEV void stay_in_branch() { asm volatile("" ::: "memory"); }
 
 constexpr float FLOOR = -1.0e37f;      // the reference exponent of rows that have seen nothing yet: finite, so that exp2(-inf - FLOOR) = 0
 
@@ -613,6 +618,7 @@ __global__ void __launch_bounds__(256, 2) span_dq_kernel(const SpanArgs p) {
           }
       }
       if (!whole) {
+        stay_in_branch();
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const int lo = span[c].x - (k0 + 4 * lg);
@@ -728,7 +734,12 @@ struct RowTile {
 template <bool CAP, bool BIAS>
 struct RowStat {
   static constexpr int FLOATS = 64 * 6;
+  const char* src;      // wave 0: lse, 1: delta, 2: spans, 3: positions, or NULL; of the group's first head
   float x, y;
+  RP_DEV void start(const SpanArgs& p, const Rows& s, int w) {
+    const long q = (long)s.b * p.seq_q, stat = ((long)s.b * p.a + s.g * s.grp) * p.seq_q;
+    src = w == 0 ? (const char*)(p.lse_in + stat) : w == 1 ? (const char*)(p.delta + stat) : w == 2 ? (const char*)(p.span + q) : (const char*)(p.q_pos ? p.q_pos + q : nullptr);
+  }
   // The loads are only issued here; the values are put in LDS a tile later.
   RP_DEV void load(const SpanArgs& p, const Rows& s, int row0, int lane, int w) {
     if (w >= (BIAS ? 4 : 3)) return;
@@ -736,16 +747,16 @@ struct RowStat {
     const bool in = r < s.total;
     int q, h;
     s.at(in ? r : 0, q, h);
-    const long stat = ((long)s.b * p.a + s.g * s.grp + h) * p.seq_q + q;
-    if (w == 0) x = in ? p.lse_in[stat] : -INFINITY;
-    if (w == 1) x = in ? p.delta[stat] : 0.f;
-    if (w == 2) {
-      const int2 v = span_of(p, s, r);
-      x = __int_as_float(v.x);
-      y = __int_as_float(v.y - v.x);
-    }
-    if (BIAS && w == 3) {
-      x = __int_as_float(p.q_pos ? p.q_pos[(long)s.b * p.seq_q + q] : q + p.seq_kv - p.seq_q);
+    if (w < 2) {
+      x = reinterpret_cast<const float*>(src)[(long)h * s.seq_q + q];
+      x = in ? x : w == 0 ? -INFINITY : 0.f;
+    } else if (w == 2) {
+      const int2 v = reinterpret_cast<const int2*>(src)[q];
+      const int lo = max(v.x, 0), n = min(v.y, p.seq_kv) - lo;
+      x = __int_as_float(lo);
+      y = __int_as_float(in && n > 0 ? n : 0);
+    } else {
+      x = __int_as_float(src ? reinterpret_cast<const int*>(src)[q] : q + p.seq_kv - s.seq_q);
       y = p.slopes[s.g * s.grp + h] * LOG2E;
     }
   }
@@ -790,6 +801,7 @@ RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, c
       }
   }
   if (!whole) {
+    stay_in_branch();
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
       const int4 lo = *reinterpret_cast<const int4*>(lds + 128 + 16 * qt + 4 * lg), n = *reinterpret_cast<const int4*>(lds + 192 + 16 * qt + 4 * lg);
@@ -807,78 +819,153 @@ RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, c
   }
 }
 
-// The row tiles that see any of a workgroup's keys, one after the other (tiles between the first and the last may see none).  What 64 neighbouring tiles see is asked for at
-// once, a tile a lane, and kept as two masks: a load on the way to every tile would be waited for.
-struct RowRange {
-  const int4* tiles;
-  int k0, k1, first, last;      // [first, last)
-  int base, u, end;             // the masks' first tile; the present tile
-  unsigned long long any, all;
-  template <int NT>
-  RP_DEV void find(const SpanArgs& p, const Rows& s, int key0, int* lds /* [2 NT / 64] */, int tid) {
-    const int n = (s.total + 63) / 64;
-    tiles = p.tiles + (long)s.b * n;
-    k0 = key0;
-    k1 = min(key0 + 128, p.seq_kv);
-    int lo = 0x7fffffff, hi = 0;
-    for (int t = tid; t < n; t += NT) {
-      const int4 v = tiles[t];
-      if (k0 < v.y && k1 > v.x) {
-        lo = min(lo, t);
-        hi = t + 1;
-      }
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      lo = min(lo, __shfl_xor(lo, o, 64));
-      hi = max(hi, __shfl_xor(hi, o, 64));
-    }
-    if ((tid & 63) == 0) {
-      lds[2 * (tid >> 6)] = lo;
-      lds[2 * (tid >> 6) + 1] = hi;
-    }
-    __syncthreads();
-    for (int w = 0; w < NT / 64; ++w) {
-      lo = min(lo, lds[2 * w]);
-      hi = max(hi, lds[2 * w + 1]);
-    }
-    __syncthreads();
-    first = __builtin_amdgcn_readfirstlane(hi > 0 ? lo : 0);
-    last = __builtin_amdgcn_readfirstlane(hi);
-  }
-  RP_DEV void look(int from, int lane) {
-    base = from;
-    const int t = min(from + lane, end - 1);
+// The first row tile that sees any of the keys k0 .. k1 - 1, and the one behind the last; all threads.  (Tiles in between may see none.)
+template <int NT>
+RP_DEV int2 row_tiles(const int4* tiles, int n, int k0, int k1, int* lds /* [2 NT / 64] */, int tid) {
+  int lo = 0x7fffffff, hi = 0;
+#pragma unroll 4
+  for (int t = tid; t < n; t += NT) {
     const int4 v = tiles[t];
-    any = __ballot(from + lane < end && k0 < v.y && k1 > v.x);
+    if (k0 < v.y && k1 > v.x) {
+      lo = min(lo, t);
+      hi = t + 1;
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    lo = min(lo, __shfl_xor(lo, o, 64));
+    hi = max(hi, __shfl_xor(hi, o, 64));
+  }
+  if ((tid & 63) == 0) {
+    lds[2 * (tid >> 6)] = lo;
+    lds[2 * (tid >> 6) + 1] = hi;
+  }
+  __syncthreads();
+  for (int w = 0; w < NT / 64; ++w) {
+    lo = min(lo, lds[2 * w]);
+    hi = max(hi, lds[2 * w + 1]);
+  }
+  __syncthreads();
+  return make_int2(__builtin_amdgcn_readfirstlane(hi > 0 ? lo : 0), __builtin_amdgcn_readfirstlane(hi));
+}
+
+// A walk over the row tiles [from, to) that see any of the keys, the last one first: the key tiles of a document have its last rows in common, so workgroups that
+// begin together read the same rows at the same time, out of their L2.  What 64 neighbouring tiles see is asked for at once, a tile a lane, and kept as two masks: a
+// load on the way to every tile would be waited for.
+struct RowWalk {
+  const int4* tiles;
+  int k0, k1;
+  int base, u, from;            // the masks' first tile; the present tile
+  unsigned long long any, all;
+  RP_DEV void look(int lane) {      // u and the 63 before it
+    base = u - 63;
+    const int t = base + lane;
+    const int4 v = tiles[max(t, from)];
+    any = __ballot(t >= from && k0 < v.y && k1 > v.x);
     all = __ballot(v.z <= k0 && v.w >= k1);
   }
-  RP_DEV void settle(int lane) {      // to the present tile or the next one that sees any key; u = end: no more
-    while (u < end) {
-      if (u >= base + 64) look(u, lane);
-      const unsigned long long m = any >> (u - base);
+  RP_DEV void settle(int lane) {      // to the present tile or the next one that sees any key; u < from: no more
+    while (u >= from) {
+      if (u < base) look(lane);
+      const unsigned long long m = any << (63 - (u - base));
       if (m) {
-        u += __builtin_ctzll(m);
+        u -= __builtin_clzll(m);
         return;
       }
-      u = base + 64;
+      u = base - 1;
     }
-    u = end;
   }
-  RP_DEV void start(int from, int to, int lane) {      // [from, to)
-    u = from;
-    end = to;
-    base = from - 64;
+  RP_DEV void start(const int4* t, int key0, int key1, int first, int end, int lane) {
+    tiles = t;
+    k0 = key0;
+    k1 = key1;
+    from = first;
+    u = end - 1;
+    base = end;
     any = all = 0;
     settle(lane);
   }
-  RP_DEV bool more() const { return u < end; }
+  RP_DEV bool more() const { return u >= from; }
   RP_DEV bool whole() const { return all >> (u - base) & 1; }      // every row of the present tile sees all of the keys
   RP_DEV void next(int lane) {
-    ++u;
+    --u;
     settle(lane);
   }
 };
+
+// ---- who does what.  The key tiles of a causal row differ by as much as there are row tiles: where a launch has only a few rounds of them, the chip waits for the longest.  So the
+// (key tile, row tile) pairs of a key head, in order, are cut into `parts` pieces of one length, and a workgroup does a piece: the end of one key tile, some whole
+// ones, the beginning of another.  What it has of a key tile that others share goes to scratch, at most two of them a workgroup, and another kernel adds those up
+// in order.  (8192 causal tokens, 64 heads of 64: a key tile a workgroup 1880 us.)  With more than MOST_TILES key tiles, or without scratch for the parts (parts 0), a
+// workgroup does a key tile.
+constexpr int MOST_TILES = 2048;
+constexpr int LEAST_PAIRS = 6;       // of a piece: beginning and ending with a key tile costs as much as two to three pairs
+
+// ranges[i]: key tile i % KT of sequence i / KT
+__global__ void __launch_bounds__(256) span_range_kernel(const SpanArgs p) {
+  __shared__ int lds[8];
+  const int kt = (p.seq_kv + 127) / 128, b = (int)blockIdx.x / kt, k0 = ((int)blockIdx.x - b * kt) * 128;
+  const int n = ((p.a / p.kh) * p.seq_q + 63) / 64;
+  const int2 r = row_tiles<256>(p.tiles + (long)b * n, n, k0, min(k0 + 128, p.seq_kv), lds, threadIdx.x);
+  if (threadIdx.x == 0) p.ranges[blockIdx.x] = r;
+}
+
+// A workgroup's share, key tile by key tile.
+template <int NT>
+struct Share {
+  int sum[MOST_TILES + 1];      // pairs before every key tile
+  int wave[NT / 64];
+  // all threads; the first workgroup of all leaves the sums behind
+  RP_DEV int add_up(const SpanArgs& p, int n, int tid) {
+    constexpr int EACH = MOST_TILES / NT;
+    int c[EACH], total = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int t = tid * EACH + i;
+      c[i] = 0;
+      if (t < n) {
+        const int2 r = p.ranges[t];
+        c[i] = r.y - r.x;
+      }
+      total += c[i];
+    }
+    int s = total;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(s, o, 64);
+      if ((tid & 63) >= o) s += v;
+    }
+    if ((tid & 63) == 63) wave[tid >> 6] = s;
+    __syncthreads();
+    int at = s - total, all = 0;
+    for (int w = 0; w < NT / 64; ++w) {
+      if (w < tid >> 6) at += wave[w];
+      all += wave[w];
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int t = tid * EACH + i;
+      if (t < n) sum[t] = at;
+      at += c[i];
+    }
+    if (tid == 0) sum[n] = all;
+    __syncthreads();
+    if (blockIdx.x == 0)
+      for (int t = tid; t <= n; t += NT) p.sums[t] = sum[t];
+    return __builtin_amdgcn_readfirstlane(all);
+  }
+  // the key tile that pair w belongs to: the last one that begins at or before it
+  RP_DEV int tile_of(int w, int n) const {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (sum[mid] <= w) lo = mid;
+      else hi = mid;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+  }
+};
+RP_DEV int piece_length(int pairs, int parts) { return max((pairs + parts - 1) / parts, LEAST_PAIRS); }
 
 // The keys of a workgroup do not mix: a column of the score tiles is a key's own.
 template <int D, bool CAP, bool BIAS>
@@ -894,18 +981,42 @@ __global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int nhb = p.kh * p.batch;
-  const int rest = (int)blockIdx.x / nhb;
-  const int hb = head_at((int)blockIdx.x, rest, nhb);
-  const int split = rest % p.splits, kv0 = (rest / p.splits) * 128, kw0 = kv0 + 32 * w;
-  const Rows s(p, hb);
   const Score sc(p);
-  RowRange range;
-  range.find<NT>(p, s, kv0, reinterpret_cast<int*>(stat), tid);
+  const int tiles_kv = (p.seq_kv + 127) / 128, all_kv = p.batch * tiles_kv;
+  Share<NT>* const share = reinterpret_cast<Share<NT>*>(dyn_smem + dkv_smem_bytes(D));
+  int pair = 0, last_pair = 1, tile, g;      // balanced: the present (key tile, row tile) pair of the head
+  if (p.parts > 0) {
+    g = (int)blockIdx.x % p.kh;
+    const int pairs = share->add_up(p, all_kv, tid), each = piece_length(pairs, p.parts);
+    pair = (int)blockIdx.x / p.kh * each;
+    last_pair = min(pair + each, pairs);
+    if (pair >= last_pair) return;      // uniform over the workgroup
+    tile = share->tile_of(pair, all_kv);
+  } else {
+    const int nhb = p.kh * p.batch, rest = (int)blockIdx.x / nhb, hb = head_at((int)blockIdx.x, rest, nhb);
+    g = hb % p.kh;
+    tile = hb / p.kh * tiles_kv + rest;
+  }
+  const bool by_tile = p.parts == 0;
+  int slot = 0;      // of the parts that go to scratch: the piece begins with it, or not
+  for (;; ++tile) {
+  const int b = tile / tiles_kv, kv0 = (tile - b * tiles_kv) * 128, kw0 = kv0 + 32 * w;
+  const Rows s(p, b * p.kh + g);
+  const int4* const row_tile = p.tiles + (long)b * ((s.total + 63) / 64);
+  const int key_end = min(kv0 + 128, p.seq_kv);
   int u0, u1;
-  slice_of(range.last - range.first, p.splits, split, u0, u1);
-  u0 += range.first;
-  u1 += range.first;
+  bool mine = true;      // the whole key tile is done here
+  if (by_tile) {
+    const int2 r = row_tiles<NT>(row_tile, (s.total + 63) / 64, kv0, key_end, reinterpret_cast<int*>(stat), tid);
+    u0 = r.x;
+    u1 = r.y;
+  } else {
+    const int begin = share->sum[tile], end = share->sum[tile + 1];
+    const int2 r = p.ranges[tile];
+    u0 = r.x + pair - begin;
+    u1 = r.x + min(last_pair, end) - begin;
+    mine = pair == begin && last_pair >= end;
+  }
   const int kpos[2] = {kw0 + lr, kw0 + 16 + lr};
   const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
   const bf16* const vb = p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D;
@@ -935,11 +1046,13 @@ __global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
   RowTile<D, NT> rows;
   rows.start(p, s, tid);
   Stat rstat;
+  rstat.start(p, s, w);
   auto prefetch = [&](int u) {
     rows.load(qreg, doreg, s, u, tid);
     rstat.load(p, s, u * 64, lane, w);
   };
-  range.start(u0, u1, lane);
+  RowWalk range;
+  range.start(row_tile, kv0, key_end, u0, u1, lane);
   if (range.more()) prefetch(range.u);
   while (range.more()) {
     const bool whole = range.whole();
@@ -1009,16 +1122,22 @@ __global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
     }
   }
   __syncthreads();
-  const long tok0 = (long)s.b * p.seq_kv;
-  if (p.splits == 1) {
-    store_acc_T<D>(dkacc, sc.grad, smem + w * 32 * (D + 8), p.dk + tok0 * p.lddk + s.g * D, p.lddk, kw0, p.seq_kv, lane);
-    store_acc_T<D>(dvacc, 1.f, smem + w * 32 * (D + 8), p.dv + tok0 * p.lddv + s.g * D, p.lddv, kw0, p.seq_kv, lane);
+  if (mine) {
+    const long tok0 = (long)s.b * p.seq_kv;
+    bf16* const stage = smem + w * 32 * (D + 8);
+    store_acc_T<D>(dkacc, sc.grad, stage, p.dk + tok0 * p.lddk + s.g * D, p.lddk, kw0, p.seq_kv, lane);
+    store_acc_T<D>(dvacc, 1.f, stage, p.dv + tok0 * p.lddv + s.g * D, p.lddv, kw0, p.seq_kv, lane);
   } else {
     float* const stage = reinterpret_cast<float*>(smem) + w * 32 * (D + 4);
-    const long ldp = (long)p.kh * D, each = (long)p.batch * p.seq_kv * ldp;
-    float* const out = p.part + split * each + tok0 * ldp + s.g * D;
-    store_acc_T_f32<D>(dkacc, sc.grad, stage, out, ldp, kw0, p.seq_kv, lane);
-    store_acc_T_f32<D>(dvacc, 1.f, stage, out + p.splits * each, ldp, kw0, p.seq_kv, lane);
+    float* const out = p.part + ((long)blockIdx.x * 2 + slot) * (2 * 128 * D);
+    store_acc_T_f32<D>(dkacc, sc.grad, stage, out, D, 32 * w, 128, lane);
+    store_acc_T_f32<D>(dvacc, 1.f, stage, out + 128 * D, D, 32 * w, 128, lane);
+  }
+  if (by_tile) return;
+  pair = share->sum[tile + 1];
+  if (pair >= last_pair) return;
+  slot = 1;
+  while (share->sum[tile + 2] == pair) ++tile;      // key tiles that nothing sees (there is a pair left, so the walk ends)
   }
 }
 
@@ -1038,18 +1157,42 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int w = w8 >> 1, h = w8 & 1;
-  const int nhb = p.kh * p.batch;
-  const int rest = (int)blockIdx.x / nhb;
-  const int hb = head_at((int)blockIdx.x, rest, nhb);
-  const int split = rest % p.splits, kv0 = (rest / p.splits) * 128, kw0 = kv0 + 32 * w;
-  const Rows s(p, hb);
   const Score sc(p);
-  RowRange range;
-  range.find<NT>(p, s, kv0, reinterpret_cast<int*>(stat), tid);
+  const int tiles_kv = (p.seq_kv + 127) / 128, all_kv = p.batch * tiles_kv;
+  Share<NT>* const share = reinterpret_cast<Share<NT>*>(dyn_smem + dkv_pair_smem_bytes(D));
+  int pair = 0, last_pair = 1, tile, g;      // balanced: the present (key tile, row tile) pair of the head
+  if (p.parts > 0) {
+    g = (int)blockIdx.x % p.kh;
+    const int pairs = share->add_up(p, all_kv, tid), each = piece_length(pairs, p.parts);
+    pair = (int)blockIdx.x / p.kh * each;
+    last_pair = min(pair + each, pairs);
+    if (pair >= last_pair) return;      // uniform over the workgroup
+    tile = share->tile_of(pair, all_kv);
+  } else {
+    const int nhb = p.kh * p.batch, rest = (int)blockIdx.x / nhb, hb = head_at((int)blockIdx.x, rest, nhb);
+    g = hb % p.kh;
+    tile = hb / p.kh * tiles_kv + rest;
+  }
+  const bool by_tile = p.parts == 0;
+  int slot = 0;      // of the parts that go to scratch: the piece begins with it, or not
+  for (;; ++tile) {
+  const int b = tile / tiles_kv, kv0 = (tile - b * tiles_kv) * 128, kw0 = kv0 + 32 * w;
+  const Rows s(p, b * p.kh + g);
+  const int4* const row_tile = p.tiles + (long)b * ((s.total + 63) / 64);
+  const int key_end = min(kv0 + 128, p.seq_kv);
   int u0, u1;
-  slice_of(range.last - range.first, p.splits, split, u0, u1);
-  u0 += range.first;
-  u1 += range.first;
+  bool mine = true;      // the whole key tile is done here
+  if (by_tile) {
+    const int2 r = row_tiles<NT>(row_tile, (s.total + 63) / 64, kv0, key_end, reinterpret_cast<int*>(stat), tid);
+    u0 = r.x;
+    u1 = r.y;
+  } else {
+    const int begin = share->sum[tile], end = share->sum[tile + 1];
+    const int2 r = p.ranges[tile];
+    u0 = r.x + pair - begin;
+    u1 = r.x + min(last_pair, end) - begin;
+    mine = pair == begin && last_pair >= end;
+  }
   const int kpos[2] = {kw0 + lr, kw0 + 16 + lr};
   const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
   const bf16* const vb = p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D;
@@ -1081,11 +1224,13 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
   RowTile<D, NT> rows;
   rows.start(p, s, tid);
   Stat rstat;
+  rstat.start(p, s, w8);
   auto prefetch = [&](int u) {
     rows.load(qreg, doreg, s, u, tid);
     rstat.load(p, s, u * 64, lane, w8);
   };
-  range.start(u0, u1, lane);
+  RowWalk range;
+  range.start(row_tile, kv0, key_end, u0, u1, lane);
   if (range.more()) prefetch(range.u);
 
   constexpr int AHEAD = 2;     // two waves per SIMD cover each other's LDS latency: a short ring is enough
@@ -1171,61 +1316,86 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
   __syncthreads();
   if (i > 0) partner_update(i - 1);
   __syncthreads();
-  const long tok0 = (long)s.b * p.seq_kv;
-  const int d0 = s.g * D + h * (D / 2);
-  if (p.splits == 1) {
+  if (mine) {
+    const long tok0 = (long)s.b * p.seq_kv;
+    const int d0 = s.g * D + h * (D / 2);
     bf16* const stage = smem + w8 * 32 * (D / 2 + 8);
     store_acc_T<D / 2>(dkacc, sc.grad, stage, p.dk + tok0 * p.lddk + d0, p.lddk, kw0, p.seq_kv, lane);
     store_acc_T<D / 2>(dvacc, 1.f, stage, p.dv + tok0 * p.lddv + d0, p.lddv, kw0, p.seq_kv, lane);
   } else {
     float* const stage = reinterpret_cast<float*>(smem) + w8 * 32 * (D / 2 + 4);
-    const long ldp = (long)p.kh * D, each = (long)p.batch * p.seq_kv * ldp;
-    float* const out = p.part + split * each + tok0 * ldp + d0;
-    store_acc_T_f32<D / 2>(dkacc, sc.grad, stage, out, ldp, kw0, p.seq_kv, lane);
-    store_acc_T_f32<D / 2>(dvacc, 1.f, stage, out + p.splits * each, ldp, kw0, p.seq_kv, lane);
+    float* const out = p.part + ((long)blockIdx.x * 2 + slot) * (2 * 128 * D) + h * (D / 2);
+    store_acc_T_f32<D / 2>(dkacc, sc.grad, stage, out, D, 32 * w, 128, lane);
+    store_acc_T_f32<D / 2>(dvacc, 1.f, stage, out + 128 * D, D, 32 * w, 128, lane);
+  }
+  if (by_tile) return;
+  pair = share->sum[tile + 1];
+  if (pair >= last_pair) return;
+  slot = 1;
+  while (share->sum[tile + 2] == pair) ++tile;      // key tiles that nothing sees (there is a pair left, so the walk ends)
   }
 }
 
-// dk, dv = the sum of a key's slices.  A "row" is a key head of dk or dv.
-template <int D, int G>
+// dk, dv of the key tiles that several workgroups share: the sum of their parts, in order; zero where nothing sees a key.  A block takes 32 keys of a key tile, of dk or of dv.
+template <int D>
 __global__ void __launch_bounds__(256) span_key_join_kernel(const SpanArgs p) {
-  constexpr int CH = D / 8, RPB = 256 / (CH * G);
-  __shared__ float red[CH * G > 64 ? 4 * CH * 8 : 1];
-  const int tid = threadIdx.x, ch = tid % CH, grp = tid / CH % G;
-  const long T = (long)p.batch * p.seq_kv, rows = T * p.kh;
-  const long item = (long)blockIdx.x * RPB + tid / (CH * G);
-  const bool in = item < 2 * rows, is_v = item >= rows;
-  const long kv = !in ? 0 : is_v ? item - rows : item;
-  const long t = kv / p.kh;
-  const int g = (int)(kv - t * p.kh);
-  const int n = in ? p.splits : 0;
-  const float* const src = p.part + (is_v ? p.splits * rows * D : 0) + kv * D + ch * 8;
-  float acc[8];
+  constexpr int CH = D / 8;
+  const int tiles_kv = (p.seq_kv + 127) / 128, all_kv = p.batch * tiles_kv;
+  const int i = (int)blockIdx.x >> 3, rows = ((int)blockIdx.x & 3) * 32, is_v = (int)blockIdx.x >> 2 & 1;
+  const int tile = i / p.kh, g = i - tile * p.kh;
+  const int begin = p.sums[tile], end = p.sums[tile + 1], each = piece_length(p.sums[all_kv], p.parts);
+  const int from = begin / each, to = (end - 1) / each;
+  if (end > begin && from == to) return;      // one workgroup had it all
+  const int b = tile / tiles_kv, kv0 = (tile - b * tiles_kv) * 128;
+  for (int e = threadIdx.x; e < 32 * CH; e += 256) {
+    const int row = rows + e / CH, ch = e % CH, key = kv0 + row;
+    if (key >= p.seq_kv) continue;
+    float acc[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    for (int x = 0; x < 8; ++x) acc[x] = 0.f;
+    if (end > begin) {
+      // the first of them began its piece earlier, unless the two begin together; the others begin with this key tile
+      const float* const src = p.part + (long)is_v * 128 * D + row * D + ch * 8;
+      add_times(acc, src + ((long)(from * p.kh + g) * 2 + (from * each == begin ? 0 : 1)) * (2 * 128 * D), 1.f);
 #pragma unroll 4
-  for (int i = grp; i < n; i += G) add_times(acc, src + i * rows * D, 1.f);
-  const bool store = add_groups<CH, G, 8>(acc, red);
-  if (in && store) *reinterpret_cast<uint4*>((is_v ? p.dv + t * p.lddv : p.dk + t * p.lddk) + g * D + ch * 8) = pack_times(acc, 1.f);
+      for (int w = from + 1; w <= to; ++w) add_times(acc, src + (long)(w * p.kh + g) * 2 * (2 * 128 * D), 1.f);
+    }
+    const long t = (long)b * p.seq_kv + key;
+    *reinterpret_cast<uint4*>((is_v ? p.dv + t * p.lddv : p.dk + t * p.lddk) + g * D + ch * 8) = pack_times(acc, 1.f);
+  }
 }
 
 constexpr int fwd_smem_bytes(int d) { return fwd_tile_bytes(d) + 64 + 16; }
 constexpr int dq_smem_bytes(int d) { return dq_tile_bytes(d) + 64; }
-constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 6 * 64 * 4, 4 * 32 * (d + 4) * 4); }
-constexpr int dkv_pair_smem_bytes(int d) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * 4 * 64 * 16 + 2 * 6 * 64 * 4; }
 
 long row_count(const SpanArgs& p) { return (long)(p.a / p.kh) * p.seq_q; }
 size_t row_part_bytes(const SpanArgs& p, int d) { return (size_t)p.kh * p.batch * row_count(p) * (d + 4) * 4; }      // o or dq, and (m, l, lt)
-size_t key_part_bytes(const SpanArgs& p, int d) { return (size_t)2 * p.batch * p.seq_kv * p.kh * d * 4; }
 size_t tiles_bytes(const SpanArgs& p) { return (size_t)p.batch * ceil_div(row_count(p), 64) * 16; }
 // Forward and dQ: two workgroups of 128 rows per CU.
 int row_splits(const SpanArgs& p, int d, size_t bytes) {
   return splits_for((long)ceil_div(row_count(p), 128) * p.kh * p.batch, 512, ceil_div(p.seq_kv, 64), 1.4, row_part_bytes(p, d), bytes);
 }
-// dK, dV: the kernel at d = 128 has a CU to itself; at d = 64 two share one, and a third takes the place of those that end early
-int key_splits(const SpanArgs& p, int d, size_t bytes) {
-  return splits_for((long)ceil_div(p.seq_kv, 128) * p.kh * p.batch, d == 128 ? 256 : 768, ceil_div(row_count(p), 64), d == 128 ? 2.2 : 1.6, key_part_bytes(p, d), bytes);
+long key_tiles(const SpanArgs& p) { return (long)p.batch * ceil_div(p.seq_kv, 128); }
+// Pieces of a key head for dK, dV: as many as the chip works on at a time (at d = 128 a workgroup has a CU to itself, at d = 64 two share one), unless there are
+// rounds enough for the key tiles to even out by themselves.
+int parts_of(const SpanArgs& p, int d) {
+  const long groups = key_tiles(p) * p.kh, slots = d == 128 ? 256 : 512;
+  if (key_tiles(p) > MOST_TILES || groups == 0 || groups >= 8 * slots) return 0;
+  long n = slots / p.kh;
+  const long most = key_tiles(p) * ceil_div(row_count(p), 64) / LEAST_PAIRS;
+  if (n > most) n = most;
+  return n < 1 ? 1 : (int)n;
 }
+size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
+struct KeyPlaces {      // in the scratch behind what the row tiles see
+  size_t ranges, sums, part, end;
+  KeyPlaces(const SpanArgs& p, int d, int parts) {
+    ranges = 0;
+    sums = round256(key_tiles(p) * 8);
+    part = sums + round256((key_tiles(p) + 1) * 4);
+    end = parts ? part + (size_t)parts * p.kh * 2 * (2 * 128 * d * 4) : 0;
+  }
+};
 
 template <int D, bool DQ>
 hipError_t join_rows(hipStream_t st, const SpanArgs& p) {
@@ -1234,14 +1404,6 @@ hipError_t join_rows(hipStream_t st, const SpanArgs& p) {
   if (g == 4) return launch(span_row_join_kernel<D, 4, DQ>, grid, 256, 0, st, p);
   return launch(span_row_join_kernel<D, 16, DQ>, grid, 256, 0, st, p);
 }
-template <int D>
-hipError_t join_keys(hipStream_t st, const SpanArgs& p) {
-  const int g = join_groups(p.splits), grid = ceil_div((long)2 * p.batch * p.seq_kv * p.kh, 256 / (D / 8 * g));
-  if (g == 1) return launch(span_key_join_kernel<D, 1>, grid, 256, 0, st, p);
-  if (g == 4) return launch(span_key_join_kernel<D, 4>, grid, 256, 0, st, p);
-  return launch(span_key_join_kernel<D, 16>, grid, 256, 0, st, p);
-}
-
 template <int D, bool CAP, bool BIAS>
 hipError_t fwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
   const int nhb = p.kh * p.batch;
@@ -1276,12 +1438,22 @@ hipError_t bwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
     }
   }
   if (e != hipSuccess || p.seq_kv == 0) return e;
-  p.splits = key_splits(p, D, bytes);
-  const int grid = ceil_div(p.seq_kv, 128) * nhb * p.splits;
-  if constexpr (D == 128) e = launch(span_dkv_pair_kernel<D, CAP, BIAS>, grid, 512, dkv_pair_smem_bytes(D), st, p);
-  else e = launch(span_dkv_kernel<D, CAP, BIAS>, grid, 256, dkv_smem_bytes(D), st, p);
-  if (e != hipSuccess || p.splits == 1) return e;
-  return join_keys<D>(st, p);
+  p.parts = rows > 0 ? parts_of(p, D) : 0;
+  const KeyPlaces at(p, D, p.parts);
+  if (bytes < at.end) p.parts = 0;
+  if (p.parts > 0) {
+    char* const mem = static_cast<char*>(scratch) + head;
+    p.ranges = reinterpret_cast<int2*>(mem + at.ranges);
+    p.sums = reinterpret_cast<int*>(mem + at.sums);
+    p.part = reinterpret_cast<float*>(mem + at.part);
+    e = launch(span_range_kernel, (int)key_tiles(p), 256, 0, st, p);
+    if (e != hipSuccess) return e;
+  }
+  const int grid = p.parts > 0 ? p.parts * p.kh : (int)key_tiles(p) * p.kh;
+  if constexpr (D == 128) e = launch(span_dkv_pair_kernel<D, CAP, BIAS>, grid, 512, dkv_pair_smem_bytes(D) + (p.parts > 0 ? (int)sizeof(Share<512>) : 0), st, p);
+  else e = launch(span_dkv_kernel<D, CAP, BIAS>, grid, 256, dkv_smem_bytes(D) + (p.parts > 0 ? (int)sizeof(Share<256>) : 0), st, p);
+  if (e != hipSuccess || p.parts == 0) return e;
+  return launch(span_key_join_kernel<D>, (int)key_tiles(p) * p.kh * 8, 256, 0, st, p);
 }
 
 // One of eight: d, cap, bias.
@@ -1301,8 +1473,8 @@ hipError_t with_kind(const SpanArgs& p, int d, F&& f) {
 // ------------------------------------------------------------------------------------------------ launchers
 void k_span_attn_scratch(const SpanArgs& p, int d, size_t* fwd_bytes, size_t* bwd_bytes) {
   const size_t all = ~(size_t)0;
-  const int rs = row_splits(p, d, all), ks = key_splits(p, d, all);
-  const size_t r = rs > 1 ? rs * row_part_bytes(p, d) : 0, k = ks > 1 ? ks * key_part_bytes(p, d) : 0;
+  const int rs = row_splits(p, d, all), parts = row_count(p) > 0 ? parts_of(p, d) : 0;
+  const size_t r = rs > 1 ? rs * row_part_bytes(p, d) : 0, k = KeyPlaces(p, d, parts).end;
   *fwd_bytes = r;
   *bwd_bytes = tiles_bytes(p) + (r > k ? r : k);
 }
