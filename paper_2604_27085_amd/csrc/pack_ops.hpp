@@ -76,6 +76,7 @@ struct SpanArgs {
   int splits;
   int2* ranges;                    // [batch * key tiles] row tiles that see any of its keys
   int* sums;                       // [batch * key tiles + 1]
+  int4* pieces;                    // [parts]
   int parts;                       // pieces of a key head's (key tile, row tile) pairs, or 0
 };
 void k_span_attn_scratch(const SpanArgs& p, int d, size_t* fwd_bytes, size_t* bwd_bytes);

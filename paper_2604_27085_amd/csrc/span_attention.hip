@@ -39,7 +39,6 @@ constexpr float LOG2E = 1.4426950408889634f;
 struct Rows {
   int b, g, grp, total, seq_q;
   unsigned inv;      // 2^32 / grp, rounded up
-  bool even;         // a tile of 64 rows begins with a query
   RP_DEV Rows(const SpanArgs& p, int hb) {
     b = hb / p.kh;
     g = hb - b * p.kh;
@@ -47,7 +46,6 @@ struct Rows {
     seq_q = p.seq_q;
     total = grp * seq_q;
     inv = grp > 1 ? 0xffffffffu / (unsigned)grp + 1u : 0u;
-    even = 64 % grp == 0;
   }
   // query and head within the group of row r: r inv / 2^32 is at most one too large
   RP_DEV void at(int r, int& q, int& h) const {
@@ -675,15 +673,22 @@ __global__ void __launch_bounds__(256, 2) span_dq_kernel(const SpanArgs p) {
 }
 
 // ================================================================================================ dK, dV
-// A thread's share of the 64-row tiles of q and dO, zero behind the last row.  Where 64 divides by the heads of a group a tile begins with a query: a thread's pieces then are
-// at the same places from there in every tile, and the descriptor, which begins at the tile's first query and ends behind the last one, does the rest.  (Queries and heads worked out
-// for every piece: 16 heads in groups of 2, a window of 1024 in 4096, 138 us for dK, dV instead of 118.)
-template <int D, int NT>
+// A thread's share of the 64-row tiles of q and dO, zero behind the last row: through descriptors that begin at the tile's first query and end behind the last one.  Where 64
+// divides by the heads of a group (EVEN) a tile begins with a query, and a thread's pieces are at the same places from there in every tile.  (Worked out for every piece: 16 heads in
+// groups of 2, a window of 1024 in 4096, 138 us for dK, dV instead of 118.)
+template <int D, int NT, bool EVEN>
 struct RowTile {
   static constexpr int CH = D / 8, NREG = 64 * CH / NT;
   const bf16 *qb, *dob;      // the group's first head of the sequence's first query
   long ldq, lddo;
   int q_off[NREG], do_off[NREG], queries;
+  RP_DEV void place(int it, const Rows& s, int row0, int q0, int tid, int& q_at, int& do_at) const {
+    int q, h;
+    s.at(row0 + (it * NT + tid) / CH, q, h);
+    const int in_row = h * D + ((it * NT + tid) % CH) * 8;
+    q_at = (int)(((q - q0) * ldq + in_row) * 2);
+    do_at = (int)(((q - q0) * lddo + in_row) * 2);
+  }
   RP_DEV void start(const SpanArgs& p, const Rows& s, int tid) {
     ldq = p.ldq;
     lddo = p.lddo;
@@ -691,40 +696,25 @@ struct RowTile {
     qb = p.q + (long)s.b * p.seq_q * ldq + (long)s.g * s.grp * D;
     dob = p.dout + (long)s.b * p.seq_q * lddo + (long)s.g * s.grp * D;
 #pragma unroll
-    for (int it = 0; it < NREG; ++it) {
-      int q, h;
-      s.at((it * NT + tid) / CH, q, h);
-      const int in_row = h * D + ((it * NT + tid) % CH) * 8;
-      q_off[it] = (int)((q * ldq + in_row) * 2);
-      do_off[it] = (int)((q * lddo + in_row) * 2);
-    }
+    for (int it = 0; it < NREG; ++it) place(it, s, 0, 0, tid, q_off[it], do_off[it]);
   }
   RP_DEV rsrc_t from(const bf16* base, long ld, const Rows& s, int q0) const {
-    const int left = min(queries, s.seq_q - q0);      // >= 1
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base + (long)q0 * ld), 0, (int)(((left - 1) * ld + (long)s.grp * D) * 2), 0x00020000);
+    const int left = min(queries + 2, s.seq_q - q0);      // >= 1
+    // (all of this is the same in all lanes; where the compiler does not see it, it loops over the lanes around every load)
+    const uint64_t at = reinterpret_cast<uint64_t>(base + (long)q0 * ld);
+    const uint64_t same = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(same), 0, __builtin_amdgcn_readfirstlane((int)(((left - 1) * ld + (long)s.grp * D) * 2)), 0x00020000);
   }
   RP_DEV void load(uint4 (&q_reg)[NREG], uint4 (&do_reg)[NREG], const Rows& s, int u, int tid) const {
-    if (s.even) {
-      const int q0 = u * queries;
-      const rsrc_t rq = from(qb, ldq, s, q0), rdo = from(dob, lddo, s, q0);
-#pragma unroll
-      for (int it = 0; it < NREG; ++it) {
-        q_reg[it] = buf_load16(rq, (uint32_t)q_off[it]);
-        do_reg[it] = buf_load16(rdo, (uint32_t)do_off[it]);
-      }
-      return;
-    }
+    int q0 = u * queries, h0;
+    if (!EVEN) s.at(u * 64, q0, h0);
+    const rsrc_t rq = from(qb, ldq, s, q0), rdo = from(dob, lddo, s, q0);
 #pragma unroll
     for (int it = 0; it < NREG; ++it) {
-      typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));      // (copied as a struct, the pieces would live in scratch memory)
-      const int r = u * 64 + (it * NT + tid) / CH;
-      int q, h;
-      s.at(r < s.total ? r : 0, q, h);
-      const int in_row = h * D + ((it * NT + tid) % CH) * 8;
-      const u32x4 x = *reinterpret_cast<const u32x4*>(qb + q * ldq + in_row), y = *reinterpret_cast<const u32x4*>(dob + q * lddo + in_row);
-      const unsigned in = r < s.total ? 0xffffffffu : 0u;      // 0 times what the first row holds may be NaN
-      q_reg[it] = make_uint4(x.x & in, x.y & in, x.z & in, x.w & in);
-      do_reg[it] = make_uint4(y.x & in, y.y & in, y.z & in, y.w & in);
+      int q_at = q_off[it], do_at = do_off[it];
+      if (!EVEN) place(it, s, u * 64, q0, tid, q_at, do_at);
+      q_reg[it] = buf_load16(rq, (uint32_t)q_at);
+      do_reg[it] = buf_load16(rdo, (uint32_t)do_at);
     }
   }
 };
@@ -875,7 +865,8 @@ struct RowWalk {
       u = base - 1;
     }
   }
-  RP_DEV void start(const int4* t, int key0, int key1, int first, int end, int lane) {
+  // (the last tile is taken in any case, so that its rows are on their way before anything is known of it: where it sees none of the keys the mask says so)
+  RP_DEV void start(const int4* t, int key0, int key1, int first, int end) {
     tiles = t;
     k0 = key0;
     k1 = key1;
@@ -883,7 +874,6 @@ struct RowWalk {
     u = end - 1;
     base = end;
     any = all = 0;
-    settle(lane);
   }
   RP_DEV bool more() const { return u >= from; }
   RP_DEV bool whole() const { return all >> (u - base) & 1; }      // every row of the present tile sees all of the keys
@@ -899,7 +889,10 @@ struct RowWalk {
 // in order.  (8192 causal tokens, 64 heads of 64: a key tile a workgroup 1880 us.)  With more than MOST_TILES key tiles, or without scratch for the parts (parts 0), a
 // workgroup does a key tile.
 constexpr int MOST_TILES = 2048;
-constexpr int LEAST_PAIRS = 6;       // of a piece: beginning and ending with a key tile costs as much as two to three pairs
+// Beginning and ending with a key tile, and the masks of the 2 grp row tiles at its edge, cost about as much as so many pairs: they count as that many before a key tile's
+// first.  (Without them the piece with the shortest key tiles lasts 20 % longer than the others at 8192 causal tokens.)
+RP_DEV int edge_pairs(int grp) { return 4 + min(grp, 16); }
+RP_DEV int piece_length(int pairs, int parts, int edge) { return max((pairs + parts - 1) / parts, 2 * edge); }
 
 // ranges[i]: key tile i % KT of sequence i / KT
 __global__ void __launch_bounds__(256) span_range_kernel(const SpanArgs p) {
@@ -910,66 +903,69 @@ __global__ void __launch_bounds__(256) span_range_kernel(const SpanArgs p) {
   if (threadIdx.x == 0) p.ranges[blockIdx.x] = r;
 }
 
-// A workgroup's share, key tile by key tile.
-template <int NT>
-struct Share {
-  int sum[MOST_TILES + 1];      // pairs before every key tile
-  int wave[NT / 64];
-  // all threads; the first workgroup of all leaves the sums behind
-  RP_DEV int add_up(const SpanArgs& p, int n, int tid) {
-    constexpr int EACH = MOST_TILES / NT;
-    int c[EACH], total = 0;
+// sums[i]: pairs before key tile i, edges included; pieces[i]: first key tile, first pair, pair behind the last.  One block.
+__global__ void __launch_bounds__(1024) span_plan_kernel(const SpanArgs p) {
+  __shared__ int sum[MOST_TILES + 1], wave[16];
+  const int tid = threadIdx.x, n = p.batch * ((p.seq_kv + 127) / 128), edge = edge_pairs(p.a / p.kh);
+  int c[2], s = 0;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int t = tid * EACH + i;
-      c[i] = 0;
-      if (t < n) {
-        const int2 r = p.ranges[t];
-        c[i] = r.y - r.x;
-      }
-      total += c[i];
-    }
-    int s = total;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(s, o, 64);
-      if ((tid & 63) >= o) s += v;
-    }
-    if ((tid & 63) == 63) wave[tid >> 6] = s;
-    __syncthreads();
-    int at = s - total, all = 0;
-    for (int w = 0; w < NT / 64; ++w) {
-      if (w < tid >> 6) at += wave[w];
-      all += wave[w];
-    }
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int t = tid * EACH + i;
-      if (t < n) sum[t] = at;
-      at += c[i];
-    }
-    if (tid == 0) sum[n] = all;
-    __syncthreads();
-    if (blockIdx.x == 0)
-      for (int t = tid; t <= n; t += NT) p.sums[t] = sum[t];
-    return __builtin_amdgcn_readfirstlane(all);
+  for (int i = 0; i < 2; ++i) {
+    const int t = 2 * tid + i;
+    const int2 r = t < n ? p.ranges[t] : make_int2(0, 0);
+    c[i] = r.y > r.x ? r.y - r.x + edge : 0;
+    s += c[i];
   }
-  // the key tile that pair w belongs to: the last one that begins at or before it
-  RP_DEV int tile_of(int w, int n) const {
-    int lo = 0, hi = n;
+  const int own = s;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(s, o, 64);
+    if ((tid & 63) >= o) s += v;
+  }
+  if ((tid & 63) == 63) wave[tid >> 6] = s;
+  __syncthreads();
+  int at = s - own, all = 0;
+  for (int w = 0; w < 16; ++w) {
+    if (w < tid >> 6) at += wave[w];
+    all += wave[w];
+  }
+  if (2 * tid <= n) p.sums[2 * tid] = sum[2 * tid] = at;
+  if (2 * tid + 1 <= n) p.sums[2 * tid + 1] = sum[2 * tid + 1] = at + c[0];
+  if (n == MOST_TILES && tid == 0) p.sums[n] = sum[n] = all;
+  __syncthreads();
+  const int each = piece_length(all, p.parts, edge);
+  for (int i = tid; i < p.parts; i += 1024) {
+    const int from = i * each, to = min(from + each, all);
+    int lo = 0, hi = n;      // the last key tile that begins at or before the first pair
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (sum[mid] <= w) lo = mid;
+      if (sum[mid] <= from) lo = mid;
       else hi = mid;
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    p.pieces[i] = make_int4(lo, from, to, 0);
   }
-};
-RP_DEV int piece_length(int pairs, int parts) { return max((pairs + parts - 1) / parts, LEAST_PAIRS); }
+}
+
+// The kernel's only argument, read anew: what is needed once for a key tile would otherwise sit in (spilled) scalar registers through the loop over its rows.
+template <typename T>
+RP_DEV void in_global(T*& p) { p = (T*)(__attribute__((address_space(1))) T*)reinterpret_cast<uint64_t>(p); }      // (else its loads would be flat ones)
+RP_DEV SpanArgs read_again() {
+  static_assert(sizeof(SpanArgs) % 8 == 0, "read by eight bytes");
+  typedef const __attribute__((address_space(4))) uint64_t* args_t;      // (the constant address space: scalar loads)
+  args_t at = (args_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  uint64_t raw[sizeof(SpanArgs) / 8];
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(SpanArgs) / 8); ++i) raw[i] = at[i];
+  SpanArgs p;
+  __builtin_memcpy(&p, raw, sizeof p);
+  in_global(p.q); in_global(p.k); in_global(p.v); in_global(p.dout); in_global(p.dk); in_global(p.dv); in_global(p.lse_in); in_global(p.delta);
+  in_global(p.span); in_global(p.q_pos); in_global(p.slopes); in_global(p.tiles); in_global(p.part); in_global(p.ranges); in_global(p.sums);
+  return p;
+}
 
 // The keys of a workgroup do not mix: a column of the score tiles is a key's own.
-template <int D, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
+template <int D, bool CAP, bool BIAS, bool EVEN>
+__global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
   constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, NT = 256;
   using T64 = Tile64<D, NT>;
   using Stat = RowStat<CAP, BIAS>;
@@ -981,42 +977,35 @@ __global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Score sc(p);
-  const int tiles_kv = (p.seq_kv + 127) / 128, all_kv = p.batch * tiles_kv;
-  Share<NT>* const share = reinterpret_cast<Share<NT>*>(dyn_smem + dkv_smem_bytes(D));
-  int pair = 0, last_pair = 1, tile, g;      // balanced: the present (key tile, row tile) pair of the head
-  if (p.parts > 0) {
-    g = (int)blockIdx.x % p.kh;
-    const int pairs = share->add_up(p, all_kv, tid), each = piece_length(pairs, p.parts);
-    pair = (int)blockIdx.x / p.kh * each;
-    last_pair = min(pair + each, pairs);
+  const Score sc(args);
+  const int tiles_kv = (args.seq_kv + 127) / 128;
+  int tile, pair = 0, last_pair = 1, g;      // the present key tile and, in pieces, (key tile, row tile) pair of the head
+  if (args.parts > 0) {
+    g = (int)blockIdx.x % args.kh;
+    const int4 piece = args.pieces[(int)blockIdx.x / args.kh];
+    tile = piece.x;
+    pair = piece.y;
+    last_pair = piece.z;
     if (pair >= last_pair) return;      // uniform over the workgroup
-    tile = share->tile_of(pair, all_kv);
   } else {
-    const int nhb = p.kh * p.batch, rest = (int)blockIdx.x / nhb, hb = head_at((int)blockIdx.x, rest, nhb);
-    g = hb % p.kh;
-    tile = hb / p.kh * tiles_kv + rest;
+    const int nhb = args.kh * args.batch, rest = (int)blockIdx.x / nhb, hb = head_at((int)blockIdx.x, rest, nhb);
+    g = hb % args.kh;
+    tile = hb / args.kh * tiles_kv + rest;
   }
-  const bool by_tile = p.parts == 0;
-  int slot = 0;      // of the parts that go to scratch: the piece begins with it, or not
-  for (;; ++tile) {
+  for (int slot = 0;; slot = 1) {      // slot: of the parts that go to scratch, the piece begins with it, or not
+  const SpanArgs p = read_again();
   const int b = tile / tiles_kv, kv0 = (tile - b * tiles_kv) * 128, kw0 = kv0 + 32 * w;
   const Rows s(p, b * p.kh + g);
-  const int4* const row_tile = p.tiles + (long)b * ((s.total + 63) / 64);
-  const int key_end = min(kv0 + 128, p.seq_kv);
-  int u0, u1;
-  bool mine = true;      // the whole key tile is done here
-  if (by_tile) {
-    const int2 r = row_tiles<NT>(row_tile, (s.total + 63) / 64, kv0, key_end, reinterpret_cast<int*>(stat), tid);
-    u0 = r.x;
-    u1 = r.y;
-  } else {
-    const int begin = share->sum[tile], end = share->sum[tile + 1];
-    const int2 r = p.ranges[tile];
-    u0 = r.x + pair - begin;
-    u1 = r.x + min(last_pair, end) - begin;
-    mine = pair == begin && last_pair >= end;
+  const int2 r = p.ranges[tile];
+  int u0 = r.x, u1 = r.y, end = 0;
+  if (p.parts > 0) {
+    const int begin = p.sums[tile], edge = edge_pairs(s.grp);
+    end = p.sums[tile + 1];
+    u0 = r.x + max(pair - begin - edge, 0);
+    u1 = r.x + max(min(last_pair, end) - begin - edge, 0);
+    if (u0 >= u1) return;      // nothing but the edge of the last key tile is left (uniform over the workgroup)
   }
+  const bool mine = u0 == r.x && u1 == r.y;      // the whole key tile is done here
   const int kpos[2] = {kw0 + lr, kw0 + 16 + lr};
   const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
   const bf16* const vb = p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D;
@@ -1043,7 +1032,7 @@ __global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
   const bf16* dotfrag = dOs + tr_base<LD>(lane);
 
   uint4 qreg[T64::NREG], doreg[T64::NREG];
-  RowTile<D, NT> rows;
+  RowTile<D, NT, EVEN> rows;
   rows.start(p, s, tid);
   Stat rstat;
   rstat.start(p, s, w);
@@ -1052,8 +1041,11 @@ __global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
     rstat.load(p, s, u * 64, lane, w);
   };
   RowWalk range;
-  range.start(row_tile, kv0, key_end, u0, u1, lane);
-  if (range.more()) prefetch(range.u);
+  range.start(p.tiles + (long)s.b * ((s.total + 63) / 64), kv0, min(kv0 + 128, p.seq_kv), u0, u1);
+  if (range.more()) {
+    prefetch(range.u);
+    range.look(lane);
+  }
   while (range.more()) {
     const bool whole = range.whole();
     __syncthreads();
@@ -1122,29 +1114,27 @@ __global__ void __launch_bounds__(256) span_dkv_kernel(const SpanArgs p) {
     }
   }
   __syncthreads();
-  if (mine) {
-    const long tok0 = (long)s.b * p.seq_kv;
-    bf16* const stage = smem + w * 32 * (D + 8);
-    store_acc_T<D>(dkacc, sc.grad, stage, p.dk + tok0 * p.lddk + s.g * D, p.lddk, kw0, p.seq_kv, lane);
-    store_acc_T<D>(dvacc, 1.f, stage, p.dv + tok0 * p.lddv + s.g * D, p.lddv, kw0, p.seq_kv, lane);
-  } else {
-    float* const stage = reinterpret_cast<float*>(smem) + w * 32 * (D + 4);
-    float* const out = p.part + ((long)blockIdx.x * 2 + slot) * (2 * 128 * D);
-    store_acc_T_f32<D>(dkacc, sc.grad, stage, out, D, 32 * w, 128, lane);
-    store_acc_T_f32<D>(dvacc, 1.f, stage, out + 128 * D, D, 32 * w, 128, lane);
+  const SpanArgs out = read_again();
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {      // dk, then dv in its place: the code once
+    const float mul = which ? 1.f : sc.grad;
+    const long ld = which ? out.lddv : out.lddk;
+    if (mine) store_acc_T<D>(dkacc, mul, smem + w * 32 * (D + 8), (which ? out.dv : out.dk) + (long)s.b * out.seq_kv * ld + s.g * D, ld, kw0, out.seq_kv, lane);
+    else store_acc_T_f32<D>(dkacc, mul, reinterpret_cast<float*>(smem) + w * 32 * (D + 4), out.part + (((long)blockIdx.x * 2 + slot) * 2 + which) * (128 * D), D, 32 * w, 128, lane);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) { dkacc[dt][0] = dvacc[dt][0]; dkacc[dt][1] = dvacc[dt][1]; }
   }
-  if (by_tile) return;
-  pair = share->sum[tile + 1];
-  if (pair >= last_pair) return;
-  slot = 1;
-  while (share->sum[tile + 2] == pair) ++tile;      // key tiles that nothing sees (there is a pair left, so the walk ends)
+  if (out.parts == 0 || end >= last_pair) return;
+  pair = end;
+  do ++tile;
+  while (out.sums[tile + 1] == pair);      // over key tiles that nothing sees (there is a pair left, so this ends)
   }
 }
 
 // Two waves per SIMD at d = 128 (see attn_bwd_dkv_pair_kernel in attention.hip): the 32 keys of a pair of waves are shared, wave h of it keeps
 // the accumulators of half h of the head dimension, makes the scores of rows 32 h .. of each tile and hands P and dS to its partner through LDS.
-template <int D, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
+template <int D, bool CAP, bool BIAS, bool EVEN>
+__global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs args) {
   constexpr int LD = tile_ld(D), KS = D / 32, DH = D / 32, NT = 512;
   using T64 = Tile64<D, NT>;
   using Stat = RowStat<CAP, BIAS>;
@@ -1157,42 +1147,35 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int w = w8 >> 1, h = w8 & 1;
-  const Score sc(p);
-  const int tiles_kv = (p.seq_kv + 127) / 128, all_kv = p.batch * tiles_kv;
-  Share<NT>* const share = reinterpret_cast<Share<NT>*>(dyn_smem + dkv_pair_smem_bytes(D));
-  int pair = 0, last_pair = 1, tile, g;      // balanced: the present (key tile, row tile) pair of the head
-  if (p.parts > 0) {
-    g = (int)blockIdx.x % p.kh;
-    const int pairs = share->add_up(p, all_kv, tid), each = piece_length(pairs, p.parts);
-    pair = (int)blockIdx.x / p.kh * each;
-    last_pair = min(pair + each, pairs);
+  const Score sc(args);
+  const int tiles_kv = (args.seq_kv + 127) / 128;
+  int tile, pair = 0, last_pair = 1, g;      // the present key tile and, in pieces, (key tile, row tile) pair of the head
+  if (args.parts > 0) {
+    g = (int)blockIdx.x % args.kh;
+    const int4 piece = args.pieces[(int)blockIdx.x / args.kh];
+    tile = piece.x;
+    pair = piece.y;
+    last_pair = piece.z;
     if (pair >= last_pair) return;      // uniform over the workgroup
-    tile = share->tile_of(pair, all_kv);
   } else {
-    const int nhb = p.kh * p.batch, rest = (int)blockIdx.x / nhb, hb = head_at((int)blockIdx.x, rest, nhb);
-    g = hb % p.kh;
-    tile = hb / p.kh * tiles_kv + rest;
+    const int nhb = args.kh * args.batch, rest = (int)blockIdx.x / nhb, hb = head_at((int)blockIdx.x, rest, nhb);
+    g = hb % args.kh;
+    tile = hb / args.kh * tiles_kv + rest;
   }
-  const bool by_tile = p.parts == 0;
-  int slot = 0;      // of the parts that go to scratch: the piece begins with it, or not
-  for (;; ++tile) {
+  for (int slot = 0;; slot = 1) {      // slot: of the parts that go to scratch, the piece begins with it, or not
+  const SpanArgs p = read_again();
   const int b = tile / tiles_kv, kv0 = (tile - b * tiles_kv) * 128, kw0 = kv0 + 32 * w;
   const Rows s(p, b * p.kh + g);
-  const int4* const row_tile = p.tiles + (long)b * ((s.total + 63) / 64);
-  const int key_end = min(kv0 + 128, p.seq_kv);
-  int u0, u1;
-  bool mine = true;      // the whole key tile is done here
-  if (by_tile) {
-    const int2 r = row_tiles<NT>(row_tile, (s.total + 63) / 64, kv0, key_end, reinterpret_cast<int*>(stat), tid);
-    u0 = r.x;
-    u1 = r.y;
-  } else {
-    const int begin = share->sum[tile], end = share->sum[tile + 1];
-    const int2 r = p.ranges[tile];
-    u0 = r.x + pair - begin;
-    u1 = r.x + min(last_pair, end) - begin;
-    mine = pair == begin && last_pair >= end;
+  const int2 r = p.ranges[tile];
+  int u0 = r.x, u1 = r.y, end = 0;
+  if (p.parts > 0) {
+    const int begin = p.sums[tile], edge = edge_pairs(s.grp);
+    end = p.sums[tile + 1];
+    u0 = r.x + max(pair - begin - edge, 0);
+    u1 = r.x + max(min(last_pair, end) - begin - edge, 0);
+    if (u0 >= u1) return;      // nothing but the edge of the last key tile is left (uniform over the workgroup)
   }
+  const bool mine = u0 == r.x && u1 == r.y;      // the whole key tile is done here
   const int kpos[2] = {kw0 + lr, kw0 + 16 + lr};
   const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
   const bf16* const vb = p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D;
@@ -1221,7 +1204,7 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
   const uint4* const ex_theirs = exch + ((w8 ^ 1) * 4) * 64 + lane;
 
   uint4 qreg[T64::NREG], doreg[T64::NREG];
-  RowTile<D, NT> rows;
+  RowTile<D, NT, EVEN> rows;
   rows.start(p, s, tid);
   Stat rstat;
   rstat.start(p, s, w8);
@@ -1230,8 +1213,7 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
     rstat.load(p, s, u * 64, lane, w8);
   };
   RowWalk range;
-  range.start(row_tile, kv0, key_end, u0, u1, lane);
-  if (range.more()) prefetch(range.u);
+  range.start(p.tiles + (long)s.b * ((s.total + 63) / 64), kv0, min(kv0 + 128, p.seq_kv), u0, u1);
 
   constexpr int AHEAD = 2;     // two waves per SIMD cover each other's LDS latency: a short ring is enough
   auto update_half = [&](int set, int t2, const uint4 (&pf)[2], const uint4 (&df)[2]) {
@@ -1262,6 +1244,10 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
     const uint4 pdf[2] = {ex_theirs[128], ex_theirs[192]};
     update_half(prev & 1, h ^ 1, ppf, pdf);
   };
+  if (range.more()) {
+    prefetch(range.u);
+    range.look(lane);
+  }
   int i = 0;
   for (; range.more(); ++i) {
     const bool whole = range.whole();
@@ -1316,23 +1302,21 @@ __global__ void __launch_bounds__(512) span_dkv_pair_kernel(const SpanArgs p) {
   __syncthreads();
   if (i > 0) partner_update(i - 1);
   __syncthreads();
-  if (mine) {
-    const long tok0 = (long)s.b * p.seq_kv;
+  const SpanArgs out = read_again();
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {      // dk, then dv in its place: the code once
+    const float mul = which ? 1.f : sc.grad;
     const int d0 = s.g * D + h * (D / 2);
-    bf16* const stage = smem + w8 * 32 * (D / 2 + 8);
-    store_acc_T<D / 2>(dkacc, sc.grad, stage, p.dk + tok0 * p.lddk + d0, p.lddk, kw0, p.seq_kv, lane);
-    store_acc_T<D / 2>(dvacc, 1.f, stage, p.dv + tok0 * p.lddv + d0, p.lddv, kw0, p.seq_kv, lane);
-  } else {
-    float* const stage = reinterpret_cast<float*>(smem) + w8 * 32 * (D / 2 + 4);
-    float* const out = p.part + ((long)blockIdx.x * 2 + slot) * (2 * 128 * D) + h * (D / 2);
-    store_acc_T_f32<D / 2>(dkacc, sc.grad, stage, out, D, 32 * w, 128, lane);
-    store_acc_T_f32<D / 2>(dvacc, 1.f, stage, out + 128 * D, D, 32 * w, 128, lane);
+    const long ld = which ? out.lddv : out.lddk;
+    if (mine) store_acc_T<D / 2>(dkacc, mul, smem + w8 * 32 * (D / 2 + 8), (which ? out.dv : out.dk) + (long)s.b * out.seq_kv * ld + d0, ld, kw0, out.seq_kv, lane);
+    else store_acc_T_f32<D / 2>(dkacc, mul, reinterpret_cast<float*>(smem) + w8 * 32 * (D / 2 + 4), out.part + (((long)blockIdx.x * 2 + slot) * 2 + which) * (128 * D) + h * (D / 2), D, 32 * w, 128, lane);
+#pragma unroll
+    for (int dt = 0; dt < DH; ++dt) { dkacc[dt][0] = dvacc[dt][0]; dkacc[dt][1] = dvacc[dt][1]; }
   }
-  if (by_tile) return;
-  pair = share->sum[tile + 1];
-  if (pair >= last_pair) return;
-  slot = 1;
-  while (share->sum[tile + 2] == pair) ++tile;      // key tiles that nothing sees (there is a pair left, so the walk ends)
+  if (out.parts == 0 || end >= last_pair) return;
+  pair = end;
+  do ++tile;
+  while (out.sums[tile + 1] == pair);      // over key tiles that nothing sees (there is a pair left, so this ends)
   }
 }
 
@@ -1343,8 +1327,8 @@ __global__ void __launch_bounds__(256) span_key_join_kernel(const SpanArgs p) {
   const int tiles_kv = (p.seq_kv + 127) / 128, all_kv = p.batch * tiles_kv;
   const int i = (int)blockIdx.x >> 3, rows = ((int)blockIdx.x & 3) * 32, is_v = (int)blockIdx.x >> 2 & 1;
   const int tile = i / p.kh, g = i - tile * p.kh;
-  const int begin = p.sums[tile], end = p.sums[tile + 1], each = piece_length(p.sums[all_kv], p.parts);
-  const int from = begin / each, to = (end - 1) / each;
+  const int edge = edge_pairs(p.a / p.kh), begin = p.sums[tile], end = p.sums[tile + 1], each = piece_length(p.sums[all_kv], p.parts, edge);
+  const int from = (begin + edge) / each, to = (end - 1) / each;      // the pieces of its first and of its last pair
   if (end > begin && from == to) return;      // one workgroup had it all
   const int b = tile / tiles_kv, kv0 = (tile - b * tiles_kv) * 128;
   for (int e = threadIdx.x; e < 32 * CH; e += 256) {
@@ -1354,9 +1338,9 @@ __global__ void __launch_bounds__(256) span_key_join_kernel(const SpanArgs p) {
 #pragma unroll
     for (int x = 0; x < 8; ++x) acc[x] = 0.f;
     if (end > begin) {
-      // the first of them began its piece earlier, unless the two begin together; the others begin with this key tile
+      // the first of them began its piece with another key tile, unless it begins in this one's edge; the others begin with this key tile
       const float* const src = p.part + (long)is_v * 128 * D + row * D + ch * 8;
-      add_times(acc, src + ((long)(from * p.kh + g) * 2 + (from * each == begin ? 0 : 1)) * (2 * 128 * D), 1.f);
+      add_times(acc, src + ((long)(from * p.kh + g) * 2 + (from * each >= begin ? 0 : 1)) * (2 * 128 * D), 1.f);
 #pragma unroll 4
       for (int w = from + 1; w <= to; ++w) add_times(acc, src + (long)(w * p.kh + g) * 2 * (2 * 128 * D), 1.f);
     }
@@ -1370,7 +1354,6 @@ constexpr int dq_smem_bytes(int d) { return dq_tile_bytes(d) + 64; }
 
 long row_count(const SpanArgs& p) { return (long)(p.a / p.kh) * p.seq_q; }
 size_t row_part_bytes(const SpanArgs& p, int d) { return (size_t)p.kh * p.batch * row_count(p) * (d + 4) * 4; }      // o or dq, and (m, l, lt)
-size_t tiles_bytes(const SpanArgs& p) { return (size_t)p.batch * ceil_div(row_count(p), 64) * 16; }
 // Forward and dQ: two workgroups of 128 rows per CU.
 int row_splits(const SpanArgs& p, int d, size_t bytes) {
   return splits_for((long)ceil_div(row_count(p), 128) * p.kh * p.batch, 512, ceil_div(p.seq_kv, 64), 1.4, row_part_bytes(p, d), bytes);
@@ -1382,17 +1365,20 @@ int parts_of(const SpanArgs& p, int d) {
   const long groups = key_tiles(p) * p.kh, slots = d == 128 ? 256 : 512;
   if (key_tiles(p) > MOST_TILES || groups == 0 || groups >= 8 * slots) return 0;
   long n = slots / p.kh;
-  const long most = key_tiles(p) * ceil_div(row_count(p), 64) / LEAST_PAIRS;
+  const long most = key_tiles(p) * ceil_div(row_count(p), 64) / 4;
   if (n > most) n = most;
   return n < 1 ? 1 : (int)n;
 }
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
-struct KeyPlaces {      // in the scratch behind what the row tiles see
-  size_t ranges, sums, part, end;
+// What the backward call cannot do without: what the row tiles see, and the row tiles of every key tile.
+size_t tiles_bytes(const SpanArgs& p) { return round256((size_t)p.batch * ceil_div(row_count(p), 64) * 16); }
+size_t least_bytes(const SpanArgs& p) { return tiles_bytes(p) + round256((size_t)key_tiles(p) * 8); }
+struct KeyPlaces {      // in the scratch behind that
+  size_t sums, pieces, part, end;
   KeyPlaces(const SpanArgs& p, int d, int parts) {
-    ranges = 0;
-    sums = round256(key_tiles(p) * 8);
-    part = sums + round256((key_tiles(p) + 1) * 4);
+    sums = 0;
+    pieces = round256((key_tiles(p) + 1) * 4);
+    part = pieces + round256((size_t)parts * 16);
     end = parts ? part + (size_t)parts * p.kh * 2 * (2 * 128 * d * 4) : 0;
   }
 };
@@ -1421,8 +1407,9 @@ template <int D, bool CAP, bool BIAS>
 hipError_t bwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
   const int nhb = p.kh * p.batch;
   const long rows = row_count(p);
-  const size_t head = tiles_bytes(p);
+  const size_t head = least_bytes(p);
   p.tiles = static_cast<int4*>(scratch);
+  p.ranges = reinterpret_cast<int2*>(static_cast<char*>(scratch) + tiles_bytes(p));
   p.part = reinterpret_cast<float*>(static_cast<char*>(scratch) + head);
   bytes -= head;
   hipError_t e = hipSuccess;
@@ -1441,17 +1428,20 @@ hipError_t bwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
   p.parts = rows > 0 ? parts_of(p, D) : 0;
   const KeyPlaces at(p, D, p.parts);
   if (bytes < at.end) p.parts = 0;
+  e = launch(span_range_kernel, (int)key_tiles(p), 256, 0, st, p);
+  if (e != hipSuccess) return e;
   if (p.parts > 0) {
     char* const mem = static_cast<char*>(scratch) + head;
-    p.ranges = reinterpret_cast<int2*>(mem + at.ranges);
     p.sums = reinterpret_cast<int*>(mem + at.sums);
+    p.pieces = reinterpret_cast<int4*>(mem + at.pieces);
     p.part = reinterpret_cast<float*>(mem + at.part);
-    e = launch(span_range_kernel, (int)key_tiles(p), 256, 0, st, p);
+    e = launch(span_plan_kernel, 1, 1024, 0, st, p);
     if (e != hipSuccess) return e;
   }
   const int grid = p.parts > 0 ? p.parts * p.kh : (int)key_tiles(p) * p.kh;
-  if constexpr (D == 128) e = launch(span_dkv_pair_kernel<D, CAP, BIAS>, grid, 512, dkv_pair_smem_bytes(D) + (p.parts > 0 ? (int)sizeof(Share<512>) : 0), st, p);
-  else e = launch(span_dkv_kernel<D, CAP, BIAS>, grid, 256, dkv_smem_bytes(D) + (p.parts > 0 ? (int)sizeof(Share<256>) : 0), st, p);
+  const bool even = 64 % (p.a / p.kh) == 0;
+  if constexpr (D == 128) e = launch(even ? span_dkv_pair_kernel<D, CAP, BIAS, true> : span_dkv_pair_kernel<D, CAP, BIAS, false>, grid, 512, dkv_pair_smem_bytes(D), st, p);
+  else e = launch(even ? span_dkv_kernel<D, CAP, BIAS, true> : span_dkv_kernel<D, CAP, BIAS, false>, grid, 256, dkv_smem_bytes(D), st, p);
   if (e != hipSuccess || p.parts == 0) return e;
   return launch(span_key_join_kernel<D>, (int)key_tiles(p) * p.kh * 8, 256, 0, st, p);
 }
@@ -1476,9 +1466,9 @@ void k_span_attn_scratch(const SpanArgs& p, int d, size_t* fwd_bytes, size_t* bw
   const int rs = row_splits(p, d, all), parts = row_count(p) > 0 ? parts_of(p, d) : 0;
   const size_t r = rs > 1 ? rs * row_part_bytes(p, d) : 0, k = KeyPlaces(p, d, parts).end;
   *fwd_bytes = r;
-  *bwd_bytes = tiles_bytes(p) + (r > k ? r : k);
+  *bwd_bytes = least_bytes(p) + (r > k ? r : k);
 }
-size_t k_span_attn_least(const SpanArgs& p) { return tiles_bytes(p); }
+size_t k_span_attn_least(const SpanArgs& p) { return least_bytes(p); }
 
 hipError_t k_span_attn_fwd(hipStream_t st, const SpanArgs& p, int d, void* scratch, size_t bytes) {
   if (p.batch == 0 || p.seq_q == 0) return hipSuccess;
