@@ -892,7 +892,7 @@ constexpr int MOST_TILES = 2048;
 // Beginning and ending with a key tile, and the masks of the 2 grp row tiles at its edge, cost about as much as so many pairs: they count as that many before a key tile's
 // first.  (Without them the piece with the shortest key tiles lasts 20 % longer than the others at 8192 causal tokens.)
 RP_DEV int edge_pairs(int grp) { return 4 + min(grp, 16); }
-RP_DEV int piece_length(int pairs, int parts, int edge) { return max((pairs + parts - 1) / parts, 2 * edge); }
+RP_DEV int piece_length(int pairs, int parts) { return max((pairs + parts - 1) / parts, 8); }      // (one may hold nothing but a part of an edge)
 
 // ranges[i]: key tile i % KT of sequence i / KT
 __global__ void __launch_bounds__(256) span_range_kernel(const SpanArgs p) {
@@ -932,7 +932,7 @@ __global__ void __launch_bounds__(1024) span_plan_kernel(const SpanArgs p) {
   if (2 * tid + 1 <= n) p.sums[2 * tid + 1] = sum[2 * tid + 1] = at + c[0];
   if (n == MOST_TILES && tid == 0) p.sums[n] = sum[n] = all;
   __syncthreads();
-  const int each = piece_length(all, p.parts, edge);
+  const int each = piece_length(all, p.parts);
   for (int i = tid; i < p.parts; i += 1024) {
     const int from = i * each, to = min(from + each, all);
     int lo = 0, hi = n;      // the last key tile that begins at or before the first pair
@@ -1327,7 +1327,7 @@ __global__ void __launch_bounds__(256) span_key_join_kernel(const SpanArgs p) {
   const int tiles_kv = (p.seq_kv + 127) / 128, all_kv = p.batch * tiles_kv;
   const int i = (int)blockIdx.x >> 3, rows = ((int)blockIdx.x & 3) * 32, is_v = (int)blockIdx.x >> 2 & 1;
   const int tile = i / p.kh, g = i - tile * p.kh;
-  const int edge = edge_pairs(p.a / p.kh), begin = p.sums[tile], end = p.sums[tile + 1], each = piece_length(p.sums[all_kv], p.parts, edge);
+  const int edge = edge_pairs(p.a / p.kh), begin = p.sums[tile], end = p.sums[tile + 1], each = piece_length(p.sums[all_kv], p.parts);
   const int from = (begin + edge) / each, to = (end - 1) / each;      // the pieces of its first and of its last pair
   if (end > begin && from == to) return;      // one workgroup had it all
   const int b = tile / tiles_kv, kv0 = (tile - b * tiles_kv) * 128;
