@@ -31,6 +31,7 @@ namespace {
 constexpr int fwd_tile_bytes(int d) { return max_i(64 * (d + 8) + 64 * (d + 32), 128 * (d + 8)) * 2; }
 constexpr int dq_tile_bytes(int d) { return max_i(2 * 64 * tile_ld(d), 128 * (d + 8)) * 2; }
 
+constexpr int step_smem_bytes(int d, int nc, int nw) { return nw * max_i(32 * tile_ld(d) * 2, 16 * nc * (3 + d + 4) * 4); }
 constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 6 * 64 * 4, 4 * 32 * (d + 4) * 4); }
 constexpr int dkv_pair_smem_bytes(int d) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * 4 * 64 * 16 + 2 * 6 * 64 * 4; }
 constexpr float LOG2E = 1.4426950408889634f;
@@ -156,7 +157,7 @@ constexpr float FLOOR = -1.0e37f;      // the reference exponent of rows that ha
 
 // ================================================================================================ forward
 template <int D, bool SPLIT, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, 2) span_fwd_kernel(const SpanArgs p) {
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_fwd_kernel(const SpanArgs p) {
   constexpr int LDK = D + 8, LDV = D + 32, KS = D / 16, DT = D / 32, NT = 256, BQ = 128, CH = D / 8;
   using T64 = Tile64<D, NT>;
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // fwd_smem_bytes(D)
@@ -400,6 +401,261 @@ __global__ void __launch_bounds__(256, 2) span_fwd_kernel(const SpanArgs p) {
   }
 }
 
+// ---- few rows: the step of a generation -----------------------------------------------------------------------
+// At most 16 NC rows per key head (the queries of a step times the heads of the group).  Bound by reading K and V once, so a wave works alone, without
+// barriers: the waves of a workgroup take the 32-key steps in turn, K goes from memory straight into the fragments of the matrix
+// instruction (16 rows x 64 bytes a load: a whole row is used by one wave), V through a piece of LDS of the wave's own, since its
+// reduction runs over the keys.  The next step's K and V are on their way during a step.  At the end the waves join in LDS.
+template <int D, int NC, int NW, bool SPLIT, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(64 * NW) span_step_kernel(const SpanArgs p) {
+  constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, CH = D / 8, NV = 32 * CH / 64;
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // step_smem_bytes(D, NC, NW)
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  bf16* const Vs = reinterpret_cast<bf16*>(dyn_smem) + w * 32 * LD;
+  const int nhb = p.kh * p.batch;
+  const int hb = (int)blockIdx.x % nhb, split = (int)blockIdx.x / nhb;
+  const Rows s(p, hb);
+  const Score sc(p);
+
+  uint4 qf[NC][KS];
+  int2 span[NC];
+  float slope2[NC];
+  int pos[NC];
+  Seen seen;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int row = 16 * c + lr;
+    const bool live = row < s.total;
+    span[c] = span_of(p, s, row);
+    Seen v;
+    v.start(span[c], live);
+    if (c == 0) seen = v;
+    else seen.add(v.lo, v.hi, v.all_lo, v.all_hi);
+    int q, h;
+    s.at(live ? row : 0, q, h);
+    const bf16* const qr = p.q + ((long)s.b * p.seq_q + q) * p.ldq + (long)(s.g * s.grp + h) * D + 8 * lg;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (live) qf[c][ks] = *reinterpret_cast<const uint4*>(qr + 32 * ks);
+    }
+    slope2[c] = 0.f;
+    pos[c] = 0;
+    if (BIAS && live) {
+      slope2[c] = p.slopes[s.g * s.grp + h] * LOG2E;
+      pos[c] = p.q_pos ? p.q_pos[(long)s.b * p.seq_q + q] : q + p.seq_kv - p.seq_q;
+    }
+  }
+  seen.lanes(1, 16);      // all the rows there are: the same in all waves
+  int j0 = 0, j1 = 0;
+  if (seen.hi > seen.lo) {
+    j0 = seen.lo / 32;
+    j1 = (seen.hi + 31) / 32;
+  }
+  if (SPLIT) {
+    int first, last;
+    slice_of(j1 - j0, p.splits, split, first, last);
+    j1 = j0 + last;
+    j0 += first;
+  }
+  const bf16* const kb = p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D;
+  const bf16* const vb = p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D;
+
+  float m_run[NC], l_run[NC], lt_run[NC];
+  f32x4 oacc[DT][NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    m_run[c] = FLOOR;
+    l_run[c] = lt_run[c] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) oacc[dt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  u32x4 kreg[2][KS];
+  uint4 vreg[NV];
+  auto load_step = [&](int j) {      // rows past the end read as zero
+    const int left = min(32, p.seq_kv - 32 * j);
+    const rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(kb + (long)(32 * j) * p.ldk), 0, (int)(((long)(left - 1) * p.ldk + D) * 2), 0x00020000);
+    const rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(vb + (long)(32 * j) * p.ldv), 0, (int)(((long)(left - 1) * p.ldv + D) * 2), 0x00020000);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        kreg[kt][ks] = __builtin_amdgcn_raw_buffer_load_b128(rk, (int)(((16 * kt + lr) * (int)p.ldk + 32 * ks + 8 * lg) * 2), 0, 0);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = 64 * i + lane;
+      vreg[i] = buf_load16(rv, (uint32_t)(((c / CH) * (int)p.ldv + (c % CH) * 8) * 2));
+    }
+  };
+  if (j0 + w < j1) load_step(j0 + w);
+  const bf16* const vfrag = Vs + tr_base<LD>(lane);
+  for (int j = j0 + w; j < j1; j += NW) {
+    const bool whole = seen.all(32 * j, 32 * j + 32);      // uniform
+    f32x4 sT[2][NC];      // [16 keys][16 rows]
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          sT[kt][c] = mfma16(__builtin_bit_cast(uint4, kreg[kt][ks]), qf[c][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sT[kt][c]);
+    unsigned bad_keys = 0u;      // whose v is not finite, of a step that some rows do not see
+    if (!whole) {
+      stay_in_branch();
+      unsigned mine = 0u;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        bool bad = false;
+        vreg[i] = finite8(vreg[i], bad);
+        mine |= bad ? 1u << i : 0u;
+      }
+      if (__any(mine != 0u))
+#pragma unroll 1
+        for (int i = 0; i < 32; ++i)      // key i is in the CH lanes from CH i % 64 on, their piece CH i / 64
+          bad_keys |= __any((mine >> (CH * i / 64) & 1u) && lane / CH == i % (64 / CH)) ? 1u << i : 0u;
+    }
+    wave_lds_order();      // the last step's V has been read
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = 64 * i + lane;
+      *reinterpret_cast<uint4*>(Vs + (c / CH) * LD + (c % CH) * 8) = vreg[i];
+    }
+    wave_lds_order();
+    if (j + NW < j1) load_step(j + NW);
+    // exponents
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const float from = BIAS ? (float)(pos[c] - (32 * j + 4 * lg)) : 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x = score2<CAP>(sT[kt][c][e], sc);
+          if (BIAS) x = __builtin_fmaf(-slope2[c], fabsf(from - (float)(16 * kt + e)), x);
+          sT[kt][c][e] = x;
+        }
+    }
+    if (!whole) {
+      stay_in_branch();
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int lo = span[c].x - (32 * j + 4 * lg);
+        const unsigned n = (unsigned)(span[c].y - span[c].x);
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sT[kt][c][e] = (unsigned)(16 * kt + e - lo) < n ? sT[kt][c][e] : -INFINITY;
+        if (bad_keys) {      // uniform
+          const int first = max(span[c].x - 32 * j, 0), last = min(span[c].y - 32 * j, 32);
+          if (last > first && (bad_keys >> first & (last - first == 32 ? ~0u : (1u << (last - first)) - 1u))) lt_run[c] = NAN;
+        }
+      }
+    }
+    bool grow = false;
+    float mx[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      mx[c] = fmaxf(fmaxf(fmaxf(sT[0][c][0], sT[0][c][1]), fmaxf(sT[0][c][2], sT[0][c][3])), fmaxf(fmaxf(sT[1][c][0], sT[1][c][1]), fmaxf(sT[1][c][2], sT[1][c][3])));
+      grow = grow || mx[c] > m_run[c] + 8.f;
+    }
+    // the reference exponent is the same in the four lanes of a column, and moves only when one of them outgrows it by 2^8
+    if (__builtin_amdgcn_ballot_w64(grow) != 0ull) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float m = fmaxf(mx[c], __shfl_xor(mx[c], 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const float m_new = m > m_run[c] + 8.f ? m : m_run[c];
+        const float alpha = fast_exp2(m_run[c] - m_new);
+        l_run[c] *= alpha;
+        lt_run[c] *= alpha;
+        m_run[c] = m_new;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) oacc[dt][c] *= alpha;
+      }
+    }
+    uint4 pf[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sT[kt][c][e] = fast_exp2(sT[kt][c][e] - m_run[c]);
+          l_run[c] += sT[kt][c][e];
+        }
+      pf[c] = pack_frag(sT[0][c], sT[1][c]);
+      lt_run[c] += sum2(pf[c].x, sum2(pf[c].y, sum2(pf[c].z, sum2(pf[c].w, 0.f))));
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const uint4 a = read_frag_tr<LD>(vfrag + 16 * dt);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) oacc[dt][c] = mfma16(a, pf[c], oacc[dt][c]);
+    }
+  }
+
+  // the waves join: wave w's reference exponent and sums of every row, then its rows of O^T
+  float* const ml = reinterpret_cast<float*>(dyn_smem);      // [NW][3][16 NC]
+  float* const os = ml + 3 * NW * 16 * NC;                   // [NW][16 NC][D + 4]
+  __syncthreads();
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const float l = column_sum(l_run[c]), lt = column_sum(lt_run[c]);
+    if (lg == 0) {
+      ml[(3 * w) * 16 * NC + 16 * c + lr] = m_run[c];
+      ml[(3 * w + 1) * 16 * NC + 16 * c + lr] = l;
+      ml[(3 * w + 2) * 16 * NC + 16 * c + lr] = lt;
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      *reinterpret_cast<f32x4*>(os + (w * 16 * NC + 16 * c + lr) * (D + 4) + 16 * dt + 4 * lg) = oacc[dt][c];
+  }
+  __syncthreads();
+  for (int i = tid; i < 16 * NC * CH; i += 64 * NW) {
+    const int row = i / CH, ch = i % CH;
+    if (row >= s.total) break;
+    float m = FLOOR, l = 0.f, lt = 0.f, acc[8];
+#pragma unroll
+    for (int u = 0; u < NW; ++u) m = fmaxf(m, ml[3 * u * 16 * NC + row]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int u = 0; u < NW; ++u) {
+      const float wgt = fast_exp2(ml[3 * u * 16 * NC + row] - m);      // (a wave without keys has sums of zero)
+      l += wgt * ml[(3 * u + 1) * 16 * NC + row];
+      lt += wgt * ml[(3 * u + 2) * 16 * NC + row];
+      const float* const src = os + (u * 16 * NC + row) * (D + 4) + 8 * ch;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += wgt * src[e];
+    }
+    if constexpr (SPLIT) {
+      const long at = ((long)split * nhb + hb) * s.total + row;
+      if (ch == 0) p.part_ml[at] = make_float4(m, l, lt, 0.f);
+      if (j0 < j1) {      // (of a slice without keys the sum is 0, and its part is not read)
+        *reinterpret_cast<float4*>(p.part + at * D + 8 * ch) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        *reinterpret_cast<float4*>(p.part + at * D + 8 * ch + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+      }
+    } else {
+      const int2 v = span_of(p, s, row);
+      const bool some = v.y > v.x;
+      const float mul = some ? 1.f / lt : 0.f;
+      if (p.lse && ch == 0) p.lse[s.stat(row, p.a)] = some ? m * 0.6931471805599453f + logf(l) : -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = some ? acc[e] * mul : 0.f;
+      const long at = s.offset(row, p.ldo, D) + 8 * ch;
+      *reinterpret_cast<uint4*>(p.o + at) = pack_times(acc, 1.f);
+      if (p.rest) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] -= (float)(bf16)acc[e];
+        *reinterpret_cast<uint4*>(p.rest + at) = pack_times(acc, 1.f);
+      }
+    }
+  }
+}
+
 // Rows of the forward (weights exp2(m_i - max m)) or, with DQ, of dq (sums).
 template <int D, int G, bool DQ>
 __global__ void __launch_bounds__(256) span_row_join_kernel(const SpanArgs p) {
@@ -461,7 +717,7 @@ __global__ void __launch_bounds__(256) span_row_join_kernel(const SpanArgs p) {
 
 // ================================================================================================ dQ
 template <int D, bool SPLIT, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, 2) span_dq_kernel(const SpanArgs p) {
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_dq_kernel(const SpanArgs p) {
   constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, NT = 256, BQ = 128;
   using T64 = Tile64<D, NT>;
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // dq_smem_bytes(D)
@@ -903,18 +1159,55 @@ __global__ void __launch_bounds__(256) span_range_kernel(const SpanArgs p) {
   if (threadIdx.x == 0) p.ranges[blockIdx.x] = r;
 }
 
-// sums[i]: pairs before key tile i, edges included; pieces[i]: first key tile, first pair, pair behind the last.  One block.
+// sums[i]: pairs before key tile i, edges included; pieces[i]: first key tile, first pair, pair behind the last.  One block, which with FIND finds the ranges too (where there
+// is little to look through: one launch instead of two).
+constexpr long FEW_LOOKS = 32768;
+template <bool FIND>
 __global__ void __launch_bounds__(1024) span_plan_kernel(const SpanArgs p) {
   __shared__ int sum[MOST_TILES + 1], wave[16];
-  const int tid = threadIdx.x, n = p.batch * ((p.seq_kv + 127) / 128), edge = edge_pairs(p.a / p.kh);
+  const int tid = threadIdx.x, kt = (p.seq_kv + 127) / 128, n = p.batch * kt, edge = edge_pairs(p.a / p.kh);
+  if (FIND) {
+    const int lane = tid & 63, rows = ((p.a / p.kh) * p.seq_q + 63) / 64;
+    for (int t = tid >> 6; t < n; t += 16) {      // a wave takes a key tile
+      const int b = t / kt, k0 = (t - b * kt) * 128, k1 = min(k0 + 128, p.seq_kv);
+      int lo = 0x7fffffff, hi = 0;
+#pragma unroll 4
+      for (int u = lane; u < rows; u += 64) {
+        const int4 v = p.tiles[(long)b * rows + u];
+        if (k0 < v.y && k1 > v.x) {
+          lo = min(lo, u);
+          hi = u + 1;
+        }
+      }
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        lo = min(lo, __shfl_xor(lo, o, 64));
+        hi = max(hi, __shfl_xor(hi, o, 64));
+      }
+      if (lane == 0) {
+        p.ranges[t] = make_int2(hi > 0 ? lo : 0, hi);
+        sum[t] = hi > 0 ? hi - lo : 0;
+      }
+    }
+    __syncthreads();
+  }
   int c[2], s = 0;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int t = 2 * tid + i;
-    const int2 r = t < n ? p.ranges[t] : make_int2(0, 0);
-    c[i] = r.y > r.x ? r.y - r.x + edge : 0;
+    c[i] = 0;
+    if (t < n) {
+      if (FIND) {
+        c[i] = sum[t];
+      } else {
+        const int2 r = p.ranges[t];
+        c[i] = r.y - r.x;
+      }
+      if (c[i] > 0) c[i] += edge;
+    }
     s += c[i];
   }
+  if (FIND) __syncthreads();      // the counts have been read
   const int own = s;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -1390,13 +1683,39 @@ hipError_t join_rows(hipStream_t st, const SpanArgs& p) {
   if (g == 4) return launch(span_row_join_kernel<D, 4, DQ>, grid, 256, 0, st, p);
   return launch(span_row_join_kernel<D, 16, DQ>, grid, 256, 0, st, p);
 }
+// Few rows: slices for two workgroups of four waves per CU, with a 32-key step for each wave at least -- or one workgroup of eight waves, without slices, where
+// its waves are through with their steps (2.1 us each, one after the other: a CU fetches 60 GB/s) before the slices would have been joined (a second launch, 3 us).
+bool few_rows(const SpanArgs& p) { return row_count(p) <= 32; }
+int step_splits(const SpanArgs& p, int d, size_t bytes) {
+  const long nhb = (long)p.kh * p.batch;
+  const size_t each = row_part_bytes(p, d);
+  const int steps = ceil_div(p.seq_kv, 32);
+  long n = nhb ? 512 / nhb : 1;
+  if (n > ceil_div(steps, 4)) n = ceil_div(steps, 4);
+  if (each && n > (long)(bytes / each)) n = (long)(bytes / each);
+  if (n < 2 || ceil_div(steps, 8) * 2.1 <= ceil_div(ceil_div(steps, (int)n), 4) * 2.1 + 3.0) return 1;
+  return (int)n;
+}
+template <int D, int NC, bool CAP, bool BIAS>
+hipError_t launch_step(hipStream_t st, const SpanArgs& p) {
+  const int nhb = p.kh * p.batch;
+  if (p.splits > 1) return launch(span_step_kernel<D, NC, 4, true, CAP, BIAS>, nhb * p.splits, 256, step_smem_bytes(D, NC, 4), st, p);
+  if (p.seq_kv > 128 && nhb < 512) return launch(span_step_kernel<D, NC, 8, false, CAP, BIAS>, nhb, 512, step_smem_bytes(D, NC, 8), st, p);
+  return launch(span_step_kernel<D, NC, 4, false, CAP, BIAS>, nhb, 256, step_smem_bytes(D, NC, 4), st, p);
+}
+
 template <int D, bool CAP, bool BIAS>
 hipError_t fwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
   const int nhb = p.kh * p.batch;
   const long rows = row_count(p);
-  p.splits = row_splits(p, D, bytes);
+  const bool few = few_rows(p);
+  p.splits = few ? step_splits(p, D, bytes) : row_splits(p, D, bytes);
   p.part = static_cast<float*>(scratch);
   p.part_ml = reinterpret_cast<float4*>(p.part + (size_t)p.splits * nhb * rows * D);
+  if (few) {
+    const hipError_t e = rows <= 16 ? launch_step<D, 1, CAP, BIAS>(st, p) : launch_step<D, 2, CAP, BIAS>(st, p);
+    return p.splits > 1 && e == hipSuccess ? join_rows<D, false>(st, p) : e;
+  }
   const int grid = ceil_div(rows, 128) * nhb * p.splits;
   if (p.splits == 1) return launch(span_fwd_kernel<D, false, CAP, BIAS>, grid, 256, fwd_smem_bytes(D), st, p);
   const hipError_t e = launch(span_fwd_kernel<D, true, CAP, BIAS>, grid, 256, fwd_smem_bytes(D), st, p);
@@ -1428,14 +1747,15 @@ hipError_t bwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
   p.parts = rows > 0 ? parts_of(p, D) : 0;
   const KeyPlaces at(p, D, p.parts);
   if (bytes < at.end) p.parts = 0;
-  e = launch(span_range_kernel, (int)key_tiles(p), 256, 0, st, p);
+  const bool find = p.parts > 0 && key_tiles(p) * ceil_div(rows, 64) <= FEW_LOOKS;
+  if (!find) e = launch(span_range_kernel, (int)key_tiles(p), 256, 0, st, p);
   if (e != hipSuccess) return e;
   if (p.parts > 0) {
     char* const mem = static_cast<char*>(scratch) + head;
     p.sums = reinterpret_cast<int*>(mem + at.sums);
     p.pieces = reinterpret_cast<int4*>(mem + at.pieces);
     p.part = reinterpret_cast<float*>(mem + at.part);
-    e = launch(span_plan_kernel, 1, 1024, 0, st, p);
+    e = launch(find ? span_plan_kernel<true> : span_plan_kernel<false>, 1, 1024, 0, st, p);
     if (e != hipSuccess) return e;
   }
   const int grid = p.parts > 0 ? p.parts * p.kh : (int)key_tiles(p) * p.kh;
@@ -1465,7 +1785,8 @@ void k_span_attn_scratch(const SpanArgs& p, int d, size_t* fwd_bytes, size_t* bw
   const size_t all = ~(size_t)0;
   const int rs = row_splits(p, d, all), parts = row_count(p) > 0 ? parts_of(p, d) : 0;
   const size_t r = rs > 1 ? rs * row_part_bytes(p, d) : 0, k = KeyPlaces(p, d, parts).end;
-  *fwd_bytes = r;
+  const int fs = few_rows(p) ? step_splits(p, d, all) : rs;
+  *fwd_bytes = fs > 1 ? fs * row_part_bytes(p, d) : 0;
   *bwd_bytes = least_bytes(p) + (r > k ? r : k);
 }
 size_t k_span_attn_least(const SpanArgs& p) { return least_bytes(p); }
