@@ -60,6 +60,98 @@ __global__ void __launch_bounds__(SMALL) embed_sort_small_kernel(const int* ids,
   sorted[place] = make_uint2(mine, (uint32_t)i);
 }
 
+// Up to 8192 tokens, one block: radix sort by one or two digits of up to 10 bits, in LDS.  A wave has a 16th of the tokens, 64 at a time; a token's rank among those of its digit
+// is that of the wave's earlier ones (counted in LDS) and of the lanes before it (found by ballots).  (4084 tokens: four launches as below 19 us, this one 10.)
+constexpr int MID = 8192, MID_EACH = MID / 1024;
+struct MidSort {
+  uint2 sorted[MID];
+  int count[16][MOST_DIGITS];
+  int wave[16];
+};
+__global__ void __launch_bounds__(1024) embed_sort_mid_kernel(const int* ids, int T, int V, int bits, int passes, uint2* out, uint32_t* marks) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];
+  MidSort& m = *reinterpret_cast<MidSort*>(dyn_smem);
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, digits = 1 << bits, each = (T + 1023) / 1024;      // each: of a lane
+  uint32_t key[MID_EACH], tok[MID_EACH];
+#pragma unroll
+  for (int j = 0; j < MID_EACH; ++j) {
+    const int i = 64 * (each * w + j) + lane;
+    tok[j] = (uint32_t)i;
+    key[j] = j < each && i < T ? key_of(ids[i], V) : 0u;
+  }
+  if (marks)
+    for (int x = tid; x < (V + 31) / 32; x += 1024) marks[x] = 0u;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * bits;
+    for (int x = tid; x < 16 * MOST_DIGITS; x += 1024) m.count[0][x] = 0;
+    __syncthreads();
+    int rank[MID_EACH];
+#pragma unroll
+    for (int j = 0; j < MID_EACH; ++j) {
+      if (j >= each) break;      // uniform
+      const bool in = 64 * (each * w + j) + lane < T;
+      const int digit = (int)(key[j] >> shift) & (digits - 1);
+      unsigned long long same = __ballot(in);
+      for (int b = 0; b < bits; ++b) {
+        const unsigned long long set = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? set : ~set;
+      }
+      const int ahead = __popcll(same & ((1ull << lane) - 1ull));
+      rank[j] = m.count[w][digit] + ahead;      // (all lanes read before the first one of each digit adds, as below)
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      if (in && ahead == 0) m.count[w][digit] += __popcll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    // a thread takes a digit: its waves' counts, then where it begins
+    int total = 0;
+    if (tid < digits)
+#pragma unroll
+      for (int u = 0; u < 16; ++u) total += m.count[u][tid];
+    int sum = total;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int n = __shfl_up(sum, o, 64);
+      if (lane >= o) sum += n;
+    }
+    if (lane == 63) m.wave[w] = sum;
+    __syncthreads();
+    int at = sum - total;
+    for (int u = 0; u < w; ++u) at += m.wave[u];
+    if (tid < digits)
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        const int n = m.count[u][tid];
+        m.count[u][tid] = at;
+        at += n;
+      }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < MID_EACH; ++j) {
+      const int i = 64 * (each * w + j) + lane;
+      if (j < each && i < T) m.sorted[m.count[w][(int)(key[j] >> shift) & (digits - 1)] + rank[j]] = make_uint2(key[j], tok[j]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < MID_EACH; ++j) {
+      const int i = 64 * (each * w + j) + lane;
+      if (j < each && i < T) {
+        const uint2 e = m.sorted[i];
+        key[j] = e.x;
+        tok[j] = e.y;
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int j = 0; j < MID_EACH; ++j) {
+    const int i = 64 * (each * w + j) + lane;
+    if (j < each && i < T) out[i] = make_uint2(key[j], tok[j]);
+  }
+}
+
 // More: radix sort by two digits (one where one is enough), each counted and then scattered.  Every block has a run of `run` tokens.  (Counted by atomics while the first
 // digit is scattered, the second one's counts of the frequent tokens meet on a few addresses: 62 us for 16384 tokens instead of 8 and a launch.)
 struct SortArgs {
@@ -344,7 +436,8 @@ struct SortPlan {
   }
 };
 // Sorted tokens that a group of threads adds up.
-int chunk_length(int T) { return T >= 8192 ? 32 : T >= 2048 ? 16 : 8; }
+// Shorter chunks keep more of the chip busy, longer ones leave fewer parts to join: 4084 tokens of 2880 in chunks of 8 | 16 25.5 | 30.4 us, 16384 of 4096 in 16 | 32 98.9 | 90.1.
+int chunk_length(int T) { return T >= 8192 ? 32 : T >= 2048 ? 8 : 4; }
 
 struct Places {      // of the scratch memory
   size_t sorted, other, counts, marks, part, end;
@@ -352,8 +445,8 @@ struct Places {      // of the scratch memory
     const SortPlan s(T, V);
     sorted = 0;
     other = round16((size_t)T * 8);
-    counts = other + (T > SMALL && s.passes > 1 ? round16((size_t)T * 8) : 0);
-    marks = counts + (T > SMALL ? (size_t)s.blocks * (4 << s.bits) : 0);
+    counts = other + (T > MID && s.passes > 1 ? round16((size_t)T * 8) : 0);
+    marks = counts + (T > MID ? (size_t)s.blocks * (4 << s.bits) : 0);
     part = marks + round16((size_t)((V + 31) / 32) * 4);
     end = part + (size_t)2 * ceil_div(T, chunk_length(T)) * h * 4;
   }
@@ -381,6 +474,12 @@ hipError_t k_embed_bwd(hipStream_t st, const EmbedGrad& g, void* scratch) {
   uint2* const sorted = reinterpret_cast<uint2*>(mem + at.sorted);
   if (g.T <= SMALL) {
     RP_LAUNCH(embed_sort_small_kernel, dim3(1), dim3(SMALL), 0, st, g.ids, g.T, g.V, sorted, marks);
+    e = hipGetLastError();
+  } else if (g.T <= MID) {
+    // (a host-side table entry, not a stream operation: allowed while a graph is captured)
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(embed_sort_mid_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(MidSort));
+    if (e != hipSuccess) return e;
+    RP_LAUNCH(embed_sort_mid_kernel, dim3(1), dim3(1024), sizeof(MidSort), st, g.ids, g.T, g.V, s.bits, s.passes, sorted, marks);
     e = hipGetLastError();
   } else {
     uint2* const other = reinterpret_cast<uint2*>(mem + at.other);

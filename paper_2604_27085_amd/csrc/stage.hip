@@ -1584,9 +1584,9 @@ rp_status rp_op_embed_bwd(void* stream, const void* dx, long lddx, const int* id
 }
 
 namespace {
-// (512 threads for 64 tokens of 256 channels)
+// (512 threads for 128 tokens of 128 channels)
 bool bad_scan(int batch, int seq, int c) {
-  return batch < 0 || seq < 0 || seq > (1 << 30) || c < 0 || c % 8 || c > (1 << 23) || (double)batch * ((double)seq / 64 + 1) * (c / 256 + 1) >= 8388608.0 ||
+  return batch < 0 || seq < 0 || seq > (1 << 30) || c < 0 || c % 8 || c > (1 << 23) || (double)batch * ((double)seq / 128 + 1) * (c / 128 + 1) >= 8388608.0 ||
          (double)batch * c >= 4294967296.0;
 }
 bool bad_state(const void* p) { return off16(p); }

@@ -52,7 +52,7 @@ def test_rows(B, T, V, h, pad, scale):
 
 @pytest.mark.parametrize("accumulate", [0, 1])
 @pytest.mark.parametrize("kind", ["zipf", "one", "even", "none"])
-@pytest.mark.parametrize("T,V,h", [(1, 1, 8), (7, 1000, 264), (32, 40, 64), (1000, 33, 2056), (1024, 5000, 40), (1025, 5000, 40), (3001, 1024, 136), (9000, 151936, 64),
+@pytest.mark.parametrize("T,V,h", [(1, 1, 8), (7, 1000, 264), (32, 40, 64), (1000, 33, 2056), (1024, 5000, 40), (1025, 5000, 40), (3001, 1024, 136), (8192, 151936, 40), (9000, 151936, 64), (9000, 900, 40),
                                    (70000, 3000, 8)])
 def test_gradient(B, T, V, h, kind, accumulate):
     g = torch.Generator().manual_seed(T + V)

@@ -86,7 +86,7 @@ def test_plan_refuses(bad):
     refused(B.rp_op_pack_plan, None, **dict(dict(starts=P, prefix=None, n_docs=2, window=0, T_=16, seq=8, span=P, pos=P, first=P), **bad))
 
 
-GOOD_SCAN = dict(weight=1, x=P, g=P, ldx=64, ldg=64, first=None, len_=None, states=P, batch=2, seq=100, c=64, scratch=Bytes(1 << 20))
+GOOD_SCAN = dict(weight=1, x=P, g=P, ldx=64, ldg=64, first=None, len_=None, states=P, batch=2, seq=300, c=64, scratch=Bytes(1 << 20))
 BAD_SCAN = [dict(weight=-1), dict(weight=3), dict(x=None), dict(g=None), dict(x=P + 2), dict(ldx=60), dict(ldx=56), dict(ldg=1 << 24), dict(states=P + 8), dict(batch=-1),
             dict(seq=-1), dict(c=-8), dict(c=60), dict(c=1 << 24), dict(seq=1 << 30), dict(batch=1 << 30), dict(scratch=None), dict(scratch=Bytes(64)),
             dict(scratch=Bytes(1 << 20, P + 4))]
@@ -107,7 +107,7 @@ def test_scan_sizes():
     refused(B.rp_op_scan_sizes, 1, 1, 12)
     assert B.rp_op_scan_sizes(0, 9, 8) == (0, 0) and B.rp_op_scan_sizes(2, 0, 8) == (0, 0)
     assert B.rp_op_scan_sizes(8, 1, 4096)[1] == 0      # the step of a generation needs no scratch
-    assert B.rp_op_scan_sizes(2, 65, 8)[0] == 2 * 2 * 8 * 4
+    assert B.rp_op_scan_sizes(2, 129, 8)[0] == 2 * 2 * 8 * 4      # a state for 128 tokens
     assert B.lib.rp_op_scan_sizes(1, 1, 8, None, None) == B.RP_OK
 
 
