@@ -29,10 +29,11 @@ __global__ void __launch_bounds__(NT) embed_rows_kernel(const bf16* table, long 
   uint4* const dst = reinterpret_cast<uint4*>(x + t * ldx);
 #pragma unroll 4
   for (int c = lane; c < h8; c += lanes) {
-    const uint4 u = src[c];
-    uint4 y = make_uint4(pack_bf16x2(bf16_lo(u.x) * scale, bf16_hi(u.x) * scale), pack_bf16x2(bf16_lo(u.y) * scale, bf16_hi(u.y) * scale),
+    uint4 u = make_uint4(0u, 0u, 0u, 0u);
+    if (in) u = src[c];
+    const uint4 y = make_uint4(pack_bf16x2(bf16_lo(u.x) * scale, bf16_hi(u.x) * scale), pack_bf16x2(bf16_lo(u.y) * scale, bf16_hi(u.y) * scale),
                          pack_bf16x2(bf16_lo(u.z) * scale, bf16_hi(u.z) * scale), pack_bf16x2(bf16_lo(u.w) * scale, bf16_hi(u.w) * scale));
-    dst[c] = in ? y : make_uint4(0u, 0u, 0u, 0u);
+    dst[c] = in ? y : u;
   }
 }
 

@@ -1657,6 +1657,7 @@ long key_tiles(const SpanArgs& p) { return (long)p.batch * ceil_div(p.seq_kv, 12
 int parts_of(const SpanArgs& p, int d) {
   const long groups = key_tiles(p) * p.kh, slots = d == 128 ? 256 : 512;
   if (key_tiles(p) > MOST_TILES || groups == 0 || groups >= 8 * slots) return 0;
+  if (key_tiles(p) * (ceil_div(row_count(p), 64) + 20) >= 1l << 31) return 0;      // (pairs are counted in 31 bits)
   long n = slots / p.kh;
   const long most = key_tiles(p) * ceil_div(row_count(p), 64) / 4;
   if (n > most) n = most;

@@ -1,0 +1,305 @@
+"""The operators for training on packed documents run together, as a small model would: plan, embedding, dropout, a layer of attention with rotary positions, a layer of
+the gated recurrence, each onto the residual stream through dropout; forward and backward, against the same model in 64 bits; captured into a graph whose replays
+have dropout masks of their own; and beside older calls."""
+import math
+
+import pytest
+
+import pack_reference as R
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+DEV = "cuda:0"
+BF16, F32, F64, I32 = torch.bfloat16, torch.float32, torch.float64, torch.int32
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2604_27085_amd import binding
+    return binding
+
+
+def kept(T, n, p, seed, offset):
+    """R.stays for whole arrays."""
+    low = 0xFFFFFFFF
+    i = torch.arange(T * n // 8, device=DEV)
+    x = [i & low, i >> 32, torch.full_like(i, offset & low), torch.full_like(i, offset >> 32)]
+    k0, k1 = seed & low, seed >> 32
+    for _ in range(10):
+        a, b = x[0] * 0xD2511F53, x[2] * 0xCD9E8D57
+        x = [(b >> 32 & low) ^ x[1] ^ k0, b & low, (a >> 32 & low) ^ x[3] ^ k1, a & low]
+        k0, k1 = (k0 + 0x9E3779B9) & low, (k1 + 0xBB67AE85) & low
+    w = torch.stack(x, 1)
+    keep = round((1.0 - float(torch.tensor(p, dtype=F32))) * 65536)
+    return (torch.stack((w & 0xFFFF, w >> 16), 2) < keep).reshape(T, n), keep / 65536
+
+
+def test_masks_of_whole_arrays():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    for args in ((3, 40, 0.3, 0x123456789ABCDEF1 >> 1, 77), (2, 16, 0.9, 5, 1 << 40)):
+        assert torch.equal(kept(*args)[0].cpu(), R.stays(*args)[0]) and kept(*args)[1] == R.stays(*args)[1]
+
+
+class Model:
+    P, SEED = 0.1, 0x5DEECE66D1234567
+
+    def __init__(self, T=256, seq=128, V=500, h=256, a=8, kh=2, d=64, c=192):
+        self.dims = (T, seq, V, h, a, kh, d, c)
+        g = torch.Generator(device=DEV).manual_seed(21)
+        rnd = lambda *s, std=1.0: (std * torch.randn(s, generator=g, device=DEV)).to(BF16)  # noqa: E731
+        self.ids = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=I32)
+        self.ids[seq - 9:seq] = -1                   # padding at the end of the first row
+        self.starts = torch.tensor([0, 50, seq - 9, seq, seq + 31, T], dtype=I32, device=DEV)
+        self.starts_list = [0, 50, seq - 9, seq, seq + 31, T]
+        self.prefix = torch.tensor([12, 0, 0, 5, 20], dtype=I32, device=DEV)
+        self.E = rnd(V, h)
+        self.g1, self.g2 = [(1 + 0.1 * torch.randn(h, generator=g, device=DEV)).to(BF16) for _ in range(2)]
+        self.w = {n: rnd(*s, std=0.06) for n, s in dict(q=(a * d, h), k=(kh * d, h), v=(kh * d, h), o=(h, a * d), x=(c, h), g=(c, h), y=(h, c)).items()}
+        self.slopes = (2.0 ** -torch.arange(2, a + 2).float()).to(DEV)
+        self.dout = rnd(T, h, std=0.1)
+        self.step = torch.zeros(1, dtype=torch.int64, device=DEV)
+        e = lambda *s, t=BF16: torch.empty(s, dtype=t, device=DEV)  # noqa: E731
+        self.t = dict(x0=e(T, h), x1=e(T, h), n1=e(T, h), q=e(T, a * d), k=e(T, kh * d), v=e(T, kh * d), o=e(T, a * d), rest=e(T, a * d), b1=e(T, h), x2=e(T, h), n2=e(T, h),
+                      xs=e(T, c), gs=e(T, c), ys=e(T, c), b2=e(T, h), x3=e(T, h), db2=e(T, h), dys=e(T, c), dxs=e(T, c), dgs=e(T, c), dn2=e(T, h), dn2b=e(T, h), dx2=e(T, h),
+                      db1=e(T, h), do=e(T, a * d), dq=e(T, a * d), dk=e(T, kh * d), dv=e(T, kh * d), dn1=e(T, h), dx1=e(T, h), dx0=e(T, h))
+        f = lambda *s: e(*s, t=F32)  # noqa: E731
+        rows = T // seq
+        self.r1, self.r2, self.lse, self.delta = f(T), f(T), f(rows, a, seq), f(rows, a, seq)
+        self.span, self.pos, self.first = e(T, 2, t=I32), e(T, t=I32), e(T, t=torch.uint8)
+        self.cs = f(seq + 8, d // 2, 2)
+        self.last = f(rows, c)
+        self.dE = f(V, h)
+        self.dw = {n: f(*t.shape) for n, t in self.w.items()}
+        self.dg1, self.dg2, self.norm_ws = f(h), f(h), f(1024 * h)
+        self.ws = None
+
+    def run(self, B):
+        T, seq, V, h, a, kh, d, c = self.dims
+        st, t, w, rows = torch.cuda.current_stream().cuda_stream, self.t, self.w, T // seq
+        if self.ws is None:
+            n = max(max(B.rp_op_span_attn_scratch(rows, seq, seq, a, kh, d)), B.rp_op_scan_sizes(rows, seq, c)[1], B.rp_op_embed_scratch(T, V, h))
+            self.ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+            self.states = torch.empty(B.rp_op_scan_sizes(rows, seq, c)[0] // 4, device=DEV)
+        qd, kd, s, ws = a * d, kh * d, d ** -0.5, self.ws
+
+        def product(x, wt, y, R=None):      # y = x wt^T (+ R)
+            B.rp_op_gemm(st, B.GEMM_NT, 0, x, wt, y, T, wt.shape[0], wt.shape[1], wt.shape[1], wt.shape[1], wt.shape[0], R=R, ldr=wt.shape[0] if R is not None else 0)
+
+        def back(dy, name, dx, x, R=None):  # dx = dy w (+ R), dw = dy^T x
+            wt = w[name]
+            n, m = wt.shape
+            B.rp_op_gemm(st, B.GEMM_NN, 0, dy, wt, dx, T, m, n, n, m, m, R=R, ldr=m if R is not None else 0)
+            B.rp_op_gemm(st, B.GEMM_TN, 1, dy, x, self.dw[name], n, m, T, n, m, m)
+
+        def drop(x, res, y, which):
+            B.rp_op_dropout(st, x, h, res, h, y, h, T, h, self.P, self.SEED, which << 32, self.step)
+
+        def heads(fwd):
+            B.rp_op_rope(st, 0 if fwd else 1, 0, d, d, t["q" if fwd else "dq"], t["k" if fwd else "dk"], qd, kd, t["q" if fwd else "dq"], t["k" if fwd else "dk"], qd, kd, self.cs,
+                         seq + 8, self.pos, T, seq, a, kh)
+
+        self.dg1.zero_()
+        self.dg2.zero_()
+        B.rp_op_pack_plan(st, self.starts, self.prefix, len(self.starts_list) - 1, 0, T, seq, self.span, self.pos, self.first)
+        B.rp_op_rope_table_scaled(st, self.cs, B.make_rope_scaling(base=1.0e4), seq + 8, d)
+        B.rp_op_embed_fwd(st, self.E, h, self.ids, 2.0, t["x0"], h, T, V, h)
+        drop(t["x0"], None, t["x1"], 0)
+        B.rp_op_rmsnorm_fwd(st, t["x1"], self.g1, t["n1"], self.r1, T, h, 1e-6)
+        for n in "qkv":
+            product(t["n1"], w[n], t[n])
+        heads(True)
+        B.rp_op_span_attn_fwd(st, t["q"], t["k"], t["v"], t["o"], t["rest"], self.lse, qd, kd, kd, qd, self.span, None, self.slopes, 5.0, rows, seq, seq, a, kh, d, s, ws)
+        product(t["o"], w["o"], t["b1"])
+        drop(t["b1"], t["x1"], t["x2"], 1)
+        B.rp_op_rmsnorm_fwd(st, t["x2"], self.g2, t["n2"], self.r2, T, h, 1e-6)
+        product(t["n2"], w["x"], t["xs"])
+        product(t["n2"], w["g"], t["gs"])
+        B.rp_op_scan_fwd(st, B.SCAN_ENERGY, t["xs"], t["gs"], t["ys"], c, c, c, self.first, None, None, self.last, self.states, rows, seq, c, ws)
+        product(t["ys"], w["y"], t["b2"])
+        drop(t["b2"], t["x2"], t["x3"], 2)
+        # and back
+        drop(self.dout, None, t["db2"], 2)
+        back(t["db2"], "y", t["dys"], t["ys"])
+        B.rp_op_scan_bwd(st, B.SCAN_ENERGY, t["xs"], t["gs"], t["dys"], t["dxs"], t["dgs"], c, c, c, c, c, self.first, None, self.states, None, None, rows, seq, c, ws)
+        back(t["dxs"], "x", t["dn2b"], t["n2"])
+        back(t["dgs"], "g", t["dn2"], t["n2"], R=t["dn2b"])
+        B.rp_op_rmsnorm_bwd(st, t["dn2"], 0, t["x2"], self.g2, self.r2, self.dout, t["dx2"], self.dg2, self.norm_ws, T, h)
+        drop(t["dx2"], None, t["db1"], 1)
+        back(t["db1"], "o", t["do"], t["o"])
+        B.rp_op_span_attn_bwd(st, t["q"], t["k"], t["v"], t["o"], t["rest"], t["do"], self.lse, self.delta, t["dq"], t["dk"], t["dv"], qd, kd, kd, qd, qd, qd, kd, kd, self.span,
+                              None, self.slopes, 5.0, rows, seq, seq, a, kh, d, s, ws)
+        heads(False)
+        back(t["dq"], "q", t["dn1"], t["n1"])
+        back(t["dk"], "k", t["dn2"], t["n1"], R=t["dn1"])
+        back(t["dv"], "v", t["dn1"], t["n1"], R=t["dn2"])
+        B.rp_op_rmsnorm_bwd(st, t["dn1"], 0, t["x1"], self.g1, self.r1, t["dx2"], t["dx1"], self.dg1, self.norm_ws, T, h)
+        drop(t["dx1"], None, t["dx0"], 0)
+        B.rp_op_embed_bwd(st, t["dx0"], h, self.ids, 2.0, self.dE, h, 0, T, V, h, ws)
+
+    def got(self):
+        out = {"x3": self.t["x3"], "last": self.last, "dE": self.dE, "dg1": self.dg1, "dg2": self.dg2}
+        out.update({"dw_" + n: x for n, x in self.dw.items()})
+        return {n: x.clone() for n, x in out.items()}
+
+    def want(self, step=0):
+        """The same in 64 bits, by autograd."""
+        T, seq, V, h, a, kh, d, c = self.dims
+        rows = T // seq
+        leaf = lambda x: x.double().requires_grad_()  # noqa: E731
+        E, g1, g2 = leaf(self.E), leaf(self.g1), leaf(self.g2)
+        w = {n: leaf(x) for n, x in self.w.items()}
+        span, pos, first = R.plan(self.starts_list, self.prefix.tolist(), 0, T, seq)
+        assert self.span.tolist() == [list(v) for v in span] and self.pos.tolist() == pos and self.first.tolist() == first
+
+        def drop(x, which):
+            stay, share = kept(T, h, self.P, self.SEED, (which << 32) + step)
+            return torch.where(stay, x / share, 0.0)
+
+        def norm(x, g):
+            return x * torch.rsqrt((x * x).mean(1, keepdim=True) + 1e-6) * g
+
+        ids = self.ids.long()
+        x1 = drop(torch.where((ids >= 0)[:, None], 2.0 * E[ids.clamp(min=0)], 0.0), 0)
+        n1 = norm(x1, g1)
+        th = 1.0e4 ** (-torch.arange(0, d, 2, dtype=F64, device=DEV) / d)
+        ang = torch.tensor(pos, dtype=F64, device=DEV)[:, None, None] * th
+        cos, sin = ang.cos(), ang.sin()
+
+        def turn(x):
+            u, v = x[..., :d // 2], x[..., d // 2:]
+            return torch.cat((u * cos - v * sin, v * cos + u * sin), -1)
+
+        q, k, v = turn((n1 @ w["q"].t()).reshape(T, a, d)), turn((n1 @ w["k"].t()).reshape(T, kh, d)), (n1 @ w["v"].t()).reshape(T, kh, d)
+        j, o = torch.arange(seq, device=DEV), []
+        sp = torch.tensor(span, device=DEV).reshape(rows, seq, 2)
+        for r in range(rows):
+            seen = (j >= sp[r, :, :1]) & (j < sp[r, :, 1:])
+            heads = []
+            for i in range(a):
+                part = slice(r * seq, (r + 1) * seq)
+                z = 5.0 * torch.tanh(q[part, i] @ k[part, i // (a // kh)].t() / math.sqrt(d) / 5.0) - self.slopes[i].double() * (j[:, None] - j).abs()
+                z = z.masked_fill(~seen, -1e30)
+                heads.append(torch.where(seen.any(1, keepdim=True), torch.softmax(z, 1) @ v[part, i // (a // kh)], 0.0))
+            o.append(torch.stack(heads, 1))
+        x2 = x1 + drop(torch.cat(o).reshape(T, a * d) @ w["o"].t(), 1)
+        n2 = norm(x2, g2)
+        xs, gs = n2 @ w["x"].t(), n2 @ w["g"].t()
+        f = gs.sigmoid()
+        u = (torch.sigmoid(-gs) * (1 + f)).sqrt() * xs
+        fs, keep = f.reshape(rows, seq, c), 1.0 - torch.tensor(first, dtype=F64, device=DEV).reshape(rows, seq, 1)
+        us, s, ys = u.reshape(rows, seq, c), torch.zeros((rows, c), dtype=F64, device=DEV), []
+        for i in range(seq):
+            s = fs[:, i] * keep[:, i] * s + us[:, i]
+            ys.append(s)
+        x3 = x2 + drop(torch.stack(ys, 1).reshape(T, c) @ w["y"].t(), 2)
+        leaves = [E, g1, g2] + [w[n] for n in self.dw]
+        grads = torch.autograd.grad(x3, leaves, self.dout.double())
+        out = dict(x3=x3.detach(), last=s.detach(), dE=grads[0], dg1=grads[1], dg2=grads[2])
+        out.update({"dw_" + n: x for n, x in zip(self.dw, grads[3:])})
+        return out
+
+
+def rel(x, y):
+    return float((x.double() - y).norm() / y.norm())
+
+
+def test_model_against_64_bits(B):
+    m = Model()
+    m.run(B)
+    torch.cuda.synchronize()
+    got, want = m.got(), m.want()
+    # every tensor on the way is rounded to bf16 (2^-8 at most, 1.7e-3 of the norm) once or twice; some 20 such roundings lie between the ends
+    for name, value in want.items():
+        assert rel(got[name], value) < 2e-2, (name, rel(got[name], value))
+    m.step.fill_(3)      # another mask, on device alone
+    m.run(B)
+    torch.cuda.synchronize()
+    other, want = m.got(), m.want(3)
+    assert rel(other["x3"], want["x3"]) < 2e-2 and rel(other["dE"], want["dE"]) < 2e-2 and rel(other["x3"], got["x3"].double()) > 0.05
+
+
+@pytest.mark.parametrize("sizes", [{}, dict(T=2304, seq=1152, V=3000, d=128, a=4, c=72)], ids=["small", "large"])
+def test_captured_and_replayed(B, sizes):
+    m = Model(**sizes)
+    m.run(B)
+    torch.cuda.synchronize()
+    eager = {}
+    for step in (0, 1, 2):
+        m.step.fill_(step)
+        m.run(B)
+        torch.cuda.synchronize()
+        eager[step] = m.got()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        m.run(B)
+    for step in (2, 0, 1, 1, 0):
+        m.step.fill_(step)
+        m.ws.fill_(255)      # scratch holds nothing between calls
+        g.replay()
+        torch.cuda.synchronize()
+        for name, x in m.got().items():
+            assert torch.equal(x, eager[step][name]), (step, name)
+        m.run(B)             # the program's own eager work between replays
+        torch.cuda.synchronize()
+        assert torch.equal(m.got()["dE"], eager[step]["dE"])
+
+
+def test_two_graphs_of_one_workspace_and_another_stream(B):
+    """Two captured models that share scratch, replayed one after the other; and a third on a stream of its own with scratch of its own."""
+    a, b, c = Model(), Model(T=384, seq=192, V=333), Model()
+    graphs = []
+    for m in (a, b):
+        m.run(B)
+    n = max(a.ws.numel(), b.ws.numel())
+    a.ws = b.ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    c.run(B)
+    torch.cuda.synchronize()
+    want = []
+    for m in (a, b):
+        m.run(B)
+        torch.cuda.synchronize()
+        want.append(m.got())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            m.run(B)
+        graphs.append(g)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        for m, g, w in zip((a, b), graphs, want):
+            with torch.cuda.stream(side):
+                c.run(B)
+            g.replay()
+            torch.cuda.synchronize()
+            for name, x in m.got().items():
+                assert torch.equal(x, w[name]), name
+            for name, x in c.got().items():
+                assert torch.equal(x, want[0][name]), name
+
+
+def test_beside_the_causal_attention(B):
+    """Spans that are plain causal ones: the numbers of rp_op_attn_fwd and _bwd, to what both round."""
+    T, a, kh, d = 300, 8, 2, 128
+    st = torch.cuda.current_stream().cuda_stream
+    g = torch.Generator(device=DEV).manual_seed(3)
+    rnd = lambda n: torch.randn((T, n, d), generator=g, device=DEV).to(BF16)  # noqa: E731
+    q, k, v, do = rnd(a), rnd(kh), rnd(kh), rnd(a)
+    span = torch.stack((torch.zeros(T, device=DEV), torch.arange(T, device=DEV) + 1), -1).to(I32).contiguous()
+    out = []
+    qd, kd = a * d, kh * d
+    for which in range(2):
+        o, rest, dq, dk, dv = [torch.empty_like(x) for x in (q, q, q, k, v)]
+        lse, delta = torch.empty((1, a, T), device=DEV), torch.empty((1, a, T), device=DEV)
+        if which:
+            ws = torch.empty(max(B.rp_op_span_attn_scratch(1, T, T, a, kh, d)), dtype=torch.uint8, device=DEV)
+            B.rp_op_span_attn_fwd(st, q, k, v, o, rest, lse, qd, kd, kd, qd, span, None, None, 0.0, 1, T, T, a, kh, d, d ** -0.5, ws)
+            B.rp_op_span_attn_bwd(st, q, k, v, o, rest, do, lse, delta, dq, dk, dv, qd, kd, kd, qd, qd, qd, kd, kd, span, None, None, 0.0, 1, T, T, a, kh, d, d ** -0.5, ws)
+        else:
+            B.rp_op_attn_fwd(st, q, k, v, o, lse, qd, kd, kd, qd, 1, T, a, kh, d)
+            B.rp_op_attn_bwd(st, q, k, v, o, do, lse, delta, dq, dk, dv, torch.empty(2 * T * a * d, device=DEV), qd, kd, kd, qd, qd, qd, kd, kd, 1, T, a, kh, d)
+        torch.cuda.synchronize()
+        out.append((o, lse, dq, dk, dv))
+    for x, y in zip(*out):      # the other one's delta carries the rounding of o
+        assert rel(x, y.double()) < 1e-2

@@ -125,6 +125,7 @@ SHAPES = [
     ("causal", 1, 300, 300, 4, 2, 64), ("causal", 2, 129, 129, 8, 8, 128), ("docs", 1, 517, 517, 6, 2, 64), ("docs", 2, 260, 260, 16, 1, 128), ("any", 2, 77, 200, 4, 4, 64),
     ("any", 1, 200, 77, 12, 4, 128), ("any", 3, 65, 640, 8, 2, 128), ("ragged", 3, 1, 700, 16, 2, 128), ("ragged", 2, 5, 70, 4, 2, 64), ("all", 1, 64, 64, 2, 1, 64),
     ("all", 1, 1, 1, 1, 1, 128), ("causal", 1, 1, 1, 4, 2, 64), ("any", 1, 1, 3000, 4, 2, 64), ("causal", 1, 40, 1500, 32, 8, 64),
+    ("causal", 1, 33, 33, 96, 1, 64), ("any", 1, 20, 150, 64, 1, 128), ("any", 2, 30, 400, 10, 2, 128), ("docs", 1, 40, 40, 71, 1, 128),
 ]
 KINDS = [(0.0, False), (20.0, False), (0.0, True), (3.0, True)]
 
