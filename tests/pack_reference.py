@@ -182,6 +182,9 @@ def embedding_gradient(dx, ids, scale, V, given=None):
     at = (ids >= 0) & (ids < V)
     rows, where = dx.double()[at] * scale, ids[at].long()
     count = torch.bincount(where, minlength=V).double()[:, None]
-    out.index_add_(0, where, rows)
-    size.index_add_(0, where, rows.abs())
+    for to, what in ((out, rows), (size, rows.abs())):
+        if int(count.max()) > 4096:      # (many additions to one place take the GPU ten seconds)
+            to.copy_(to.cpu().index_add_(0, where.cpu(), what.cpu()))
+        else:
+            to.index_add_(0, where, what)
     return out, size * 2.0 ** -24 * (3 + torch.minimum(count, 32 + 8 + count / 256))
