@@ -138,8 +138,18 @@ RP_DEV uint32_t finite2(uint32_t u, bool& bad) {
   return (lo ? 0u : u & 0xffffu) | (hi ? 0u : u & 0xffff0000u);
 }
 RP_DEV uint4 finite8(const uint4& u, bool& bad) { return make_uint4(finite2(u.x, bad), finite2(u.y, bad), finite2(u.z, bad), finite2(u.w, bad)); }
+// Whether any lane of the wave has one: three instructions for two values.  (An exponent of all ones carries into the bit above.)
+RP_DEV uint32_t carries(uint32_t u) { return (u & 0x7f807f80u) + 0x00800080u; }
+template <int N>
+RP_DEV bool any_not_finite(const uint4 (&r)[N]) {
+  uint32_t c = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) c |= carries(r[i].x) | carries(r[i].y) | carries(r[i].z) | carries(r[i].w);
+  return __any((c & 0x80008000u) != 0u);
+}
 template <int N>
 RP_DEV void make_finite(uint4 (&r)[N]) {
+  if (!any_not_finite(r)) return;
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < N; ++i) r[i] = finite8(r[i], bad);
@@ -236,7 +246,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_fwd_kernel(const Sp
     const int kv0 = j * 64;
     const bool whole = block.all(kv0, kv0 + 64);      // uniform over the workgroup
     __syncthreads();
-    if (!whole) {
+    if (!whole && any_not_finite(vreg)) {
 #pragma unroll
       for (int it = 0; it < T64::NREG; ++it) {
         bool bad = false;
@@ -503,7 +513,7 @@ __global__ void __launch_bounds__(64 * NW) span_step_kernel(const SpanArgs p) {
         for (int c = 0; c < NC; ++c)
           sT[kt][c] = mfma16(__builtin_bit_cast(uint4, kreg[kt][ks]), qf[c][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sT[kt][c]);
     unsigned bad_keys = 0u;      // whose v is not finite, of a step that some rows do not see
-    if (!whole) {
+    if (!whole && any_not_finite(vreg)) {
       stay_in_branch();
       unsigned mine = 0u;
 #pragma unroll
@@ -512,10 +522,9 @@ __global__ void __launch_bounds__(64 * NW) span_step_kernel(const SpanArgs p) {
         vreg[i] = finite8(vreg[i], bad);
         mine |= bad ? 1u << i : 0u;
       }
-      if (__any(mine != 0u))
 #pragma unroll 1
-        for (int i = 0; i < 32; ++i)      // key i is in the CH lanes from CH i % 64 on, their piece CH i / 64
-          bad_keys |= __any((mine >> (CH * i / 64) & 1u) && lane / CH == i % (64 / CH)) ? 1u << i : 0u;
+      for (int i = 0; i < 32; ++i)      // key i is in the CH lanes from CH i % 64 on, their piece CH i / 64
+        bad_keys |= __any((mine >> (CH * i / 64) & 1u) && lane / CH == i % (64 / CH)) ? 1u << i : 0u;
     }
     wave_lds_order();      // the last step's V has been read
 #pragma unroll
