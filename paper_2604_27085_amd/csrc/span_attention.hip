@@ -69,12 +69,11 @@ struct Rows {
 
 // What a row sees; nothing: 0, 0.  Rows behind the last one see nothing either.
 RP_DEV int2 span_of(const SpanArgs& p, const Rows& s, int r) {
-  if (r >= s.total) return make_int2(0, 0);
   int q, h;
-  s.at(r, q, h);
+  s.at(r < s.total ? r : 0, q, h);
   const int2 v = p.span[(long)s.b * p.seq_q + q];
   const int lo = max(v.x, 0), hi = min(v.y, p.seq_kv);
-  return hi > lo ? make_int2(lo, hi) : make_int2(0, 0);
+  return r < s.total && hi > lo ? make_int2(lo, hi) : make_int2(0, 0);
 }
 
 // Of several rows: the keys that any of them sees, [lo, hi), and those that all of them see, [all_lo, all_hi).
@@ -726,7 +725,7 @@ __global__ void __launch_bounds__(256) span_row_join_kernel(const SpanArgs p) {
 
 // ================================================================================================ dQ
 template <int D, bool SPLIT, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_dq_kernel(const SpanArgs p) {
+__global__ void __launch_bounds__(256, D == 64 && !(CAP && BIAS) ? 3 : 2) span_dq_kernel(const SpanArgs p) {
   constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, NT = 256, BQ = 128;
   using T64 = Tile64<D, NT>;
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // dq_smem_bytes(D)
@@ -747,13 +746,32 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_dq_kernel(const Spa
   const Score sc(p);
 
   int2 span[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) span[c] = span_of(p, s, r0 + 32 * w + 16 * c + lr);
+  // A lane's rows, all on their way at once and while the spans are put together (a row behind the last one takes row 0's: nothing of it leaves the kernel).
+  uint4 qf[2][KS], dof[2][KS], of[2][2][KS];     // column tiles c = 0, 1; o, and what its rounding left over
+  float lse2[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int row = r0 + 32 * w + 16 * c + lr, rc = row < s.total ? row : 0;
+    const bf16* const qr = p.q + s.offset(rc, p.ldq, D) + 8 * lg;
+    const bf16* const dor = p.dout + s.offset(rc, p.lddo, D) + 8 * lg;
+    const long at_o = s.offset(rc, p.ldo, D) + 8 * lg;
+    lse2[c] = p.lse_in[s.stat(rc, p.a)];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[c][ks] = *reinterpret_cast<const uint4*>(qr + 32 * ks);
+      dof[c][ks] = *reinterpret_cast<const uint4*>(dor + 32 * ks);
+      of[0][c][ks] = *reinterpret_cast<const uint4*>(p.o_in + at_o + 32 * ks);
+      of[1][c][ks] = make_uint4(0u, 0u, 0u, 0u);
+      if (p.rest_in) of[1][c][ks] = *reinterpret_cast<const uint4*>(p.rest_in + at_o + 32 * ks);
+    }
+  }
   Seen mine;
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
-    const int row = r0 + 32 * w + 16 * c + lr;
-    span[c] = span_of(p, s, row);
     Seen v;
-    v.start(span[c], row < s.total);
+    v.start(span[c], r0 + 32 * w + 16 * c + lr < s.total);
     if (c == 0) mine = v;
     else mine.add(v.lo, v.hi, v.all_lo, v.all_hi);
   }
@@ -777,38 +795,32 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_dq_kernel(const Spa
   }
   const KeyTile<D, NT> kt_(p.k + (long)s.b * p.seq_kv * p.ldk + s.g * D, p.ldk, p.seq_kv), vt_(p.v + (long)s.b * p.seq_kv * p.ldv + s.g * D, p.ldv, p.seq_kv);
 
-  uint4 qf[2][KS], dof[2][KS];     // a lane's rows: column tiles c = 0, 1
-  float lse2[2], dl[2], slope2[2] = {0.f, 0.f};
+  uint4 kreg[T64::NREG], vreg[T64::NREG];
+  auto load_tiles = [&](int j) {
+    kt_.load(kreg, j * 64, tid);
+    vt_.load(vreg, j * 64, tid);
+  };
+  if (j0 < j1) load_tiles(j0);
+  float dl[2], slope2[2] = {0.f, 0.f};
   int pos[2] = {0, 0};
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
     const int row = r0 + 32 * w + 16 * c + lr;
     const bool ok = row < s.total;
     const int rc = ok ? row : 0;
-    const bf16* const qr = p.q + s.offset(rc, p.ldq, D) + 8 * lg;
-    const bf16* const dor = p.dout + s.offset(rc, p.lddo, D) + 8 * lg;
-    const long at_o = s.offset(rc, p.ldo, D) + 8 * lg;
     float sum = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      qf[c][ks] = make_uint4(0u, 0u, 0u, 0u);
-      dof[c][ks] = make_uint4(0u, 0u, 0u, 0u);
-      if (ok) {
-        qf[c][ks] = *reinterpret_cast<const uint4*>(qr + 32 * ks);
-        dof[c][ks] = *reinterpret_cast<const uint4*>(dor + 32 * ks);
-        uint4 o[2];
-        o[0] = *reinterpret_cast<const uint4*>(p.o_in + at_o + 32 * ks);
-        o[1] = make_uint4(0u, 0u, 0u, 0u);
-        if (p.rest_in) o[1] = *reinterpret_cast<const uint4*>(p.rest_in + at_o + 32 * ks);
-        const uint4 d = dof[c][ks];
+      const uint4 d = dof[c][ks];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          sum += bf16_lo(o[i].x) * bf16_lo(d.x) + bf16_hi(o[i].x) * bf16_hi(d.x) + bf16_lo(o[i].y) * bf16_lo(d.y) + bf16_hi(o[i].y) * bf16_hi(d.y) +
-                 bf16_lo(o[i].z) * bf16_lo(d.z) + bf16_hi(o[i].z) * bf16_hi(d.z) + bf16_lo(o[i].w) * bf16_lo(d.w) + bf16_hi(o[i].w) * bf16_hi(d.w);
+      for (int i = 0; i < 2; ++i) {
+        const uint4 o = of[i][c][ks];
+        sum += bf16_lo(o.x) * bf16_lo(d.x) + bf16_hi(o.x) * bf16_hi(d.x) + bf16_lo(o.y) * bf16_lo(d.y) + bf16_hi(o.y) * bf16_hi(d.y) +
+               bf16_lo(o.z) * bf16_lo(d.z) + bf16_hi(o.z) * bf16_hi(d.z) + bf16_lo(o.w) * bf16_lo(d.w) + bf16_hi(o.w) * bf16_hi(d.w);
       }
     }
     const bool some = span[c].y > span[c].x;
-    lse2[c] = some ? p.lse_in[s.stat(rc, p.a)] * LOG2E : INFINITY;      // rows that see nothing get P = 0
+    lse2[c] = some ? lse2[c] * LOG2E : INFINITY;      // rows that see nothing get P = 0
     sum = column_sum(sum);
     dl[c] = some ? sum : 0.f;
     if (BIAS) {
@@ -822,15 +834,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_dq_kernel(const Spa
 
   const bf16* const kfrag = Ks + lr * LD + 8 * lg;      // (V lies 64 rows further on)
   const bf16* const ktfrag = Ks + tr_base<LD>(lane);
-  uint4 kreg[T64::NREG], vreg[T64::NREG];
-  auto load_tiles = [&](int j) {
-    kt_.load(kreg, j * 64, tid);
-    vt_.load(vreg, j * 64, tid);
-  };
   f32x4 dqacc[DT][2];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dqacc[dt][0] = dqacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (j0 < j1) load_tiles(j0);
   for (int j = j0; j < j1; ++j) {
     const bool whole = block.all(j * 64, j * 64 + 64);      // uniform over the workgroup
     __syncthreads();
@@ -1085,34 +1091,26 @@ RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, c
   }
 }
 
-// The first row tile that sees any of the keys k0 .. k1 - 1, and the one behind the last; all threads.  (Tiles in between may see none.)
-template <int NT>
-RP_DEV int2 row_tiles(const int4* tiles, int n, int k0, int k1, int* lds /* [2 NT / 64] */, int tid) {
-  int lo = 0x7fffffff, hi = 0;
+// Of the row tiles: x: the first one that sees any of the keys k0 .. k1 - 1, y: the one behind the last, z: how many see some of them, but not all rows all.  (Tiles in between may see none.)
+// Over the tiles first, first + step, ..
+RP_DEV int4 look_through(const int4* tiles, int n, int k0, int k1, int first, int step) {
+  int lo = 0x7fffffff, hi = 0, part = 0;
 #pragma unroll 4
-  for (int t = tid; t < n; t += NT) {
+  for (int t = first; t < n; t += step) {
     const int4 v = tiles[t];
     if (k0 < v.y && k1 > v.x) {
       lo = min(lo, t);
       hi = t + 1;
+      part += v.z > k0 || v.w < k1;
     }
   }
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
+  for (int o = 1; o < 64; o <<= 1) {      // of the wave
     lo = min(lo, __shfl_xor(lo, o, 64));
     hi = max(hi, __shfl_xor(hi, o, 64));
+    part += __shfl_xor(part, o, 64);
   }
-  if ((tid & 63) == 0) {
-    lds[2 * (tid >> 6)] = lo;
-    lds[2 * (tid >> 6) + 1] = hi;
-  }
-  __syncthreads();
-  for (int w = 0; w < NT / 64; ++w) {
-    lo = min(lo, lds[2 * w]);
-    hi = max(hi, lds[2 * w + 1]);
-  }
-  __syncthreads();
-  return make_int2(__builtin_amdgcn_readfirstlane(hi > 0 ? lo : 0), __builtin_amdgcn_readfirstlane(hi));
+  return make_int4(lo, hi, part, 0);
 }
 
 // A walk over the row tiles [from, to) that see any of the keys, the last one first: the key tiles of a document have its last rows in common, so workgroups that
@@ -1165,18 +1163,31 @@ struct RowWalk {
 // in order.  (8192 causal tokens, 64 heads of 64: a key tile a workgroup 1880 us.)  With more than MOST_TILES key tiles, or without scratch for the parts (parts 0), a
 // workgroup does a key tile.
 constexpr int MOST_TILES = 2048;
-// Beginning and ending with a key tile, and the masks of the 2 grp row tiles at its edge, cost about as much as so many pairs: they count as that many before a key tile's
-// first.  (Without them the piece with the shortest key tiles lasts 20 % longer than the others at 8192 causal tokens.)
-RP_DEV int edge_pairs(int grp) { return 4 + min(grp, 16); }
-RP_DEV int piece_length(int pairs, int parts) { return max((pairs + parts - 1) / parts, 8); }      // (one may hold nothing but a part of an edge)
+// A key tile counts for more pairs than its row tiles: beginning and ending with it costs about as much as FRONT of them, before its first, and the mask of a row tile that sees a part
+// of it 3/8 of one, spread over them all (16384 tokens, 32 heads of 128: a key tile of 32 to 256 row tiles costs 4.3 of them more, a causal one 0.34 to 0.39 more for each of the eight
+// at its edge).  A key tile with the end of one document and the beginning of a long one is masked all along: without counting that, the piece with it lasted 14 % longer than the others.
+constexpr int FRONT = 4;
+RP_DEV int edge_pairs(int part) { return FRONT + (3 * part + 4) / 8; }
+// The row tiles of a key tile, of `rows` in `pairs`, that come before pair `pair` of it.  At most one a pair: the last pair has the last row tile, and eight have four or more.
+RP_DEV int rows_before(int pair, int rows, int pairs) {
+  return pair <= FRONT ? 0 : pair >= pairs ? rows : (int)((unsigned long long)(pair - FRONT) * rows / (pairs - FRONT));
+}
+// The first pair that has a row tile (rows > 0).
+RP_DEV int first_pair(int rows, int pairs) { return FRONT + (pairs - FRONT - 1) / rows; }
+RP_DEV int piece_length(int pairs, int parts) { return max((pairs + parts - 1) / parts, 8); }      // (one may hold nothing but a part of a front)
 
-// ranges[i]: key tile i % KT of sequence i / KT
+// ranges[i]: of key tile i % KT of sequence i / KT
 __global__ void __launch_bounds__(256) span_range_kernel(const SpanArgs p) {
-  __shared__ int lds[8];
+  __shared__ int4 lds[4];
   const int kt = (p.seq_kv + 127) / 128, b = (int)blockIdx.x / kt, k0 = ((int)blockIdx.x - b * kt) * 128;
   const int n = ((p.a / p.kh) * p.seq_q + 63) / 64;
-  const int2 r = row_tiles<256>(p.tiles + (long)b * n, n, k0, min(k0 + 128, p.seq_kv), lds, threadIdx.x);
-  if (threadIdx.x == 0) p.ranges[blockIdx.x] = r;
+  const int4 v = look_through(p.tiles + (long)b * n, n, k0, min(k0 + 128, p.seq_kv), threadIdx.x, 256);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  const int lo = min(min(lds[0].x, lds[1].x), min(lds[2].x, lds[3].x)), hi = max(max(lds[0].y, lds[1].y), max(lds[2].y, lds[3].y));
+  p.ranges[blockIdx.x] = make_int2(hi > 0 ? lo : 0, hi);
+  if (p.parts > 0) p.sums[blockIdx.x] = edge_pairs(lds[0].z + lds[1].z + lds[2].z + lds[3].z);      // (for the plan, which writes them anew)
 }
 
 // sums[i]: pairs before key tile i, edges included; pieces[i]: first key tile, first pair, pair behind the last.  One block, which with FIND finds the ranges too (where there
@@ -1185,28 +1196,15 @@ constexpr long FEW_LOOKS = 32768;
 template <bool FIND>
 __global__ void __launch_bounds__(1024) span_plan_kernel(const SpanArgs p) {
   __shared__ int sum[MOST_TILES + 1], wave[16];
-  const int tid = threadIdx.x, kt = (p.seq_kv + 127) / 128, n = p.batch * kt, edge = edge_pairs(p.a / p.kh);
+  const int tid = threadIdx.x, kt = (p.seq_kv + 127) / 128, n = p.batch * kt;
   if (FIND) {
     const int lane = tid & 63, rows = ((p.a / p.kh) * p.seq_q + 63) / 64;
     for (int t = tid >> 6; t < n; t += 16) {      // a wave takes a key tile
       const int b = t / kt, k0 = (t - b * kt) * 128, k1 = min(k0 + 128, p.seq_kv);
-      int lo = 0x7fffffff, hi = 0;
-#pragma unroll 4
-      for (int u = lane; u < rows; u += 64) {
-        const int4 v = p.tiles[(long)b * rows + u];
-        if (k0 < v.y && k1 > v.x) {
-          lo = min(lo, u);
-          hi = u + 1;
-        }
-      }
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        lo = min(lo, __shfl_xor(lo, o, 64));
-        hi = max(hi, __shfl_xor(hi, o, 64));
-      }
+      const int4 v = look_through(p.tiles + (long)b * rows, rows, k0, k1, lane, 64);
       if (lane == 0) {
-        p.ranges[t] = make_int2(hi > 0 ? lo : 0, hi);
-        sum[t] = hi > 0 ? hi - lo : 0;
+        p.ranges[t] = make_int2(v.y > 0 ? v.x : 0, v.y);
+        sum[t] = v.y > 0 ? v.y - v.x + edge_pairs(v.z) : 0;
       }
     }
     __syncthreads();
@@ -1221,13 +1219,12 @@ __global__ void __launch_bounds__(1024) span_plan_kernel(const SpanArgs p) {
         c[i] = sum[t];
       } else {
         const int2 r = p.ranges[t];
-        c[i] = r.y - r.x;
+        c[i] = r.y > r.x ? r.y - r.x + p.sums[t] : 0;
       }
-      if (c[i] > 0) c[i] += edge;
     }
     s += c[i];
   }
-  if (FIND) __syncthreads();      // the counts have been read
+  __syncthreads();      // the counts have been read
   const int own = s;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -1312,11 +1309,11 @@ __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
   const int2 r = p.ranges[tile];
   int u0 = r.x, u1 = r.y, end = 0;
   if (p.parts > 0) {
-    const int begin = p.sums[tile], edge = edge_pairs(s.grp);
     end = p.sums[tile + 1];
-    u0 = r.x + max(pair - begin - edge, 0);
-    u1 = r.x + max(min(last_pair, end) - begin - edge, 0);
-    if (u0 >= u1) return;      // nothing but the edge of the last key tile is left (uniform over the workgroup)
+    const int begin = p.sums[tile];
+    u0 = r.x + rows_before(pair - begin, r.y - r.x, end - begin);
+    u1 = r.x + rows_before(last_pair - begin, r.y - r.x, end - begin);
+    if (u0 >= u1) return;      // nothing but the front of the last key tile is left (uniform over the workgroup)
   }
   const bool mine = u0 == r.x && u1 == r.y;      // the whole key tile is done here
   const int kpos[2] = {kw0 + lr, kw0 + 16 + lr};
@@ -1483,11 +1480,11 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
   const int2 r = p.ranges[tile];
   int u0 = r.x, u1 = r.y, end = 0;
   if (p.parts > 0) {
-    const int begin = p.sums[tile], edge = edge_pairs(s.grp);
     end = p.sums[tile + 1];
-    u0 = r.x + max(pair - begin - edge, 0);
-    u1 = r.x + max(min(last_pair, end) - begin - edge, 0);
-    if (u0 >= u1) return;      // nothing but the edge of the last key tile is left (uniform over the workgroup)
+    const int begin = p.sums[tile];
+    u0 = r.x + rows_before(pair - begin, r.y - r.x, end - begin);
+    u1 = r.x + rows_before(last_pair - begin, r.y - r.x, end - begin);
+    if (u0 >= u1) return;      // nothing but the front of the last key tile is left (uniform over the workgroup)
   }
   const bool mine = u0 == r.x && u1 == r.y;      // the whole key tile is done here
   const int kpos[2] = {kw0 + lr, kw0 + 16 + lr};
@@ -1642,8 +1639,9 @@ __global__ void __launch_bounds__(256) span_key_join_kernel(const SpanArgs p) {
   const int tiles_kv = (p.seq_kv + 127) / 128, all_kv = p.batch * tiles_kv;
   const int i = (int)blockIdx.x >> 3, rows = ((int)blockIdx.x & 3) * 32, is_v = (int)blockIdx.x >> 2 & 1;
   const int tile = i / p.kh, g = i - tile * p.kh;
-  const int edge = edge_pairs(p.a / p.kh), begin = p.sums[tile], end = p.sums[tile + 1], each = piece_length(p.sums[all_kv], p.parts);
-  const int from = (begin + edge) / each, to = (end - 1) / each;      // the pieces of its first and of its last pair
+  const int2 r = p.ranges[tile];
+  const int begin = p.sums[tile], end = p.sums[tile + 1], each = piece_length(p.sums[all_kv], p.parts);
+  const int from = end > begin ? (begin + first_pair(r.y - r.x, end - begin)) / each : 0, to = (end - 1) / each;      // the pieces of its first and of its last row tile
   if (end > begin && from == to) return;      // one workgroup had it all
   const int b = tile / tiles_kv, kv0 = (tile - b * tiles_kv) * 128;
   for (int e = threadIdx.x; e < 32 * CH; e += 256) {
@@ -1653,7 +1651,7 @@ __global__ void __launch_bounds__(256) span_key_join_kernel(const SpanArgs p) {
 #pragma unroll
     for (int x = 0; x < 8; ++x) acc[x] = 0.f;
     if (end > begin) {
-      // the first of them began its piece with another key tile, unless it begins in this one's edge; the others begin with this key tile
+      // the first of them began its piece with another key tile, unless it begins in this one's front; the others begin with this key tile
       const float* const src = p.part + (long)is_v * 128 * D + row * D + ch * 8;
       add_times(acc, src + ((long)(from * p.kh + g) * 2 + (from * each >= begin ? 0 : 1)) * (2 * 128 * D), 1.f);
 #pragma unroll 4
@@ -1679,7 +1677,7 @@ long key_tiles(const SpanArgs& p) { return (long)p.batch * ceil_div(p.seq_kv, 12
 int parts_of(const SpanArgs& p, int d) {
   const long groups = key_tiles(p) * p.kh, slots = d == 128 ? 256 : 512;
   if (key_tiles(p) > MOST_TILES || groups == 0 || groups >= 8 * slots) return 0;
-  if (key_tiles(p) * (ceil_div(row_count(p), 64) + 20) >= 1l << 31) return 0;      // (pairs are counted in 31 bits)
+  if (key_tiles(p) * (ceil_div(row_count(p), 64) * 3l / 2 + 20) >= 1l << 31) return 0;      // (pairs are counted in 31 bits)
   long n = slots / p.kh;
   const long most = key_tiles(p) * ceil_div(row_count(p), 64) / 4;
   if (n > most) n = most;
@@ -1771,13 +1769,15 @@ hipError_t bwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
   const KeyPlaces at(p, D, p.parts);
   if (bytes < at.end) p.parts = 0;
   const bool find = p.parts > 0 && key_tiles(p) * ceil_div(rows, 64) <= FEW_LOOKS;
-  if (!find) e = launch(span_range_kernel, (int)key_tiles(p), 256, 0, st, p);
-  if (e != hipSuccess) return e;
   if (p.parts > 0) {
     char* const mem = static_cast<char*>(scratch) + head;
     p.sums = reinterpret_cast<int*>(mem + at.sums);
     p.pieces = reinterpret_cast<int4*>(mem + at.pieces);
     p.part = reinterpret_cast<float*>(mem + at.part);
+  }
+  if (!find) e = launch(span_range_kernel, (int)key_tiles(p), 256, 0, st, p);
+  if (e != hipSuccess) return e;
+  if (p.parts > 0) {
     e = launch(find ? span_plan_kernel<true> : span_plan_kernel<false>, 1, 1024, 0, st, p);
     if (e != hipSuccess) return e;
   }

@@ -152,6 +152,16 @@ def test_strides_positions_and_optional_outputs(B):
     assert bool(c.lse.isnan().all())
 
 
+@pytest.mark.parametrize("scratch", ["all", "least"])
+@pytest.mark.parametrize("a,kh,d", [(4, 2, 64), (6, 2, 128), (4, 1, 128)])
+def test_key_tiles_of_two_documents(B, a, kh, d, scratch):
+    """Documents that begin inside a key tile, the last one long: the row tiles of such a key tile are masked all along, and several workgroups share them."""
+    T = 3001
+    c = Case("causal", 1, T, T, a, kh, d)
+    c.span.copy_(torch.tensor(R.plan([0, 3, 700, 1301, T], None, 0, T, T)[0], dtype=I32))
+    c.run(B, *([] if scratch == "all" else [scratch])).check()
+
+
 @pytest.mark.parametrize("b,nq,nk", [(0, 5, 5), (2, 0, 5), (2, 5, 0), (1, 0, 0)])
 def test_empty(B, b, nq, nk):
     c = Case("any", b, nq, nk, 4, 2, 64).run(B)
