@@ -20,6 +20,14 @@
 // P (for P v and dV) and dS are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most); scores, statistics, dP - delta and every sum are
 // fp32.  The forward divides by the sum of the rounded P: what all terms of a row were rounded by alike drops out, and where a row lies on one key o is that key's v.  o goes out in two
 // parts, its bf16 and that of what the rounding left over, so that delta = dO.(o + rest) does not carry o's rounding, which would be as large as dP - delta in such rows.
+//
+// What bounds it (rocprofv3; docs: 16384 tokens of 4 documents, 32 heads of 128 in groups of 4; window: 4096 tokens, 16 heads of 128 in groups of 2, 1024 keys, capped; prefix: 2 x 1021 tokens of 3
+// documents, 64 heads of 64 in groups of 8, biased; matrix pipe and vector issue busy, waves waiting):
+//   forward  docs 1030 us 48 %, 50 %, 17 %;  window 70 us 26 %, 58 %, 19 %;  prefix 37 us 17 %, 76 %, 26 %
+//   dQ       docs 1265 us 55 %, 43 %, 20 %;  window 82 us 29 %, 48 %, 34 %;  prefix 38 us 21 %, 55 %, 40 %
+//   dK, dV   docs 1995 us 46 %, 33 %, 24 %;  window 116 us 29 %, 41 %, 28 %;  prefix 57 us 23 %, 45 %, 32 %
+// docs: the exponentials and conversions beside the products, and the clock that the matrix pipe's power leaves (2.0 to 2.3 GHz; 8192 causal tokens take 570, 705 and 1015 us, 590 to 660 TFLOP/s);
+// window: the same with the tangent's exponential and quotient, and masks in an eighth of the tiles; prefix: 5 to 9 tiles a workgroup, most of them masked, between launches of a round or two.
 #include <type_traits>
 
 #include "attention_slices.hpp"
@@ -1113,8 +1121,7 @@ RP_DEV int4 look_through(const int4* tiles, int n, int k0, int k1, int first, in
   return make_int4(lo, hi, part, 0);
 }
 
-// A walk over the row tiles [from, to) that see any of the keys, the last one first: the key tiles of a document have its last rows in common, so workgroups that
-// begin together read the same rows at the same time, out of their L2.  What 64 neighbouring tiles see is asked for at once, a tile a lane, and kept as two masks: a
+// A walk over the row tiles [from, to) that see any of the keys, the last one first (the other way round takes as long).  What 64 neighbouring tiles see is asked for at once, a tile a lane, and kept as two masks: a
 // load on the way to every tile would be waited for.
 struct RowWalk {
   const int4* tiles;
@@ -1705,7 +1712,8 @@ hipError_t join_rows(hipStream_t st, const SpanArgs& p) {
   return launch(span_row_join_kernel<D, 16, DQ>, grid, 256, 0, st, p);
 }
 // Few rows: slices for two workgroups of four waves per CU, with a 32-key step for each wave at least -- or one workgroup of eight waves, without slices, where
-// its waves are through with their steps (2.1 us each, one after the other: a CU fetches 60 GB/s) before the slices would have been joined (a second launch, 3 us).
+// its waves are through with their steps before the slices would have been joined, a second launch of 3 us.  (A step takes 2.1 us at d = 128, 1.1 at d = 64, one after the other: one
+// query of 8 key heads against 512, 1024, 4096 keys of 128 8.3, 12.5, 38.5 us without slices, 8.4 and 9.3 with them from 1024 on; of 64 5.7, 7.8, 20.8 and 7.3, 8.6.)
 bool few_rows(const SpanArgs& p) { return row_count(p) <= 32; }
 int step_splits(const SpanArgs& p, int d, size_t bytes) {
   const long nhb = (long)p.kh * p.batch;
