@@ -1198,8 +1198,8 @@ __global__ void __launch_bounds__(256) span_range_kernel(const SpanArgs p) {
 }
 
 // sums[i]: pairs before key tile i, edges included; pieces[i]: first key tile, first pair, pair behind the last.  One block, which with FIND finds the ranges too (where there
-// is little to look through: one launch instead of two).
-constexpr long FEW_LOOKS = 32768;
+// is little to look through: one launch instead of two; 64 key tiles x 512 row tiles 20 us, 5 and 5 in two).
+constexpr long FEW_LOOKS = 8192;
 template <bool FIND>
 __global__ void __launch_bounds__(1024) span_plan_kernel(const SpanArgs p) {
   __shared__ int sum[MOST_TILES + 1], wave[16];
