@@ -17,7 +17,7 @@
 // reach the rows beside them: a document is not touched by what is in another.  (Forward: a row that does see such a value of v becomes NaN as a whole.  Backward: lse and
 // delta of such rows are NaN by then.)
 //
-// P (for P v and dV) and dS are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most); scores, statistics, dP - delta and every sum are
+// P (for P v and dV) and dS are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most; dS of up to 512 keys in two parts, 2^-16); scores, statistics, dP - delta and every sum are
 // fp32.  The forward divides by the sum of the rounded P: what all terms of a row were rounded by alike drops out, and where a row lies on one key o is that key's v.  o goes out in two
 // parts, its bf16 and that of what the rounding left over, so that delta = dO.(o + rest) does not carry o's rounding, which would be as large as dP - delta in such rows.
 //
@@ -41,7 +41,7 @@ constexpr int dq_tile_bytes(int d) { return max_i(2 * 64 * tile_ld(d), 128 * (d 
 
 constexpr int step_smem_bytes(int d, int nc, int nw) { return nw * max_i(32 * tile_ld(d) * 2, 16 * nc * (3 + d + 4) * 4); }
 constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 6 * 64 * 4, 4 * 32 * (d + 4) * 4); }
-constexpr int dkv_pair_smem_bytes(int d) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * 4 * 64 * 16 + 2 * 6 * 64 * 4; }
+constexpr int dkv_pair_smem_bytes(int d, bool two) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * (two ? 6 : 4) * 64 * 16 + 2 * 6 * 64 * 4; }
 constexpr float LOG2E = 1.4426950408889634f;
 
 // Sizes of one sequence and key head.
@@ -166,6 +166,31 @@ RP_DEV float sum2(uint32_t pair, float acc) {      // the two bf16 of a register
   typedef __bf16 v2 __attribute__((ext_vector_type(2)));
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2, pair), __builtin_bit_cast(v2, 0x3f803f80u), acc, false);
 }
+
+// dS of up to FEW_KEYS keys goes to the products in two parts, its bf16 and that of what the rounding left over: dQ and dK are then off by their own rounding alone.  In one part the two are
+// 1.45 times as far from the exact result as that rounding is, and where few keys share a row, chance makes it up to 1.56 (relative 2-norm, 10^-3: 2.4 to 2.5 | 2.6, in two 1.7).  The products
+// more cost little there (200 tokens, 16 heads of 128: dQ 13.8 -> 14.3 us, dK, dV 19.0 -> 19.3; 512 tokens, 32 heads: 22 -> 25 and 29 -> 32); beyond, both would take a fifth longer
+// (8192 causal tokens, 32 heads of 128: 718 -> 882 and 1087 -> 1306).
+constexpr int FEW_KEYS = 512;
+template <bool TWO>
+struct Parts {
+  uint4 hi[2], lo[2];      // of the column tiles
+  RP_DEV static uint32_t left(float a, float b, uint32_t rounded) { return pack_bf16x2(a - bf16_lo(rounded), b - bf16_hi(rounded)); }
+  RP_DEV Parts() {}
+  RP_DEV Parts(const f32x4 (&x)[2][2]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      hi[c] = pack_frag(x[0][c], x[1][c]);
+      if (TWO)
+        lo[c] = make_uint4(left(x[0][c][0], x[0][c][1], hi[c].x), left(x[0][c][2], x[0][c][3], hi[c].y), left(x[1][c][0], x[1][c][1], hi[c].z),
+                           left(x[1][c][2], x[1][c][3], hi[c].w));
+    }
+  }
+  RP_DEV f32x4 times(const uint4& a, int c, f32x4 acc) const {
+    if (TWO) acc = mfma16(a, lo[c], acc);
+    return mfma16(a, hi[c], acc);
+  }
+};
 
 // In a branch that is taken for the few tiles at the edge of a span: keeps the compiler from doing the work for every tile and selecting.
 RP_DEV void stay_in_branch() { asm volatile("" ::: "memory"); }
@@ -732,8 +757,8 @@ __global__ void __launch_bounds__(256) span_row_join_kernel(const SpanArgs p) {
 }
 
 // ================================================================================================ dQ
-template <int D, bool SPLIT, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, D == 64 && !(CAP && BIAS) ? 3 : 2) span_dq_kernel(const SpanArgs p) {
+template <int D, bool SPLIT, bool CAP, bool BIAS, bool TWO>
+__global__ void __launch_bounds__(256, D == 64 && !TWO && !(CAP && BIAS) ? 3 : 2) span_dq_kernel(const SpanArgs p) {
   constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, NT = 256, BQ = 128;
   using T64 = Tile64<D, NT>;
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];   // dq_smem_bytes(D)
@@ -907,7 +932,7 @@ __global__ void __launch_bounds__(256, D == 64 && !(CAP && BIAS) ? 3 : 2) span_d
         }
       }
       constexpr int AHEAD = 4;      // K^T fragments requested that many pairs of products early
-      const uint4 df[2] = {pack_frag(sT[0][0], sT[1][0]), pack_frag(sT[0][1], sT[1][1])};
+      const Parts<TWO> df(sT);
       auto ufrag_at = [&](int n) { return read_frag_tr<LD>(ktfrag + 32 * k2 * LD + 16 * n); };
       uint4 uring[AHEAD];
 #pragma unroll
@@ -917,7 +942,7 @@ __global__ void __launch_bounds__(256, D == 64 && !(CAP && BIAS) ? 3 : 2) span_d
         const uint4 a = uring[n % AHEAD];
         if (n + AHEAD < DT) uring[n % AHEAD] = ufrag_at(n + AHEAD);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) dqacc[n][c] = mfma16(a, df[c], dqacc[n][c]);
+        for (int c = 0; c < 2; ++c) dqacc[n][c] = df.times(a, c, dqacc[n][c]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -1281,7 +1306,7 @@ RP_DEV SpanArgs read_again() {
 }
 
 // The keys of a workgroup do not mix: a column of the score tiles is a key's own.
-template <int D, bool CAP, bool BIAS, bool EVEN>
+template <int D, bool CAP, bool BIAS, bool EVEN, bool TWO>
 __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
   constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, NT = 256;
   using T64 = Tile64<D, NT>;
@@ -1415,7 +1440,7 @@ __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
       probabilities<CAP, BIAS>(z, dp, sc, stat + 32 * t2, lg, 32 * w + lr, kv0, whole);
       {
         const uint4 pfg[2] = {pack_frag(z[0][0], z[1][0]), pack_frag(z[0][1], z[1][1])};
-        const uint4 dfg[2] = {pack_frag(dp[0][0], dp[1][0]), pack_frag(dp[0][1], dp[1][1])};
+        const Parts<TWO> dfg(dp);
 #pragma unroll
         for (int n = 0; n < NU; ++n) {
           const uint4 a = uring[n % AHEAD];
@@ -1423,7 +1448,7 @@ __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
           const int dt = n >> 1;
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            if (n & 1) dkacc[dt][c] = mfma16(a, dfg[c], dkacc[dt][c]);
+            if (n & 1) dkacc[dt][c] = dfg.times(a, c, dkacc[dt][c]);
             else dvacc[dt][c] = mfma16(a, pfg[c], dvacc[dt][c]);
           }
           __builtin_amdgcn_sched_barrier(0);
@@ -1451,16 +1476,16 @@ __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
 
 // Two waves per SIMD at d = 128 (see attn_bwd_dkv_pair_kernel in attention.hip): the 32 keys of a pair of waves are shared, wave h of it keeps
 // the accumulators of half h of the head dimension, makes the scores of rows 32 h .. of each tile and hands P and dS to its partner through LDS.
-template <int D, bool CAP, bool BIAS, bool EVEN>
+template <int D, bool CAP, bool BIAS, bool EVEN, bool TWO>
 __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs args) {
-  constexpr int LD = tile_ld(D), KS = D / 32, DH = D / 32, NT = 512;
+  constexpr int LD = tile_ld(D), KS = D / 32, DH = D / 32, NT = 512, NX = TWO ? 6 : 4;
   using T64 = Tile64<D, NT>;
   using Stat = RowStat<CAP, BIAS>;
   extern __shared__ __attribute__((aligned(16))) unsigned char dyn_smem[];
   bf16* const smem = reinterpret_cast<bf16*>(dyn_smem);             // two sets (tile parity) of Q | dO, then the exchange
   constexpr int TSET = 2 * 64 * LD;
-  uint4* const exch = reinterpret_cast<uint4*>(smem + 2 * TSET);    // [8 waves][4 fragments][64 lanes]
-  float* const stat = reinterpret_cast<float*>(exch + 8 * 4 * 64);  // [2 sets]
+  uint4* const exch = reinterpret_cast<uint4*>(smem + 2 * TSET);    // [8 waves][NX fragments][64 lanes]
+  float* const stat = reinterpret_cast<float*>(exch + 8 * NX * 64); // [2 sets]
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1518,8 +1543,8 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
   const bf16* dofrag = qfrag + 64 * LD;
   const bf16* qtfrag = smem + tr_base<LD>(lane) + 16 * DH * h;      // its half of the head dimension
   const bf16* dotfrag = qtfrag + 64 * LD;
-  uint4* const ex_mine = exch + (w8 * 4) * 64 + lane;
-  const uint4* const ex_theirs = exch + ((w8 ^ 1) * 4) * 64 + lane;
+  uint4* const ex_mine = exch + (w8 * NX) * 64 + lane;
+  const uint4* const ex_theirs = exch + ((w8 ^ 1) * NX) * 64 + lane;
 
   uint4 qreg[T64::NREG], doreg[T64::NREG];
   RowTile<D, NT, EVEN> rows;
@@ -1534,7 +1559,7 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
   range.start(p.tiles + (long)s.b * ((s.total + 63) / 64), kv0, min(kv0 + 128, p.seq_kv), u0, u1);
 
   constexpr int AHEAD = 2;     // two waves per SIMD cover each other's LDS latency: a short ring is enough
-  auto update_half = [&](int set, int t2, const uint4 (&pf)[2], const uint4 (&df)[2]) {
+  auto update_half = [&](int set, int t2, const uint4 (&pf)[2], const Parts<TWO>& df) {
     constexpr int NU = 2 * DH;     // n = dt * 2 + which
     auto ufrag_at = [&](int n) { return read_frag_tr<LD>(((n & 1) ? qtfrag : dotfrag) + set * TSET + 32 * t2 * LD + 16 * (n >> 1)); };
     uint4 uring[AHEAD];
@@ -1548,7 +1573,7 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
       const int dt = n >> 1;
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        if (n & 1) dkacc[dt][c] = mfma16(a, df[c], dkacc[dt][c]);
+        if (n & 1) dkacc[dt][c] = df.times(a, c, dkacc[dt][c]);
         else dvacc[dt][c] = mfma16(a, pf[c], dvacc[dt][c]);
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -1559,7 +1584,12 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
   // new tile is stored (into the other set) while the accumulators take the partner's half of the PREVIOUS tile.
   auto partner_update = [&](int prev) {
     const uint4 ppf[2] = {ex_theirs[0], ex_theirs[64]};
-    const uint4 pdf[2] = {ex_theirs[128], ex_theirs[192]};
+    Parts<TWO> pdf;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      pdf.hi[c] = ex_theirs[128 + 64 * c];
+      if (TWO) pdf.lo[c] = ex_theirs[256 + 64 * c];
+    }
     update_half(prev & 1, h ^ 1, ppf, pdf);
   };
   if (range.more()) {
@@ -1613,9 +1643,10 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
     }
     probabilities<CAP, BIAS>(z, dp, sc, st_set + 32 * h, lg, 32 * w + lr, kv0, whole);
     const uint4 pfg[2] = {pack_frag(z[0][0], z[1][0]), pack_frag(z[0][1], z[1][1])};
-    const uint4 dfg[2] = {pack_frag(dp[0][0], dp[1][0]), pack_frag(dp[0][1], dp[1][1])};
+    const Parts<TWO> dfg(dp);
     // the partner read last tile's fragments before the barrier above: the slots are free
-    ex_mine[0] = pfg[0]; ex_mine[64] = pfg[1]; ex_mine[128] = dfg[0]; ex_mine[192] = dfg[1];
+    ex_mine[0] = pfg[0]; ex_mine[64] = pfg[1]; ex_mine[128] = dfg.hi[0]; ex_mine[192] = dfg.hi[1];
+    if (TWO) { ex_mine[256] = dfg.lo[0]; ex_mine[320] = dfg.lo[1]; }
     update_half(i & 1, h, pfg, dfg);
   }
   __syncthreads();
@@ -1751,8 +1782,8 @@ hipError_t fwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
   return e == hipSuccess ? join_rows<D, false>(st, p) : e;
 }
 
-template <int D, bool CAP, bool BIAS>
-hipError_t bwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
+template <int D, bool CAP, bool BIAS, bool TWO>
+hipError_t bwd_parts(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
   const int nhb = p.kh * p.batch;
   const long rows = row_count(p);
   const size_t head = least_bytes(p);
@@ -1766,10 +1797,10 @@ hipError_t bwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
     p.splits = row_splits(p, D, bytes);
     const int grid = ceil_div(rows, 128) * nhb * p.splits;
     if (p.splits > 1) {
-      e = launch(span_dq_kernel<D, true, CAP, BIAS>, grid, 256, dq_smem_bytes(D), st, p);
+      e = launch(span_dq_kernel<D, true, CAP, BIAS, TWO>, grid, 256, dq_smem_bytes(D), st, p);
       if (e == hipSuccess) e = join_rows<D, true>(st, p);
     } else {
-      e = launch(span_dq_kernel<D, false, CAP, BIAS>, grid, 256, dq_smem_bytes(D), st, p);
+      e = launch(span_dq_kernel<D, false, CAP, BIAS, TWO>, grid, 256, dq_smem_bytes(D), st, p);
     }
   }
   if (e != hipSuccess || p.seq_kv == 0) return e;
@@ -1790,11 +1821,17 @@ hipError_t bwd(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
     if (e != hipSuccess) return e;
   }
   const int grid = p.parts > 0 ? p.parts * p.kh : (int)key_tiles(p) * p.kh;
-  const bool even = 64 % (p.a / p.kh) == 0;
-  if constexpr (D == 128) e = launch(even ? span_dkv_pair_kernel<D, CAP, BIAS, true> : span_dkv_pair_kernel<D, CAP, BIAS, false>, grid, 512, dkv_pair_smem_bytes(D), st, p);
-  else e = launch(even ? span_dkv_kernel<D, CAP, BIAS, true> : span_dkv_kernel<D, CAP, BIAS, false>, grid, 256, dkv_smem_bytes(D), st, p);
+  constexpr bool E = !TWO;      // (few keys: one kernel for all groups)
+  const bool even = E && 64 % (p.a / p.kh) == 0;
+  if constexpr (D == 128) e = launch(even ? span_dkv_pair_kernel<D, CAP, BIAS, E, TWO> : span_dkv_pair_kernel<D, CAP, BIAS, false, TWO>, grid, 512, dkv_pair_smem_bytes(D, TWO), st, p);
+  else e = launch(even ? span_dkv_kernel<D, CAP, BIAS, E, TWO> : span_dkv_kernel<D, CAP, BIAS, false, TWO>, grid, 256, dkv_smem_bytes(D), st, p);
   if (e != hipSuccess || p.parts == 0) return e;
   return launch(span_key_join_kernel<D>, (int)key_tiles(p) * p.kh * 8, 256, 0, st, p);
+}
+
+template <int D, bool CAP, bool BIAS>
+hipError_t bwd(hipStream_t st, const SpanArgs& p, void* scratch, size_t bytes) {
+  return p.seq_kv <= FEW_KEYS ? bwd_parts<D, CAP, BIAS, true>(st, p, scratch, bytes) : bwd_parts<D, CAP, BIAS, false>(st, p, scratch, bytes);
 }
 
 // One of eight: d, cap, bias.
