@@ -1532,7 +1532,7 @@ rp_status rp_op_span_attn_bwd(void* stream, const void* q, const void* k, const 
 
 rp_status rp_op_dropout(void* stream, const void* x, long ldx, const void* res, long ldr, void* y, long ldy, int T, int n, float p, unsigned long long seed,
                         unsigned long long offset, const unsigned long long* step) {
-  if (T < 0 || n < 0 || n % 8 || !(p >= 0.f && p <= 1.f) || (double)T * n > 137438953472.0 || reinterpret_cast<uintptr_t>(step) % 8)
+  if (T < 0 || n < 0 || n % 8 || !(p >= 0.f && p <= 1.f) || (double)T * n >= 137438953472.0 || reinterpret_cast<uintptr_t>(step) % 8)
     return fail(nullptr, RP_EINVAL, "rp_op_dropout: bad arguments");
   if (bad_rows(x, T, n, ldx) || bad_rows(y, T, n, ldy) || (res && bad_rows(res, T, n, ldr)) || (y == x && ldy != ldx) || (res && y == res && ldy != ldr))
     return fail(nullptr, RP_EINVAL, "rp_op_dropout: tensors missing, not on 16-byte boundaries, or bad strides");
@@ -1626,7 +1626,8 @@ rp_status rp_op_scan_bwd(void* stream, int weight, const void* x, const void* g,
   if (bad_scan(batch, seq, c) || weight < RP_SCAN_PLAIN || weight > RP_SCAN_ENERGY) return fail(nullptr, RP_EINVAL, "rp_op_scan_bwd: bad sizes or weight");
   const long T = (long)batch * seq;
   if (bad_rows(x, T, c, ldx) || bad_rows(g, T, c, ldg) || bad_rows(dy, T, c, lddy) || bad_rows(dx, T, c, lddx) || bad_rows(dg, T, c, lddg) ||
-      (T && c && !states) || bad_state(states) || bad_state(dlast) || bad_state(dh0))
+      (T && c && !states) || bad_state(states) || bad_state(dlast) || bad_state(dh0) || (dx && ((dx == x && lddx != ldx) || (dx == dy && lddx != lddy))) ||
+      (dg && dg == g && lddg != ldg))
     return fail(nullptr, RP_EINVAL, "rp_op_scan_bwd: tensors missing, not on 16-byte boundaries, or bad strides");
   size_t n = 0, need = 0;
   k_scan_sizes(batch, seq, c, &n, &need);

@@ -103,6 +103,12 @@ def test_scan_backward_refuses(bad):
     refused(B.rp_op_scan_bwd, None, **dict(dict(GOOD_SCAN, dy=P, dx=P, dg=P, lddy=64, lddx=64, lddg=64, dlast=None, dh0=None), **bad))
 
 
+@pytest.mark.parametrize("bad", [dict(dx=3 * P, x=3 * P, lddx=72), dict(dx=4 * P, dy=4 * P, lddx=72), dict(dg=5 * P, g=5 * P, lddg=72)])
+def test_scan_backward_in_place_keeps_the_stride(bad):
+    apart = dict(x=P, g=2 * P, dy=6 * P, dx=7 * P, dg=8 * P, lddy=64, lddx=64, lddg=64, dlast=None, dh0=None)
+    refused(B.rp_op_scan_bwd, None, **dict(dict(GOOD_SCAN, **apart), **bad))
+
+
 def test_scan_sizes():
     refused(B.rp_op_scan_sizes, 1, 1, 12)
     assert B.rp_op_scan_sizes(0, 9, 8) == (0, 0) and B.rp_op_scan_sizes(2, 0, 8) == (0, 0)
