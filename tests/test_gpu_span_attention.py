@@ -136,6 +136,36 @@ def test_forward_and_backward(B, shape, cap, bias):
     Case(*shape, cap=cap, bias=bias).run(B).check()
 
 
+LONG = [("docs", 1, 700, 700, 6, 2, 128), ("causal", 2, 600, 600, 8, 2, 128), ("docs", 1, 900, 900, 8, 2, 64), ("any", 1, 550, 777, 6, 2, 64), ("any", 2, 300, 1030, 4, 1, 128),
+        ("ragged", 2, 130, 1300, 10, 2, 64)]      # (beyond what dS of few keys goes through in two parts)
+
+
+@pytest.mark.parametrize("scratch", ["full", "least"])
+@pytest.mark.parametrize("cap,bias", KINDS)
+@pytest.mark.parametrize("shape", LONG, ids=lambda s: "-".join(map(str, s)))
+def test_more_keys(B, shape, cap, bias, scratch):
+    Case(*shape, cap=cap, bias=bias, pad=8).run(B, scratch).check()
+
+
+@pytest.mark.parametrize("bad", [NAN, float("inf")])
+@pytest.mark.parametrize("a,kh,d,cap,bias", [(4, 2, 64, 0.0, False), (6, 2, 64, 20.0, True), (4, 2, 128, 20.0, True), (6, 2, 128, 0.0, False)])
+def test_a_document_does_not_reach_another_of_many_keys(B, bad, a, kh, d, cap, bias):
+    T, lo, hi = 850, 190, 555
+    runs = []
+    for spoil in (False, True):
+        c = Case("causal", 1, T, T, a, kh, d, cap=cap, bias=bias)
+        c.span.copy_(torch.tensor(R.plan([0, lo, hi, T], None, 0, T, T)[0], dtype=I32))
+        if spoil:
+            for t in (c.q, c.k, c.v, c.do):
+                t[lo:hi:3, ::5] = bad
+        runs.append(c.run(B).got())
+    for name, t in runs[1].items():
+        rows = torch.arange(T, device=DEV)
+        keep = (rows < lo) | (rows >= hi)
+        x, y = (r[name][:, :, keep] if name == "lse" else r[name][:, keep] for r in runs)
+        assert torch.equal(x, y), name
+
+
 @pytest.mark.parametrize("scratch", ["least", "some"])
 @pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[6], SHAPES[7], SHAPES[12]], ids=lambda s: "-".join(map(str, s)))
 def test_less_scratch(B, shape, scratch):
