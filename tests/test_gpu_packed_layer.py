@@ -303,3 +303,68 @@ def test_beside_the_causal_attention(B):
         out.append((o, lse, dq, dk, dv))
     for x, y in zip(*out):      # the other one's delta carries the rounding of o
         assert rel(x, y.double()) < 1e-2
+
+
+def test_rows_that_lie_far_apart(B):
+    """Rows 65536 elements apart, offsets beyond 32 bits: the same bits as of rows one behind another."""
+    T, ld, a, kh, d = 33000, 65536, 2, 1, 128
+    g = torch.Generator(device=DEV).manual_seed(5)
+    far = torch.empty((T, ld), dtype=BF16, device=DEV)
+    used = [0]
+
+    class Rows:
+        """Of n columns: together, and as columns of the large array."""
+
+        def __init__(self, n, std=0.0):
+            self.near = torch.randn((T, n), generator=g, device=DEV).mul(std).to(BF16)
+            self.far = far[:, used[0]:used[0] + n]
+            self.far.copy_(self.near)
+            used[0] += n
+
+        def at(self, i):
+            return (self.near.data_ptr(), self.near.shape[1]) if i == 0 else (self.far.data_ptr(), ld)
+
+        def same(self):
+            assert torch.equal(self.near, self.far)
+
+    st = torch.cuda.current_stream().cuda_stream
+    # attention: a window over all rows, forward and backward; then the last query alone, over all keys
+    q, do, k, v = Rows(a * d, 2.0), Rows(a * d, 1.0), Rows(kh * d, 1.0), Rows(kh * d, 1.0)
+    o, rest, dq, dk, dv = [Rows(n * d) for n in (a, a, a, kh, kh)]
+    t = torch.arange(T, device=DEV)
+    span = torch.stack(((t - 300).clamp(min=0), t + 1), -1).to(torch.int32).contiguous()
+    everything = torch.tensor([[0, T]], dtype=torch.int32, device=DEV)
+    fwd, bwd, _ = B.rp_op_span_attn_scratch(1, T, T, a, kh, d)
+    step, _, _ = B.rp_op_span_attn_scratch(1, 1, T, a, kh, d)
+    ws = torch.empty(max(fwd, bwd, step, 16), dtype=torch.uint8, device=DEV)
+    lse, delta, one, last = [], torch.empty((a, T), device=DEV), torch.empty((2, a * d), dtype=BF16, device=DEV), (T - 1) * 2
+    for i in (0, 1):
+        (pq, lq), (pdo, ldo), (pk, lk), (pv, lv), (po, lo), (pr, _), (pdq, ldq), (pdk, ldk), (pdv, ldv) = [r.at(i) for r in (q, do, k, v, o, rest, dq, dk, dv)]
+        lse.append(torch.empty((a, T), device=DEV))
+        B.rp_op_span_attn_fwd(st, pq, pk, pv, po, pr, lse[i], lq, lk, lv, lo, span, None, None, 0.0, 1, T, T, a, kh, d, 0.1, ws)
+        B.rp_op_span_attn_bwd(st, pq, pk, pv, po, pr, pdo, lse[i], delta, pdq, pdk, pdv, lq, lk, lv, lo, ldo, ldq, ldk, ldv, span, None, None, 0.0, 1, T, T, a, kh, d, 0.1, ws)
+        B.rp_op_span_attn_fwd(st, pq + last * lq, pk, pv, one[i], None, None, lq, lk, lv, a * d, everything, None, None, 0.0, 1, 1, T, a, kh, d, 0.1, ws)
+    for r in (o, rest, dq, dk, dv):
+        r.same()
+        assert bool(torch.isfinite(r.near).all()) and bool(r.near[-1].any())
+    assert torch.equal(*lse) and torch.equal(one[0], one[1]) and bool(one[0].any())
+    # recurrence, dropout, embedding
+    x, gate, dy, y, dx, dg, drop = [Rows(64, s) for s in (1.0, 2.0, 1.0, 0.0, 0.0, 0.0, 0.0)]
+    states, scratch = B.rp_op_scan_sizes(1, T, 64)
+    states, ws = torch.empty(states // 4, device=DEV), torch.empty(scratch, dtype=torch.uint8, device=DEV)
+    for i in (0, 1):
+        (px, lx), (pg, lg), (pdy, ldy), (py, ly), (pdx, ldx), (pdg, ldg), (pd, ldd) = [r.at(i) for r in (x, gate, dy, y, dx, dg, drop)]
+        B.rp_op_scan_fwd(st, B.SCAN_MEAN, px, pg, py, lx, lg, ly, None, None, None, None, states, 1, T, 64, ws)
+        B.rp_op_scan_bwd(st, B.SCAN_MEAN, px, pg, pdy, pdx, pdg, lx, lg, ldy, ldx, ldg, None, None, states, None, None, 1, T, 64, ws)
+        B.rp_op_dropout(st, px, lx, pdy, ldy, pd, ldd, T, 64, 0.3, 7, 0, None)
+    for r in (y, dx, dg, drop):
+        r.same()
+        assert bool(r.near[-1].any())
+    ids = torch.randint(T - 500, T, (700,), generator=g, device=DEV, dtype=torch.int32)
+    ws = torch.empty(B.rp_op_embed_scratch(700, T, 64), dtype=torch.uint8, device=DEV)
+    rows, grads = [torch.empty((700, 64), dtype=BF16, device=DEV) for _ in (0, 1)], [torch.empty((T, 64), device=DEV), far.view(torch.float32)[:, :64]]
+    for i in (0, 1):
+        px, lx = x.at(i)
+        B.rp_op_embed_fwd(st, px, lx, ids, 3.0, rows[i], 64, 700, T, 64)
+        B.rp_op_embed_bwd(st, rows[0], 64, ids, 0.5, grads[i].data_ptr(), grads[i].stride(0), 0, 700, T, 64, ws)
+    assert torch.equal(*rows) and torch.equal(*grads) and bool(rows[0].any()) and bool(grads[0][-500:].any())
