@@ -9,7 +9,7 @@
 // kernel adds those up in order.  Sums are fp32.
 //
 // What bounds it: memory.  16384 tokens of 4096 from 151936 rows: rows 49 us (5.5 TB/s), sort 24, sums 75, join 9, and 405 for the zeros of the rows without tokens (2.4 GB at 5.9 TB/s).
-// 4084 tokens of 2880, gradient added to what is there: rows 10, sort 13, sums 17, join 6: three launches that wait for one another.
+// 4084 tokens of 2880, gradient added to what is there: rows 10, sort 11, sums 17, join 6: three launches that wait for one another.
 #include "pack_ops.hpp"
 
 namespace {
@@ -47,6 +47,18 @@ __global__ void __launch_bounds__(NT) embed_rows_kernel(const bf16* table, long 
 }
 
 // ------------------------------------------------------------------------------------------------ sorting
+// Of the lanes that are `in`, those with this lane's digit: four instructions a bit.
+RP_DEV unsigned long long same_digit(int digit, int bits, bool in) {
+  const unsigned long long used = __ballot(in);
+  uint32_t lo = (uint32_t)used, hi = (uint32_t)(used >> 32);
+  for (int b = 0; b < bits; ++b) {
+    const int mine = __builtin_amdgcn_sbfe(digit, b, 1);      // 0 or -1
+    const unsigned long long set = __ballot(mine != 0);
+    lo &= ~((uint32_t)set ^ (uint32_t)mine);
+    hi &= ~((uint32_t)(set >> 32) ^ (uint32_t)mine);
+  }
+  return (unsigned long long)hi << 32 | lo;
+}
 RP_DEV uint32_t key_of(int id, int V) { return (unsigned)id < (unsigned)V ? (uint32_t)id : (uint32_t)V; }
 
 // Up to 1024 tokens, one block: a token's place is the number of those before it in the order, found by comparing it with all of them in LDS.  Also clears
@@ -71,7 +83,7 @@ __global__ void __launch_bounds__(SMALL) embed_sort_small_kernel(const int* ids,
 }
 
 // Up to 8192 tokens, one block: radix sort by one or two digits of up to 10 bits, in LDS.  A wave has a 16th of the tokens, 64 at a time; a token's rank among those of its digit
-// is that of the wave's earlier ones (counted in LDS) and of the lanes before it (found by ballots).  (4084 tokens: four launches as below 19 us, this one 13.)
+// is that of the wave's earlier ones (counted in LDS) and of the lanes before it (found by ballots).  (4084 tokens: four launches as below 19 us, this one 11.)
 constexpr int MID = 8192, MID_EACH = MID / 1024;
 struct MidSort {
   uint2 sorted[MID];
@@ -93,19 +105,16 @@ __global__ void __launch_bounds__(1024) embed_sort_mid_kernel(const int* ids, in
     for (int x = tid; x < (V + 31) / 32; x += 1024) marks[x] = 0u;
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * bits;
-    for (int x = tid; x < 16 * MOST_DIGITS; x += 1024) m.count[0][x] = 0;
-    __syncthreads();
+    for (int d = lane; d < digits; d += 64) m.count[w][d] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
     int rank[MID_EACH];
 #pragma unroll
     for (int j = 0; j < MID_EACH; ++j) {
       if (j >= each) break;      // uniform
       const bool in = 64 * (each * w + j) + lane < T;
       const int digit = (int)(key[j] >> shift) & (digits - 1);
-      unsigned long long same = __ballot(in);
-      for (int b = 0; b < bits; ++b) {
-        const unsigned long long set = __ballot((digit >> b) & 1);
-        same &= (digit >> b) & 1 ? set : ~set;
-      }
+      const unsigned long long same = same_digit(digit, bits, in);
       const int ahead = __popcll(same & ((1ull << lane) - 1ull));
       rank[j] = m.count[w][digit] + ahead;      // (all lanes read before the first one of each digit adds, as below)
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -129,14 +138,16 @@ __global__ void __launch_bounds__(1024) embed_sort_mid_kernel(const int* ids, in
     if (lane == 63) m.wave[w] = sum;
     __syncthreads();
     int at = sum - total;
-    for (int u = 0; u < w; ++u) at += m.wave[u];
-    if (tid < digits)
+    if (tid < digits) {
+#pragma unroll
+      for (int u = 0; u < 16; ++u) at += u < w ? m.wave[u] : 0;
 #pragma unroll
       for (int u = 0; u < 16; ++u) {
         const int n = m.count[u][tid];
         m.count[u][tid] = at;
         at += n;
       }
+    }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < MID_EACH; ++j) {
@@ -248,11 +259,7 @@ __global__ void __launch_bounds__(NT) embed_scatter_kernel(const SortArgs p) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const bool in = i0 + 256 * w + 64 * j + lane < last;
-      unsigned long long same = __ballot(in);      // the lanes with this one's digit
-      for (int b = 0; b < p.bits; ++b) {
-        const unsigned long long set = __ballot((digit[j] >> b) & 1);
-        same &= (digit[j] >> b) & 1 ? set : ~set;
-      }
+      const unsigned long long same = same_digit(digit[j], p.bits, in);
       const int ahead = __popcll(same & ((1ull << lane) - 1ull));
       // all lanes read before the first one of each digit adds (LDS works in order for a wave, so the fences are for the compiler)
       rank[j] = count[w][digit[j]] + ahead;
