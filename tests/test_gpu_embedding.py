@@ -78,6 +78,12 @@ def test_gradient(B, T, V, h, kind, accumulate):
         assert torch.equal(runs[0][at], given[at])
 
 
+@pytest.mark.parametrize("kind", ["zipf", "one", "even"])
+@pytest.mark.parametrize("T", [63, 64, 65, 127, 128, 129, 2047, 2048, 4097, 8191, 8193])
+def test_gradient_around_the_sorts_limits(B, T, kind):
+    test_gradient(B, T, 700, 72, kind, 0)
+
+
 def test_gradient_strides_and_nothing_to_do(B):
     T, V, h = 50, 20, 40
     g = torch.Generator().manual_seed(3)
