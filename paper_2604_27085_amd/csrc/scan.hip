@@ -178,15 +178,18 @@ RP_DEV word_t state_word(float h) { return (word_t)STATE << 32 | __float_as_uint
 RP_DEV void publish(word_t* at, word_t w) { __hip_atomic_store(at, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 RP_DEV word_t look(const word_t* at) { return __hip_atomic_load(const_cast<word_t*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// What a chunk starts from, for all waves of its workgroup.  Wave 0 publishes the chunk's map; every wave then waits for one of the eight chunks before and puts what it says into
-// LDS, and all of them go from the nearest end state through the maps behind it.  Where none of the eight has its end state yet, they look again.
+// What a chunk starts from, for all waves of its workgroup.  Wave 0 publishes the chunk's map; every wave then waits for EACH of the 8 EACH chunks before and puts what they say into
+// LDS, and all of them go from the nearest end state through the maps behind it.  Where none of those chunks has its end state yet, they look again.  EACH is 4 where all of a launch's
+// workgroups are on the chip at once, and the chain of looks is what takes the time (18467 tokens of 72 channels: forward 41 -> 29 us, backward 44 -> 32), else 1 (16384 tokens of 4096:
+// 108 and 147 us, with 4 118 and 158).
 // `given`: the state before the first chunk (behind the last one, BACK); end: wave 0's, the chunk's own end state.
+template <int EACH>
 struct Looks {
-  fch a[NW][64], b[NW][64];
-  int state[NW];
+  fch a[EACH * NW][64], b[EACH * NW][64];
+  int state[EACH * NW];
 };
-template <bool BACK>
-RP_DEV fch start_of(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], const fch (&Bs)[NW][64], Looks& looks, const fch& given, fch& end) {
+template <int EACH, bool BACK>
+RP_DEV fch start_of(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], const fch (&Bs)[NW][64], Looks<EACH>& looks, const fch& given, fch& end) {
   const int before = BACK ? p.chunks - 1 - s.chunk : s.chunk;
   word_t* const mine = p.words + (s.in ? s.at(p) : 0);
   fch A = As[BACK ? NW - 1 : 0][s.lane], B = Bs[BACK ? NW - 1 : 0][s.lane];
@@ -207,39 +210,50 @@ RP_DEV fch start_of(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], 
   }
   fch h = given;
   if (before > 0) {      // uniform over the workgroup
-    const word_t* const theirs = mine + (BACK ? 1 : -1) * (long)(s.w + 1) * p.c;
     int from;
     for (;;) {
-      bool state = false;
-      if (s.w < before) {
-        word_t w[LANES];
-        for (;;) {      // ends: that chunk's workgroup took its place before this one
-          bool there = true;
-          state = true;
+      bool there[EACH], state[EACH];
+      word_t w[EACH][LANES];
+      for (;;) {      // ends: those chunks' workgroups took their places before this one
+        bool all = true;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+          const int n = s.w + k * NW;      // that many chunks between
+          const word_t* const theirs = mine + (BACK ? 1 : -1) * (long)(n + 1) * p.c;
+#pragma unroll
+          for (int e = 0; e < LANES; ++e) w[k][e] = s.in && n < before ? look(theirs + e) : state_word(0.f);
+        }
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+          there[k] = state[k] = true;
 #pragma unroll
           for (int e = 0; e < LANES; ++e) {
-            w[e] = s.in ? look(theirs + e) : state_word(0.f);
-            there = there && (uint32_t)(w[e] >> 32) != 0u;
-            state = state && (uint32_t)(w[e] >> 32) == STATE;
+            there[k] = there[k] && (uint32_t)(w[k][e] >> 32) != 0u;
+            state[k] = state[k] && (uint32_t)(w[k][e] >> 32) == STATE;
           }
-          if (__all(there)) break;
-          __builtin_amdgcn_s_sleep(1);
+          all = all && there[k];
         }
+        if (__all(all)) break;
+        __builtin_amdgcn_s_sleep(1);
+      }
+#pragma unroll
+      for (int k = 0; k < EACH; ++k) {
+        const int n = s.w + k * NW;
         fch a, b;
 #pragma unroll
         for (int e = 0; e < LANES; ++e) {
-          a[e] = __uint_as_float((uint32_t)(w[e] >> 32));
-          b[e] = __uint_as_float((uint32_t)w[e]);
+          a[e] = __uint_as_float((uint32_t)(w[k][e] >> 32));
+          b[e] = __uint_as_float((uint32_t)w[k][e]);
         }
-        looks.a[s.w][s.lane] = a;
-        looks.b[s.w][s.lane] = b;
-        state = __all(state);
+        looks.a[n][s.lane] = a;
+        looks.b[n][s.lane] = b;
+        const bool is = __all(state[k]) && n < before;
+        if (s.lane == 0) looks.state[n] = is;
       }
-      if (s.lane == 0) looks.state[s.w] = state;
       __syncthreads();
       from = -1;
 #pragma unroll
-      for (int i = NW - 1; i >= 0; --i)
+      for (int i = EACH * NW - 1; i >= 0; --i)
         if (looks.state[i]) from = i;
       if (__builtin_amdgcn_readfirstlane(from) >= 0) break;
       __syncthreads();      // all have seen that there is none
@@ -280,10 +294,10 @@ RP_DEV fch enter(const fch (&As)[NW][64], const fch (&Bs)[NW][64], const Place& 
   }
   return h;
 }
-// ONE: a sequence is one chunk, which starts from the call's own state
-template <bool ONE>
+// EACH 0: a sequence is one chunk, which starts from the call's own state
+template <int EACH>
 RP_DEV int take_place(const ScanArgs& p, int* lds) {
-  if (ONE) return (int)blockIdx.x;
+  if (EACH == 0) return (int)blockIdx.x;
   if (threadIdx.x == 0) *lds = (int)atomicAdd(p.counter, 1u);
   __syncthreads();
   return __builtin_amdgcn_readfirstlane(*lds);
@@ -292,23 +306,23 @@ RP_DEV fch given_state(const float* src, const ScanArgs& p, const Place& s) {
   return src && s.in ? *reinterpret_cast<const fch*>(src + (long)s.b * p.c + s.ch) : fch{0.f, 0.f};
 }
 // What the chunk starts from; the waves have put their maps into LDS.  The state behind the last chunk goes to `last`.
-template <bool ONE, bool BACK>
-RP_DEV fch chunk_start(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], const fch (&Bs)[NW][64], Looks* looks, const float* given, float* last) {
+template <int EACH, bool BACK>
+RP_DEV fch chunk_start(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], const fch (&Bs)[NW][64], Looks<EACH ? EACH : 1>* looks, const float* given, float* last) {
   fch h = given_state(given, p, s);
-  if constexpr (!ONE) {
+  if constexpr (EACH > 0) {
     fch end;
-    h = start_of<BACK>(p, s, As, Bs, *looks, h, end);
+    h = start_of<EACH, BACK>(p, s, As, Bs, *looks, h, end);
     if (last && s.w == 0 && s.in && s.chunk == (BACK ? 0 : p.chunks - 1)) *reinterpret_cast<fch*>(last + (long)s.b * p.c + s.ch) = end;
   }
   return h;
 }
 
-template <int W, bool ONE>
+template <int W, int EACH>
 __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p) {
   __shared__ fch As[NW][64], Bs[NW][64];
-  __shared__ Looks looks;
+  __shared__ Looks<EACH ? EACH : 1> looks;
   __shared__ int place;
-  const Place s(p, take_place<ONE>(p, &place), false);
+  const Place s(p, take_place<EACH>(p, &place), false);
   raw_t gr[TOK], xr[TOK];
   TokenRows(p.g, p.ldg, s, p, s.len).load(gr);
   TokenRows(p.x, p.ldx, s, p, s.len).load(xr);
@@ -321,7 +335,7 @@ __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p) {
     Bs[s.w][s.lane] = B;
   }
   __syncthreads();
-  const fch start = chunk_start<ONE, false>(p, s, As, Bs, &looks, p.h0, p.last);
+  const fch start = chunk_start<EACH, false>(p, s, As, Bs, &looks, p.h0, p.last);
   fch h = enter<false>(As, Bs, s, start);
   if (s.in && s.w == 0 && p.states && p.seq > 0) *reinterpret_cast<fch*>(p.states + s.at(p)) = start;
   const TokenRows out(p.y, p.ldy, s, p, p.seq);
@@ -338,15 +352,15 @@ __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p) {
       out.store(i, PLAIN || live ? pack(h) : 0u);
       }
   });
-  if (ONE && p.last && s.w == NW - 1 && s.in) *reinterpret_cast<fch*>(p.last + (long)s.b * p.c + s.ch) = h;      // (waves without tokens pass the state on)
+  if (EACH == 0 && p.last && s.w == NW - 1 && s.in) *reinterpret_cast<fch*>(p.last + (long)s.b * p.c + s.ch) = h;      // (waves without tokens pass the state on)
 }
 
-template <int W, bool ONE>
+template <int W, int EACH>
 __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p) {
   __shared__ fch As[NW][64], Bs[NW][64], Ab[NW][64], Bb[NW][64];
-  __shared__ Looks looks;
+  __shared__ Looks<EACH ? EACH : 1> looks;
   __shared__ int place;
-  const Place s(p, take_place<ONE>(p, &place), true);
+  const Place s(p, take_place<EACH>(p, &place), true);
   raw_t xr[TOK], dyr[TOK];
   uint32_t first;
   fch ts[TOK];
@@ -370,7 +384,7 @@ __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p) 
     });
   }
   __syncthreads();
-  fch mu = chunk_start<ONE, true>(p, s, Ab, Bb, &looks, p.dlast, p.dh0);
+  fch mu = chunk_start<EACH, true>(p, s, Ab, Bb, &looks, p.dlast, p.dh0);
   h = enter<false>(As, Bs, s, h);
   mu = enter<true>(Ab, Bb, s, mu);
   forget(xr);
@@ -416,23 +430,24 @@ __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p) 
       dg.store(i, PLAIN || live ? pack(gg) : 0u);
       }
   });
-  if (ONE && p.dh0 && s.w == 0 && s.in) *reinterpret_cast<fch*>(p.dh0 + (long)s.b * p.c + s.ch) = mu;
+  if (EACH == 0 && p.dh0 && s.w == 0 && s.in) *reinterpret_cast<fch*>(p.dh0 + (long)s.b * p.c + s.ch) = mu;
 }
 
 int chunks_of(int seq) { return (seq + CHUNK - 1) / CHUNK; }
 // The counter, and a word for every channel of every chunk.
 size_t scratch_bytes(int batch, int chunks, int c) { return chunks > 1 ? 16 + 8 * (size_t)batch * chunks * c : 0; }
 
-template <int W>
+template <int W, int EACH>
 void enqueue(hipStream_t st, const ScanArgs& p, bool back) {
   const dim3 grid((unsigned)p.batch * p.chunks * p.blocks), block(64 * NW);
-  if (back) {
-    if (p.chunks == 1) RP_LAUNCH((scan_bwd_kernel<W, true>), grid, block, 0, st, p);
-    else RP_LAUNCH((scan_bwd_kernel<W, false>), grid, block, 0, st, p);
-  } else {
-    if (p.chunks == 1) RP_LAUNCH((scan_fwd_kernel<W, true>), grid, block, 0, st, p);
-    else RP_LAUNCH((scan_fwd_kernel<W, false>), grid, block, 0, st, p);
-  }
+  if (back) RP_LAUNCH((scan_bwd_kernel<W, EACH>), grid, block, 0, st, p);
+  else RP_LAUNCH((scan_fwd_kernel<W, EACH>), grid, block, 0, st, p);
+}
+template <int W>
+void enqueue(hipStream_t st, const ScanArgs& p, bool back) {
+  if (p.chunks == 1) enqueue<W, 0>(st, p, back);
+  else if (p.chunks > NW && (long)p.batch * p.chunks * p.blocks <= 512) enqueue<W, 4>(st, p, back);      // (two workgroups a CU)
+  else enqueue<W, 1>(st, p, back);
 }
 
 hipError_t run(hipStream_t st, int weight, ScanArgs p, void* scratch, bool back) {

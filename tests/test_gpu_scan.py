@@ -92,6 +92,12 @@ def test_forward_and_backward(B, weight, b, n, c):
     Case(weight, b, n, c).run(B).check()
 
 
+@pytest.mark.parametrize("b,n,c,docs", [(3, 1200, 2304, True), (1, 1153, 7304, False), (2, 4500, 136, True), (1, 9001, 8, False)])
+def test_many_chunks(B, b, n, c, docs):
+    """More chunks a sequence than are looked at at once, with workgroups for more than one round, and with few."""
+    Case(2, b, n, c, docs=docs).run(B).check()
+
+
 @pytest.mark.parametrize("weight", [0, 1, 2])
 def test_documents_lengths_and_strides(B, weight):
     Case(weight, 2, 500, 136, docs=True, state=False).run(B).check()
