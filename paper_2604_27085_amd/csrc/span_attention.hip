@@ -1200,13 +1200,15 @@ constexpr int MOST_TILES = 2048;
 // at its edge).  A key tile with the end of one document and the beginning of a long one is masked all along: without counting that, the piece with it lasted 14 % longer than the others.
 constexpr int FRONT = 4;
 RP_DEV int edge_pairs(int part) { return FRONT + (3 * part + 4) / 8; }
-// The row tiles of a key tile, of `rows` in `pairs`, that come before pair `pair` of it.  At most one a pair: the last pair has the last row tile, and eight have four or more.
+// The row tiles of a key tile, of `rows` in `pairs`, that come before pair `pair` of it.  At most one a pair: the last pair has the last row tile, and four behind the front have two or more.
 RP_DEV int rows_before(int pair, int rows, int pairs) {
   return pair <= FRONT ? 0 : pair >= pairs ? rows : (int)((unsigned long long)(pair - FRONT) * rows / (pairs - FRONT));
 }
 // The first pair that has a row tile (rows > 0).
 RP_DEV int first_pair(int rows, int pairs) { return FRONT + (pairs - FRONT - 1) / rows; }
-RP_DEV int piece_length(int pairs, int parts) { return max((pairs + parts - 1) / parts, 8); }      // (one may hold nothing but a part of a front)
+// (No shorter than what a piece costs by itself; it may hold nothing but a part of a front.  788 tokens, 6 heads of 128 in groups of 3, a window of 43: with eight pairs at least 26 us, with
+// four 20.)
+RP_DEV int piece_length(int pairs, int parts) { return max((pairs + parts - 1) / parts, FRONT); }
 
 // ranges[i]: of key tile i % KT of sequence i / KT
 __global__ void __launch_bounds__(256) span_range_kernel(const SpanArgs p) {
