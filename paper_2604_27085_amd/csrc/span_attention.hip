@@ -17,7 +17,7 @@
 // reach the rows beside them: a document is not touched by what is in another.  (Forward: a row that does see such a value of v becomes NaN as a whole.  Backward: lse and
 // delta of such rows are NaN by then.)
 //
-// P (for P v and dV) and dS are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most; dS of up to 512 keys in two parts, 2^-16); scores, statistics, dP - delta and every sum are
+// P (for P v and dV) and dS are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most; dS in small calls in two parts, 2^-16); scores, statistics, dP - delta and every sum are
 // fp32.  The forward divides by the sum of the rounded P: what all terms of a row were rounded by alike drops out, and where a row lies on one key o is that key's v.  o goes out in two
 // parts, its bf16 and that of what the rounding left over, so that delta = dO.(o + rest) does not carry o's rounding, which would be as large as dP - delta in such rows.
 //
@@ -167,11 +167,11 @@ RP_DEV float sum2(uint32_t pair, float acc) {      // the two bf16 of a register
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2, pair), __builtin_bit_cast(v2, 0x3f803f80u), acc, false);
 }
 
-// dS of up to FEW_KEYS keys goes to the products in two parts, its bf16 and that of what the rounding left over: dQ and dK are then off by their own rounding alone.  In one part the two are
-// 1.45 times as far from the exact result as that rounding is, and where few keys share a row, chance makes it up to 1.56 (relative 2-norm, 10^-3: 2.4 to 2.5 | 2.6, in two 1.7).  The products
-// more cost little there (200 tokens, 16 heads of 128: dQ 13.8 -> 14.3 us, dK, dV 19.0 -> 19.3; 512 tokens, 32 heads: 22 -> 25 and 29 -> 32); beyond, both would take a fifth longer
-// (8192 causal tokens, 32 heads of 128: 718 -> 882 and 1087 -> 1306).
-constexpr int FEW_KEYS = 512;
+// dS of up to FEW_KEYS keys, in calls of up to FEW_ROWS rows of all heads, goes to the products in two parts, its bf16 and that of what the rounding left over: dQ and dK are
+// then off by their own rounding alone.  In one part the two are 1.45 times as far from the exact result as that rounding is, and where few rows see few keys, chance makes it up to
+// 1.56 (relative 2-norm, 10^-3: 2.4 to 2.5 | 2.6, in two 1.7).  The products more cost little there (200 tokens, 16 heads of 128: dQ 13.8 -> 14.3 us, dK, dV 19.0 -> 19.3; 512
+// tokens, 32 heads: 22 -> 25 and 29 -> 32); beyond, both would take a fifth longer (8192 causal tokens, 32 heads of 128: 718 -> 882 and 1087 -> 1306).
+constexpr int FEW_KEYS = 512, FEW_ROWS = 16384;
 template <bool TWO>
 struct Parts {
   uint4 hi[2], lo[2];      // of the column tiles
@@ -1844,7 +1844,7 @@ hipError_t bwd_parts(hipStream_t st, SpanArgs p, void* scratch, size_t bytes) {
 
 template <int D, bool CAP, bool BIAS>
 hipError_t bwd(hipStream_t st, const SpanArgs& p, void* scratch, size_t bytes) {
-  return p.seq_kv <= FEW_KEYS ? bwd_parts<D, CAP, BIAS, true>(st, p, scratch, bytes) : bwd_parts<D, CAP, BIAS, false>(st, p, scratch, bytes);
+  return p.seq_kv <= FEW_KEYS && (long)p.batch * p.a * p.seq_q <= FEW_ROWS ? bwd_parts<D, CAP, BIAS, true>(st, p, scratch, bytes) : bwd_parts<D, CAP, BIAS, false>(st, p, scratch, bytes);
 }
 
 // One of eight: d, cap, bias.
