@@ -137,6 +137,16 @@ struct Score {
 RP_DEV float cap_r(float z, const Score& c) { return __builtin_amdgcn_rcpf(1.f + fast_exp2(z * c.k1)); }
 template <bool CAP>
 RP_DEV float score2(float z, const Score& c) { return CAP ? __builtin_fmaf(-2.f * c.k2, cap_r(z, c), c.k2) : z * c.k1; }
+// The same to 2^-22 of itself, for lse of a few keys, which may be small: tanh(u) of small u by its series (the next term is below 2^-26 there).  Where vector instructions do not count.
+RP_DEV float fine_capped2(float z, const Score& c) {
+  const float u = z * (c.k1 * 0.34657359027997264f), v = u * u;
+  float t = __builtin_fmaf(v, -1382.f / 155925.f, 62.f / 2835.f);
+  t = __builtin_fmaf(v, t, -17.f / 315.f);
+  t = __builtin_fmaf(v, t, 2.f / 15.f);
+  t = __builtin_fmaf(v, t, -1.f / 3.f);
+  t = __builtin_fmaf(v * u, t, u);
+  return fabsf(u) < 0.35f ? c.k2 * t : score2<true>(z, c);
+}
 
 // 16 bytes with infinities and NaN made zero; `bad` where there was one.
 RP_DEV uint32_t finite2(uint32_t u, bool& bad) {
@@ -574,7 +584,7 @@ __global__ void __launch_bounds__(64 * NW) span_step_kernel(const SpanArgs p) {
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float x = score2<CAP>(sT[kt][c][e], sc);
+          float x = CAP ? fine_capped2(sT[kt][c][e], sc) : score2<false>(sT[kt][c][e], sc);
           if (BIAS) x = __builtin_fmaf(-slope2[c], fabsf(from - (float)(16 * kt + e)), x);
           sT[kt][c][e] = x;
         }
