@@ -26,7 +26,7 @@
 //   forward  docs 1030 us 48 %, 50 %, 17 %;  window 70 us 26 %, 58 %, 19 %;  prefix 37 us 17 %, 76 %, 26 %
 //   dQ       docs 1265 us 55 %, 43 %, 20 %;  window 82 us 29 %, 48 %, 34 %;  prefix 38 us 21 %, 55 %, 40 %
 //   dK, dV   docs 1995 us 46 %, 33 %, 24 %;  window 116 us 29 %, 41 %, 28 %;  prefix 57 us 23 %, 45 %, 32 %
-// docs: the exponentials and conversions beside the products, and the clock that the matrix pipe's power leaves (2.0 to 2.3 GHz; 8192 causal tokens take 570, 705 and 1015 us, 590 to 660 TFLOP/s);
+// docs: the exponentials and conversions beside the products, and the clock that the matrix pipe's power leaves (2.0 to 2.3 GHz; 8192 causal tokens take 570, 705 and 1015 us, 960, 1170 and 1080 TFLOP/s of their products);
 // window: the same with the tangent's exponential and quotient, and masks in an eighth of the tiles; prefix: 5 to 9 tiles a workgroup, most of them masked, between launches of a round or two.
 #include <type_traits>
 
