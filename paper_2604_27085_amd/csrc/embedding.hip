@@ -8,7 +8,7 @@
 // numbers within them: however often a token comes, the work is spread evenly, and no sum depends on timing.  A run that goes on into the next chunk leaves its part in scratch; a second
 // kernel adds those up in order.  Sums are fp32.
 //
-// What bounds it: memory.  16384 tokens of 4096 from 151936 rows: rows 49 us (5.5 TB/s), sort 24, sums 75, join 9, and 405 for the zeros of the rows without tokens (2.4 GB at 5.9 TB/s).
+// What bounds it: memory.  16384 tokens of 4096 from 151936 rows: rows 49 us (5.5 TB/s), sort 24, sums 75, join 9, and 388 for the zeros of the rows without tokens (2.4 GB at 6.1 TB/s).
 // 4084 tokens of 2880, gradient added to what is there: rows 10, sort 11, sums 17, join 6: three launches that wait for one another.
 #include "pack_ops.hpp"
 
