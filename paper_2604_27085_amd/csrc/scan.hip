@@ -182,14 +182,14 @@ RP_DEV word_t look(const word_t* at) { return __hip_atomic_load(const_cast<word_
 // LDS, and all of them go from the nearest end state through the maps behind it.  Where none of those chunks has its end state yet, they look again.  EACH is 4 where all of a launch's
 // workgroups are on the chip at once, and the chain of looks is what takes the time (18467 tokens of 72 channels: forward 41 -> 29 us, backward 44 -> 32), else 1 (16384 tokens of 4096:
 // 108 and 147 us, with 4 118 and 158).
-// `given`: the state before the first chunk (behind the last one, BACK); end: wave 0's, the chunk's own end state.
+// `given`: the state before the first chunk (behind the last one, BACK), in LDS; end: wave 0's, the chunk's own end state.
 template <int EACH>
 struct Looks {
   fch a[EACH * NW][64], b[EACH * NW][64];
   int state[EACH * NW];
 };
 template <int EACH, bool BACK>
-RP_DEV fch start_of(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], const fch (&Bs)[NW][64], Looks<EACH>& looks, const fch& given, fch& end) {
+RP_DEV fch start_of(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], const fch (&Bs)[NW][64], Looks<EACH>& looks, const fch (&given)[64], fch& end) {
   const int before = BACK ? p.chunks - 1 - s.chunk : s.chunk;
   word_t* const mine = p.words + (s.in ? s.at(p) : 0);
   fch A = As[BACK ? NW - 1 : 0][s.lane], B = Bs[BACK ? NW - 1 : 0][s.lane];
@@ -208,7 +208,7 @@ RP_DEV fch start_of(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], 
 #pragma unroll
       for (int e = 0; e < LANES; ++e) publish(mine + e, map_word(A[e], B[e]));
   }
-  fch h = given;
+  fch h = given[s.lane];
   if (before > 0) {      // uniform over the workgroup
     int from;
     for (;;) {
@@ -302,16 +302,22 @@ RP_DEV int take_place(const ScanArgs& p, int* lds) {
   __syncthreads();
   return __builtin_amdgcn_readfirstlane(*lds);
 }
-RP_DEV fch given_state(const float* src, const ScanArgs& p, const Place& s) {
-  return src && s.in ? *reinterpret_cast<const fch*>(src + (long)s.b * p.c + s.ch) : fch{0.f, 0.f};
+// The call's own state goes to LDS, before the barrier behind the waves' maps: it is read by the first chunk's wave 0 alone (the last chunk's, BACK), and once that barrier is passed it
+// is not read again, so that whoever is told of this chunk's end may write the state in its place (`last` may be h0).
+template <bool BACK>
+RP_DEV void keep_given(const float* src, const ScanArgs& p, const Place& s, fch (&given)[64]) {
+  if (s.w != 0) return;      // uniform
+  fch h = {0.f, 0.f};
+  if (src && s.in && s.chunk == (BACK ? p.chunks - 1 : 0)) h = *reinterpret_cast<const fch*>(src + (long)s.b * p.c + s.ch);
+  given[s.lane] = h;
 }
-// What the chunk starts from; the waves have put their maps into LDS.  The state behind the last chunk goes to `last`.
+// What the chunk starts from; the waves have put their maps into LDS, wave 0 the call's own state.  The state behind the last chunk goes to `last`.
 template <int EACH, bool BACK>
-RP_DEV fch chunk_start(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], const fch (&Bs)[NW][64], Looks<EACH ? EACH : 1>* looks, const float* given, float* last) {
-  fch h = given_state(given, p, s);
+RP_DEV fch chunk_start(const ScanArgs& p, const Place& s, const fch (&As)[NW][64], const fch (&Bs)[NW][64], Looks<EACH ? EACH : 1>* looks, const fch (&given)[64], float* last) {
+  fch h = given[s.lane];
   if constexpr (EACH > 0) {
     fch end;
-    h = start_of<EACH, BACK>(p, s, As, Bs, *looks, h, end);
+    h = start_of<EACH, BACK>(p, s, As, Bs, *looks, given, end);
     if (last && s.w == 0 && s.in && s.chunk == (BACK ? 0 : p.chunks - 1)) *reinterpret_cast<fch*>(last + (long)s.b * p.c + s.ch) = end;
   }
   return h;
@@ -319,10 +325,11 @@ RP_DEV fch chunk_start(const ScanArgs& p, const Place& s, const fch (&As)[NW][64
 
 template <int W, int EACH>
 __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p) {
-  __shared__ fch As[NW][64], Bs[NW][64];
+  __shared__ fch As[NW][64], Bs[NW][64], given[64];
   __shared__ Looks<EACH ? EACH : 1> looks;
   __shared__ int place;
   const Place s(p, take_place<EACH>(p, &place), false);
+  keep_given<false>(p.h0, p, s, given);
   raw_t gr[TOK], xr[TOK];
   TokenRows(p.g, p.ldg, s, p, s.len).load(gr);
   TokenRows(p.x, p.ldx, s, p, s.len).load(xr);
@@ -335,7 +342,7 @@ __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p) {
     Bs[s.w][s.lane] = B;
   }
   __syncthreads();
-  const fch start = chunk_start<EACH, false>(p, s, As, Bs, &looks, p.h0, p.last);
+  const fch start = chunk_start<EACH, false>(p, s, As, Bs, &looks, given, p.last);
   fch h = enter<false>(As, Bs, s, start);
   if (s.in && s.w == 0 && p.states && p.seq > 0) *reinterpret_cast<fch*>(p.states + s.at(p)) = start;
   const TokenRows out(p.y, p.ldy, s, p, p.seq);
@@ -357,10 +364,11 @@ __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p) {
 
 template <int W, int EACH>
 __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p) {
-  __shared__ fch As[NW][64], Bs[NW][64], Ab[NW][64], Bb[NW][64];
+  __shared__ fch As[NW][64], Bs[NW][64], Ab[NW][64], Bb[NW][64], given[64];
   __shared__ Looks<EACH ? EACH : 1> looks;
   __shared__ int place;
   const Place s(p, take_place<EACH>(p, &place), true);
+  keep_given<true>(p.dlast, p, s, given);
   raw_t xr[TOK], dyr[TOK];
   uint32_t first;
   fch ts[TOK];
@@ -384,7 +392,7 @@ __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p) 
     });
   }
   __syncthreads();
-  fch mu = chunk_start<EACH, true>(p, s, Ab, Bb, &looks, p.dlast, p.dh0);
+  fch mu = chunk_start<EACH, true>(p, s, Ab, Bb, &looks, given, p.dh0);
   h = enter<false>(As, Bs, s, h);
   mu = enter<true>(Ab, Bb, s, mu);
   forget(xr);
