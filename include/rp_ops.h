@@ -217,7 +217,8 @@ RP_API rp_status rp_op_span_attn_bwd(void* stream, const void* q, const void* k,
 /* Gated linear recurrence, every channel by itself:  h_t = f_t h_(t-1) + w(f_t) x_t,  f_t = sigmoid(g_t),  y_t = h_t.
  * x, g, y bf16 [batch * seq, c], c a multiple of 8, row strides ld* in elements.  h0, last fp32 [batch, c] or NULL: the state before the first token (else 0) and
  * behind the last (last may be h0: the step of a generation).  first [dev] uint8 [batch * seq] or NULL: where not 0 a document begins, and the state before counts for
- * nothing.  len [dev] int32 [batch] or NULL: how many tokens of a padded sequence are in use; y behind them becomes 0, last is the state at their end.
+ * nothing.  len [dev] int32 [batch] or NULL: how many tokens of a padded sequence are in use; y behind them becomes 0, last is the state at their end.  Infinities and NaN stay in their
+ * channel to the end of their document, and their gradients' to its beginning, however small the gates are.
  * states [dev] or NULL: for the backward call, state_bytes of rp_op_scan_sizes.  scratch [dev, scratch_bytes]: a call of its own each. */
 enum { RP_SCAN_PLAIN = 0, RP_SCAN_MEAN = 1, RP_SCAN_ENERGY = 2 };      /* w: 1, 1 - f, sqrt(1 - f^2) */
 RP_API rp_status rp_op_scan_sizes(int batch, int seq, int c, size_t* state_bytes, size_t* scratch_bytes);
