@@ -198,7 +198,8 @@ RP_API rp_status rp_op_pack_plan(void* stream, const int* starts, const int* pre
  *   or t + seq_kv - seq_q where q_pos is NULL;  lse = log sum exp s;  o = sum exp(s - lse) v.
  * scale 1e-30 to 1e30.  lse fp32 [batch, a, seq_q] (natural log), or NULL.  A query that sees nothing has o = 0, lse = -inf, and gives and gets no gradient.  What a
  * query does not see does not reach it, also where it is infinite or NaN; a key that it sees with an infinity or NaN in v makes its whole row NaN where only some
- * queries near it see that key.
+ * queries near it see that key.  Backward: such values show as the formulas have it, and where only some queries near see a key, one in k makes all of dq NaN in the rows that see
+ * that key, and one in q or dout all of dk and dv of the keys that its row sees.
  * o_rest bf16, laid out as o, or NULL: what o's rounding left over (o + o_rest is good to 2^-16).  The backward call makes sum_j P dP from both; without it that is as exact as o.
  * scratch [dev, scratch_bytes]: the forward call cuts the keys of few rows into as many slices as it allows, and does without (NULL); the backward call needs the
  * smaller number, least_bytes, and cuts with more.  It holds nothing between calls; two calls that may run at the same time need one each.  No output may

@@ -14,8 +14,8 @@
 // scratch; no atomics, so the result does not depend on timing).
 //
 // In a tile that some rows do not see, scores are replaced, and what the products sum over (V; K of dQ; Q and dO) has its infinities and NaN taken out, since 0 times those would
-// reach the rows beside them: a document is not touched by what is in another.  (Forward: a row that does see such a value of v becomes NaN as a whole.  Backward: lse and
-// delta of such rows are NaN by then.)
+// reach the rows beside them: a document is not touched by what is in another.  What does see such a value is made NaN as a whole: the row of o that sees it in v, the row of dQ that sees it in
+// k, and dK, dV of the keys that a row with it in q or dO sees (marked a bit a key, or a row, in LDS: lse and delta need not show it).
 //
 // P (for P v and dV) and dS are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most; dS in small calls in two parts, 2^-16); scores, statistics, dP - delta and every sum are
 // fp32.  The forward divides by the sum of the rounded P: what all terms of a row were rounded by alike drops out, and where a row lies on one key o is that key's v.  o goes out in two
@@ -41,8 +41,8 @@ constexpr int fwd_tile_bytes(int d) { return max_i(64 * (d + 8) + 64 * (d + 32),
 constexpr int dq_tile_bytes(int d) { return max_i(2 * 64 * tile_ld(d), 128 * (d + 8)) * 2; }
 
 constexpr int step_smem_bytes(int d, int nc, int nw) { return nw * max_i(32 * tile_ld(d) * 2, 16 * nc * (3 + d + 4) * 4); }
-constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 6 * 64 * 4, 4 * 32 * (d + 4) * 4); }
-constexpr int dkv_pair_smem_bytes(int d, bool two) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * (two ? 6 : 4) * 64 * 16 + 2 * 6 * 64 * 4; }
+constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 6 * 64 * 4 + 16, 4 * 32 * (d + 4) * 4); }
+constexpr int dkv_pair_smem_bytes(int d, bool two) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * (two ? 6 : 4) * 64 * 16 + 2 * 6 * 64 * 4 + 16; }
 constexpr float LOG2E = 1.4426950408889634f;
 
 // Sizes of one sequence and key head.
@@ -149,28 +149,39 @@ RP_DEV float fine_capped2(float z, const Score& c) {
   return fabsf(u) < 0.35f ? c.k2 * t : score2<true>(z, c);
 }
 
-// 16 bytes with infinities and NaN made zero; `bad` where there was one.
-RP_DEV uint32_t finite2(uint32_t u, bool& bad) {
-  const bool lo = (u & 0x7f80u) == 0x7f80u, hi = (u & 0x7f800000u) == 0x7f800000u;
-  bad = bad || lo || hi;
-  return (lo ? 0u : u & 0xffffu) | (hi ? 0u : u & 0xffff0000u);
+// 16 bytes with infinities and NaN made zero.
+RP_DEV uint32_t finite2(uint32_t u) {
+  return ((u & 0x7f80u) == 0x7f80u ? 0u : u & 0xffffu) | ((u & 0x7f800000u) == 0x7f800000u ? 0u : u & 0xffff0000u);
 }
-RP_DEV uint4 finite8(const uint4& u, bool& bad) { return make_uint4(finite2(u.x, bad), finite2(u.y, bad), finite2(u.z, bad), finite2(u.w, bad)); }
-// Whether any lane of the wave has one: three instructions for two values.  (An exponent of all ones carries into the bit above.)
+RP_DEV uint4 finite8(const uint4& u) { return make_uint4(finite2(u.x), finite2(u.y), finite2(u.z), finite2(u.w)); }
+// Whether there are any: three instructions for two values.  (An exponent of all ones carries into the bit above.)
 RP_DEV uint32_t carries(uint32_t u) { return (u & 0x7f807f80u) + 0x00800080u; }
+RP_DEV uint32_t carries(const uint4& u) { return carries(u.x) | carries(u.y) | carries(u.z) | carries(u.w); }
+RP_DEV bool not_finite(uint32_t carried) { return (carried & 0x80008000u) != 0u; }
+// In any lane of the wave.
 template <int N>
 RP_DEV bool any_not_finite(const uint4 (&r)[N]) {
   uint32_t c = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) c |= carries(r[i].x) | carries(r[i].y) | carries(r[i].z) | carries(r[i].w);
-  return __any((c & 0x80008000u) != 0u);
+  for (int i = 0; i < N; ++i) c |= carries(r[i]);
+  return __any(not_finite(c));
 }
-template <int N>
-RP_DEV void make_finite(uint4 (&r)[N]) {
+// What is made of x in a branch that is hardly ever taken is made there, not before a loop and kept in registers.
+RP_DEV int found_here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+// A thread's pieces of a 64-row tile (NT threads, CH pieces a row): infinities and NaN made zero, and the rows that had any marked in LDS [2], a bit a row.
+template <int CH, int NT, int N>
+RP_DEV void make_finite(uint4 (&r)[N], unsigned* marks, int tid) {
   if (!any_not_finite(r)) return;
-  bool bad = false;
+  const int t = found_here(tid);
 #pragma unroll
-  for (int i = 0; i < N; ++i) r[i] = finite8(r[i], bad);
+  for (int i = 0; i < N; ++i) {
+    const int row = (i * NT + t) / CH;
+    if (not_finite(carries(r[i]))) atomicOr(marks + (row >> 5), 1u << (row & 31));
+    r[i] = finite8(r[i]);
+  }
 }
 
 RP_DEV float sum2(uint32_t pair, float acc) {      // the two bf16 of a register, added up in fp32
@@ -200,6 +211,24 @@ struct Parts {
   RP_DEV f32x4 times(const uint4& a, int c, f32x4 acc) const {
     if (TWO) acc = mfma16(a, lo[c], acc);
     return mfma16(a, hi[c], acc);
+  }
+};
+
+// The marks of the present tile, the same in all lanes: asked for behind the barrier that they are complete at, in tiles that make use of them, and taken where the next tile's loads are on their way.
+// Two tiles take turns with the two words of LDS; what a tile has left there the next one clears.  (Read where the masks are applied: 2 x 1021 tokens, 64 heads of 64, prefixes 134.4 us instead of
+// 132.1, and 131.0 without marks; a window of 4096 256.7, 256.0, 254.2.)
+struct Marks {
+  unsigned half[2];
+  uint2 word;
+  RP_DEV void none() { half[0] = half[1] = 0u; }
+  RP_DEV void ask(bool whole, unsigned* lds, int parity, int tid) {
+    if ((half[0] | half[1]) && tid < 2) lds[2 * (parity ^ 1) + tid] = 0u;      // (of the tile before: last read before the barriers above, next written behind the next one)
+    word = make_uint2(0u, 0u);
+    if (!whole) word = *reinterpret_cast<const uint2*>(lds + 2 * parity);
+  }
+  RP_DEV void take() {
+    half[0] = __builtin_amdgcn_readfirstlane(word.x);
+    half[1] = __builtin_amdgcn_readfirstlane(word.y);
   }
 };
 
@@ -289,15 +318,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_fwd_kernel(const Sp
     const int kv0 = j * 64;
     const bool whole = block.all(kv0, kv0 + 64);      // uniform over the workgroup
     __syncthreads();
-    if (!whole && any_not_finite(vreg)) {
-#pragma unroll
-      for (int it = 0; it < T64::NREG; ++it) {
-        bool bad = false;
-        vreg[it] = finite8(vreg[it], bad);
-        const int key = (it * NT + tid) / CH;
-        if (bad) atomicOr(bad_keys + 2 * (j & 1) + (key >> 5), 1u << (key & 31));
-      }
-    }
+    if (!whole) make_finite<CH, NT>(vreg, bad_keys + 2 * (j & 1), tid);
     T64::template store<LDK>(kreg, Ks, tid);
     T64::template store<LDV>(vreg, Vs, tid);
     __syncthreads();
@@ -561,9 +582,8 @@ __global__ void __launch_bounds__(64 * NW) span_step_kernel(const SpanArgs p) {
       unsigned mine = 0u;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        bool bad = false;
-        vreg[i] = finite8(vreg[i], bad);
-        mine |= bad ? 1u << i : 0u;
+        mine |= not_finite(carries(vreg[i])) ? 1u << i : 0u;
+        vreg[i] = finite8(vreg[i]);
       }
 #pragma unroll 1
       for (int i = 0; i < 32; ++i)      // key i is in the CH lanes from CH i % 64 on, their piece CH i / 64
@@ -777,6 +797,7 @@ __global__ void __launch_bounds__(256, D == 64 && !TWO && !(CAP && BIAS) ? 3 : 2
   bf16* const Ks = smem;
   bf16* const Vs = smem + 64 * LD;
   int4* const seen_lds = reinterpret_cast<int4*>(dyn_smem + dq_tile_bytes(D));       // [4]
+  unsigned* const bad_keys = reinterpret_cast<unsigned*>(seen_lds + 4);              // [2 tiles][2]: a bit a key
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -820,6 +841,7 @@ __global__ void __launch_bounds__(256, D == 64 && !TWO && !(CAP && BIAS) ? 3 : 2
     else mine.add(v.lo, v.hi, v.all_lo, v.all_hi);
   }
   mine.lanes(1, 16);
+  if (tid < 4) bad_keys[tid] = 0u;
   const Seen block = seen_by_all(mine, seen_lds, w, lane);
   // what dK, dV have to know of the two tiles of 64 rows
   if (s.g == 0 && split == 0 && (tid & 127) == 0 && r0 + 32 * w < s.total) {
@@ -881,14 +903,18 @@ __global__ void __launch_bounds__(256, D == 64 && !TWO && !(CAP && BIAS) ? 3 : 2
   f32x4 dqacc[DT][2];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dqacc[dt][0] = dqacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  Marks bad;
+  bad.none();
   for (int j = j0; j < j1; ++j) {
     const bool whole = block.all(j * 64, j * 64 + 64);      // uniform over the workgroup
     __syncthreads();
-    if (!whole) make_finite(kreg);
+    if (!whole) make_finite<D / 8, NT>(kreg, bad_keys + 2 * (j & 1), tid);
     T64::template store<LD>(kreg, Ks, tid);
     T64::template store<LD>(vreg, Vs, tid);
     __syncthreads();
+    bad.ask(whole, bad_keys, j & 1, tid);
     if (j + 1 < j1) load_tiles(j + 1);
+    bad.take();
     // the two 32-key halves of the tile one after the other: half as many score registers live at a time
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2) {
@@ -932,6 +958,15 @@ __global__ void __launch_bounds__(256, D == 64 && !TWO && !(CAP && BIAS) ? 3 : 2
       }
       if (!whole) {
         stay_in_branch();
+        if (bad.half[k2]) {
+          const unsigned mine4 = bad.half[k2] >> found_here(4 * lg);
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sT[kt][c][e] = mine4 >> (16 * kt + e) & 1u ? NAN : sT[kt][c][e];
+        }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const int lo = span[c].x - (k0 + 4 * lg);
@@ -1046,7 +1081,7 @@ RP_DEV int lane_now() {
 }
 
 // What there is to know of the rows of a 64-row tile, a row per lane of waves 0 to 3, in LDS as six arrays of 64: what the score starts from, -delta, first key,
-// key behind the last, position from the tile's first key, slope.  Rows that see nothing, and rows behind the last: P = exp(-inf) = 0.
+// key behind the last, position from the tile's first key, slope.  Rows behind the last one: P = exp(-inf) = 0.  Rows that see nothing are masked.
 // load() only issues loads, and store(), a tile later, works on what came: whatever it did to them at once would have these waves, and at the next barrier all others, wait for
 // the tile's rows too, whose loads are in flight before them (8192 causal tokens, 32 heads of 128: dK, dV 1250 us instead of 1170).
 template <bool CAP, bool BIAS>
@@ -1081,7 +1116,7 @@ struct RowStat {
   }
   RP_DEV void store(float* lds, const SpanArgs& p, int kv0, int lane, int w) const {
     const float f = __int_as_float(x);
-    if (w == 0) lds[lane] = lane >= left || f == -INFINITY ? -INFINITY : CAP ? __builtin_fmaf(f, start_mul, p.cap * LOG2E) : f * start_mul;
+    if (w == 0) lds[lane] = lane >= left ? -INFINITY : CAP ? __builtin_fmaf(f, start_mul, p.cap * LOG2E) : f * start_mul;
     if (w == 1) lds[64 + lane] = lane < left ? -f : 0.f;
     if (w == 2) lds[128 + lane] = __int_as_float(max(x, 0));
     if (w == 3) lds[192 + lane] = __int_as_float(lane < left ? min(x, p.seq_kv) : 0);
@@ -1090,9 +1125,10 @@ struct RowStat {
   }
 };
 
-// P and dS of 2 x 16 rows by 2 x 16 keys, in place of the scores and dP - delta.  lds: RowStat's, from the first of the rows on; key: the lane's first key, from kv0.
+// P and dS of 2 x 16 rows by 2 x 16 keys, in place of the scores and dP - delta.  lds: RowStat's, from the first of the rows on; bad: those of them (a bit each) whose q or dO is
+// not finite, where some rows do not see all keys; key: the lane's first key, from kv0.
 template <bool CAP, bool BIAS>
-RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, const float* lds, int lg, int key, int kv0, bool whole) {
+RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, const float* lds, unsigned bad, int lg, int key, int kv0, bool whole) {
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
     const float* const at = lds + 16 * qt + 4 * lg;
@@ -1117,6 +1153,16 @@ RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, c
   }
   if (!whole) {
     stay_in_branch();
+    if (bad) {
+      const unsigned mine4 = bad >> found_here(4 * lg);
+#pragma unroll
+      for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            if (mine4 >> (16 * qt + e) & 1u) s[qt][t][e] = dp[qt][t][e] = NAN;
+    }
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
       const int4 lo = *reinterpret_cast<const int4*>(lds + 128 + 16 * qt + 4 * lg), hi = *reinterpret_cast<const int4*>(lds + 192 + 16 * qt + 4 * lg);
@@ -1338,6 +1384,7 @@ __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
   bf16* const Qs = smem;
   bf16* const dOs = smem + 64 * LD;
   float* const stat = reinterpret_cast<float*>(smem + 2 * 64 * LD);
+  unsigned* const bad_rows = reinterpret_cast<unsigned*>(stat + Stat::FLOATS);      // [2 tiles][2]: a bit a row
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1410,20 +1457,25 @@ __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
     prefetch(range.u);
     range.look(lane);
   }
+  if (tid < 4) bad_rows[tid] = 0u;
+  Marks bad;
+  bad.none();
   wait_for_loads();
-  while (range.more()) {
+  for (int i = 0; range.more(); i ^= 1) {
     const bool whole = range.whole();
     __syncthreads();
     if (!whole) {
-      make_finite(qreg);
-      make_finite(doreg);
+      make_finite<D / 8, NT>(qreg, bad_rows + 2 * i, tid);
+      make_finite<D / 8, NT>(doreg, bad_rows + 2 * i, tid);
     }
     T64::template store<LD>(qreg, Qs, tid);
     T64::template store<LD>(doreg, dOs, tid);
     rstat.store(stat, p, kv0, lane, w);
     __syncthreads();
+    bad.ask(whole, bad_rows, i, tid);
     range.next(lane);
     if (range.more()) prefetch(range.u);
+    bad.take();
     // the two 32-row halves of the tile one after the other: half as many score registers live at a time
 #pragma unroll
     for (int t2 = 0; t2 < 2; ++t2) {
@@ -1459,7 +1511,7 @@ __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
       __builtin_amdgcn_sched_barrier(0);
-      probabilities<CAP, BIAS>(z, dp, sc, stat + 32 * t2, lg, 32 * w + lr, kv0, whole);
+      probabilities<CAP, BIAS>(z, dp, sc, stat + 32 * t2, bad.half[t2], lg, 32 * w + lr, kv0, whole);
       {
         const uint4 pfg[2] = {pack_frag(z[0][0], z[1][0]), pack_frag(z[0][1], z[1][1])};
         const Parts<TWO> dfg(dp);
@@ -1508,6 +1560,7 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
   constexpr int TSET = 2 * 64 * LD;
   uint4* const exch = reinterpret_cast<uint4*>(smem + 2 * TSET);    // [8 waves][NX fragments][64 lanes]
   float* const stat = reinterpret_cast<float*>(exch + 8 * NX * 64); // [2 sets]
+  unsigned* const bad_rows = reinterpret_cast<unsigned*>(stat + 2 * Stat::FLOATS);      // [2 tiles][2]: a bit a row
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1618,6 +1671,9 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
     prefetch(range.u);
     range.look(lane_now());
   }
+  if (tid < 4) bad_rows[tid] = 0u;
+  Marks bad;
+  bad.none();
   wait_for_loads();
   int i = 0;
   for (; range.more(); ++i) {
@@ -1626,16 +1682,18 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
     bf16* const q_set = smem + (i & 1) * TSET;
     float* const st_set = stat + (i & 1) * Stat::FLOATS;
     if (!whole) {
-      make_finite(qreg);
-      make_finite(doreg);
+      make_finite<D / 8, NT>(qreg, bad_rows + 2 * (i & 1), tid);
+      make_finite<D / 8, NT>(doreg, bad_rows + 2 * (i & 1), tid);
     }
     T64::template store<LD>(qreg, q_set, tid);
     T64::template store<LD>(doreg, q_set + 64 * LD, tid);
     rstat.store(st_set, p, kv0, lane_now(), w8);
     if (i > 0) partner_update(i - 1);
     __syncthreads();
+    bad.ask(whole, bad_rows, i & 1, tid);
     range.next(lane_now());
     if (range.more()) prefetch(range.u);
+    bad.take();
     f32x4 z[2][2], dp[2][2], z0[2], dp0[2];      // [16 rows][16 keys]; what they start from
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
@@ -1663,7 +1721,7 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
       }
       MFMA_PHASE_END();
     }
-    probabilities<CAP, BIAS>(z, dp, sc, st_set + 32 * h, lg, 32 * w + lr, kv0, whole);
+    probabilities<CAP, BIAS>(z, dp, sc, st_set + 32 * h, h ? bad.half[1] : bad.half[0], lg, 32 * w + lr, kv0, whole);
     const uint4 pfg[2] = {pack_frag(z[0][0], z[1][0]), pack_frag(z[0][1], z[1][1])};
     const Parts<TWO> dfg(dp);
     // the partner read last tile's fragments before the barrier above: the slots are free
@@ -1723,7 +1781,7 @@ __global__ void __launch_bounds__(256) span_key_join_kernel(const SpanArgs p) {
 }
 
 constexpr int fwd_smem_bytes(int d) { return fwd_tile_bytes(d) + 64 + 16; }
-constexpr int dq_smem_bytes(int d) { return dq_tile_bytes(d) + 64; }
+constexpr int dq_smem_bytes(int d) { return dq_tile_bytes(d) + 64 + 16; }
 
 long row_count(const SpanArgs& p) { return (long)(p.a / p.kh) * p.seq_q; }
 size_t row_part_bytes(const SpanArgs& p, int d) { return (size_t)p.kh * p.batch * row_count(p) * (d + 4) * 4; }      // o or dq, and (m, l, lt)
