@@ -434,8 +434,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_fwd_kernel(const Sp
   if constexpr (SPLIT) {
     const long at = ((long)split * nhb + hb) * s.total + row;
     if (live) {
-      if (lk == 0) p.part_ml[at] = make_float4(m_run, l_tot, lt_tot, 0.f);
-      if (j0 < j1)      // (of a slice without keys the sum is 0, and its part is not read)
+      if (lk == 0) p.part_ml[at] = make_float4(m_run, l_tot, lt_tot, j0 < j1 ? 1.f : 0.f);
+      if (j0 < j1)      // (else the slice has no keys, and its part is not read)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -705,8 +705,8 @@ __global__ void __launch_bounds__(64 * NW) span_step_kernel(const SpanArgs p) {
     }
     if constexpr (SPLIT) {
       const long at = ((long)split * nhb + hb) * s.total + row;
-      if (ch == 0) p.part_ml[at] = make_float4(m, l, lt, 0.f);
-      if (j0 < j1) {      // (of a slice without keys the sum is 0, and its part is not read)
+      if (ch == 0) p.part_ml[at] = make_float4(m, l, lt, j0 < j1 ? 1.f : 0.f);
+      if (j0 < j1) {      // (else the slice has no keys, and its part is not read)
         *reinterpret_cast<float4*>(p.part + at * D + 8 * ch) = make_float4(acc[0], acc[1], acc[2], acc[3]);
         *reinterpret_cast<float4*>(p.part + at * D + 8 * ch + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
       }
@@ -758,7 +758,7 @@ __global__ void __launch_bounds__(256) span_row_join_kernel(const SpanArgs p) {
       add_times(acc, p.part + (i * step + row) * D + ch * 8, 1.f);
     } else {
       const float4 ml = p.part_ml[i * step + row];
-      if (ml.y != 0.f) {      // the slice has keys that the row sees
+      if (ml.w != 0.f) {      // the slice has keys.  (Its weights may all be 0 and its part NaN all the same, of a v that is not finite.)
         const float wgt = fast_exp2(ml.x - m);
         acc[8] += wgt * ml.y;
         acc[9] += wgt * ml.z;

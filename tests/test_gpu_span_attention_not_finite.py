@@ -149,3 +149,23 @@ def test_a_query_whose_scores_are_all_minus_infinity(B, size, heads, kind):  # n
     assert bool(got["o"][0, lo + 1:hi].isfinite().all())
     for name in ("o", "dq", "dk", "dv"):
         assert bool(got[name][0, :lo].isfinite().all()) and bool(got[name][0, hi:].isfinite().all()), name
+
+
+@pytest.mark.parametrize("scratch", ["full", "least"])
+@pytest.mark.parametrize("bad", [INF, NAN])
+@pytest.mark.parametrize("kind,b,nq,nk,a,kh,d", [("all", 1, 1, 4096, 8, 8, 128), ("ragged", 2, 3, 3000, 8, 2, 64), ("all", 1, 150, 2048, 4, 4, 64), ("causal", 1, 150, 2500, 4, 4, 128)])
+def test_v_of_keys_without_weight(B, kind, b, nq, nk, a, kh, d, bad, scratch):  # noqa: F811
+    """0 times what is not finite, in a slice of the keys (or a call in one) that has no weight at all: NaN in o, and in what o is made of alone."""
+    c = Case(kind, b, nq, nk, a, kh, d)
+    c.q[:b * nq] = c.q[:b * nq].abs() + 0.5
+    c.k[:nk - 40, 3::d] = -INF      # the scores of all keys of the first sequence but its last 40 are -inf
+    want = {n: t.clone() for n, t in c.run(B, scratch, backward=False).got().items()}
+    some = c.span[0, :, 1] > nk - 40      # (a causal query may see none of those: -inf throughout, 0 / 0)
+    assert bool(some.any()) and bool(want["o"][0, some].isfinite().all()) and bool(want["lse"][0, :, some].isfinite().all()) and bool(want["o"][0, ~some].isnan().all())
+    c.v[77, d + 5] = bad            # (of key head 1)
+    got = c.run(B, scratch, backward=False).got()
+    assert torch.equal(got["lse"], want["lse"])
+    mine = list(range(a // kh, 2 * (a // kh)))
+    assert bool(got["o"][0, :, mine, 5].isnan().all())
+    others = [h for h in range(a) if h not in mine]
+    assert torch.equal(got["o"][0, some][:, others], want["o"][0, some][:, others]) and torch.equal(got["o"][1:], want["o"][1:])
