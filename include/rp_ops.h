@@ -183,9 +183,10 @@ RP_API rp_status rp_op_moe_balance(void* stream, const float* logits, const int*
 /* What the documents of packed rows make of every token.  The T tokens are rows of `seq`; starts [dev] int32 [n_docs + 1], not descending: document i is the
  * tokens starts[i] .. starts[i + 1] - 1 (an empty one has none); tokens before starts[0] and from starts[n_docs] on are padding.  A document that a row's
  * end cuts does not see beyond it.  Each output may be NULL.
- *   span [dev] int32 [T, 2]  the keys that the token sees, first and last + 1, counted from its row's first token (rp_op_span_attn_fwd): its document up to itself; the last
- *                            `window` of those where window > 0; and, where prefix [dev] int32 [n_docs] is given, its document's first prefix[i] tokens, which see one
- *                            another both ways.  Padding sees nothing.
+ *   span [dev] int32 [T, 2]  the keys that the token sees, first and last + 1, counted from its row's first token (rp_op_span_attn_fwd): its document up to itself, and, where prefix
+ *                            [dev] int32 [n_docs] is given, a token among its document's first prefix[i] sees to their end.  Where window > 0, none of them is before the last `window`
+ *                            tokens up to itself, in a prefix neither: with both, a token sees of the prefix before it only what the window reaches (a span is one run of keys, and cannot
+ *                            hold a prefix and a window apart from it).  Padding sees nothing.
  *   pos [dev] int32 [T]      place within the document (rp_op_rope); 0 for padding
  *   first [dev] uint8 [T]    1 where a document begins, and for padding (rp_op_scan_fwd) */
 RP_API rp_status rp_op_pack_plan(void* stream, const int* starts, const int* prefix, int n_docs, int window, int T, int seq, int* span, int* pos,
