@@ -462,7 +462,7 @@ struct Places {      // of the scratch memory
     sorted = 0;
     other = round16((size_t)T * 8);
     counts = other + (T > MID && s.passes > 1 ? round16((size_t)T * 8) : 0);
-    marks = counts + (T > MID ? (size_t)s.blocks * (4 << s.bits) : 0);
+    marks = counts + (T > MID ? round16((size_t)s.blocks * (4 << s.bits)) : 0);
     part = marks + round16((size_t)((V + 31) / 32) * 4);
     end = part + (size_t)2 * ceil_div(T, chunk_length(T)) * h * 4;
   }
