@@ -242,7 +242,7 @@ RP_API rp_status rp_op_embed_scratch(int T, int V, int h, size_t* scratch_bytes)
 RP_API rp_status rp_op_embed_bwd(void* stream, const void* dx, long lddx, const int* ids, float scale, float* dtable, long lddt, int accumulate, int T, int V,
                           int h, void* scratch, size_t scratch_bytes);
 
-/* Dropout onto a residual: y = res + x / share where an element stays, res where it does not (res NULL: 0).  x, res, y bf16 [T, n], n a multiple of 8, row strides ld* in
+/* Dropout onto a residual: y = res + x / share where an element stays, res where it does not (res NULL: 0).  x, res, y bf16 [T, n], n a multiple of 8, T n at most 2^37 - 2^13, row strides ld* in
  * elements; y may be x or res with the same stride.  Element i = t n + column stays where 16 bits of a counter-based generator are below keep = round(65536 (1 - p)),
  * 0 <= p <= 1; share = keep / 65536.  The bits: with words w[0..3] = Philox 4x32-10 of the counter {i / 8 (64 bits), offset + *step (64 bits)} under the key seed, element i has
  * the low (even i) or high (odd) half of w[i % 8 / 2].  The mask is stored nowhere: the backward call is the same one with the gradient in x's place (and the one it adds to in

@@ -1532,7 +1532,8 @@ rp_status rp_op_span_attn_bwd(void* stream, const void* q, const void* k, const 
 
 rp_status rp_op_dropout(void* stream, const void* x, long ldx, const void* res, long ldr, void* y, long ldy, int T, int n, float p, unsigned long long seed,
                         unsigned long long offset, const unsigned long long* step) {
-  if (T < 0 || n < 0 || n % 8 || !(p >= 0.f && p <= 1.f) || (double)T * n >= 137438953472.0 || reinterpret_cast<uintptr_t>(step) % 8)
+  // (a launch has fewer than 2^32 threads: 256 for 8192 elements)
+  if (T < 0 || n < 0 || n % 8 || !(p >= 0.f && p <= 1.f) || (double)T * n > 16777215.0 * 8192 || reinterpret_cast<uintptr_t>(step) % 8)
     return fail(nullptr, RP_EINVAL, "rp_op_dropout: bad arguments");
   if (bad_rows(x, T, n, ldx) || bad_rows(y, T, n, ldy) || (res && bad_rows(res, T, n, ldr)) || (y == x && ldy != ldx) || (res && y == res && ldy != ldr))
     return fail(nullptr, RP_EINVAL, "rp_op_dropout: tensors missing, not on 16-byte boundaries, or bad strides");
