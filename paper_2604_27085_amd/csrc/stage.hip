@@ -1556,7 +1556,7 @@ bool bad_embedding(int T, int V, int h) { return T < 0 || T >= (1 << 24) || V < 
 
 rp_status rp_op_embed_fwd(void* stream, const void* table, long ldt, const int* ids, float scale, void* x, long ldx, int T, int V, int h) {
   if (bad_embedding(T, V, h) || (T && !ids) || !isfinite(scale)) return fail(nullptr, RP_EINVAL, "rp_op_embed_fwd: bad sizes, tokens or scale");
-  if (bad_rows(table, V, h, ldt) || bad_rows(x, T, h, ldx) || (T && h && !table))
+  if (bad_rows(table, V, h, ldt) || bad_rows(x, T, h, ldx))
     return fail(nullptr, RP_EINVAL, "rp_op_embed_fwd: tensors missing, not on 16-byte boundaries, or bad strides");
   StreamDevice on(reinterpret_cast<hipStream_t>(stream));
   if (on.err != hipSuccess) OP_RET(on.err);

@@ -23,3 +23,12 @@ def test_gradient(B, T, V, h, kind, accumulate):  # noqa: F811
     want, bound = R.embedding_gradient(dx, ids, 0.5, V, given if accumulate else None)
     assert bool(((dt.double() - want).abs() <= bound + 1e-30).all())
     assert bool(ws[n // 4:].isnan().all())
+
+
+def test_a_table_without_rows(B):  # noqa: F811
+    """No row, no table: every token is padding."""
+    ids = torch.arange(-2, 5, dtype=torch.int32, device=DEV)
+    x = torch.full((8, 40), float("nan"), dtype=torch.bfloat16, device=DEV)
+    B.rp_op_embed_fwd(stream(), None, 40, ids, 2.0, x, 40, 7, 0, 40)
+    assert bool((x[:7] == 0).all()) and bool(x[7].isnan().all())
+    B.rp_op_embed_bwd(stream(), x, 40, ids, 2.0, None, 40, 0, 7, 0, 40, None)      # (nothing to write)
