@@ -227,7 +227,7 @@ RP_API rp_status rp_op_scan_sizes(int batch, int seq, int c, size_t* state_bytes
 RP_API rp_status rp_op_scan_fwd(void* stream, int weight, const void* x, const void* g, void* y, long ldx, long ldg, long ldy, const unsigned char* first,
                          const int* len, const float* h0, float* last, float* states, int batch, int seq, int c, void* scratch, size_t scratch_bytes);
 /* dy bf16 [batch * seq, c]; dlast fp32 [batch, c] or NULL: the gradient of the last state.  dx, dg bf16 overwritten (0 behind len; dx may be dy or x, dg may be g, with the
- * same stride); dh0 fp32 [batch, c] or NULL. */
+ * same stride); dh0 fp32 [batch, c] or NULL (may be dlast). */
 RP_API rp_status rp_op_scan_bwd(void* stream, int weight, const void* x, const void* g, const void* dy, void* dx, void* dg, long ldx, long ldg, long lddy,
                          long lddx, long lddg, const unsigned char* first, const int* len, const float* states, const float* dlast, float* dh0, int batch,
                          int seq, int c, void* scratch, size_t scratch_bytes);

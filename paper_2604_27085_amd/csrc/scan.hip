@@ -321,19 +321,23 @@ RP_DEV fch enter(const fch (&As)[NW][64], const fch (&Bs)[NW][64], const Place& 
 // EACH 0: a sequence is one chunk, which starts from the call's own state
 template <int EACH>
 RP_DEV int take_place(const ScanArgs& p, int* lds) {
-  if (EACH == 0) return (int)blockIdx.x;
+  if (EACH == 0) {
+    int id = (int)blockIdx.x;
+    asm volatile("" : "+s"(id)::"memory");      // (with its number known the backward pass spills inside its loops: 128 sequences of 128 tokens 181 us instead of 139, plain weights)
+    return id;
+  }
   if (threadIdx.x == 0) *lds = (int)atomicAdd(p.counter, 1u);
   __syncthreads();
   return __builtin_amdgcn_readfirstlane(*lds);
 }
+RP_DEV fch given_state(const float* src, const ScanArgs& p, const Place& s) {
+  return src && s.in ? *reinterpret_cast<const fch*>(src + (long)s.b * p.c + s.ch) : fch{0.f, 0.f};
+}
 // The call's own state goes to LDS, before the barrier behind the waves' maps: it is read by the first chunk's wave 0 alone (the last chunk's, BACK), and once that barrier is passed it
-// is not read again, so that whoever is told of this chunk's end may write the state in its place (`last` may be h0).
+// is not read again, so that whoever is told of this chunk's end may write the state in its place (`last` may be h0, dh0 dlast).
 template <bool BACK>
 RP_DEV void keep_given(const float* src, const ScanArgs& p, const Place& s, fch (&given)[64]) {
-  if (s.w != 0) return;      // uniform
-  fch h = {0.f, 0.f};
-  if (src && s.in && s.chunk == (BACK ? p.chunks - 1 : 0)) h = *reinterpret_cast<const fch*>(src + (long)s.b * p.c + s.ch);
-  given[s.lane] = h;
+  if (s.w == 0) given[s.lane] = given_state(s.chunk == (BACK ? p.chunks - 1 : 0) ? src : nullptr, p, s);      // uniform
 }
 // What the chunk starts from; the waves have put their maps into LDS, wave 0 the call's own state.  The state behind the last chunk goes to `last`.
 template <int EACH, bool BACK>
@@ -353,7 +357,6 @@ __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p) {
   __shared__ Looks<EACH ? EACH : 1> looks;
   __shared__ int place;
   const Place s(p, take_place<EACH>(p, &place), false);
-  keep_given<false>(p.h0, p, s, given);
   raw_t gr[TOK], xr[TOK];
   TokenRows(p.g, p.ldg, s, p, s.len).load(gr);
   TokenRows(p.x, p.ldx, s, p, s.len).load(xr);
@@ -365,6 +368,7 @@ __global__ void __launch_bounds__(64 * NW) scan_fwd_kernel(const ScanArgs p) {
     As[s.w][s.lane] = A;
     Bs[s.w][s.lane] = B;
   }
+  keep_given<false>(p.h0, p, s, given);
   __syncthreads();
   const fch start = chunk_start<EACH, false>(p, s, As, Bs, &looks, given, p.last);
   fch h = enter<false>(As, Bs, s, start);
@@ -392,7 +396,6 @@ __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p) 
   __shared__ Looks<EACH ? EACH : 1> looks;
   __shared__ int place;
   const Place s(p, take_place<EACH>(p, &place), true);
-  keep_given<true>(p.dlast, p, s, given);
   raw_t xr[TOK], dyr[TOK];
   uint32_t first;
   fch ts[TOK];
@@ -415,8 +418,12 @@ __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p) 
       Bb[s.w][s.lane] = B;
     });
   }
+  if (EACH > 0) keep_given<true>(p.dlast, p, s, given);
   __syncthreads();
-  fch mu = chunk_start<EACH, true>(p, s, Ab, Bb, &looks, given, p.dh0);
+  // (one chunk: every wave reads the state for itself, and dh0 waits for all of them; through LDS the compiler spills in other places, 128 sequences of 128 tokens 143 us instead of 130)
+  fch mu;
+  if constexpr (EACH == 0) mu = given_state(p.dlast, p, s);
+  else mu = chunk_start<EACH, true>(p, s, Ab, Bb, &looks, given, p.dh0);
   h = enter<false>(As, Bs, s, h);
   mu = enter<true>(Ab, Bb, s, mu);
   forget(xr);
@@ -462,7 +469,10 @@ __global__ void __launch_bounds__(64 * NW, 4) scan_bwd_kernel(const ScanArgs p) 
       dg.store(i, PLAIN || live ? pack(gg) : 0u);
       }
   });
-  if (EACH == 0 && p.dh0 && s.w == 0 && s.in) *reinterpret_cast<fch*>(p.dh0 + (long)s.b * p.c + s.ch) = mu;
+  if (EACH == 0 && p.dh0) {
+    __syncthreads();
+    if (s.w == 0 && s.in) *reinterpret_cast<fch*>(p.dh0 + (long)s.b * p.c + s.ch) = mu;
+  }
 }
 
 int chunks_of(int seq) { return (seq + CHUNK - 1) / CHUNK; }
