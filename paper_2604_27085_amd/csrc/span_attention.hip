@@ -15,7 +15,7 @@
 //
 // In a tile that some rows do not see, scores are replaced, and what the products sum over (V; K of dQ; Q and dO) has its infinities and NaN taken out, since 0 times those would
 // reach the rows beside them: a document is not touched by what is in another.  What does see such a value is made NaN as a whole: the row of o that sees it in v, the row of dQ that sees it in
-// k, and dK, dV of the keys that a row with it in q or dO sees (marked a bit a key, or a row, in LDS: lse and delta need not show it).
+// k (both marked key by key in LDS), and dK, dV of the keys that a row with it in q or dO sees (by a delta of its own: lse need not show it, and dV does not know of delta).
 //
 // P (for P v and dV) and dS are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most; dS in small calls in two parts, 2^-16); scores, statistics, dP - delta and every sum are
 // fp32.  The forward divides by the sum of the rounded P: what all terms of a row were rounded by alike drops out, and where a row lies on one key o is that key's v.  o goes out in two
@@ -41,8 +41,8 @@ constexpr int fwd_tile_bytes(int d) { return max_i(64 * (d + 8) + 64 * (d + 32),
 constexpr int dq_tile_bytes(int d) { return max_i(2 * 64 * tile_ld(d), 128 * (d + 8)) * 2; }
 
 constexpr int step_smem_bytes(int d, int nc, int nw) { return nw * max_i(32 * tile_ld(d) * 2, 16 * nc * (3 + d + 4) * 4); }
-constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 6 * 64 * 4 + 16, 4 * 32 * (d + 4) * 4); }
-constexpr int dkv_pair_smem_bytes(int d, bool two) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * (two ? 6 : 4) * 64 * 16 + 2 * 6 * 64 * 4 + 16; }
+constexpr int dkv_smem_bytes(int d) { return max_i(2 * 64 * tile_ld(d) * 2 + 6 * 64 * 4, 4 * 32 * (d + 4) * 4); }
+constexpr int dkv_pair_smem_bytes(int d, bool two) { return 2 * (2 * 64 * tile_ld(d)) * 2 + 8 * (two ? 6 : 4) * 64 * 16 + 2 * 6 * 64 * 4; }
 constexpr float LOG2E = 1.4426950408889634f;
 
 // Sizes of one sequence and key head.
@@ -171,18 +171,35 @@ RP_DEV int found_here(int x) {
   asm volatile("" : "+v"(x));
   return x;
 }
-// A thread's pieces of a 64-row tile (NT threads, CH pieces a row): infinities and NaN made zero, and the rows that had any marked in LDS [2], a bit a row.
-template <int CH, int NT, int N>
-RP_DEV void make_finite(uint4 (&r)[N], unsigned* marks, int tid) {
+template <int N>
+RP_DEV void make_finite(uint4 (&r)[N]) {
   if (!any_not_finite(r)) return;
-  const int t = found_here(tid);
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int row = (i * NT + t) / CH;
-    if (not_finite(carries(r[i]))) atomicOr(marks + (row >> 5), 1u << (row & 31));
-    r[i] = finite8(r[i]);
-  }
+  for (int i = 0; i < N; ++i) r[i] = finite8(r[i]);
 }
+// Which keys of a 64-key tile held an infinity or NaN, in LDS: key by key the number of the last tile where that was so, and the number of the last tile with any.  Nothing is cleared
+// from tile to tile, and a tile without any costs one read, asked for before the next tile's loads.  (Asked for where the masks are applied: dQ of 2 x 1021 tokens, 64 heads of 64, prefixes 39.8 us
+// instead of 38.9; 38.1 without marks.)
+struct BadKeys {
+  int* lds;      // [64], then one for all
+  static constexpr int BYTES = 272;
+  RP_DEV void start(int tid) const {      // before a barrier
+    if (tid < 65) lds[tid] = -1;
+  }
+  // a thread's pieces (NT threads, CH a key) of tile j, made finite, in the barriers between which they are stored
+  template <int CH, int NT, int N>
+  RP_DEV void make_finite(uint4 (&r)[N], int j, int tid) const {
+    if (!any_not_finite(r)) return;
+    const int t = found_here(tid);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (not_finite(carries(r[i]))) lds[(i * NT + t) / CH] = lds[64] = j;      // (the same from all lanes)
+      r[i] = finite8(r[i]);
+    }
+  }
+  RP_DEV int last() const { return lds[64]; }      // of the tiles stored
+  RP_DEV unsigned long long of(int j, int lane) const { return __ballot(lds[lane] == j); }      // a bit a key; all lanes
+};
 
 RP_DEV float sum2(uint32_t pair, float acc) {      // the two bf16 of a register, added up in fp32
   typedef __bf16 v2 __attribute__((ext_vector_type(2)));
@@ -214,26 +231,11 @@ struct Parts {
   }
 };
 
-// The marks of the present tile, the same in all lanes: asked for behind the barrier that they are complete at, in tiles that make use of them, and taken where the next tile's loads are on their way.
-// Two tiles take turns with the two words of LDS; what a tile has left there the next one clears.  (Read where the masks are applied: 2 x 1021 tokens, 64 heads of 64, prefixes 134.4 us instead of
-// 132.1, and 131.0 without marks; a window of 4096 256.7, 256.0, 254.2.)
-struct Marks {
-  unsigned half[2];
-  uint2 word;
-  RP_DEV void none() { half[0] = half[1] = 0u; }
-  RP_DEV void ask(bool whole, unsigned* lds, int parity, int tid) {
-    if ((half[0] | half[1]) && tid < 2) lds[2 * (parity ^ 1) + tid] = 0u;      // (of the tile before: last read before the barriers above, next written behind the next one)
-    word = make_uint2(0u, 0u);
-    if (!whole) word = *reinterpret_cast<const uint2*>(lds + 2 * parity);
-  }
-  RP_DEV void take() {
-    half[0] = __builtin_amdgcn_readfirstlane(word.x);
-    half[1] = __builtin_amdgcn_readfirstlane(word.y);
-  }
-};
-
 // In a branch that is taken for the few tiles at the edge of a span: keeps the compiler from doing the work for every tile and selecting.
 RP_DEV void stay_in_branch() { asm volatile("" ::: "memory"); }
+
+// delta of a row whose q or dO is not finite: a NaN that dK, dV know it by, in place of a score and a sum that are made from zeros there.
+constexpr uint32_t SPOILT = 0x7fc0bad0u;
 
 constexpr float FLOOR = -1.0e37f;      // the reference exponent of rows that have seen nothing yet: finite, so that exp2(-inf - FLOOR) = 0
 
@@ -247,7 +249,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_fwd_kernel(const Sp
   bf16* const Ks = smem;
   bf16* const Vs = smem + 64 * LDK;
   int4* const seen_lds = reinterpret_cast<int4*>(dyn_smem + fwd_tile_bytes(D));       // [4]
-  unsigned* const bad_keys = reinterpret_cast<unsigned*>(seen_lds + 4);               // [2 tiles][2]: a bit a key
+  const BadKeys bad_keys{reinterpret_cast<int*>(seen_lds + 4)};
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, lk = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -266,7 +268,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_fwd_kernel(const Sp
   Seen mine;
   mine.start(span, live);
   mine.lanes(1, 32);
-  if (tid < 4) bad_keys[tid] = 0u;
+  bad_keys.start(tid);
   const Seen block = seen_by_all(mine, seen_lds, w, lane);
   int j0 = 0, j1 = 0;
   if (block.hi > block.lo) {
@@ -318,12 +320,12 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_fwd_kernel(const Sp
     const int kv0 = j * 64;
     const bool whole = block.all(kv0, kv0 + 64);      // uniform over the workgroup
     __syncthreads();
-    if (!whole) make_finite<CH, NT>(vreg, bad_keys + 2 * (j & 1), tid);
+    if (!whole) bad_keys.make_finite<CH, NT>(vreg, j, tid);
     T64::template store<LDK>(kreg, Ks, tid);
     T64::template store<LDV>(vreg, Vs, tid);
     __syncthreads();
     if (j + 1 < j1) load_tiles(j + 1);
-    if (tid < 2) bad_keys[2 * ((j + 1) & 1) + tid] = 0u;      // (last read before the barriers above, next written behind the next one)
+    const int last_bad = whole ? -1 : bad_keys.last();
     if (!mine.any(kv0, kv0 + 64)) continue;                   // uniform over the wave
     f32x16 sT[2];
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -372,9 +374,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_fwd_kernel(const Sp
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int v = 0; v < 16; ++v) sT[kt][v] = (unsigned)(32 * kt + 8 * (v >> 2) + (v & 3) - lo) < n ? sT[kt][v] : -INFINITY;
-      const unsigned b0 = __builtin_amdgcn_readfirstlane(bad_keys[2 * (j & 1)]), b1 = __builtin_amdgcn_readfirstlane(bad_keys[2 * (j & 1) + 1]);
-      if (b0 | b1) {      // does the row see one of the keys whose v was not finite?
-        const unsigned long long bad = b0 | (unsigned long long)b1 << 32;
+      if (__builtin_amdgcn_readfirstlane(last_bad) == j) {      // does the row see one of the keys whose v was not finite?
+        const unsigned long long bad = bad_keys.of(j, lane);
         const int from = max(span.x - kv0, 0), to = min(span.y - kv0, 64);
         if (to > from && (bad >> from & (to - from == 64 ? ~0ull : (1ull << (to - from)) - 1ull))) lt_run = NAN;
       }
@@ -797,7 +798,7 @@ __global__ void __launch_bounds__(256, D == 64 && !TWO && !(CAP && BIAS) ? 3 : 2
   bf16* const Ks = smem;
   bf16* const Vs = smem + 64 * LD;
   int4* const seen_lds = reinterpret_cast<int4*>(dyn_smem + dq_tile_bytes(D));       // [4]
-  unsigned* const bad_keys = reinterpret_cast<unsigned*>(seen_lds + 4);              // [2 tiles][2]: a bit a key
+  const BadKeys bad_keys{reinterpret_cast<int*>(seen_lds + 4)};
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -841,7 +842,7 @@ __global__ void __launch_bounds__(256, D == 64 && !TWO && !(CAP && BIAS) ? 3 : 2
     else mine.add(v.lo, v.hi, v.all_lo, v.all_hi);
   }
   mine.lanes(1, 16);
-  if (tid < 4) bad_keys[tid] = 0u;
+  bad_keys.start(tid);
   const Seen block = seen_by_all(mine, seen_lds, w, lane);
   // what dK, dV have to know of the two tiles of 64 rows
   if (s.g == 0 && split == 0 && (tid & 127) == 0 && r0 + 32 * w < s.total) {
@@ -889,13 +890,24 @@ __global__ void __launch_bounds__(256, D == 64 && !TWO && !(CAP && BIAS) ? 3 : 2
     lse2[c] = some ? lse2[c] * LOG2E : INFINITY;      // rows that see nothing get P = 0
     sum = column_sum(sum);
     dl[c] = some ? sum : 0.f;
+    // (a dO that is not finite has a delta that is not, whatever o is; a q that is not, scores and an lse that are not, unless capped)
+    uint32_t carried = 0u;
+    if (CAP)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) carried |= carries(qf[c][ks]);
+    if (__any(!__builtin_isfinite(sum) || not_finite(carried))) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) carried |= carries(dof[c][ks]);
+      carried |= __shfl_xor(carried, 16, 64);
+      carried |= __shfl_xor(carried, 32, 64);
+    }
     if (BIAS) {
       int q, h;
       s.at(rc, q, h);
       slope2[c] = p.slopes[s.g * s.grp + h] * LOG2E;
       pos[c] = p.q_pos ? p.q_pos[(long)s.b * p.seq_q + q] : q + p.seq_kv - p.seq_q;
     }
-    if (lg == 0 && ok && split == 0) p.delta[s.stat(row, p.a)] = dl[c];
+    if (lg == 0 && ok && split == 0) p.delta[s.stat(row, p.a)] = some && not_finite(carried) ? __uint_as_float(SPOILT) : dl[c];
   }
 
   const bf16* const kfrag = Ks + lr * LD + 8 * lg;      // (V lies 64 rows further on)
@@ -903,18 +915,16 @@ __global__ void __launch_bounds__(256, D == 64 && !TWO && !(CAP && BIAS) ? 3 : 2
   f32x4 dqacc[DT][2];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) dqacc[dt][0] = dqacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Marks bad;
-  bad.none();
   for (int j = j0; j < j1; ++j) {
     const bool whole = block.all(j * 64, j * 64 + 64);      // uniform over the workgroup
     __syncthreads();
-    if (!whole) make_finite<D / 8, NT>(kreg, bad_keys + 2 * (j & 1), tid);
+    if (!whole) bad_keys.make_finite<D / 8, NT>(kreg, j, tid);
     T64::template store<LD>(kreg, Ks, tid);
     T64::template store<LD>(vreg, Vs, tid);
     __syncthreads();
-    bad.ask(whole, bad_keys, j & 1, tid);
+    const int asked = whole ? -1 : bad_keys.last();
     if (j + 1 < j1) load_tiles(j + 1);
-    bad.take();
+    const int last_bad = __builtin_amdgcn_readfirstlane(asked);
     // the two 32-key halves of the tile one after the other: half as many score registers live at a time
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2) {
@@ -958,8 +968,8 @@ __global__ void __launch_bounds__(256, D == 64 && !TWO && !(CAP && BIAS) ? 3 : 2
       }
       if (!whole) {
         stay_in_branch();
-        if (bad.half[k2]) {
-          const unsigned mine4 = bad.half[k2] >> found_here(4 * lg);
+        if (last_bad == j) {
+          const unsigned mine4 = (unsigned)(bad_keys.of(j, lane) >> 32 * k2) >> found_here(4 * lg);
 #pragma unroll
           for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -1081,7 +1091,7 @@ RP_DEV int lane_now() {
 }
 
 // What there is to know of the rows of a 64-row tile, a row per lane of waves 0 to 3, in LDS as six arrays of 64: what the score starts from, -delta, first key,
-// key behind the last, position from the tile's first key, slope.  Rows behind the last one: P = exp(-inf) = 0.  Rows that see nothing are masked.
+// key behind the last, position from the tile's first key, slope.  Rows behind the last one: P = exp(-inf) = 0.  Rows that see nothing are masked.  Rows whose q or dO is not finite: P is NaN.
 // load() only issues loads, and store(), a tile later, works on what came: whatever it did to them at once would have these waves, and at the next barrier all others, wait for
 // the tile's rows too, whose loads are in flight before them (8192 causal tokens, 32 heads of 128: dK, dV 1250 us instead of 1170).
 template <bool CAP, bool BIAS>
@@ -1092,7 +1102,7 @@ struct RowStat {
   long per_q, per_h;   // their strides
   int left;            // rows of the sequence from the tile's first one on
   float start_mul;     // the same in all lanes
-  int x, y;
+  int x, y, z;
   RP_DEV void start(const SpanArgs& p, const Rows& s, int w) {
     // plain scores: the product starts from -lse / scale, so that it comes out as z - lse; a capped or biased one is taken off after
     start_mul = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(CAP || BIAS ? -LOG2E : -1.f / p.scale)));
@@ -1108,6 +1118,7 @@ struct RowStat {
     int q, h;
     s.at(lane < left ? row0 + lane : 0, q, h);
     x = src[q * per_q + h * per_h];
+    if (w == 0) z = __float_as_int(p.delta[((long)s.b * p.a + s.g * s.grp + h) * s.seq_q + q]);
     if (BIAS && w == 0) {
       y = q + p.seq_kv - s.seq_q;
       if (src2) y = src2[q];
@@ -1115,7 +1126,7 @@ struct RowStat {
     if (BIAS && w == 1) y = src2[h];
   }
   RP_DEV void store(float* lds, const SpanArgs& p, int kv0, int lane, int w) const {
-    const float f = __int_as_float(x);
+    const float f = w == 0 && z == (int)SPOILT ? NAN : __int_as_float(x);
     if (w == 0) lds[lane] = lane >= left ? -INFINITY : CAP ? __builtin_fmaf(f, start_mul, p.cap * LOG2E) : f * start_mul;
     if (w == 1) lds[64 + lane] = lane < left ? -f : 0.f;
     if (w == 2) lds[128 + lane] = __int_as_float(max(x, 0));
@@ -1125,10 +1136,9 @@ struct RowStat {
   }
 };
 
-// P and dS of 2 x 16 rows by 2 x 16 keys, in place of the scores and dP - delta.  lds: RowStat's, from the first of the rows on; bad: those of them (a bit each) whose q or dO is
-// not finite, where some rows do not see all keys; key: the lane's first key, from kv0.
+// P and dS of 2 x 16 rows by 2 x 16 keys, in place of the scores and dP - delta.  lds: RowStat's, from the first of the rows on; key: the lane's first key, from kv0.
 template <bool CAP, bool BIAS>
-RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, const float* lds, unsigned bad, int lg, int key, int kv0, bool whole) {
+RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, const float* lds, int lg, int key, int kv0, bool whole) {
 #pragma unroll
   for (int qt = 0; qt < 2; ++qt) {
     const float* const at = lds + 16 * qt + 4 * lg;
@@ -1153,16 +1163,6 @@ RP_DEV void probabilities(f32x4 (&s)[2][2], f32x4 (&dp)[2][2], const Score& c, c
   }
   if (!whole) {
     stay_in_branch();
-    if (bad) {
-      const unsigned mine4 = bad >> found_here(4 * lg);
-#pragma unroll
-      for (int qt = 0; qt < 2; ++qt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-            if (mine4 >> (16 * qt + e) & 1u) s[qt][t][e] = dp[qt][t][e] = NAN;
-    }
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
       const int4 lo = *reinterpret_cast<const int4*>(lds + 128 + 16 * qt + 4 * lg), hi = *reinterpret_cast<const int4*>(lds + 192 + 16 * qt + 4 * lg);
@@ -1384,7 +1384,6 @@ __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
   bf16* const Qs = smem;
   bf16* const dOs = smem + 64 * LD;
   float* const stat = reinterpret_cast<float*>(smem + 2 * 64 * LD);
-  unsigned* const bad_rows = reinterpret_cast<unsigned*>(stat + Stat::FLOATS);      // [2 tiles][2]: a bit a row
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1457,25 +1456,20 @@ __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
     prefetch(range.u);
     range.look(lane);
   }
-  if (tid < 4) bad_rows[tid] = 0u;
-  Marks bad;
-  bad.none();
   wait_for_loads();
-  for (int i = 0; range.more(); i ^= 1) {
+  while (range.more()) {
     const bool whole = range.whole();
     __syncthreads();
     if (!whole) {
-      make_finite<D / 8, NT>(qreg, bad_rows + 2 * i, tid);
-      make_finite<D / 8, NT>(doreg, bad_rows + 2 * i, tid);
+      make_finite(qreg);
+      make_finite(doreg);
     }
     T64::template store<LD>(qreg, Qs, tid);
     T64::template store<LD>(doreg, dOs, tid);
     rstat.store(stat, p, kv0, lane, w);
     __syncthreads();
-    bad.ask(whole, bad_rows, i, tid);
     range.next(lane);
     if (range.more()) prefetch(range.u);
-    bad.take();
     // the two 32-row halves of the tile one after the other: half as many score registers live at a time
 #pragma unroll
     for (int t2 = 0; t2 < 2; ++t2) {
@@ -1511,7 +1505,7 @@ __global__ void __launch_bounds__(256, 2) span_dkv_kernel(const SpanArgs args) {
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) uring[n] = ufrag_at(n);
       __builtin_amdgcn_sched_barrier(0);
-      probabilities<CAP, BIAS>(z, dp, sc, stat + 32 * t2, bad.half[t2], lg, 32 * w + lr, kv0, whole);
+      probabilities<CAP, BIAS>(z, dp, sc, stat + 32 * t2, lg, 32 * w + lr, kv0, whole);
       {
         const uint4 pfg[2] = {pack_frag(z[0][0], z[1][0]), pack_frag(z[0][1], z[1][1])};
         const Parts<TWO> dfg(dp);
@@ -1560,7 +1554,6 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
   constexpr int TSET = 2 * 64 * LD;
   uint4* const exch = reinterpret_cast<uint4*>(smem + 2 * TSET);    // [8 waves][NX fragments][64 lanes]
   float* const stat = reinterpret_cast<float*>(exch + 8 * NX * 64); // [2 sets]
-  unsigned* const bad_rows = reinterpret_cast<unsigned*>(stat + 2 * Stat::FLOATS);      // [2 tiles][2]: a bit a row
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int w8 = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1671,9 +1664,6 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
     prefetch(range.u);
     range.look(lane_now());
   }
-  if (tid < 4) bad_rows[tid] = 0u;
-  Marks bad;
-  bad.none();
   wait_for_loads();
   int i = 0;
   for (; range.more(); ++i) {
@@ -1682,18 +1672,16 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
     bf16* const q_set = smem + (i & 1) * TSET;
     float* const st_set = stat + (i & 1) * Stat::FLOATS;
     if (!whole) {
-      make_finite<D / 8, NT>(qreg, bad_rows + 2 * (i & 1), tid);
-      make_finite<D / 8, NT>(doreg, bad_rows + 2 * (i & 1), tid);
+      make_finite(qreg);
+      make_finite(doreg);
     }
     T64::template store<LD>(qreg, q_set, tid);
     T64::template store<LD>(doreg, q_set + 64 * LD, tid);
     rstat.store(st_set, p, kv0, lane_now(), w8);
     if (i > 0) partner_update(i - 1);
     __syncthreads();
-    bad.ask(whole, bad_rows, i & 1, tid);
     range.next(lane_now());
     if (range.more()) prefetch(range.u);
-    bad.take();
     f32x4 z[2][2], dp[2][2], z0[2], dp0[2];      // [16 rows][16 keys]; what they start from
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
@@ -1721,7 +1709,7 @@ __global__ void __launch_bounds__(512, 2) span_dkv_pair_kernel(const SpanArgs ar
       }
       MFMA_PHASE_END();
     }
-    probabilities<CAP, BIAS>(z, dp, sc, st_set + 32 * h, h ? bad.half[1] : bad.half[0], lg, 32 * w + lr, kv0, whole);
+    probabilities<CAP, BIAS>(z, dp, sc, st_set + 32 * h, lg, 32 * w + lr, kv0, whole);
     const uint4 pfg[2] = {pack_frag(z[0][0], z[1][0]), pack_frag(z[0][1], z[1][1])};
     const Parts<TWO> dfg(dp);
     // the partner read last tile's fragments before the barrier above: the slots are free
@@ -1780,8 +1768,8 @@ __global__ void __launch_bounds__(256) span_key_join_kernel(const SpanArgs p) {
   }
 }
 
-constexpr int fwd_smem_bytes(int d) { return fwd_tile_bytes(d) + 64 + 16; }
-constexpr int dq_smem_bytes(int d) { return dq_tile_bytes(d) + 64 + 16; }
+constexpr int fwd_smem_bytes(int d) { return fwd_tile_bytes(d) + 64 + BadKeys::BYTES; }
+constexpr int dq_smem_bytes(int d) { return dq_tile_bytes(d) + 64 + BadKeys::BYTES; }
 
 long row_count(const SpanArgs& p) { return (long)(p.a / p.kh) * p.seq_q; }
 size_t row_part_bytes(const SpanArgs& p, int d) { return (size_t)p.kh * p.batch * row_count(p) * (d + 4) * 4; }      // o or dq, and (m, l, lt)
