@@ -17,7 +17,7 @@
 // reach the rows beside them: a document is not touched by what is in another.  What does see such a value is made NaN as a whole: the row of o that sees it in v, the row of dQ that sees it in
 // k (both marked key by key in LDS), and dK, dV of the keys that a row with it in q or dO sees (by a delta of its own: lse need not show it, and dV does not know of delta).
 //
-// P (for P v and dV) and dS are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most; dS in small calls in two parts, 2^-16); scores, statistics, dP - delta and every sum are
+// P (for P v and dV) and dS are rounded to bf16, as the matrix instruction takes them (2^-8 a term at most; P of few rows, and dS in small calls, in two parts, 2^-16); scores, statistics, dP - delta and every sum are
 // fp32.  The forward divides by the sum of the rounded P: what all terms of a row were rounded by alike drops out, and where a row lies on one key o is that key's v.  o goes out in two
 // parts, its bf16 and that of what the rounding left over, so that delta = dO.(o + rest) does not carry o's rounding, which would be as large as dP - delta in such rows.
 //
@@ -211,18 +211,19 @@ RP_DEV float sum2(uint32_t pair, float acc) {      // the two bf16 of a register
 // 1.56 (relative 2-norm, 10^-3: 2.4 to 2.5 | 2.6, in two 1.7).  The products more cost little there (200 tokens, 16 heads of 128: dQ 13.8 -> 14.3 us, dK, dV 19.0 -> 19.3; 512
 // tokens, 32 heads: 22 -> 25 and 29 -> 32); beyond, both would take a fifth longer (8192 causal tokens, 32 heads of 128: 718 -> 882 and 1087 -> 1306).
 constexpr int FEW_KEYS = 512, FEW_ROWS = 16384;
+RP_DEV uint32_t left_over(float a, float b, uint32_t rounded) { return pack_bf16x2(a - bf16_lo(rounded), b - bf16_hi(rounded)); }
+RP_DEV uint4 left_over(const f32x4& a, const f32x4& b, const uint4& rounded) {      // rounded: pack_frag(a, b)
+  return make_uint4(left_over(a[0], a[1], rounded.x), left_over(a[2], a[3], rounded.y), left_over(b[0], b[1], rounded.z), left_over(b[2], b[3], rounded.w));
+}
 template <bool TWO>
 struct Parts {
   uint4 hi[2], lo[2];      // of the column tiles
-  RP_DEV static uint32_t left(float a, float b, uint32_t rounded) { return pack_bf16x2(a - bf16_lo(rounded), b - bf16_hi(rounded)); }
   RP_DEV Parts() {}
   RP_DEV Parts(const f32x4 (&x)[2][2]) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       hi[c] = pack_frag(x[0][c], x[1][c]);
-      if (TWO)
-        lo[c] = make_uint4(left(x[0][c][0], x[0][c][1], hi[c].x), left(x[0][c][2], x[0][c][3], hi[c].y), left(x[1][c][0], x[1][c][1], hi[c].z),
-                           left(x[1][c][2], x[1][c][3], hi[c].w));
+      if (TWO) lo[c] = left_over(x[0][c], x[1][c], hi[c]);
     }
   }
   RP_DEV f32x4 times(const uint4& a, int c, f32x4 acc) const {
@@ -480,7 +481,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) span_fwd_kernel(const Sp
 // At most 16 NC rows per key head (the queries of a step times the heads of the group).  Bound by reading K and V once, so a wave works alone, without
 // barriers: the waves of a workgroup take the 32-key steps in turn, K goes from memory straight into the fragments of the matrix
 // instruction (16 rows x 64 bytes a load: a whole row is used by one wave), V through a piece of LDS of the wave's own, since its
-// reduction runs over the keys.  The next step's K and V are on their way during a step.  At the end the waves join in LDS.
+// reduction runs over the keys.  The next step's K and V are on their way during a step.  At the end the waves join in LDS.  P goes to the product in two parts, its bf16 and that of what
+// the rounding left over, since the matrix pipe has little to do: o is then off by its own rounding alone (relative 2-norm from 64 bits 1.6e-3, in one part 1.9e-3; one query of 8 sequences against
+// 4096 keys, 32 heads of 128 in groups of 4: 35.0 -> 35.1 us, of one sequence 11.57 -> 11.66).
 template <int D, int NC, int NW, bool SPLIT, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(64 * NW) span_step_kernel(const SpanArgs p) {
   constexpr int LD = tile_ld(D), KS = D / 32, DT = D / 16, CH = D / 8, NV = 32 * CH / 64;
@@ -649,7 +652,7 @@ __global__ void __launch_bounds__(64 * NW) span_step_kernel(const SpanArgs p) {
         for (int dt = 0; dt < DT; ++dt) oacc[dt][c] *= alpha;
       }
     }
-    uint4 pf[NC];
+    uint4 pf[NC], pf_left[NC];      // P, and what its rounding left over
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
 #pragma unroll
@@ -660,13 +663,14 @@ __global__ void __launch_bounds__(64 * NW) span_step_kernel(const SpanArgs p) {
           l_run[c] += sT[kt][c][e];
         }
       pf[c] = pack_frag(sT[0][c], sT[1][c]);
-      lt_run[c] += sum2(pf[c].x, sum2(pf[c].y, sum2(pf[c].z, sum2(pf[c].w, 0.f))));
+      pf_left[c] = left_over(sT[0][c], sT[1][c], pf[c]);
+      lt_run[c] += sum2(pf[c].x, sum2(pf[c].y, sum2(pf[c].z, sum2(pf[c].w, sum2(pf_left[c].x, sum2(pf_left[c].y, sum2(pf_left[c].z, sum2(pf_left[c].w, 0.f))))))));
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       const uint4 a = read_frag_tr<LD>(vfrag + 16 * dt);
 #pragma unroll
-      for (int c = 0; c < NC; ++c) oacc[dt][c] = mfma16(a, pf[c], oacc[dt][c]);
+      for (int c = 0; c < NC; ++c) oacc[dt][c] = mfma16(a, pf[c], mfma16(a, pf_left[c], oacc[dt][c]));
     }
   }
 
