@@ -200,7 +200,7 @@ RP_API rp_status rp_op_pack_plan(void* stream, const int* starts, const int* pre
  * scale 1e-30 to 1e30.  lse fp32 [batch, a, seq_q] (natural log), or NULL.  A query that sees nothing has o = 0, lse = -inf, and gives and gets no gradient.  What a
  * query does not see does not reach it, also where it is infinite or NaN; a key that it sees with an infinity or NaN in v makes its whole row NaN where only some
  * queries near it see that key.  Backward: such values show as the formulas have it, and where only some queries near see a key, one in k makes all of dq NaN in the rows that see
- * that key, and one in q or dout all of dk and dv of the keys that its row sees.
+ * that key; one in q or dout leaves nothing finite of dk and dv of the keys that its row sees.
  * o_rest bf16, laid out as o, or NULL: what o's rounding left over (o + o_rest is good to 2^-16).  The backward call makes sum_j P dP from both; without it that is as exact as o.
  * scratch [dev, scratch_bytes]: the forward call cuts the keys of few rows into as many slices as it allows, and does without (NULL); the backward call needs the
  * smaller number, least_bytes, and cuts with more.  It holds nothing between calls; two calls that may run at the same time need one each.  No output may
@@ -235,7 +235,7 @@ RP_API rp_status rp_op_scan_bwd(void* stream, int weight, const void* x, const v
 /* Embedding: x_t = scale E[ids_t].  table bf16 [V, h] (V < 2^20), ids [dev] int32 [T] (T < 2^24), x bf16 [T, h]; h a multiple of 8, at most 65536; row strides ld* in
  * elements.  A token outside 0 .. V - 1 (padding) has the row 0. */
 RP_API rp_status rp_op_embed_fwd(void* stream, const void* table, long ldt, const int* ids, float scale, void* x, long ldx, int T, int V, int h);
-/* Its gradient: dtable fp32 [V, h] = (+= where accumulate) scale times the sums of dx's rows (bf16) over the tokens of every number, in ascending order of the tokens
+/* Its gradient: dtable fp32 [V, h] = (+= where accumulate) scale times the sums of dx's rows (bf16) over the tokens of every number, in an order that ids alone decide
  * (the same bits every time).  Accumulating leaves the rows of other numbers alone; it may go on top of the head's gradient where the two share their weights.
  * scratch [dev, scratch_bytes], rp_op_embed_scratch bytes; a call of its own each. */
 RP_API rp_status rp_op_embed_scratch(int T, int V, int h, size_t* scratch_bytes);

@@ -3,7 +3,7 @@
 
 namespace {
 
-// A thread takes a token: its document by bisection of the starts (up to 20 loads that follow one another, all of them in the caches after the first wave).
+// A thread takes a token: its document by bisection of the starts (as many loads that follow one another as their number has bits, 31 at most, all of them in the caches after the first wave).
 __global__ void __launch_bounds__(256) pack_plan_kernel(const PackArgs p) {
   const long t = (long)blockIdx.x * 256 + threadIdx.x;
   if (t >= p.T) return;

@@ -8,16 +8,18 @@
 //
 // h_t = a_t h_(t-1) + b_t is a scan over the maps (a, b), which compose as (a2, b2) after (a1, b1) = (a2 a1, a2 b1 + b2).  Chunks of 128 tokens by 128 channels; a wave
 // has 16 tokens, a lane two channels, all in registers, so every input is read once: a workgroup makes its chunk's map, publishes it, finds out what its chunk starts from, and writes
-// the outputs.  That it finds by looking back over the chunks before: from the nearest one whose end state is there, through the maps of those in between.  Workgroups take their
+// the outputs.  That it finds by looking back over the chunks before (the decoupled look-back of Merrill and Garland, Single-pass parallel prefix scan, 2016): from the nearest one whose
+// end state is there, through the maps of those in between.  Workgroups take their
 // chunks in order of time by a counter, so whoever waits waits for workgroups that have started and that wait only for earlier ones; the first waits for none.  A
 // chunk's end state is the same sequence of operations wherever the looking ended: the results do not depend on timing.
 // The backward pass is the same from behind; h_(t-1) is made again from the states that the forward pass left, in fp32 (4 bytes for 128 tokens), not from y, which is
 // rounded.  States, sums and products are fp32 throughout.
 //
-// What bounds it: memory where the chunks need not wait for one another (128 sequences of 128 tokens, 4096 channels: forward 81 us, backward 132, 5.0 and 5.1 TB/s).  One sequence of 16384 tokens
-// takes 106 and 148 us, 3.8 and 4.6 TB/s: a workgroup holds its registers while it waits for the ones before it, and two of them share a CU.  4 x 1021 tokens of 2880 channels, 736 workgroups
-// for 512 places, 27 and 40 us.  Chunks of 64 tokens (half the tokens a wave, or half the waves) take 150 to 175 and 180 us for the 16384 tokens, 16 waves of 8 tokens or of 16 are behind, too; three
-// workgroups a CU spill (119 us), a backward pass without its few spills has room for one (169).
+// What bounds it (w = 1 - f; forward and backward in turn, three sets of inputs): memory where the chunks need not wait for one another (128 sequences of 128 tokens, 4096 channels: forward 84 us,
+// backward 131, 4.8 and 5.1 TB/s).  One sequence of 16384 tokens takes 103 and 139 us, 3.9 and 4.8 TB/s: a workgroup holds its registers while it waits for the ones before it, and two of them share a
+// CU; with documents that begin in it every 1000 tokens, whose waves go by selects and read a byte a token besides, 120 and 166.  4 x 1021 tokens of 2880 channels, 736 workgroups for 512 places
+// (those behind a length too), 29 and 40 us.  When the 16384 tokens took 106 and 148 us: chunks of 64 tokens (half the tokens a wave, or half the waves) 150 to 175 and 180, 16 waves of 8 tokens or of 16
+// behind, too; three workgroups a CU spill (119), a backward pass without its few spills has room for one (169).
 #include <type_traits>
 
 #include "pack_ops.hpp"
@@ -201,8 +203,8 @@ RP_DEV word_t look(const word_t* at) { return __hip_atomic_load(const_cast<word_
 
 // What a chunk starts from, for all waves of its workgroup.  Wave 0 publishes the chunk's map; every wave then waits for EACH of the 8 EACH chunks before and puts what they say into
 // LDS, and all of them go from the nearest end state through the maps behind it.  Where none of those chunks has its end state yet, they look again.  EACH is 4 where all of a launch's
-// workgroups are on the chip at once, and the chain of looks is what takes the time (18467 tokens of 72 channels: forward 41 -> 29 us, backward 44 -> 32), else 1 (16384 tokens of 4096:
-// 108 and 147 us, with 4 118 and 158).
+// workgroups are on the chip at once, and the chain of looks is what takes the time (18467 tokens of 72 channels: forward 34.5 -> 22 us, backward 36.7 -> 23), else 1 (16384 tokens of 4096:
+// 103 and 139 us, with 4 112 and 149).
 // `given`: the state before the first chunk (behind the last one, BACK), in LDS; end: wave 0's, the chunk's own end state.
 template <int EACH>
 struct Looks {

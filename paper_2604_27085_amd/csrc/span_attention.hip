@@ -24,7 +24,7 @@
 // What bounds it (rocprofv3; docs: 16384 tokens of 4 documents, 32 heads of 128 in groups of 4; window: 4096 tokens, 16 heads of 128 in groups of 2, 1024 keys, capped; prefix: 2 x 1021 tokens of 3
 // documents, 64 heads of 64 in groups of 8, biased; matrix pipe and vector issue busy, waves waiting):
 //   forward  docs 1030 us 48 %, 50 %, 17 %;  window 70 us 26 %, 57 %, 18 %;  prefix 37 us 17 %, 73 %, 27 %
-//   dQ       docs 1265 us 56 %, 43 %, 16 %;  window 82 us 30 %, 49 %, 19 %;  prefix 38 us 23 %, 58 %, 25 %
+//   dQ       docs 1265 us 56 %, 43 %, 16 %;  window 82 us 30 %, 49 %, 19 %;  prefix 39 us 22 %, 57 %, 26 %
 //   dK, dV   docs 1995 us 45 %, 32 %, 25 %;  window 116 us 29 %, 39 %, 29 %;  prefix 57 us 25 %, 45 %, 32 %
 // docs: the exponentials and conversions beside the products, and the clock that the matrix pipe's power leaves (2.0 to 2.3 GHz; 8192 causal tokens take 570, 705 and 1015 us, 960,
 // 1170 and 1080 TFLOP/s of their products);
